@@ -47,7 +47,12 @@ typedef enum dsattn_status {
     DSATTN_ENODEVICE = -5     /* the plan was made host-only (device = -1) */
 } dsattn_status;
 
-typedef enum dsattn_dtype { DSATTN_F32 = 0, DSATTN_BF16 = 1 } dsattn_dtype;
+typedef enum dsattn_dtype {
+    DSATTN_F32 = 0,
+    DSATTN_BF16 = 1,
+    DSATTN_E4M3 = 2 /* 8 bits (OCP e4m3, largest 448) with fp32 scales beside the tensor: what
+                       dsattn_rmsnorm writes and dsattn_linear_act reads; no other call takes it */
+} dsattn_dtype;
 
 /* dsattn_desc.flags */
 #define DSATTN_FLAG_FORCE_GENERIC 1u /* planner must pick the generic vector-ALU kernel */
@@ -347,6 +352,135 @@ int dsattn_temporal_layer_workspace(const dsattn_plan_t *plan, size_t *bytes);
 int dsattn_temporal_layer(const dsattn_plan_t *plan, const void *X, const void *const *W,
                           const float *const *bias, void *workspace, size_t workspace_bytes,
                           void *Y, void *stream);
+
+/*
+ * Root-mean-square normalisation with the residual's addition, the norm of the transformer blocks
+ * around a temporal attention.  For each row of `channels` numbers
+ *   s = x + residual                          in fp32; `sum` receives s rounded once
+ *   y = s / sqrt(mean(s^2) + eps) * gamma     from the unrounded s, rounded once
+ * With out_dtype DSATTN_E4M3 a row gets a scale of its own, max(max|y| / 448, 2^-126), which is
+ * written to `scales`, and Y receives y / scale in 8 bits (to nearest, ties to even): the X and
+ * x_scales of a dsattn_linear_act.  A row that holds an infinity or a NaN has a NaN scale.
+ */
+typedef struct dsattn_rms_desc {
+    int64_t rows;      /* >= 1, at most 2^31 - 1: tokens, or tokens times heads for a norm per head */
+    int32_t channels;  /* >= 1, at most 2^20 */
+    int32_t io_dtype;  /* DSATTN_F32 or DSATTN_BF16, of X, residual and sum */
+    int32_t out_dtype; /* of Y: io_dtype or DSATTN_E4M3 */
+    float eps;         /* >= 0 */
+} dsattn_rms_desc;
+
+/*
+ *   X        : device, [rows, channels] of io_dtype, 16-byte aligned
+ *   residual : device, like X, or NULL for none
+ *   gamma    : device, [channels] fp32, 16-byte aligned, or NULL for 1
+ *   sum      : device, like X, receives s; NULL: not wanted.  May be X or residual itself
+ *   Y        : device, [rows, channels] of out_dtype, 16-byte aligned.  May be X or residual itself
+ *              where the types are the same
+ *   scales   : device, [rows] fp32; with DSATTN_E4M3 only, and then needed
+ * Outputs overlap the inputs in no other way, and not each other.  Runs on the current device;
+ * enqueues one kernel on `stream`; allocates nothing.  Errors: EINVAL, EHIP.
+ */
+int dsattn_rmsnorm(const dsattn_rms_desc *desc, const void *X, const void *residual,
+                   const float *gamma, void *sum, void *Y, float *scales, void *stream);
+
+/*
+ * Token-wise product with everything that follows it in a transformer block done in its epilogue:
+ *   z_k = (X W_k^T) * x_scale[row] * w_scale_k[channel] + b_k       (scales with DSATTN_E4M3 only)
+ *   Y   = act(z_0) + residual              n_w = 1
+ *   Y   = act(z_0) * z_1 + residual        n_w = 2, a gate and its value (W_0 is the gate)
+ * Products are accumulated in fp32, the epilogue is computed in fp32 and rounded once.
+ */
+typedef enum dsattn_act {
+    DSATTN_ACT_NONE = 0,
+    DSATTN_ACT_RELU = 1,
+    DSATTN_ACT_GELU = 2,      /* x / 2 * (1 + erf(x / sqrt(2))) */
+    DSATTN_ACT_GELU_TANH = 3, /* x / 2 * (1 + tanh(sqrt(2 / pi) * (x + 0.044715 x^3))) */
+    DSATTN_ACT_SILU = 4       /* x / (1 + exp(-x)) */
+} dsattn_act;
+
+typedef struct dsattn_linear_act_desc {
+    int64_t rows;      /* M >= 1 tokens, at most 2^31 - 1 */
+    int32_t c_in;      /* >= 1 */
+    int32_t c_out;     /* >= 1: channels of Y and of every W_k */
+    int32_t n_w;       /* 1, or 2: gated */
+    int32_t act;       /* dsattn_act */
+    int32_t io_dtype;  /* dsattn_dtype of X and W */
+    int32_t out_dtype; /* of Y and residual: DSATTN_F32, or DSATTN_BF16 unless io_dtype is DSATTN_F32 */
+    uint32_t flags;    /* DSATTN_FLAG_FORCE_GENERIC or 0 */
+} dsattn_linear_act_desc;
+
+/*
+ *   X        : device, [rows, c_in] of io_dtype, 16-byte aligned
+ *   x_scales : device, [rows] fp32; with DSATTN_E4M3, NULL for 1
+ *   W        : HOST array of n_w device pointers, each [c_out][c_in] of io_dtype, 16-byte aligned
+ *   w_scales : HOST array of n_w device pointers, each [c_out] fp32 or NULL for 1; with
+ *              DSATTN_E4M3; the array may be NULL
+ *   bias     : NULL, or HOST array of n_w device pointers, each [c_out] fp32 or NULL
+ *   residual : device, [rows, c_out] of out_dtype, 16-byte aligned, or NULL; may be Y itself
+ *   Y        : device, [rows, c_out] of out_dtype, 16-byte aligned; must not overlap X or W, nor
+ *              the residual otherwise
+ * The pointer arrays are read during the call only.  Runs on the current device; enqueues one
+ * kernel on `stream`; allocates nothing.  Errors: EINVAL, EUNSUPPORTED (too large), EHIP.
+ */
+int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void *X, const float *x_scales,
+                      const void *const *W, const float *const *w_scales,
+                      const float *const *bias, const void *residual, void *Y, void *stream);
+
+/*
+ * Attention of a stream of frames over a window of the latest ones and a few first ones that stay
+ * visible (sinks), with the cache that it reads and keeps up to date: the streaming counterpart of
+ * dsattn_forward, whose clips look both ways and need the whole video.  Frames are numbered from 0
+ * within a stream.  A call brings the frames start .. start + count - 1 of every stream, count at
+ * most `frames`; the query of frame a sees frame f, at its own position and head, iff
+ *   0 <= f <= a  and  (f < sinks  or  a - f < window)
+ * and O = softmax(scale * q.k) v over those, 0 where there is none (or none with a score above
+ * -infinity).  Query head i reads head
+ * i / (heads / kv_heads) of K and V.
+ *
+ * The cache holds sinks + ring frames per stream: frame f < sinks at slot f, any other at slot
+ * sinks + (f - sinks) % ring.  A call reads frames before `start` from it, its own frames from K
+ * and V, and leaves its own frames in it (of more than one with the same slot, the last).
+ */
+typedef struct dsattn_sink_desc {
+    int32_t streams;   /* B >= 1 independent streams */
+    int32_t frames;    /* T >= 1 new frames per stream and call, at most */
+    int32_t spatial;   /* P >= 1 positions */
+    int32_t heads;     /* >= 1 */
+    int32_t kv_heads;  /* >= 1, divides heads */
+    int32_t head_dim;  /* 1 .. 512 */
+    int32_t sinks;     /* >= 0 first frames that every later one sees */
+    int32_t window;    /* >= 0 latest frames that a query sees, its own included */
+    int32_t ring;      /* >= max(window, 1): frames that the cache holds besides the sinks */
+    int32_t io_dtype;  /* DSATTN_F32 or DSATTN_BF16 of all tensors; accumulation is fp32 */
+    float scale;       /* softmax scale; <= 0 selects 1/sqrt(head_dim) */
+    uint32_t flags;    /* DSATTN_FLAG_FORCE_GENERIC or 0 */
+} dsattn_sink_desc;
+
+/* Bytes of device workspace dsattn_sink_forward needs for this shape; may be 0. */
+int dsattn_sink_workspace(const dsattn_sink_desc *desc, size_t *bytes);
+
+/*
+ *   start     : device, [streams] int32 in [0, 2^31 - 1 - frames] (values outside count as the
+ *               nearest inside): the index of each stream's first new frame; NULL: 0 for all.
+ *               Read by the kernels, so that a captured call can be replayed for every frame
+ *   counts    : device, [streams] int32 in [0, frames] (likewise): new frames of each stream; NULL:
+ *               `frames` for all.  Rows behind a stream's last new frame are neither read nor
+ *               written
+ *   Q, O      : device, [streams, frames, P, heads * head_dim], 16-byte aligned
+ *   K, V      : device, [streams, frames, P, kv_heads * head_dim], 16-byte aligned
+ *   Kcache,
+ *   Vcache    : device, [streams, sinks + ring, P, kv_heads * head_dim], 16-byte aligned; both NULL
+ *               (only where start is NULL): nothing is kept
+ *   workspace : device, at least dsattn_sink_workspace() bytes, 16-byte aligned; NULL if those are
+ *               0.  Contents are overwritten; calls sharing a workspace must not overlap in time
+ * O and the caches overlap no other tensor of the call.  Runs on the current device; enqueues one
+ * to three kernels on `stream`; allocates nothing.
+ * Errors: EINVAL, EUNSUPPORTED (too large), EHIP.
+ */
+int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, const int32_t *counts,
+                        const void *Q, const void *K, const void *V, void *Kcache, void *Vcache,
+                        void *O, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Static description of a status code; never NULL. */
 const char *dsattn_strerror(int code);

@@ -12,6 +12,7 @@ _BINDING_NAMES = (
     "dsattn_plan_launch_info", "dsattn_gather_context", "dsattn_forward", "dsattn_forward_ctx",
     "dsattn_copy_probe", "dsattn_strerror", "dsattn_last_error", "dsattn_groupnorm",
     "dsattn_groupnorm_workspace", "Plan", "DsattnError",
+    "dsattn_rmsnorm", "dsattn_linear_act", "dsattn_sink_workspace", "dsattn_sink_forward", "DSATTN_E4M3",
     "DSATTN_F32", "DSATTN_BF16", "DSATTN_FLAG_FORCE_GENERIC", "DSATTN_FLAG_SLIDING_WINDOW",
 )
 

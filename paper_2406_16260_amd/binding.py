@@ -22,6 +22,12 @@ DSATTN_ENODEVICE = -5
 
 DSATTN_F32 = 0
 DSATTN_BF16 = 1
+DSATTN_E4M3 = 2
+DSATTN_ACT_NONE = 0
+DSATTN_ACT_RELU = 1
+DSATTN_ACT_GELU = 2
+DSATTN_ACT_GELU_TANH = 3
+DSATTN_ACT_SILU = 4
 DSATTN_FLAG_FORCE_GENERIC = 1
 DSATTN_FLAG_SLIDING_WINDOW = 2
 DSATTN_FLAG_DEDUP_GLOBAL = 4
@@ -32,7 +38,8 @@ EXPORTS = (
     "dsattn_copy_probe", "dsattn_strerror", "dsattn_last_error", "dsattn_groupnorm_workspace",
     "dsattn_groupnorm", "dsattn_temporal_conv_info", "dsattn_temporal_conv", "dsattn_linear_info",
     "dsattn_linear", "dsattn_groupnorm_static", "dsattn_groupnorm_static_max_bytes",
-    "dsattn_temporal_layer_workspace", "dsattn_temporal_layer",
+    "dsattn_temporal_layer_workspace", "dsattn_temporal_layer", "dsattn_rmsnorm", "dsattn_linear_act",
+    "dsattn_sink_workspace", "dsattn_sink_forward",
 )
 
 
@@ -67,6 +74,30 @@ class DsattnLinearDesc(ctypes.Structure):
         ("rows", ctypes.c_int64), ("c_in", ctypes.c_int32), ("c_out", ctypes.c_int32),
         ("n_out", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
         ("flags", ctypes.c_uint32),
+    ]
+
+
+class DsattnRmsDesc(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64), ("channels", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+    ]
+
+
+class DsattnLinearActDesc(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64), ("c_in", ctypes.c_int32), ("c_out", ctypes.c_int32),
+        ("n_w", ctypes.c_int32), ("act", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+    ]
+
+
+class DsattnSinkDesc(ctypes.Structure):
+    _fields_ = [
+        ("streams", ctypes.c_int32), ("frames", ctypes.c_int32), ("spatial", ctypes.c_int32),
+        ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("sinks", ctypes.c_int32), ("window", ctypes.c_int32), ("ring", ctypes.c_int32),
+        ("io_dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("flags", ctypes.c_uint32),
     ]
 
 
@@ -164,6 +195,16 @@ def load():
     lib.dsattn_temporal_layer.restype = ctypes.c_int
     lib.dsattn_temporal_layer.argtypes = [vp, vp, ctypes.POINTER(vp), ctypes.POINTER(vp), vp,
                                           ctypes.c_size_t, vp, vp]
+    lib.dsattn_rmsnorm.restype = ctypes.c_int
+    lib.dsattn_rmsnorm.argtypes = [ctypes.POINTER(DsattnRmsDesc), vp, vp, vp, vp, vp, vp, vp]
+    lib.dsattn_linear_act.restype = ctypes.c_int
+    lib.dsattn_linear_act.argtypes = [ctypes.POINTER(DsattnLinearActDesc), vp, vp, ctypes.POINTER(vp),
+                                      ctypes.POINTER(vp), ctypes.POINTER(vp), vp, vp, vp]
+    lib.dsattn_sink_workspace.restype = ctypes.c_int
+    lib.dsattn_sink_workspace.argtypes = [ctypes.POINTER(DsattnSinkDesc), ctypes.POINTER(ctypes.c_size_t)]
+    lib.dsattn_sink_forward.restype = ctypes.c_int
+    lib.dsattn_sink_forward.argtypes = [ctypes.POINTER(DsattnSinkDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                        ctypes.c_size_t, vp]
     lib.dsattn_strerror.restype = ctypes.c_char_p
     lib.dsattn_strerror.argtypes = [ctypes.c_int]
     lib.dsattn_last_error.restype = ctypes.c_char_p
@@ -210,12 +251,14 @@ def _stream(stream):
 # remembered about a tensor from one call to the next.
 _torch = None
 _DTYPES = {}
+_I32 = "int32"  # (in the place of a dtype code, for index tensors)
 
 
 def _setup_torch():
     global _torch
     import torch
-    _DTYPES.update({DSATTN_F32: torch.float32, DSATTN_BF16: torch.bfloat16})
+    _DTYPES.update({DSATTN_F32: torch.float32, DSATTN_BF16: torch.bfloat16,
+                    DSATTN_E4M3: torch.float8_e4m3fn, _I32: torch.int32})
     _torch = torch
 
 
@@ -254,7 +297,9 @@ def _raw_stream(stream):
 
 
 def _dtype_name(code):
-    return "float32" if code == DSATTN_F32 else "bfloat16"
+    if _torch is None:
+        _setup_torch()
+    return str(_DTYPES.get(code, _torch.bfloat16)).replace("torch.", "")
 
 
 def _check_tensors(who, items, device):
@@ -276,7 +321,9 @@ def _check_tensors(who, items, device):
         elif t.numel() != numel:
             raise ValueError(f"{who}: {name}: {t.numel()} elements, {numel} expected")
         if dtype_code is not None:
-            want = torch.float32 if dtype_code == DSATTN_F32 else torch.bfloat16
+            if _torch is None:
+                _setup_torch()
+            want = _DTYPES.get(dtype_code, torch.bfloat16)
             if t.dtype != want:
                 raise ValueError(f"{who}: {name}: dtype {t.dtype}, {_dtype_name(dtype_code)} expected")
     if device is None:
@@ -635,3 +682,111 @@ def dsattn_temporal_layer(plan, X, Ws, workspace, Y, biases=None, stream=None):
                                         None if biases is None else _ptr_array(biases, 4),
                                         _ptr(workspace), nbytes, _ptr(Y), _stream(stream)),
            "dsattn_temporal_layer")
+
+
+def dsattn_rmsnorm(rows, channels, X, Y, residual=None, gamma=None, sum_out=None, scales=None,
+                   io_dtype=DSATTN_BF16, out_dtype=None, eps=1e-6, stream=None):
+    """sum_out receives X + residual (which it may be itself), scales the rows' scales of an output in
+    8 bits (out_dtype = DSATTN_E4M3; Y is then a torch.float8_e4m3fn tensor)."""
+    out = io_dtype if out_dtype is None else out_dtype
+    desc = DsattnRmsDesc(rows, channels, io_dtype, out, eps)
+    dev, n = _device_of(X), rows * channels
+    px, py = _addr(X, n, io_dtype, dev), _addr(Y, n, out, dev)
+    pr, okr = _addr_or_null(residual, n, io_dtype, dev)
+    pg, okg = _addr_or_null(gamma, channels, DSATTN_F32, dev)
+    pt, okt = _addr_or_null(sum_out, n, io_dtype, dev)
+    ps, oks = _addr_or_null(scales, rows, DSATTN_F32, dev)
+    if px is not None and py is not None and okr and okg and okt and oks:
+        _check((_lib or load()).dsattn_rmsnorm(ctypes.byref(desc), px, pr, pg, pt, py, ps,
+                                               _raw_stream(stream)), "dsattn_rmsnorm")
+        return
+    _check_tensors("dsattn_rmsnorm",
+                   [(X, "X", n, io_dtype), (residual, "residual", n, io_dtype),
+                    (gamma, "gamma", channels, DSATTN_F32), (sum_out, "sum_out", n, io_dtype),
+                    (Y, "Y", n, out), (scales, "scales", rows, DSATTN_F32)], "current")
+    _check(load().dsattn_rmsnorm(ctypes.byref(desc), _ptr(X), _ptr(residual), _ptr(gamma), _ptr(sum_out),
+                                 _ptr(Y), _ptr(scales), _stream(stream)), "dsattn_rmsnorm")
+
+
+def dsattn_linear_act(rows, c_in, c_out, X, Ws, Y, biases=None, residual=None, x_scales=None, w_scales=None,
+                      act=DSATTN_ACT_NONE, io_dtype=DSATTN_BF16, out_dtype=None, flags=0, stream=None):
+    """Ws: one weight set, or two (gate, value); biases and w_scales: None, or as many entries (each a
+    tensor or None).  residual may be Y.  out_dtype: bf16 for operands in 8 bits unless given."""
+    n = len(Ws)
+    if n not in (1, 2) or any(s is not None and len(s) != n for s in (biases, w_scales)):
+        raise ValueError("dsattn_linear_act: one or two weight sets, and as many biases and scales, expected")
+    out = (DSATTN_BF16 if io_dtype == DSATTN_E4M3 else io_dtype) if out_dtype is None else out_dtype
+    desc = DsattnLinearActDesc(rows, c_in, c_out, n, act, io_dtype, out, flags)
+    dev = _device_of(X)
+    px, py = _addr(X, rows * c_in, io_dtype, dev), _addr(Y, rows * c_out, out, dev)
+    pr, okr = _addr_or_null(residual, rows * c_out, out, dev)
+    ps, oks = _addr_or_null(x_scales, rows, DSATTN_F32, dev)
+    if px is not None and py is not None and okr and oks:
+        w = _addr_array(Ws, n, c_out * c_in, io_dtype, dev)
+        b = None if biases is None else _addr_array(biases, n, c_out, DSATTN_F32, dev, optional=True)
+        sw = None if w_scales is None else _addr_array(w_scales, n, c_out, DSATTN_F32, dev, optional=True)
+        if w is not None and (biases is None or b is not None) and (w_scales is None or sw is not None):
+            _check((_lib or load()).dsattn_linear_act(ctypes.byref(desc), px, ps, w, sw, b, pr, py,
+                                                      _raw_stream(stream)), "dsattn_linear_act")
+            return
+    items = [(X, "X", rows * c_in, io_dtype), (Y, "Y", rows * c_out, out),
+             (residual, "residual", rows * c_out, out), (x_scales, "x_scales", rows, DSATTN_F32)]
+    for g in range(n):
+        items.append((Ws[g], f"W[{g}]", c_out * c_in, io_dtype))
+        if biases is not None:
+            items.append((biases[g], f"bias[{g}]", c_out, DSATTN_F32))
+        if w_scales is not None:
+            items.append((w_scales[g], f"w_scales[{g}]", c_out, DSATTN_F32))
+    _check_tensors("dsattn_linear_act", items, "current")
+    _check(load().dsattn_linear_act(ctypes.byref(desc), _ptr(X), _ptr(x_scales), _ptr_array(Ws, n),
+                                    None if w_scales is None else _ptr_array(w_scales, n),
+                                    None if biases is None else _ptr_array(biases, n), _ptr(residual),
+                                    _ptr(Y), _stream(stream)), "dsattn_linear_act")
+
+
+def dsattn_sink_workspace(streams, frames, spatial, heads, kv_heads, head_dim, sinks, window, ring=None,
+                          io_dtype=DSATTN_BF16, scale=0.0, flags=0) -> int:
+    """Bytes of device workspace dsattn_sink_forward needs for this shape (may be 0)."""
+    desc = DsattnSinkDesc(streams, frames, spatial, heads, kv_heads, head_dim, sinks, window,
+                          max(window, 1) if ring is None else ring, io_dtype, scale, flags)
+    out = ctypes.c_size_t()
+    _check(load().dsattn_sink_workspace(ctypes.byref(desc), ctypes.byref(out)), "dsattn_sink_workspace")
+    return int(out.value)
+
+
+def dsattn_sink_forward(streams, frames, spatial, heads, kv_heads, head_dim, sinks, window, ring, Q, K, V, O,
+                        Kcache=None, Vcache=None, start=None, counts=None, workspace=None,
+                        io_dtype=DSATTN_BF16, scale=0.0, flags=0, stream=None):
+    """start, counts: int32 device tensors of one entry per stream, or None; workspace: a uint8 device
+    tensor of at least dsattn_sink_workspace() bytes, or None where that is 0; ring: None without caches."""
+    ring = max(window, 1) if ring is None else ring
+    desc = DsattnSinkDesc(streams, frames, spatial, heads, kv_heads, head_dim, sinks, window, ring, io_dtype,
+                          scale, flags)
+    dev = _device_of(Q)
+    row = streams * spatial * head_dim
+    nq, nk, nc = row * frames * heads, row * frames * kv_heads, row * (sinks + ring) * kv_heads
+    ps = _addr(Q, nq, io_dtype, dev), _addr(K, nk, io_dtype, dev), _addr(V, nk, io_dtype, dev), _addr(O, nq, io_dtype, dev)
+    pk, okk = _addr_or_null(Kcache, nc, io_dtype, dev)
+    pv, okv = _addr_or_null(Vcache, nc, io_dtype, dev)
+    pf, okf = _addr_or_null(start, streams, _I32, dev)
+    pc, okc = _addr_or_null(counts, streams, _I32, dev)
+    if (None not in ps and okk and okv and okf and okc
+            and (workspace is None or (isinstance(workspace, _torch.Tensor) and workspace.element_size() == 1
+                                       and workspace.get_device() == dev and workspace.is_contiguous()))):
+        pw, nw = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+        _check((_lib or load()).dsattn_sink_forward(ctypes.byref(desc), pf, pc, ps[0], ps[1], ps[2], pk, pv, ps[3],
+                                                    pw, nw, _raw_stream(stream)), "dsattn_sink_forward")
+        return
+    items = [(Q, "Q", nq, io_dtype), (K, "K", nk, io_dtype), (V, "V", nk, io_dtype), (O, "O", nq, io_dtype),
+             (Kcache, "Kcache", nc, io_dtype), (Vcache, "Vcache", nc, io_dtype),
+             (start, "start", streams, _I32), (counts, "counts", streams, _I32)]
+    nbytes = 0
+    if hasattr(workspace, "data_ptr"):
+        if workspace.element_size() != 1:
+            raise ValueError("dsattn_sink_forward: workspace: a byte tensor (uint8) expected")
+        nbytes = workspace.numel()
+        items.append((workspace, "workspace", ("min", 0), None))
+    _check_tensors("dsattn_sink_forward", items, "current")
+    _check(load().dsattn_sink_forward(ctypes.byref(desc), _ptr(start), _ptr(counts), _ptr(Q), _ptr(K), _ptr(V),
+                                      _ptr(Kcache), _ptr(Vcache), _ptr(O), _ptr(workspace), nbytes,
+                                      _stream(stream)), "dsattn_sink_forward")

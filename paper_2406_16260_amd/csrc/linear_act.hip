@@ -1,0 +1,155 @@
+// Token-wise product with bias, activation, gate and residual in its epilogue (dsattn_linear_act).
+//
+//   z_k = (X W_k^T) x_scale w_scale_k + b_k,   Y = act(z_0) [* z_1] + R
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "dsattn.h"
+#include "plan.h"
+
+namespace dsattn {
+namespace {
+
+struct ActArgs {
+    const void *X;
+    const void *W[2];
+    const float *bias[2];      // [c_out] or null
+    const float *xs, *ws[2];   // scales of rows and channels, or null
+    const void *R;             // [M][c_out] or null
+    void *Y;
+    int64_t M;
+    int32_t Cin, Cout, n_w, act;
+};
+
+struct e4m3 { uint8_t bits; };
+
+template <typename T>
+__device__ __forceinline__ float to_float(T x)
+{
+    if constexpr (std::is_same_v<T, e4m3>)
+        return __builtin_amdgcn_cvt_f32_fp8((int)x.bits, 0);
+    else
+        return (float)x;
+}
+
+__device__ __forceinline__ float activate(float x, int act)
+{
+    switch (act) {
+    case DSATTN_ACT_RELU: return x > 0.f || x != x ? x : 0.f;
+    case DSATTN_ACT_GELU: return 0.5f * x * (1.f + erff(x * 0.70710678f));
+    case DSATTN_ACT_GELU_TANH: {
+        // 1 + tanh(u) = 2 / (1 + exp(-2 u))
+        const float u = 0.79788456f * (x + 0.044715f * x * x * x);
+        return x / (1.f + expf(-2.f * u));
+    }
+    case DSATTN_ACT_SILU: return x / (1.f + expf(-x));
+    default: return x;
+    }
+}
+
+// Plain vector kernel: one thread per output element, output channel fastest.
+template <typename Tin, typename Tout>
+__global__ __launch_bounds__(256) void act_generic_kernel(const ActArgs a)
+{
+    const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (idx >= a.M * a.Cout) return;
+    const int64_t m = idx / a.Cout;
+    const int co = (int)(idx - m * a.Cout);
+    const Tin *x = (const Tin *)a.X + m * a.Cin;
+    float z[2] = {0.f, 0.f};
+    for (int k = 0; k < a.n_w; ++k) {
+        const Tin *w = (const Tin *)a.W[k] + (int64_t)co * a.Cin;
+        float acc = 0.f;
+        for (int c = 0; c < a.Cin; ++c) acc = fmaf(to_float(w[c]), to_float(x[c]), acc);
+        if (a.xs) acc *= a.xs[m];
+        if (a.ws[k]) acc *= a.ws[k][co];
+        z[k] = acc + (a.bias[k] ? a.bias[k][co] : 0.f);
+    }
+    float y = activate(z[0], a.act);
+    if (a.n_w == 2) y *= z[1];
+    if (a.R) y += (float)((const Tout *)a.R)[idx];
+    ((Tout *)a.Y)[idx] = (Tout)y;
+}
+
+bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
+}
+
+int64_t dtype_bytes(int32_t t) { return t == DSATTN_F32 ? 4 : t == DSATTN_BF16 ? 2 : 1; }
+
+}  // namespace
+}  // namespace dsattn
+
+using namespace dsattn;
+
+extern "C" int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void *X, const float *x_scales,
+                                 const void *const *W, const float *const *w_scales,
+                                 const float *const *bias, const void *residual, void *Y, void *stream)
+{
+    const char *who = "dsattn_linear_act";
+    if (!desc) return fail(DSATTN_EINVAL, "%s: null descriptor", who);
+    const dsattn_linear_act_desc &d = *desc;
+    if (d.rows < 1 || d.rows > 0x7fffffffLL || d.c_in < 1 || d.c_out < 1)
+        return fail(DSATTN_EINVAL, "%s: sizes must be positive (rows at most 2^31 - 1)", who);
+    if (d.n_w < 1 || d.n_w > 2) return fail(DSATTN_EINVAL, "%s: n_w %d is neither 1 nor 2", who, d.n_w);
+    if (d.act < DSATTN_ACT_NONE || d.act > DSATTN_ACT_SILU)
+        return fail(DSATTN_EINVAL, "%s: unknown activation", who);
+    if (d.io_dtype != DSATTN_F32 && d.io_dtype != DSATTN_BF16 && d.io_dtype != DSATTN_E4M3)
+        return fail(DSATTN_EINVAL, "%s: unknown input dtype", who);
+    if (d.out_dtype != DSATTN_F32 && (d.out_dtype != DSATTN_BF16 || d.io_dtype == DSATTN_F32))
+        return fail(DSATTN_EINVAL, "%s: the output is fp32, or bf16 of inputs of 16 or 8 bits", who);
+    if (d.flags & ~DSATTN_FLAG_FORCE_GENERIC)
+        return fail(DSATTN_EINVAL, "%s: unknown flag bits 0x%x", who, d.flags);
+    if (!X || !W || !Y) return fail(DSATTN_EINVAL, "%s: null pointer", who);
+    const int64_t es = dtype_bytes(d.io_dtype), os = dtype_bytes(d.out_dtype);
+    const int64_t xn = d.rows * d.c_in * es, wn = (int64_t)d.c_out * d.c_in * es, yn = d.rows * d.c_out * os;
+    if (((uintptr_t)X | (uintptr_t)Y | (uintptr_t)residual) & 15u)
+        return fail(DSATTN_EINVAL, "%s: pointers must be 16-byte aligned", who);
+    if (d.io_dtype != DSATTN_E4M3 && (x_scales || w_scales))
+        return fail(DSATTN_EINVAL, "%s: scales belong to operands in 8 bits", who);
+    if ((uintptr_t)x_scales & 3u) return fail(DSATTN_EINVAL, "%s: scales must be 4-byte aligned", who);
+    ActArgs a{};
+    a.X = X;
+    a.xs = x_scales;
+    a.R = residual;
+    a.Y = Y;
+    a.M = d.rows;
+    a.Cin = d.c_in;
+    a.Cout = d.c_out;
+    a.n_w = d.n_w;
+    a.act = d.act;
+    for (int k = 0; k < d.n_w; ++k) {
+        a.W[k] = W[k];
+        a.bias[k] = bias ? bias[k] : nullptr;
+        a.ws[k] = w_scales ? w_scales[k] : nullptr;
+        if (!W[k]) return fail(DSATTN_EINVAL, "%s: null pointer in set %d", who, k);
+        if ((uintptr_t)W[k] & 15u) return fail(DSATTN_EINVAL, "%s: pointers must be 16-byte aligned", who);
+        if (((uintptr_t)a.bias[k] | (uintptr_t)a.ws[k]) & 3u)
+            return fail(DSATTN_EINVAL, "%s: biases and scales must be 4-byte aligned", who);
+        if (overlap(Y, yn, W[k], wn)) return fail(DSATTN_EINVAL, "%s: Y overlaps W", who);
+        if (overlap(Y, yn, a.bias[k], 4 * (int64_t)d.c_out) || overlap(Y, yn, a.ws[k], 4 * (int64_t)d.c_out))
+            return fail(DSATTN_EINVAL, "%s: Y overlaps a bias or a scale", who);
+    }
+    if (overlap(Y, yn, X, xn) || overlap(Y, yn, x_scales, 4 * d.rows))
+        return fail(DSATTN_EINVAL, "%s: Y overlaps X or its scales", who);
+    if (residual != Y && overlap(Y, yn, residual, yn))
+        return fail(DSATTN_EINVAL, "%s: Y overlaps the residual without being it", who);
+    // (a launch has less than 2^32 threads)
+    const int64_t blocks = (d.rows * d.c_out + 255) / 256;
+    if (blocks > 0xffffff) return fail(DSATTN_EUNSUPPORTED, "%s: too large for the generic kernel", who);
+    const bool f32 = d.out_dtype == DSATTN_F32;
+    const void *fn = d.io_dtype == DSATTN_F32 ? (const void *)&act_generic_kernel<float, float>
+                     : d.io_dtype == DSATTN_BF16
+                         ? (f32 ? (const void *)&act_generic_kernel<__bf16, float> : (const void *)&act_generic_kernel<__bf16, __bf16>)
+                         : (f32 ? (const void *)&act_generic_kernel<e4m3, float> : (const void *)&act_generic_kernel<e4m3, __bf16>);
+    void *params[] = {&a};
+    const hipError_t e = hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(256), params, 0, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
+    return DSATTN_OK;
+}

@@ -1,0 +1,252 @@
+// Attention of a stream of frames over a window and a few first frames (dsattn_sink_forward), and the
+// upkeep of the cache that it reads.
+//
+// A query of frame a sees the frames [0, ns) and [lo, a], where lo = max(0, a - window + 1) is the first
+// frame of its window and ns = min(sinks, lo): two runs that do not meet.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "dsattn.h"
+#include "plan.h"
+
+namespace dsattn {
+namespace {
+
+struct SinkArgs {
+    const void *Q, *K, *V;
+    void *Kc, *Vc, *O;
+    const int32_t *start, *counts;  // or null
+    int32_t B, T, P, h, hk, D, sinks, window, ring;
+    float sc;  // softmax scale * log2(e)
+};
+
+// A stream's place: its first new frame, and how many there are.
+struct Stream {
+    int start, count;
+};
+__device__ __forceinline__ Stream stream_of(const SinkArgs &a, int b)
+{
+    Stream s;
+    s.start = a.start ? min(max(a.start[b], 0), 0x7fffffff - a.T) : 0;
+    s.count = a.counts ? min(max(a.counts[b], 0), a.T) : a.T;
+    return s;
+}
+
+// slot of a frame in the cache
+__device__ __forceinline__ int slot_of(const SinkArgs &a, int f)
+{
+    return f < a.sinks ? f : a.sinks + (f - a.sinks) % a.ring;
+}
+
+// Row of frame f of stream b in K or V, or in their caches.
+template <typename T>
+__device__ __forceinline__ const T *frame_row(const SinkArgs &a, const void *fresh, const void *cache, int b, const Stream &s, int f)
+{
+    const int64_t row = (int64_t)a.P * a.hk * a.D;
+    if (f >= s.start) return (const T *)fresh + ((int64_t)b * a.T + (f - s.start)) * row;
+    return (const T *)cache + ((int64_t)b * (a.sinks + a.ring) + slot_of(a, f)) * row;
+}
+
+__device__ __forceinline__ float wave_sum(float x)
+{
+    for (int w = 32; w > 0; w >>= 1) x += __shfl_xor(x, w);
+    return x;
+}
+
+// Plain vector kernel for every shape: a wavefront a query and head, lane l has channels l, l + 64, ...
+constexpr int kMaxDim = 512;
+template <typename T>
+__global__ __launch_bounds__(256) void sink_generic_kernel(const SinkArgs a)
+{
+    const int64_t tasks = (int64_t)a.B * a.T * a.P * a.h;
+    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (id >= tasks) return;
+    const int lane = threadIdx.x & 63, D = a.D;
+    const int g = (int)(id % a.h);
+    const int64_t tok = id / a.h;  // (b T + t) P + p
+    const int p = (int)(tok % a.P);
+    const int t = (int)(tok / a.P % a.T), b = (int)(tok / a.P / a.T);
+    const Stream s = stream_of(a, b);
+    if (t >= s.count) return;
+    const int frame = s.start + t;
+    const T *q = (const T *)a.Q + id * D;
+    const int64_t at = ((int64_t)p * a.hk + g / (a.h / a.hk)) * D;  // within a frame of K and V
+    constexpr int R = kMaxDim / 64;
+    float qv[R], o[R], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        qv[r] = lane + 64 * r < D ? (float)q[lane + 64 * r] * a.sc : 0.f;
+        o[r] = 0.f;
+    }
+    const int lo = (int)max((int64_t)0, (int64_t)frame - a.window + 1), ns = min(a.sinks, lo);
+    const int n = ns + (frame + 1 - lo);
+    for (int j = 0; j < n; ++j) {
+        const int f = j < ns ? j : lo + (j - ns);
+        const T *k = frame_row<T>(a, a.K, a.Kc, b, s, f) + at, *v = frame_row<T>(a, a.V, a.Vc, b, s, f) + at;
+        float x = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (lane + 64 * r < D) x = fmaf(qv[r], (float)k[lane + 64 * r], x);
+        x = wave_sum(x);
+        const float mn = fmaxf(m, x), shift = mn == -INFINITY ? 0.f : mn;
+        const float w = exp2f(x - shift), old = exp2f(m - shift);
+        m = mn;
+        l = fmaf(l, old, w);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (lane + 64 * r < D) o[r] = fmaf(w, (float)v[lane + 64 * r], o[r] * old);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T *out = (T *)a.O + id * D;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (lane + 64 * r < D) out[lane + 64 * r] = (T)(o[r] * inv);
+}
+
+// New frames into the cache, in units that divide a frame's row: blockIdx.y is the new frame (and every
+// gridDim.y-th after it), blockIdx.z the stream and K or V.
+template <typename U>
+__global__ __launch_bounds__(256) void sink_append_kernel(const SinkArgs a, int64_t units)
+{
+    const int b = (int)(blockIdx.z >> 1);
+    const Stream s = stream_of(a, b);
+    const bool v = blockIdx.z & 1;
+    for (int t = (int)blockIdx.y; t < s.count; t += (int)gridDim.y) {
+        const int f = s.start + t;
+        // (of several frames with one slot the last one stays)
+        if (f >= a.sinks && s.count - t > a.ring) continue;
+        const U *from = (const U *)(v ? a.V : a.K) + ((int64_t)b * a.T + t) * units;
+        U *to = (U *)(v ? a.Vc : a.Kc) + ((int64_t)b * (a.sinks + a.ring) + slot_of(a, f)) * units;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (int64_t)gridDim.x * 256) to[i] = from[i];
+    }
+}
+
+bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
+}
+
+int sink_validate(const dsattn_sink_desc *d, const char *who)
+{
+    if (!d) return fail(DSATTN_EINVAL, "%s: null descriptor", who);
+    if (d->streams < 1 || d->frames < 1 || d->spatial < 1 || d->heads < 1 || d->kv_heads < 1)
+        return fail(DSATTN_EINVAL, "%s: sizes must be positive", who);
+    if (d->head_dim < 1 || d->head_dim > kMaxDim)
+        return fail(DSATTN_EINVAL, "%s: head_dim %d outside [1, %d]", who, d->head_dim, kMaxDim);
+    if (d->heads % d->kv_heads != 0)
+        return fail(DSATTN_EINVAL, "%s: kv_heads %d does not divide heads %d", who, d->kv_heads, d->heads);
+    if (d->sinks < 0 || d->window < 0) return fail(DSATTN_EINVAL, "%s: sinks and window must be >= 0", who);
+    if (d->ring < 1 || d->ring < d->window)
+        return fail(DSATTN_EINVAL, "%s: a ring of %d frames does not hold a window of %d", who, d->ring, d->window);
+    if (d->io_dtype != DSATTN_F32 && d->io_dtype != DSATTN_BF16)
+        return fail(DSATTN_EINVAL, "%s: unknown dtype", who);
+    if (!std::isfinite(d->scale)) return fail(DSATTN_EINVAL, "%s: scale is not finite", who);
+    if (d->flags & ~DSATTN_FLAG_FORCE_GENERIC)
+        return fail(DSATTN_EINVAL, "%s: unknown flag bits 0x%x", who, d->flags);
+    // 2^24 frames, 2^20 channels, 2^40 numbers a tensor at most
+    const int64_t C = (int64_t)d->heads * d->head_dim, slots = (int64_t)d->sinks + d->ring;
+    const int64_t most = (int64_t)1 << 40, frames = std::max<int64_t>(d->frames, slots);
+    if (C > (1 << 20) || d->frames > (1 << 24) || slots > (1 << 24) || d->streams > 65535 / 2 ||
+        (int64_t)d->streams * d->spatial > most / C || (int64_t)d->streams * d->spatial * C > most / frames)
+        return fail(DSATTN_EINVAL, "%s: problem too large", who);
+    return DSATTN_OK;
+}
+
+}  // namespace
+}  // namespace dsattn
+
+using namespace dsattn;
+
+extern "C" {
+
+int dsattn_sink_workspace(const dsattn_sink_desc *desc, size_t *bytes)
+{
+    const int rc = sink_validate(desc, "dsattn_sink_workspace");
+    if (rc != DSATTN_OK) return rc;
+    if (!bytes) return fail(DSATTN_EINVAL, "dsattn_sink_workspace: null output");
+    *bytes = 0;
+    return DSATTN_OK;
+}
+
+int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, const int32_t *counts,
+                        const void *Q, const void *K, const void *V, void *Kcache, void *Vcache, void *O,
+                        void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *who = "dsattn_sink_forward";
+    const int rc = sink_validate(desc, who);
+    if (rc != DSATTN_OK) return rc;
+    const dsattn_sink_desc &d = *desc;
+    if (!Q || !K || !V || !O) return fail(DSATTN_EINVAL, "%s: null pointer", who);
+    if (!Kcache != !Vcache) return fail(DSATTN_EINVAL, "%s: one cache without the other", who);
+    if (!Kcache && start) return fail(DSATTN_EINVAL, "%s: a start without caches", who);
+    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)Kcache | (uintptr_t)Vcache |
+         (uintptr_t)workspace) & 15u)
+        return fail(DSATTN_EINVAL, "%s: pointers must be 16-byte aligned", who);
+    if (((uintptr_t)start | (uintptr_t)counts) & 3u)
+        return fail(DSATTN_EINVAL, "%s: start and counts must be 4-byte aligned", who);
+    size_t need = 0;
+    dsattn_sink_workspace(desc, &need);
+    if (workspace_bytes < need || (need && !workspace))
+        return fail(DSATTN_EINVAL, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
+    const int64_t es = d.io_dtype == DSATTN_BF16 ? 2 : 4;
+    const int64_t per = (int64_t)d.streams * d.spatial * d.head_dim * es, row = d.spatial * (int64_t)d.kv_heads * d.head_dim;
+    const int64_t qn = per * d.frames * d.heads, kn = per * d.frames * d.kv_heads;
+    const int64_t cn = per * d.kv_heads * ((int64_t)d.sinks + d.ring), sn = 4 * (int64_t)d.streams;
+    const struct { const void *p; int64_t n; } all[] = {
+        {O, qn}, {Kcache, cn}, {Vcache, cn}, {workspace, (int64_t)need}, {Q, qn}, {K, kn}, {V, kn}, {start, sn}, {counts, sn}};
+    for (int o = 0; o < 4; ++o)
+        for (int i = o + 1; i < 9; ++i)
+            if (overlap(all[o].p, all[o].n, all[i].p, all[i].n))
+                return fail(DSATTN_EINVAL, "%s: an output, a cache or the workspace overlaps another tensor", who);
+    SinkArgs a{};
+    a.Q = Q;
+    a.K = K;
+    a.V = V;
+    a.Kc = Kcache;
+    a.Vc = Vcache;
+    a.O = O;
+    a.start = start;
+    a.counts = counts;
+    a.B = d.streams;
+    a.T = d.frames;
+    a.P = d.spatial;
+    a.h = d.heads;
+    a.hk = d.kv_heads;
+    a.D = d.head_dim;
+    a.sinks = d.sinks;
+    a.window = d.window;
+    a.ring = d.ring;
+    a.sc = (d.scale > 0.f ? d.scale : 1.f / sqrtf((float)d.head_dim)) * 1.44269504f;
+    const hipStream_t st = (hipStream_t)stream;
+    // (a launch has less than 2^32 threads)
+    const int64_t blocks = ((int64_t)a.B * a.T * a.P * a.h + 3) / 4;
+    if (blocks > 0xffffff) return fail(DSATTN_EUNSUPPORTED, "%s: too large for the generic kernel", who);
+    if (d.io_dtype == DSATTN_F32)
+        hipLaunchKernelGGL((sink_generic_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((sink_generic_kernel<__bf16>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && Kcache) {
+        // in units that divide a frame's row
+        const bool wide = row * es % 16 == 0;
+        const int64_t units = wide ? row * es / 16 : row;
+        const unsigned x = (unsigned)std::min<int64_t>((units + 255) / 256, 256);
+        const dim3 grid(x, (unsigned)std::min(a.T, 65535), 2u * a.B);
+        if (wide)
+            hipLaunchKernelGGL((sink_append_kernel<uint4>), grid, dim3(256), 0, st, a, units);
+        else if (es == 4)
+            hipLaunchKernelGGL((sink_append_kernel<uint32_t>), grid, dim3(256), 0, st, a, units);
+        else
+            hipLaunchKernelGGL((sink_append_kernel<uint16_t>), grid, dim3(256), 0, st, a, units);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
+    return DSATTN_OK;
+}
+
+}  // extern "C"
