@@ -379,7 +379,8 @@ typedef struct dsattn_rms_desc {
  *              where the types are the same
  *   scales   : device, [rows] fp32; with DSATTN_E4M3 only, and then needed
  * Outputs overlap the inputs in no other way, and not each other.  Runs on the current device;
- * enqueues one kernel on `stream`; allocates nothing.  Errors: EINVAL, EHIP.
+ * enqueues one kernel on `stream`; allocates nothing.  Errors: EINVAL, EUNSUPPORTED (more
+ * rows than one launch takes: 2^32 threads, 8 to 1,024 a row), EHIP.
  */
 int dsattn_rmsnorm(const dsattn_rms_desc *desc, const void *X, const void *residual,
                    const float *gamma, void *sum, void *Y, float *scales, void *stream);

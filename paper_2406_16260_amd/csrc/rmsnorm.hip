@@ -2,8 +2,10 @@
 //
 //   s = x + r,  y = s * rsqrt(mean(s^2) + eps) * gamma,  optionally y / scale in 8 bits
 //
-// One workgroup a row: a pass for the sum of squares and for max|s gamma| (the largest |y| is that
-// times the row's factor, so a scale needs no pass of its own), a second one that writes.
+// Bound by memory: each number of x and r is read once, each of the sum and of y written once.  A row stays in
+// registers between the sum of its squares and its output: L lanes have it, NV pieces of V numbers each, and a
+// wavefront has 64 / L rows (L <= 64) or a workgroup one (L = 256 or 1,024).  The largest |y|, which a scale is
+// made of, is max|s gamma| times the row's factor, and so comes with the sum of squares.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -42,6 +44,141 @@ __device__ __forceinline__ float row_scale(float top, float rstd)
     return s < 0x1p-126f ? 0x1p-126f : s;  // (a NaN stays)
 }
 
+// L lanes a row, NV pieces of V numbers a lane.
+template <typename T, int V, int L, int NV, bool E8>
+__global__ __launch_bounds__(L <= 256 ? 256 : L) void rms_vec_kernel(const RmsArgs a)
+{
+    typedef T Piece __attribute__((ext_vector_type(V)));
+    typedef float Floats __attribute__((ext_vector_type(V)));
+    constexpr int THREADS = L <= 256 ? 256 : L, NW = L / 64;  // wavefronts of a row
+    const int64_t row = (int64_t)blockIdx.x * (THREADS / L) + threadIdx.x / L;
+    const int C = a.C, at = (int)(threadIdx.x % L) * V;
+    const bool there = row < a.rows;
+    const int64_t base = (there ? row : a.rows - 1) * C;
+    Piece x[NV], r[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = at + i * (L * V);
+        x[i] = r[i] = Piece{};
+        if (c < C) {
+            x[i] = *(const Piece *)((const T *)a.X + base + c);
+            if (a.R) r[i] = *(const Piece *)((const T *)a.R + base + c);
+        }
+    }
+    Floats s[NV], g[NV];
+    float ss = 0.f, top = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = at + i * (L * V);
+        g[i] = Floats{} + 1.f;
+        if (a.gamma && c < C) g[i] = *(const Floats *)(a.gamma + c);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            s[i][e] = a.R ? (float)x[i][e] + (float)r[i][e] : (float)x[i][e];
+            ss = fmaf(s[i][e], s[i][e], ss);
+            if constexpr (E8) top = max_or_nan(top, fabsf(s[i][e] * g[i][e]));
+        }
+    }
+#pragma unroll
+    for (int w = 1; w < (L < 64 ? L : 64); w *= 2) {
+        ss += __shfl_xor(ss, w);
+        if constexpr (E8) top = max_or_nan(top, __shfl_xor(top, w));
+    }
+    if constexpr (L > 64) {
+        __shared__ float part[2][NW];
+        if ((threadIdx.x & 63) == 0) {
+            part[0][threadIdx.x >> 6] = ss;
+            part[1][threadIdx.x >> 6] = top;
+        }
+        __syncthreads();
+        ss = part[0][0];
+        top = part[1][0];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            ss += part[0][w];
+            top = max_or_nan(top, part[1][w]);
+        }
+    }
+    const float rstd = 1.f / sqrtf(ss / (float)C + a.eps);
+    const float scale = E8 ? row_scale(top, rstd) : 1.f, inv = 1.f / scale;  // (its product with rstd may overflow)
+    if (!there) return;
+    if (E8 && at == 0) a.scales[row] = scale;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = at + i * (L * V);
+        if (c >= C) continue;
+        if (a.S) {
+            Piece t;
+#pragma unroll
+            for (int e = 0; e < V; ++e) t[e] = (T)s[i][e];
+            *(Piece *)((T *)a.S + base + c) = t;
+        }
+        Floats y;
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = s[i][e] * g[i][e] * rstd;
+        if constexpr (E8) {
+            uint8_t *to = (uint8_t *)a.Y + base + c;
+            if constexpr (V % 4 == 0) {
+                typedef int Words __attribute__((ext_vector_type(V / 4)));
+                Words w;
+#pragma unroll
+                for (int q = 0; q < V / 4; ++q) {
+                    w[q] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * q] * inv, y[4 * q + 1] * inv, 0, false);
+                    w[q] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * q + 2] * inv, y[4 * q + 3] * inv, w[q], true);
+                }
+                *(Words *)to = w;
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e) to[e] = to_e4m3(y[e] * inv);
+            }
+        } else {
+            Piece t;
+#pragma unroll
+            for (int e = 0; e < V; ++e) t[e] = (T)y[e];
+            *(Piece *)((T *)a.Y + base + c) = t;
+        }
+    }
+}
+
+// The kernel of a shape: the fewest lanes that hold the row in four pieces each (eight where its numbers go one by
+// one, in rows that are not whole 16-byte pieces); null: longer than 1,024 lanes hold.
+struct RmsKernel {
+    const void *fn;
+    int lanes;
+};
+template <typename T, int V, bool E8, int L>
+const void *rms_kernel_of(int nv)
+{
+    switch (nv) {
+    case 1: return (const void *)&rms_vec_kernel<T, V, L, 1, E8>;
+    case 2: return (const void *)&rms_vec_kernel<T, V, L, 2, E8>;
+    case 3: return (const void *)&rms_vec_kernel<T, V, L, 3, E8>;
+    case 4: return (const void *)&rms_vec_kernel<T, V, L, 4, E8>;
+    default: return nullptr;
+    }
+}
+template <typename T, int V, bool E8>
+RmsKernel rms_pick_of(int C)
+{
+    const int pieces = (C + V - 1) / V;
+    if (pieces <= 8) return {(const void *)&rms_vec_kernel<T, V, 8, 1, E8>, 8};
+    if (pieces <= 16) return {(const void *)&rms_vec_kernel<T, V, 16, 1, E8>, 16};
+    if (pieces <= 32) return {(const void *)&rms_vec_kernel<T, V, 32, 1, E8>, 32};
+    if (pieces <= 256) return {rms_kernel_of<T, V, E8, 64>((pieces + 63) / 64), 64};
+    if (V == 1 && pieces <= 512) return {(const void *)&rms_vec_kernel<T, V, 64, 8, E8>, 64};
+    if (pieces <= 1024) return {rms_kernel_of<T, V, E8, 256>((pieces + 255) / 256), 256};
+    if (V == 1 && pieces <= 2048) return {(const void *)&rms_vec_kernel<T, V, 256, 8, E8>, 256};
+    if (pieces <= 4096) return {rms_kernel_of<T, V, E8, 1024>((pieces + 1023) / 1024), 1024};
+    return {nullptr, 0};
+}
+template <typename T, bool E8>
+RmsKernel rms_pick(int C)
+{
+    constexpr int V = 16 / (int)sizeof(T);
+    return C % V == 0 ? rms_pick_of<T, V, E8>(C) : rms_pick_of<T, 1, E8>(C);
+}
+
+// Rows longer than that: a workgroup a row, two passes over it.
 template <typename T, bool E8>
 __global__ __launch_bounds__(256) void rms_row_kernel(const RmsArgs a)
 {
@@ -130,10 +267,23 @@ extern "C" int dsattn_rmsnorm(const dsattn_rms_desc *desc, const void *X, const 
     }
     const RmsArgs a{X, residual, gamma, sum, Y, scales, d.rows, d.channels, d.eps};
     const bool f32 = d.io_dtype == DSATTN_F32;
-    const void *fn = f32 ? (e8 ? (const void *)&rms_row_kernel<float, true> : (const void *)&rms_row_kernel<float, false>)
-                         : (e8 ? (const void *)&rms_row_kernel<__bf16, true> : (const void *)&rms_row_kernel<__bf16, false>);
+    const RmsKernel k = f32 ? (e8 ? rms_pick<float, true>(d.channels) : rms_pick<float, false>(d.channels))
+                            : (e8 ? rms_pick<__bf16, true>(d.channels) : rms_pick<__bf16, false>(d.channels));
+    const void *fn = k.fn;
+    unsigned groups = (unsigned)d.rows, threads = 256;
+    if (fn) {
+        const int per = k.lanes <= 256 ? 256 / k.lanes : 1;  // rows of a workgroup
+        groups = (unsigned)((d.rows + per - 1) / per);
+        threads = k.lanes <= 256 ? 256u : (unsigned)k.lanes;
+    } else {
+        fn = f32 ? (e8 ? (const void *)&rms_row_kernel<float, true> : (const void *)&rms_row_kernel<float, false>)
+                 : (e8 ? (const void *)&rms_row_kernel<__bf16, true> : (const void *)&rms_row_kernel<__bf16, false>);
+    }
+    // (a launch has less than 2^32 threads: rows of a workgroup in batches of launches would be needed past that)
+    if ((uint64_t)groups * threads > 0xffffffffull)
+        return fail(DSATTN_EUNSUPPORTED, "%s: too many rows for one launch", who);
     void *params[] = {(void *)&a};
-    const hipError_t e = hipLaunchKernel(fn, dim3((unsigned)d.rows), dim3(256), params, 0, (hipStream_t)stream);
+    const hipError_t e = hipLaunchKernel(fn, dim3(groups), dim3(threads), params, 0, (hipStream_t)stream);
     if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
     return DSATTN_OK;
 }
