@@ -1,0 +1,390 @@
+// The matrix-core kernels of dsattn_linear_act: both operands are rows of c_in numbers, a stage of the
+// contraction is one 128-byte line of each (32 fp32, 64 bf16 or 128 e4m3 channels), which goes straight
+// from memory into LDS, 16-byte chunks swizzled by their row.
+#pragma once
+
+namespace dsattn {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kRow = 128;  // bytes of an operand row in a stage
+constexpr int kXcds = 8;
+
+// s_waitcnt of at most n outstanding vector memory operations, and all LDS operations done
+__host__ __device__ constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4); }
+
+// What a kernel multiplies with.  A fragment is a lane's 16 bytes (32 in 8 bits) of an operand row; which
+// channels an instruction contracts is free as long as both operands agree.
+//   bf16  v_mfma_f32_16x16x32_bf16, two a stage: chunk 4 kk + lane / 16 of row lane % 16
+//   fp32  the same chunk, its four numbers with four v_mfma_f32_16x16x4_f32
+//   e4m3  v_mfma_f32_32x32x64_f8f6f4, two a stage: chunks 4 kk + lane / 32 and two further on, of row lane % 32.
+//         (16x16x128, one a stage, has the same rate and needs twice the fragments at a time.)  The instructions on
+//         8 bits, of every shape, line the products of a group up with its largest one and drop what is more than 13
+//         bits below it: 1.3e-5 of the result's 2-norm at 64 to 1,280 channels of normal numbers, 1/130 of a bf16
+//         output's own rounding.  So these serve a bf16 output; for an fp32 output
+//   e4m3w the numbers are converted to bf16, exactly, and multiplied with 16x16x32: fp32 sums at half the rate
+// Block: rows of a fragment, BS; the accumulator's element 4 q + e of lane l is channel 8 q + 4 (l / BS) + e
+// of the block of W rows and row l % BS of the block of X rows (q = 0 only where BS is 16).
+template <typename T>
+struct Mul {
+    static constexpr int BS = 16, QUADS = 1, kk_bytes = 64;
+    using Acc = f32x4;
+    using Frag = std::conditional_t<sizeof(T) == 4, f32x4, bf16x8>;
+    static __device__ __forceinline__ int offset(int lane, int kk) { return (((4 * kk) | (lane >> 4)) ^ (lane & 7)) * 16; }
+    static __device__ __forceinline__ Frag read(const unsigned char *row, int off) { return *(const Frag *)(row + off); }
+    static __device__ __forceinline__ Acc mul(const Frag &w, const Frag &x, Acc c)
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) c = __builtin_amdgcn_mfma_f32_16x16x4f32(w[s], x[s], c, 0, 0, 0);
+            return c;
+        } else {
+            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, c, 0, 0, 0);
+        }
+    }
+};
+template <>
+struct Mul<e4m3> {
+    static constexpr int BS = 32, QUADS = 4, kk_bytes = 64;
+    using Acc = f32x16;
+    using Frag = i32x8;
+    // (position p of row r holds chunk p ^ r % 8: the second chunk is two further on, two bits of the position changed)
+    static __device__ __forceinline__ int offset(int lane, int kk) { return (((4 * kk) | (lane >> 5)) ^ (lane & 7)) * 16; }
+    static __device__ __forceinline__ Frag read(const unsigned char *row, int off)
+    {
+        const i32x4 a = *(const i32x4 *)(row + off), b = *(const i32x4 *)(row + (off ^ 32));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    static __device__ __forceinline__ Acc mul(const Frag &w, const Frag &x, Acc c)
+    {
+        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 0, 0, 0, 0, 0, 0);
+    }
+};
+
+template <>
+struct Mul<e4m3w> {
+    static constexpr int BS = 16, QUADS = 1, kk_bytes = 64;
+    using Acc = f32x4;
+    struct Frag { bf16x8 half[2]; };
+    static __device__ __forceinline__ int offset(int lane, int kk) { return Mul<__bf16>::offset(lane, kk); }
+    static __device__ __forceinline__ Frag read(const unsigned char *row, int off)
+    {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        const i32x4 a = *(const i32x4 *)(row + off);
+        Frag f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a[w], 1.f, false);
+            const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a[w], 1.f, true);
+            f.half[w / 2][4 * (w & 1)] = lo[0];
+            f.half[w / 2][4 * (w & 1) + 1] = lo[1];
+            f.half[w / 2][4 * (w & 1) + 2] = hi[0];
+            f.half[w / 2][4 * (w & 1) + 3] = hi[1];
+        }
+        return f;
+    }
+    static __device__ __forceinline__ Acc mul(const Frag &w, const Frag &x, Acc c)
+    {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.half[0], x.half[0], c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.half[1], x.half[1], c, 0, 0, 0);
+    }
+};
+
+// 2^x on the instruction
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// x / 2 * (1 + erf(x / sqrt 2)): erf by the rational approximation 7.1.26 of Abramowitz and Stegun, off by at
+// most 1.5e-7: a fifth of erff()'s instructions, which an epilogue on the matrix cores' heels would feel.
+__device__ __forceinline__ float gelu_erf(float x)
+{
+    const float z = fabsf(x) * 0.70710678f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    const float q = p * t * exp2_fast(z * z * -1.44269504f);  // 1 - erf(z)
+    return 0.5f * x * (x < 0.f ? q : 2.f - q);
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_fast(float x)
+{
+    if constexpr (ACT == DSATTN_ACT_RELU) return x > 0.f || x != x ? x : 0.f;
+    if constexpr (ACT == DSATTN_ACT_GELU) return gelu_erf(x);
+    if constexpr (ACT == DSATTN_ACT_GELU_TANH) {
+        // -2 log2(e) sqrt(2 / pi) (x + 0.044715 x^3)
+        const float u = x * fmaf(x * x, -0.10294324f, -2.3022082f);
+        return x * __builtin_amdgcn_rcpf(1.f + exp2_fast(u));
+    }
+    if constexpr (ACT == DSATTN_ACT_SILU) return x * __builtin_amdgcn_rcpf(1.f + exp2_fast(x * -1.44269504f));
+    return x;
+}
+
+// f(activation as a constant): the switch is outside of the loops that f holds
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F &&f)
+{
+    switch (act) {
+    case DSATTN_ACT_RELU: f(std::integral_constant<int, DSATTN_ACT_RELU>{}); break;
+    case DSATTN_ACT_GELU: f(std::integral_constant<int, DSATTN_ACT_GELU>{}); break;
+    case DSATTN_ACT_GELU_TANH: f(std::integral_constant<int, DSATTN_ACT_GELU_TANH>{}); break;
+    case DSATTN_ACT_SILU: f(std::integral_constant<int, DSATTN_ACT_SILU>{}); break;
+    default: f(std::integral_constant<int, DSATTN_ACT_NONE>{}); break;
+    }
+}
+
+// What the epilogue wants of a wavefront's channels, in LDS: bias and scale of each column of its part (gated: of
+// the gate's columns and the value's).
+struct ColumnLds {
+    float *bias, *scale;
+};
+
+// The column of W behind row r of a column tile: set, and channel from the tile's first on.  Gated, blocks of BS
+// rows of the gate and of the value alternate, so that a lane holds both of a channel.
+template <int BS, bool GATED>
+__device__ __forceinline__ int set_of(int r) { return GATED ? (r / BS) & 1 : 0; }
+template <int BS, bool GATED>
+__device__ __forceinline__ int channel_of(int r) { return GATED ? r / (2 * BS) * BS + r % BS : r; }
+
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The epilogue of a wavefront's part, MB x NB blocks from row m0 and output channel c0 on: MP x NP blocks at a time go
+// through `stage`, the wavefront's own (BS MP) rows of (BS NP output channels + 4) floats, and leave as whole rows
+// with the residual added.  (fp32 on the way: the sum with the residual is rounded once.)
+template <typename T, int MB, int NB, int MP, int NP, bool GATED, typename TO, bool SCALED>
+__device__ __forceinline__ void epilogue(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], int64_t m0, int c0,
+                                         const float *bias, const float *wscale, float *stage, int lane)
+{
+    using M = Mul<T>;
+    constexpr int BS = M::BS, NO = GATED ? 2 : 1;      // blocks of W rows behind a block of channels
+    constexpr int CH = BS * NP / NO, SR = CH + 4;      // channels of a pass, floats of a staged row
+    constexpr int PER = 16 / (int)sizeof(TO);          // channels of a 16-byte piece
+    constexpr int CPR = CH / PER, PIECES = BS * MP * CPR;
+    static_assert(MB % MP == 0 && NB % NP == 0 && NP % NO == 0 && CH % PER == 0, "whole passes");
+    const int rl = lane % BS, cq = 4 * (lane / BS);
+    const bool whole = a.Cout % PER == 0;
+#pragma unroll
+    for (int ip = 0; ip < MB; ip += MP)
+#pragma unroll
+        for (int jp = 0; jp < NB; jp += NP) {
+            const int64_t mp = m0 + BS * ip;
+            const int cp = c0 + BS * jp / NO;
+            float xs[MP];
+            if constexpr (SCALED) {
+#pragma unroll
+                for (int i = 0; i < MP; ++i) {
+                    const int64_t m = mp + BS * i + rl;
+                    xs[i] = a.xs ? a.xs[m < a.M ? m : a.M - 1] : 1.f;
+                }
+            }
+            with_act(a.act, [&](auto act) __attribute__((always_inline)) {
+                constexpr int ACT = decltype(act)::value;
+#pragma unroll
+                for (int j = 0; j < NP; j += NO)
+#pragma unroll
+                    for (int q = 0; q < M::QUADS; ++q) {
+                        f32x4 b[NO], s[NO];
+#pragma unroll
+                        for (int k = 0; k < NO; ++k) {
+                            const int at = BS * (jp + j + k) + 8 * q + cq;
+                            b[k] = *(const f32x4 *)(bias + at);
+                            if constexpr (SCALED) s[k] = *(const f32x4 *)(wscale + at);
+                        }
+#pragma unroll
+                        for (int i = 0; i < MP; ++i) {
+                            f32x4 y;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                float z[NO];
+#pragma unroll
+                                for (int k = 0; k < NO; ++k) {
+                                    z[k] = acc[ip + i][jp + j + k][4 * q + e];
+                                    if constexpr (SCALED) z[k] *= xs[i] * s[k][e];
+                                    z[k] += b[k][e];
+                                }
+                                y[e] = act_fast<ACT>(z[0]);
+                                if constexpr (GATED) y[e] *= z[1];
+                            }
+                            *(f32x4 *)(stage + (BS * i + rl) * SR + BS * j / NO + 8 * q + cq) = y;
+                        }
+                    }
+            });
+            wave_sync();
+#pragma unroll
+            for (int it = 0; it < (PIECES + 63) / 64; ++it) {
+                const int p = lane + 64 * it;
+                const int row = p / CPR, ch = (p - row * CPR) * PER;
+                const int64_t m = mp + row;
+                if ((PIECES % 64 != 0 && p >= PIECES) || m >= a.M || cp + ch >= a.Cout) continue;
+                const float *from = stage + row * SR + ch;
+                const int64_t at = m * a.Cout + cp + ch;
+                TO *to = (TO *)a.Y + at;
+                const TO *r = (const TO *)a.R + at;
+                if (whole) {
+                    typedef TO Piece __attribute__((ext_vector_type(PER)));
+                    Piece y;
+                    if (a.R) {
+                        const Piece rv = *(const Piece *)r;
+#pragma unroll
+                        for (int e = 0; e < PER; ++e) y[e] = (TO)(from[e] + (float)rv[e]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < PER; ++e) y[e] = (TO)from[e];
+                    }
+                    *(Piece *)to = y;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        if (cp + ch + e < a.Cout) to[e] = (TO)(a.R ? from[e] + (float)r[e] : from[e]);
+                }
+            }
+            wave_sync();
+        }
+}
+
+// Bias and scale of column r of a column tile (of the tile from output channel n0 on); past c_out: 0.
+template <int BS, bool GATED, bool SCALED>
+__device__ __forceinline__ void column(const ActArgs &a, int n0, int r, float &bias, float &scale)
+{
+    const int set = set_of<BS, GATED>(r), c = n0 + channel_of<BS, GATED>(r);
+    const float *b = set ? a.bias[1] : a.bias[0], *s = set ? a.ws[1] : a.ws[0];
+    bias = b && c < a.Cout ? b[c] : 0.f;
+    if constexpr (SCALED) scale = !s ? 1.f : c < a.Cout ? s[c] : 0.f;
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *p, int64_t row, int64_t rows, int rowbytes)
+{
+    const int64_t left = max((int64_t)0, (rows - row) * rowbytes);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)((const unsigned char *)p + row * rowbytes), 0,
+                                             (int)min(left, (int64_t)0x7fffffff), 0x00020000);
+}
+
+constexpr uint32_t kOob = 0xfffffff0u;
+
+// One tile a workgroup: two LDS slots, two to four workgroups on a compute unit, whose loads and barriers hide behind each
+// other's multiplies.  A workgroup of WVM x WVN wavefronts computes a (BS MB WVM) x (BS NB WVN) tile.
+template <typename T, int MB, int NB, int WVM, int WVN, bool GATED, typename TO>
+__global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const ActArgs a)
+{
+    using M = Mul<T>;
+    constexpr int BS = M::BS, NW = WVM * WVN;
+    constexpr bool SCALED = sizeof(T) == 1;
+    constexpr int BM = BS * MB * WVM, BN = BS * NB * WVN;
+    constexpr int GA = BM / 8 / NW, GB = BN / 8 / NW;  // 8-row groups (one load instruction) per wavefront
+    static_assert(GA * 8 * NW == BM && GB * 8 * NW == BN, "the wavefronts share the loads evenly");
+    constexpr int ABYTES = BM * kRow, BUF = (BM + BN) * kRow;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    __shared__ __attribute__((aligned(16))) float cols[2][BN];
+
+    // workgroup -> tile: XCD x (= blockIdx % 8) owns a contiguous run of tiles
+    const int tile = (int)(blockIdx.x % kXcds) * a.per_xcd + (int)(blockIdx.x / kXcds);
+    if (tile >= a.tiles) return;  // whole workgroup: no barrier has been reached yet
+    const int mt = tile / a.tiles_n;
+    const int64_t m0 = (int64_t)mt * BM;
+    constexpr int BO = GATED ? BN / 2 : BN;  // output channels of the tile
+    const int n0 = (tile - mt * a.tiles_n) * BO;
+
+    const int lane = threadIdx.x & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wv / WVN, wn = wv - wm * WVN;
+    const int rowbytes = a.Cin * (int)sizeof(T);
+
+    // Lane l fetches chunk (l % 8) ^ (l / 8) of row l / 8 of an 8-row group.  Rows past the end and chunks past
+    // c_in read as zeros through the descriptors' range checks.
+    const int lr = lane >> 3, lc = (lane & 7) ^ lr;
+    const __amdgpu_buffer_rsrc_t xres = rows_from(a.X, m0, a.M, rowbytes);
+    const __amdgpu_buffer_rsrc_t wres0 = rows_from(a.W[0], n0, a.Cout, rowbytes);
+    const __amdgpu_buffer_rsrc_t wres1 = GATED ? rows_from(a.W[1], n0, a.Cout, rowbytes) : wres0;
+    const uint32_t xoff = (uint32_t)((wv * (8 * GA) + lr) * rowbytes + lc * 16);
+    int stage_no = 0;
+    auto issue_stage = [&]() __attribute__((always_inline)) {
+        const bool live = stage_no * kRow + lc * 16 < rowbytes;
+        unsigned char *as = smem + (stage_no & 1) * BUF + wv * (GA * 1024);
+        unsigned char *bs = smem + (stage_no & 1) * BUF + ABYTES + wv * (GB * 1024);
+#pragma unroll
+        for (int l = 0; l < GA; ++l)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                xres, (__attribute__((address_space(3))) void *)(as + l * 1024), 16,
+                live ? xoff + (uint32_t)(8 * l * rowbytes + stage_no * kRow) : kOob, 0, 0, 0);
+#pragma unroll
+        for (int l = 0; l < GB; ++l) {
+            const int r = wv * (8 * GB) + 8 * l;  // (an 8-row group is within a block)
+            const uint32_t off = (uint32_t)((channel_of<BS, GATED>(r) + lr) * rowbytes + lc * 16 + stage_no * kRow);
+            if (GATED && set_of<BS, GATED>(r))
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(wres1, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16,
+                                                         live ? off : kOob, 0, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(wres0, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16,
+                                                         live ? off : kOob, 0, 0, 0);
+        }
+        ++stage_no;
+    };
+    issue_stage();
+    for (int r = threadIdx.x; r < BN; r += 64 * NW) {
+        float b, s = 1.f;
+        column<BS, GATED, SCALED>(a, n0, r, b, s);
+        cols[0][r] = b;
+        if constexpr (SCALED) cols[1][r] = s;
+    }
+
+    typename M::Acc acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = typename M::Acc{};
+    int koff[2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) koff[kk] = M::offset(lane, kk);
+    const int abase = (wm * BS * MB + lane % BS) * kRow, bbase = ABYTES + (wn * BS * NB + lane % BS) * kRow;
+    const int stages = (rowbytes + kRow - 1) / kRow;
+    for (int ks = 0; ks < stages; ++ks) {
+        // This wavefront's loads of stage ks have landed and its reads of stage ks - 1 are done; behind the
+        // barrier everybody's are, and the slot of stage ks - 1 is free.
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if (ks + 1 < stages) issue_stage();
+        const unsigned char *buf = smem + (ks & 1) * BUF;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            typename M::Frag af[MB], bf[NB];
+#pragma unroll
+            for (int i = 0; i < MB; ++i) af[i] = M::read(buf + abase + i * (BS * kRow), koff[kk]);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) bf[j] = M::read(buf + bbase + j * (BS * kRow), koff[kk]);
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int i = 0; i < MB; ++i) acc[i][j] = M::mul(bf[j], af[i], acc[i][j]);
+        }
+    }
+    // everybody is through with the ring: it becomes the staging area
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    constexpr int CHP = BS * NB / (GATED ? 2 : 1);  // output channels of the part
+    // all of the part at once, or a block of rows, or half of its channels
+    constexpr int per = NW * BS * (CHP + 4) * 4;
+    constexpr int MP = MB * per <= 2 * BUF ? MB : 1, NP = MP * per <= 2 * BUF ? NB : NB / 2;
+    constexpr int SR = CHP * NP / NB + 4;
+    static_assert(NW * BS * MP * SR * 4 <= 2 * BUF, "the staging area fits in the ring");
+    epilogue<T, MB, NB, MP, NP, GATED, TO, SCALED>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, &cols[0][wn * BS * NB],
+                                                   &cols[1][wn * BS * NB], (float *)smem + wv * (BS * MP * SR), lane);
+}
+
+}  // namespace
+}  // namespace dsattn

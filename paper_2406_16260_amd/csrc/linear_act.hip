@@ -23,9 +23,11 @@ struct ActArgs {
     void *Y;
     int64_t M;
     int32_t Cin, Cout, n_w, act;
+    int32_t tiles_n, tiles, per_xcd;  // column tiles; all of them; ceil(tiles / 8)
 };
 
 struct e4m3 { uint8_t bits; };
+struct e4m3w { uint8_t bits; };  // the same, to be multiplied in 16 bits
 
 template <typename T>
 __device__ __forceinline__ float to_float(T x)
@@ -75,10 +77,77 @@ __global__ __launch_bounds__(256) void act_generic_kernel(const ActArgs a)
     ((Tout *)a.Y)[idx] = (Tout)y;
 }
 
+}  // namespace
+}  // namespace dsattn
+
+#include "act_tile.h"
+
+namespace dsattn {
+namespace {
+
+// Kernels of one tile shape, by operands, gate and output.
+struct ActVariant {
+    int rows, cols, waves, lds;  // tile (rows of X, rows of W of both sets), wavefronts, bytes of dynamic LDS
+    const void *fn[2][2];        // gated, fp32 output
+};
+#define DSATTN_ACT_TILE(T, MB, NB, WVM, WVN)                                                                        \
+    {Mul<T>::BS * MB * WVM, Mul<T>::BS * NB * WVN, WVM * WVN,                                                       \
+     2 * (Mul<T>::BS * MB * WVM + Mul<T>::BS * NB * WVN) * kRow,                                                    \
+     {{(const void *)&act_tile_kernel<T, MB, NB, WVM, WVN, false, __bf16>,                                          \
+       (const void *)&act_tile_kernel<T, MB, NB, WVM, WVN, false, float>},                                          \
+      {(const void *)&act_tile_kernel<T, MB, NB, WVM, WVN, true, __bf16>,                                           \
+       (const void *)&act_tile_kernel<T, MB, NB, WVM, WVN, true, float>}}}
+// (16-row blocks to the fp32 output's kernel, 32-row ones to the other)
+#define DSATTN_ACT_TILE_E4M3(MB, NB, WVM, WVN)                                                                      \
+    {32 * MB * WVM, 32 * NB * WVN, WVM * WVN, 2 * (32 * MB * WVM + 32 * NB * WVN) * kRow,                           \
+     {{(const void *)&act_tile_kernel<e4m3, MB, NB, WVM, WVN, false, __bf16>,                                       \
+       (const void *)&act_tile_kernel<e4m3w, 2 * MB, 2 * NB, WVM, WVN, false, float>},                              \
+      {(const void *)&act_tile_kernel<e4m3, MB, NB, WVM, WVN, true, __bf16>,                                        \
+       (const void *)&act_tile_kernel<e4m3w, 2 * MB, 2 * NB, WVM, WVN, true, float>}}}
+#define DSATTN_ACT_TILE_F32(MB, NB, WVM, WVN)                                                                       \
+    {16 * MB * WVM, 16 * NB * WVN, WVM * WVN, 2 * (16 * MB * WVM + 16 * NB * WVN) * kRow,                           \
+     {{nullptr, (const void *)&act_tile_kernel<float, MB, NB, WVM, WVN, false, float>},                             \
+      {nullptr, (const void *)&act_tile_kernel<float, MB, NB, WVM, WVN, true, float>}}}
+const ActVariant kBf16Variants[] = {DSATTN_ACT_TILE(__bf16, 2, 4, 4, 2), DSATTN_ACT_TILE(__bf16, 2, 2, 2, 2)};
+const ActVariant kF32Variants[] = {DSATTN_ACT_TILE_F32(2, 4, 4, 2), DSATTN_ACT_TILE_F32(2, 2, 2, 2)};
+const ActVariant kE4m3Variants[] = {DSATTN_ACT_TILE_E4M3(1, 2, 4, 2), DSATTN_ACT_TILE_E4M3(1, 2, 2, 1)};
+
+const ActVariant *act_pick(const dsattn_linear_act_desc &d, int64_t es)
+{
+    const int64_t rowbytes = d.c_in * es;
+    // rows are whole 16-byte chunks, and a tile's are addressed with 32-bit offsets
+    if (rowbytes % 16 != 0 || rowbytes * 256 >= ((int64_t)1 << 31) || (d.flags & DSATTN_FLAG_FORCE_GENERIC)) return nullptr;
+    const ActVariant *v = d.io_dtype == DSATTN_F32 ? kF32Variants : d.io_dtype == DSATTN_BF16 ? kBf16Variants : kE4m3Variants;
+    const int64_t cols = (int64_t)d.c_out * d.n_w;
+    auto tiles = [&](const ActVariant &t) { return (d.rows + t.rows - 1) / t.rows * ((cols + t.cols - 1) / t.cols); };
+    const ActVariant *best = tiles(v[0]) >= 384 ? &v[0] : &v[1];
+    // (a launch has less than 2^32 threads)
+    return tiles(*best) < ((int64_t)1 << 32) / (64 * best->waves) - kXcds ? best : nullptr;
+}
+
 bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
 {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
     return a && b && x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
+}
+
+// The default cap on dynamic LDS is 64 KB.
+template <size_t N>
+hipError_t raise_lds(const ActVariant (&table)[N])
+{
+    for (const ActVariant &v : table)
+        for (const auto &gated : v.fn)
+            for (const void *fn : gated) {
+                const hipError_t e = fn ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, v.lds) : hipSuccess;
+                if (e != hipSuccess) return e;
+            }
+    return hipSuccess;
+}
+hipError_t act_prepare()
+{
+    hipError_t e = raise_lds(kBf16Variants);
+    if (e == hipSuccess) e = raise_lds(kF32Variants);
+    return e == hipSuccess ? raise_lds(kE4m3Variants) : e;
 }
 
 int64_t dtype_bytes(int32_t t) { return t == DSATTN_F32 ? 4 : t == DSATTN_BF16 ? 2 : 1; }
@@ -140,10 +209,30 @@ extern "C" int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void 
         return fail(DSATTN_EINVAL, "%s: Y overlaps X or its scales", who);
     if (residual != Y && overlap(Y, yn, residual, yn))
         return fail(DSATTN_EINVAL, "%s: Y overlaps the residual without being it", who);
+    const bool f32 = d.out_dtype == DSATTN_F32;
+    if (const ActVariant *v = act_pick(d, es)) {
+        static std::atomic<uint64_t> prepared;  // devices whose kernels may use all of the LDS
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e == hipSuccess && (dev >= 64 || !(prepared.load(std::memory_order_acquire) >> dev & 1))) {
+            e = act_prepare();
+            if (e == hipSuccess && dev < 64) prepared.fetch_or((uint64_t)1 << dev, std::memory_order_release);
+        }
+        if (e == hipSuccess) {
+            const int cols = v->cols / d.n_w;
+            a.tiles_n = (d.c_out + cols - 1) / cols;
+            a.tiles = (int32_t)((d.rows + v->rows - 1) / v->rows) * a.tiles_n;
+            a.per_xcd = (a.tiles + kXcds - 1) / kXcds;
+            void *params[] = {&a};
+            e = hipLaunchKernel(v->fn[d.n_w == 2][f32], dim3((unsigned)a.per_xcd * kXcds), dim3(64 * v->waves), params,
+                                (size_t)v->lds, (hipStream_t)stream);
+        }
+        if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
+        return DSATTN_OK;
+    }
     // (a launch has less than 2^32 threads)
     const int64_t blocks = (d.rows * d.c_out + 255) / 256;
     if (blocks > 0xffffff) return fail(DSATTN_EUNSUPPORTED, "%s: too large for the generic kernel", who);
-    const bool f32 = d.out_dtype == DSATTN_F32;
     const void *fn = d.io_dtype == DSATTN_F32 ? (const void *)&act_generic_kernel<float, float>
                      : d.io_dtype == DSATTN_BF16
                          ? (f32 ? (const void *)&act_generic_kernel<__bf16, float> : (const void *)&act_generic_kernel<__bf16, __bf16>)
