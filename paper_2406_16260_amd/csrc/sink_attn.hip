@@ -22,6 +22,8 @@ struct SinkArgs {
     const int32_t *start, *counts;  // or null
     int32_t B, T, P, h, hk, D, sinks, window, ring;
     float sc;  // softmax scale * log2(e)
+    int32_t U, splits, fused;  // see sink_rows.h: units of a wavefront; parts of a row's frames; new frames are put into the cache
+    float *parts;              // partial results of the splits
 };
 
 // A stream's place: its first new frame, and how many there are.
@@ -40,6 +42,37 @@ __device__ __forceinline__ Stream stream_of(const SinkArgs &a, int b)
 __device__ __forceinline__ int slot_of(const SinkArgs &a, int f)
 {
     return f < a.sinks ? f : a.sinks + (f - a.sinks) % a.ring;
+}
+
+// The frames that the queries of the new frames t0 .. t1 see between them: the first ns, and the frames from lo on; n in all, and
+// frame(j) the j-th of them.
+struct Frames {
+    int ns, lo, n, base, base_slot;
+    __device__ __forceinline__ int frame(int j) const { return j < ns ? j : j + (lo - ns); }
+    // slot_of() for these frames: the ones behind the sinks are within one turn of the ring
+    __device__ __forceinline__ int slot(const SinkArgs &a, int f) const
+    {
+        const int s = base_slot + (f - base);
+        return f < a.sinks ? f : s >= a.sinks + a.ring ? s - a.ring : s;
+    }
+};
+__device__ __forceinline__ Frames frames_of(const SinkArgs &a, const Stream &s, int t0, int t1)
+{
+    Frames f;
+    f.lo = max(0, s.start + t0 - a.window + 1);
+    f.ns = min(a.sinks, f.lo);
+    f.n = f.ns + (s.start + t1 + 1 - f.lo);
+    f.base = max(f.lo, a.sinks);
+    f.base_slot = slot_of(a, f.base);
+    return f;
+}
+
+// A split's partial result for row r of a unit: maximum, sum, two unused numbers, weighted sum.
+constexpr int kPartHead = 4;
+__device__ __forceinline__ float *part_of(const SinkArgs &a, int b, int64_t unit, int r, int rows, int split)
+{
+    const int64_t row = (((int64_t)b * a.P * a.hk + unit) * rows + r) * a.splits + split;
+    return a.parts + row * (a.D + kPartHead);
 }
 
 // Row of frame f of stream b in K or V, or in their caches.
@@ -125,6 +158,49 @@ __global__ __launch_bounds__(256) void sink_append_kernel(const SinkArgs a, int6
     }
 }
 
+}  // namespace
+}  // namespace dsattn
+
+#include "sink_rows.h"
+
+namespace dsattn {
+namespace {
+
+// Joins the splits of a row: a wavefront a row, lane l has channels l, l + 64, ...
+template <typename T>
+__global__ __launch_bounds__(256) void sink_join_kernel(const SinkArgs a)
+{
+    const int g = a.h / a.hk, rows = a.T * g, lane = threadIdx.x & 63, D = a.D;
+    const int64_t all = (int64_t)a.B * a.P * a.hk * rows, id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (id >= all) return;
+    const int r = (int)(id % rows);
+    const int64_t unit = id / rows % ((int64_t)a.P * a.hk);
+    const int b = (int)(id / rows / ((int64_t)a.P * a.hk)), t = r / g;
+    if (t >= stream_of(a, b).count) return;
+    const float *parts = part_of(a, b, unit, r, rows, 0);
+    const int stride = D + kPartHead;
+    float top = -INFINITY;
+    for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, parts[s * stride]);
+    for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
+    const float shift = top == -INFINITY ? 0.f : top;
+    constexpr int R = kMaxDim / 64;
+    float l = 0.f, o[R] = {};
+    for (int s = 0; s < a.splits; ++s) {
+        const float *from = parts + s * stride;
+        const float f = __builtin_amdgcn_exp2f(from[0] - shift);
+        l = fmaf(from[1], f, l);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (lane + 64 * i < D) o[i] = fmaf(from[kPartHead + lane + 64 * i], f, o[i]);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int p = (int)(unit / a.hk), head = (int)(unit % a.hk) * g + r % g;
+    T *to = (T *)a.O + (((int64_t)b * a.T + t) * a.P + p) * a.h * D + (int64_t)head * D;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (lane + 64 * i < D) to[lane + 64 * i] = (T)(o[i] * inv);
+}
+
 bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
 {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
@@ -157,6 +233,27 @@ int sink_validate(const dsattn_sink_desc *d, const char *who)
     return DSATTN_OK;
 }
 
+// How a shape runs: all of it follows from the descriptor, so that the workspace does too.
+struct SinkLaunch {
+    RowsLaunch rows;
+    int splits = 1;
+};
+SinkLaunch sink_launch(const dsattn_sink_desc &d)
+{
+    SinkLaunch k{};
+    k.splits = 1;
+    if (d.flags & DSATTN_FLAG_FORCE_GENERIC) return k;
+    k.rows = rows_launch(d);
+    if (k.rows.fn) k.splits = k.rows.splits;
+    return k;
+}
+size_t sink_workspace_bytes(const dsattn_sink_desc &d)
+{
+    const SinkLaunch k = sink_launch(d);
+    if (k.splits == 1) return 0;
+    return (size_t)d.streams * d.spatial * d.heads * d.frames * k.splits * (d.head_dim + kPartHead) * sizeof(float);
+}
+
 }  // namespace
 }  // namespace dsattn
 
@@ -169,7 +266,7 @@ int dsattn_sink_workspace(const dsattn_sink_desc *desc, size_t *bytes)
     const int rc = sink_validate(desc, "dsattn_sink_workspace");
     if (rc != DSATTN_OK) return rc;
     if (!bytes) return fail(DSATTN_EINVAL, "dsattn_sink_workspace: null output");
-    *bytes = 0;
+    *bytes = sink_workspace_bytes(*desc);
     return DSATTN_OK;
 }
 
@@ -189,8 +286,7 @@ int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, cons
         return fail(DSATTN_EINVAL, "%s: pointers must be 16-byte aligned", who);
     if (((uintptr_t)start | (uintptr_t)counts) & 3u)
         return fail(DSATTN_EINVAL, "%s: start and counts must be 4-byte aligned", who);
-    size_t need = 0;
-    dsattn_sink_workspace(desc, &need);
+    const size_t need = sink_workspace_bytes(d);
     if (workspace_bytes < need || (need && !workspace))
         return fail(DSATTN_EINVAL, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
     const int64_t es = d.io_dtype == DSATTN_BF16 ? 2 : 4;
@@ -223,15 +319,36 @@ int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, cons
     a.ring = d.ring;
     a.sc = (d.scale > 0.f ? d.scale : 1.f / sqrtf((float)d.head_dim)) * 1.44269504f;
     const hipStream_t st = (hipStream_t)stream;
-    // (a launch has less than 2^32 threads)
-    const int64_t blocks = ((int64_t)a.B * a.T * a.P * a.h + 3) / 4;
-    if (blocks > 0xffffff) return fail(DSATTN_EUNSUPPORTED, "%s: too large for the generic kernel", who);
-    if (d.io_dtype == DSATTN_F32)
-        hipLaunchKernelGGL((sink_generic_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((sink_generic_kernel<__bf16>), dim3((unsigned)blocks), dim3(256), 0, st, a);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && Kcache) {
+    const SinkLaunch k = sink_launch(d);
+    const bool f32 = d.io_dtype == DSATTN_F32;
+    a.splits = k.splits;
+    a.parts = (float *)workspace;
+    hipError_t e = hipSuccess;
+    if (k.rows.fn) {
+        a.U = k.rows.U;
+        // (a frame that goes into the cache must not take a slot that another query of the call still reads)
+        a.fused = Kcache && d.window >= 1 && d.ring >= (int64_t)d.window + d.frames - 1;
+        void *params[] = {&a};
+        e = hipLaunchKernel(k.rows.fn, dim3((unsigned)k.rows.blocks), dim3(256), params, (size_t)k.rows.lds, st);
+    } else {
+        // (a launch has less than 2^32 threads)
+        const int64_t blocks = ((int64_t)a.B * a.T * a.P * a.h + 3) / 4;
+        if (blocks > 0xffffff) return fail(DSATTN_EUNSUPPORTED, "%s: too large for the generic kernel", who);
+        if (f32)
+            hipLaunchKernelGGL((sink_generic_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((sink_generic_kernel<__bf16>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && k.splits > 1) {
+        const unsigned blocks = (unsigned)(((int64_t)a.B * a.T * a.P * a.h + 3) / 4);
+        if (f32)
+            hipLaunchKernelGGL((sink_join_kernel<float>), dim3(blocks), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((sink_join_kernel<__bf16>), dim3(blocks), dim3(256), 0, st, a);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && Kcache && !a.fused) {
         // in units that divide a frame's row
         const bool wide = row * es % 16 == 0;
         const int64_t units = wide ? row * es / 16 : row;
