@@ -24,7 +24,12 @@ struct SinkArgs {
     float sc;  // softmax scale * log2(e)
     int32_t U, splits, fused;  // see sink_rows.h: units of a wavefront; parts of a row's frames; new frames are put into the cache
     float *parts;              // partial results of the splits
+    int32_t per_xcd, row_tiles;  // see sink_tile.h: workgroups of an XCD, row tiles of a unit, tasks in all
+    int64_t tasks;
 };
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // A stream's place: its first new frame, and how many there are.
 struct Stream {
@@ -90,22 +95,13 @@ __device__ __forceinline__ float wave_sum(float x)
     return x;
 }
 
-// Plain vector kernel for every shape: a wavefront a query and head, lane l has channels l, l + 64, ...
+// One query and head on a wavefront's vector ALUs: lane l has channels l, l + 64, ...
 constexpr int kMaxDim = 512;
 template <typename T>
-__global__ __launch_bounds__(256) void sink_generic_kernel(const SinkArgs a)
+__device__ __forceinline__ void vector_row(const SinkArgs &a, int b, const Stream &s, int t, int p, int g, int lane)
 {
-    const int64_t tasks = (int64_t)a.B * a.T * a.P * a.h;
-    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (id >= tasks) return;
-    const int lane = threadIdx.x & 63, D = a.D;
-    const int g = (int)(id % a.h);
-    const int64_t tok = id / a.h;  // (b T + t) P + p
-    const int p = (int)(tok % a.P);
-    const int t = (int)(tok / a.P % a.T), b = (int)(tok / a.P / a.T);
-    const Stream s = stream_of(a, b);
-    if (t >= s.count) return;
-    const int frame = s.start + t;
+    const int frame = s.start + t, D = a.D;
+    const int64_t id = (((int64_t)b * a.T + t) * a.P + p) * a.h + g;
     const T *q = (const T *)a.Q + id * D;
     const int64_t at = ((int64_t)p * a.hk + g / (a.h / a.hk)) * D;  // within a frame of K and V
     constexpr int R = kMaxDim / 64;
@@ -115,10 +111,9 @@ __global__ __launch_bounds__(256) void sink_generic_kernel(const SinkArgs a)
         qv[r] = lane + 64 * r < D ? (float)q[lane + 64 * r] * a.sc : 0.f;
         o[r] = 0.f;
     }
-    const int lo = (int)max((int64_t)0, (int64_t)frame - a.window + 1), ns = min(a.sinks, lo);
-    const int n = ns + (frame + 1 - lo);
-    for (int j = 0; j < n; ++j) {
-        const int f = j < ns ? j : lo + (j - ns);
+    const Frames fr = frames_of(a, s, t, t);
+    for (int j = 0; j < fr.n; ++j) {
+        const int f = fr.frame(j);
         const T *k = frame_row<T>(a, a.K, a.Kc, b, s, f) + at, *v = frame_row<T>(a, a.V, a.Vc, b, s, f) + at;
         float x = 0.f;
 #pragma unroll
@@ -138,6 +133,21 @@ __global__ __launch_bounds__(256) void sink_generic_kernel(const SinkArgs a)
 #pragma unroll
     for (int r = 0; r < R; ++r)
         if (lane + 64 * r < D) out[lane + 64 * r] = (T)(o[r] * inv);
+}
+
+// Plain vector kernel for every shape: a wavefront a query and head.
+template <typename T>
+__global__ __launch_bounds__(256) void sink_generic_kernel(const SinkArgs a)
+{
+    const int64_t tasks = (int64_t)a.B * a.T * a.P * a.h;
+    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (id >= tasks) return;
+    const int g = (int)(id % a.h);
+    const int64_t tok = id / a.h;  // (b T + t) P + p
+    const int p = (int)(tok % a.P);
+    const int t = (int)(tok / a.P % a.T), b = (int)(tok / a.P / a.T);
+    const Stream s = stream_of(a, b);
+    if (t < s.count) vector_row<T>(a, b, s, t, p, g, threadIdx.x & 63);
 }
 
 // New frames into the cache, in units that divide a frame's row: blockIdx.y is the new frame (and every
@@ -162,6 +172,7 @@ __global__ __launch_bounds__(256) void sink_append_kernel(const SinkArgs a, int6
 }  // namespace dsattn
 
 #include "sink_rows.h"
+#include "sink_tile.h"
 
 namespace dsattn {
 namespace {
@@ -195,6 +206,13 @@ __global__ __launch_bounds__(256) void sink_join_kernel(const SinkArgs a)
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int p = (int)(unit / a.hk), head = (int)(unit % a.hk) * g + r % g;
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < R; ++i) nan = nan || o[i] * inv != o[i] * inv;
+    if (__any(nan)) {  // (a hidden frame's infinity times its weight of zero)
+        vector_row<T>(a, b, stream_of(a, b), t, p, head, lane);
+        return;
+    }
     T *to = (T *)a.O + (((int64_t)b * a.T + t) * a.P + p) * a.h * D + (int64_t)head * D;
 #pragma unroll
     for (int i = 0; i < R; ++i)
@@ -236,7 +254,8 @@ int sink_validate(const dsattn_sink_desc *d, const char *who)
 // How a shape runs: all of it follows from the descriptor, so that the workspace does too.
 struct SinkLaunch {
     RowsLaunch rows;
-    int splits = 1;
+    TileLaunch tile;
+    int splits;
 };
 SinkLaunch sink_launch(const dsattn_sink_desc &d)
 {
@@ -244,7 +263,12 @@ SinkLaunch sink_launch(const dsattn_sink_desc &d)
     k.splits = 1;
     if (d.flags & DSATTN_FLAG_FORCE_GENERIC) return k;
     k.rows = rows_launch(d);
-    if (k.rows.fn) k.splits = k.rows.splits;
+    if (k.rows.fn) {
+        k.splits = k.rows.splits;
+        return k;
+    }
+    k.tile = tile_launch(d);
+    if (k.tile.fn) k.splits = k.tile.splits;
     return k;
 }
 size_t sink_workspace_bytes(const dsattn_sink_desc &d)
@@ -330,6 +354,15 @@ int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, cons
         a.fused = Kcache && d.window >= 1 && d.ring >= (int64_t)d.window + d.frames - 1;
         void *params[] = {&a};
         e = hipLaunchKernel(k.rows.fn, dim3((unsigned)k.rows.blocks), dim3(256), params, (size_t)k.rows.lds, st);
+    } else if (k.tile.fn) {
+        a.row_tiles = k.tile.row_tiles;
+        a.tasks = k.tile.tasks;
+        a.per_xcd = (int)((k.tile.workgroups + 7) / 8);
+        void *params[] = {&a};
+        // the default cap on dynamic LDS is 64 KB
+        if (k.tile.lds > 64 << 10) e = hipFuncSetAttribute(k.tile.fn, hipFuncAttributeMaxDynamicSharedMemorySize, k.tile.lds);
+        if (e == hipSuccess)
+            e = hipLaunchKernel(k.tile.fn, dim3((unsigned)a.per_xcd * 8u), dim3(256), params, (size_t)k.tile.lds, st);
     } else {
         // (a launch has less than 2^32 threads)
         const int64_t blocks = ((int64_t)a.B * a.T * a.P * a.h + 3) / 4;
