@@ -386,5 +386,257 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const ActAr
                                                    &cols[1][wn * BS * NB], (float *)smem + wv * (BS * MP * SR), lane);
 }
 
+// Large products: persistent workgroups of eight wavefronts (two per SIMD), at most one per compute unit, on 256 x 256 tiles.
+// The stages of successive tiles are one stream through two LDS slots: while a tile's last stage is multiplied out, the
+// next tile's first one is on its way into the other slot.  A wavefront's part is MB x NB blocks; its multiplies run in
+// halves (X blocks [0, HB), then [HB, MB)) so that one set of fragments, refilled in place under the multiplies, is
+// enough beside the accumulators: LDS reads and the next stage's loads sit between the matrix instructions by hand.
+template <typename T, int MB, int NB, bool GATED, typename TO>
+__global__ __launch_bounds__(512, 2) void act_stream_kernel(const ActArgs a)
+{
+    using M = Mul<T>;
+    constexpr int BS = M::BS, NW = 8, WVM = 4, WVN = 2;
+    constexpr bool SCALED = sizeof(T) == 1;
+    constexpr int BM = BS * MB * WVM, BN = BS * NB * WVN, BO = GATED ? BN / 2 : BN;
+    static_assert(BM == 256 && BN == 256, "tiles of 256 x 256");
+    constexpr int GA = BM / 8 / NW, GB = BN / 8 / NW, NL = GA + GB;
+    constexpr int ABYTES = BM * kRow, BUF = (BM + BN) * kRow;
+    // the epilogue's staging area, 32 rows x 64 channels of every wavefront: the slot that the tile's last stage has
+    // left, and the gap between the slots
+    constexpr int CHP = BS * NB / (GATED ? 2 : 1), MP = 32 / BS, NP = 64 * NB / CHP, SR = 64 + 4;
+    static_assert(CHP % 64 == 0, "passes of 64 channels");
+    constexpr int STAGING = NW * 32 * SR * 4, GAP = STAGING > BUF ? STAGING - BUF : 0, SLOT = BUF + GAP;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    float *cols = (float *)(smem + SLOT + BUF);  // [2][BN]: bias and scale of the tile's columns
+
+    // workgroup -> tiles: XCD x (= blockIdx % 8) owns tiles [x * per_xcd, (x + 1) * per_xcd), which its workgroups take in
+    // turn; column tiles are numbered in panels of a.panel of them, row tile by row tile (see act_panel())
+    const int xcd = (int)(blockIdx.x % kXcds), nper = (int)(gridDim.x / kXcds);
+    const int t_end = min((xcd + 1) * a.per_xcd, a.tiles);
+    int tile = xcd * a.per_xcd + (int)(blockIdx.x / kXcds);
+    if (tile >= t_end) return;  // whole workgroup: no barrier has been reached yet
+    const int tiles_m = a.tiles / a.tiles_n;
+    struct Place {
+        int first, c, mt;  // column tile first + c, row tile mt
+    };
+    const int dmt = nper / a.panel, dc = nper - dmt * a.panel;
+    auto step = [&](Place &p) __attribute__((always_inline)) {
+        p.c += dc;
+        p.mt += dmt;
+        if (p.c >= a.panel) {
+            p.c -= a.panel;
+            ++p.mt;
+        }
+        while (p.mt >= tiles_m) {
+            p.mt -= tiles_m;
+            p.first += a.panel;
+        }
+    };
+    Place place;
+    {
+        const int row = tile / a.panel, pn = row / tiles_m;
+        place = {pn * a.panel, tile - row * a.panel, row - pn * tiles_m};
+    }
+
+    const int lane = threadIdx.x & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wv / WVN, wn = wv - wm * WVN;
+    const int rowbytes = a.Cin * (int)sizeof(T);
+    const int stages = (rowbytes + kRow - 1) / kRow;
+    const int lr = lane >> 3, lc = (lane & 7) ^ lr;
+    // (the empty asm keeps an offset in a register: recomputing it would put multiplies between the matrix instructions)
+    int xoff = (wv * (8 * GA) + lr) * rowbytes + lc * 16;
+    asm volatile("" : "+v"(xoff));
+    int woff[GB];
+#pragma unroll
+    for (int l = 0; l < GB; ++l) {
+        woff[l] = (channel_of<BS, GATED>(wv * (8 * GB) + 8 * l) + lr) * rowbytes + lc * 16;
+        asm volatile("" : "+v"(woff[l]));
+    }
+    const int group_bytes = 8 * rowbytes;
+
+    // ---- the load side, up to two stages ahead of the multiplies
+    int ld_tile = tile, su_ks = 0, ld_gs = 0;
+    Place ld_place = place;
+    bool ld_has = true, ld_live = false;
+    __amdgpu_buffer_rsrc_t xres, wres0, wres1;
+    uint32_t ld_x = 0, ld_w = 0;
+    unsigned char *ld_as = smem, *ld_bs = smem;
+    auto ld_open = [&]() __attribute__((always_inline)) {
+        xres = rows_from(a.X, (int64_t)ld_place.mt * BM, a.M, rowbytes);
+        const int n0 = (ld_place.first + ld_place.c) * BO;
+        wres0 = rows_from(a.W[0], n0, a.Cout, rowbytes);
+        wres1 = GATED ? rows_from(a.W[1], n0, a.Cout, rowbytes) : wres0;
+        su_ks = 0;
+    };
+    // Past the workgroup's last tile every lane of the loads is an out-of-range one: no traffic, the same number of loads in
+    // flight, no branch among the multiplies.
+    auto stage_setup = [&]() __attribute__((always_inline)) {
+        if (su_ks == stages) {
+            ld_tile += nper;
+            ld_has = ld_tile < t_end;
+            if (ld_has) step(ld_place);
+            ld_open();
+        }
+        ld_live = ld_has && su_ks * kRow + lc * 16 < rowbytes;
+        ld_x = ld_w = (uint32_t)(su_ks * kRow);
+        ++su_ks;
+        const int slot = ld_gs++ & 1;
+        ld_as = smem + slot * SLOT + wv * (GA * 1024);
+        ld_bs = smem + slot * SLOT + ABYTES + wv * (GB * 1024);
+    };
+    auto issue_one = [&](int l) __attribute__((always_inline)) {
+        if (l < GA) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xres, (__attribute__((address_space(3))) void *)(ld_as + l * 1024), 16,
+                                                     ld_live ? (uint32_t)xoff + ld_x : kOob, 0, 0, 0);
+            ld_x += group_bytes;
+        } else {
+            // (a wavefront's 32 rows of W: one block of 32, or two of 16)
+            const bool second = GATED && (BS == 32 ? (wv & 1) : (l - GA) >= GB / 2);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? wres1 : wres0,
+                                                     (__attribute__((address_space(3))) void *)(ld_bs + (l - GA) * 1024), 16,
+                                                     ld_live ? (uint32_t)woff[l - GA] + ld_w : kOob, 0, 0, 0);
+        }
+    };
+    static_assert(GB * 8 == 32, "a wavefront loads 32 rows of W");
+
+    typename M::Acc acc[MB][NB];
+    auto clear_acc = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = typename M::Acc{};
+    };
+    clear_acc();
+    int koff[2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) koff[kk] = M::offset(lane, kk);
+    const int abase = (wm * BS * MB + lane % BS) * kRow, bbase = ABYTES + (wn * BS * NB + lane % BS) * kRow;
+    constexpr int HB = MB / 2, NMH = HB * NB;  // X blocks and multiplies of a half
+    typename M::Frag af[MB], bf[NB];
+    // the loads of the next stage are spread over this many multiplies from the barrier on (of 4 NMH between two of them)
+    constexpr int TAIL = NMH, kSpread = 5 * NMH / 2;
+    auto read_a = [&](const unsigned char *base, int kk, int i) __attribute__((always_inline)) {
+        af[i] = M::read(base + abase + i * (BS * kRow), koff[kk]);
+    };
+    auto read_b = [&](const unsigned char *base, int kk, int j) __attribute__((always_inline)) {
+        bf[j] = M::read(base + bbase + j * (BS * kRow), koff[kk]);
+    };
+    auto loads_at = [&](int g, bool do_loads) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < NL; ++q)
+            if (do_loads && (q * kSpread) / NL == g) {
+                issue_one(q);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    };
+    // first half of a sub-step; fetches the second half's X fragments
+    auto half1 = [&](const unsigned char *base, int kk, int g0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < NMH; ++m) {
+            loads_at(g0 + m, true);
+#pragma unroll
+            for (int r = 0; r < HB; ++r)
+                if ((r * (NMH / 2)) / HB == m) {
+                    read_a(base, kk, HB + r);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            // (back and forth: one operand stays the same from one multiply to the next)
+            const int j = m / HB, i0 = m - j * HB, i = j & 1 ? HB - 1 - i0 : i0;
+            acc[i][j] = M::mul(bf[j], af[i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // second half; fetches the next sub-step's first X fragments and, column by column, its W fragments
+    auto half2 = [&](const unsigned char *nbase, int nkk, int g0, bool do_loads) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < NMH; ++m) {
+            loads_at(g0 + m, do_loads);
+            const int j = m / HB, i0 = m - j * HB, i = j & 1 ? HB - 1 - i0 : i0;
+            if (i0 == 0 && j > 0) {
+                read_b(nbase, nkk, j - 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (i0 == HB - 1 && j < HB) {
+                read_a(nbase, nkk, j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            acc[HB + i][j] = M::mul(bf[j], af[HB + i], acc[HB + i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        read_b(nbase, nkk, NB - 1);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto issue_tail_loads = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < NL; ++q)
+            if ((q * kSpread) / NL < TAIL) issue_one(q);
+    };
+
+    ld_open();
+    stage_setup();
+#pragma unroll
+    for (int l = 0; l < NL; ++l) issue_one(l);
+    __builtin_amdgcn_s_waitcnt(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    stage_setup();
+    issue_tail_loads();
+#pragma unroll
+    for (int i = 0; i < HB; ++i) read_a(smem, 0, i);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) read_b(smem, 0, j);
+
+    int cs = 0;  // stages multiplied out so far
+    for (;;) {
+        const int64_t m0 = (int64_t)place.mt * BM;
+        const int n0 = (place.first + place.c) * BO;
+        // the tile's biases and scales: fetched now, put into LDS before the epilogue
+        float cb = 0.f, csc = 1.f;
+        if (threadIdx.x < BN) column<BS, GATED, SCALED>(a, n0, (int)threadIdx.x, cb, csc);
+        for (int ks = 0; ks < stages; ++ks, ++cs) {
+            const unsigned char *bufc = smem + (cs & 1) * SLOT, *bufn = smem + ((cs + 1) & 1) * SLOT;
+            // (the younger of two wavefronts on a SIMD goes first here, so that they draw apart)
+            if (wv >= NW / 2) __builtin_amdgcn_s_setprio(1);
+            half1(bufc, 0, TAIL);
+            half2(bufc, 1, TAIL + NMH, true);
+            __builtin_amdgcn_s_setprio(0);
+            stage_setup();
+            half1(bufc, 1, TAIL + 2 * NMH);
+            // this wavefront's loads of the next stage have landed and its reads of this slot are done; behind the barrier
+            // everybody's are
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            // (after a tile's last stage the slot just left is the staging area: its loads wait for the epilogue)
+            half2(bufn, 0, 0, ks + 1 < stages);
+        }
+        int le = lane;
+        asm volatile("" : "+v"(le));  // (or the epilogue's addresses are kept alive through the main loop)
+        if (threadIdx.x < BN) {
+            cols[threadIdx.x] = cb;
+            if constexpr (SCALED) cols[BN + threadIdx.x] = csc;
+        }
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        float *stage = (float *)(smem + (((cs - 1) & 1) ? SLOT + BUF - STAGING : 0)) + wv * (32 * SR);
+        epilogue<T, MB, NB, MP, NP, GATED, TO, SCALED>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, cols + wn * BS * NB,
+                                                       cols + BN + wn * BS * NB, stage, le);
+        tile += nper;
+        if (tile >= t_end) break;
+        step(place);
+        clear_acc();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();  // everybody has left the staging area and the columns
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        issue_tail_loads();
+    }
+}
+constexpr int kStreamLds = 2 * 65536 + (8 * 32 * 68 * 4 - 65536) + 2 * 256 * 4;
+
 }  // namespace
 }  // namespace dsattn

@@ -24,6 +24,7 @@ struct ActArgs {
     int64_t M;
     int32_t Cin, Cout, n_w, act;
     int32_t tiles_n, tiles, per_xcd;  // column tiles; all of them; ceil(tiles / 8)
+    int32_t panel;                    // persistent kernels: column tiles that are numbered together
 };
 
 struct e4m3 { uint8_t bits; };
@@ -89,6 +90,7 @@ namespace {
 struct ActVariant {
     int rows, cols, waves, lds;  // tile (rows of X, rows of W of both sets), wavefronts, bytes of dynamic LDS
     const void *fn[2][2];        // gated, fp32 output
+    bool stream = false;         // persistent workgroups
 };
 #define DSATTN_ACT_TILE(T, MB, NB, WVM, WVN)                                                                        \
     {Mul<T>::BS * MB * WVM, Mul<T>::BS * NB * WVN, WVM * WVN,                                                       \
@@ -108,21 +110,65 @@ struct ActVariant {
     {16 * MB * WVM, 16 * NB * WVN, WVM * WVN, 2 * (16 * MB * WVM + 16 * NB * WVN) * kRow,                           \
      {{nullptr, (const void *)&act_tile_kernel<float, MB, NB, WVM, WVN, false, float>},                             \
       {nullptr, (const void *)&act_tile_kernel<float, MB, NB, WVM, WVN, true, float>}}}
-const ActVariant kBf16Variants[] = {DSATTN_ACT_TILE(__bf16, 2, 4, 4, 2), DSATTN_ACT_TILE(__bf16, 2, 2, 2, 2)};
+const ActVariant kBf16Variants[] = {
+    {256, 256, 8, kStreamLds,
+     {{(const void *)&act_stream_kernel<__bf16, 4, 8, false, __bf16>, (const void *)&act_stream_kernel<__bf16, 4, 8, false, float>},
+      {(const void *)&act_stream_kernel<__bf16, 4, 8, true, __bf16>, (const void *)&act_stream_kernel<__bf16, 4, 8, true, float>}},
+     true},
+    DSATTN_ACT_TILE(__bf16, 2, 4, 4, 2), DSATTN_ACT_TILE(__bf16, 2, 2, 2, 2)};
 const ActVariant kF32Variants[] = {DSATTN_ACT_TILE_F32(2, 4, 4, 2), DSATTN_ACT_TILE_F32(2, 2, 2, 2)};
-const ActVariant kE4m3Variants[] = {DSATTN_ACT_TILE_E4M3(1, 2, 4, 2), DSATTN_ACT_TILE_E4M3(1, 2, 2, 1)};
+const ActVariant kE4m3Variants[] = {
+    {256, 256, 8, kStreamLds,
+     {{(const void *)&act_stream_kernel<e4m3, 2, 4, false, __bf16>, nullptr},
+      {(const void *)&act_stream_kernel<e4m3, 2, 4, true, __bf16>, nullptr}},
+     true},
+    DSATTN_ACT_TILE_E4M3(1, 2, 4, 2), DSATTN_ACT_TILE_E4M3(1, 2, 2, 1)};
 
 const ActVariant *act_pick(const dsattn_linear_act_desc &d, int64_t es)
 {
     const int64_t rowbytes = d.c_in * es;
     // rows are whole 16-byte chunks, and a tile's are addressed with 32-bit offsets
     if (rowbytes % 16 != 0 || rowbytes * 256 >= ((int64_t)1 << 31) || (d.flags & DSATTN_FLAG_FORCE_GENERIC)) return nullptr;
-    const ActVariant *v = d.io_dtype == DSATTN_F32 ? kF32Variants : d.io_dtype == DSATTN_BF16 ? kBf16Variants : kE4m3Variants;
+    const bool f32 = d.out_dtype == DSATTN_F32;
     const int64_t cols = (int64_t)d.c_out * d.n_w;
     auto tiles = [&](const ActVariant &t) { return (d.rows + t.rows - 1) / t.rows * ((cols + t.cols - 1) / t.cols); };
-    const ActVariant *best = tiles(v[0]) >= 384 ? &v[0] : &v[1];
+    const ActVariant *v, *best;
+    if (d.io_dtype == DSATTN_F32) {
+        v = kF32Variants;
+    } else {
+        v = d.io_dtype == DSATTN_BF16 ? kBf16Variants : kE4m3Variants;
+        // (tiles are numbered with 32 bits)
+        if (v->fn[d.n_w == 2][f32] && tiles(*v) >= 256 && tiles(*v) < (1 << 30)) return v;
+        ++v;
+    }
+    best = tiles(v[0]) >= 384 ? &v[0] : &v[1];
     // (a launch has less than 2^32 threads)
     return tiles(*best) < ((int64_t)1 << 32) / (64 * best->waves) - kXcds ? best : nullptr;
+}
+
+// Column tiles that are numbered together.  An XCD's 32 tiles in flight are this many wide and 32 / width row tiles high,
+// and read as many rows of X and of W as the sum of the two: the width for which that is least, in panels of one size.
+int act_panel(int tiles_n)
+{
+    int best = 1, least = 1 << 30;
+    for (int width = 1; width <= std::min(tiles_n, 32); ++width) {
+        const int rows = width + (32 + width - 1) / width;
+        if (tiles_n % width == 0 && rows < least) {
+            least = rows;
+            best = width;
+        }
+    }
+    return best;
+}
+
+int compute_units(int dev)
+{
+    static std::atomic<int> cached[64];
+    int n = dev < 64 ? cached[dev].load(std::memory_order_relaxed) : 0;
+    if (n > 0) return n;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
+    if (dev < 64) cached[dev].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
@@ -223,8 +269,10 @@ extern "C" int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void 
             a.tiles_n = (d.c_out + cols - 1) / cols;
             a.tiles = (int32_t)((d.rows + v->rows - 1) / v->rows) * a.tiles_n;
             a.per_xcd = (a.tiles + kXcds - 1) / kXcds;
+            a.panel = act_panel(a.tiles_n);
             void *params[] = {&a};
-            e = hipLaunchKernel(v->fn[d.n_w == 2][f32], dim3((unsigned)a.per_xcd * kXcds), dim3(64 * v->waves), params,
+            const int per_xcd = v->stream ? std::min(a.per_xcd, (compute_units(dev) + kXcds - 1) / kXcds) : a.per_xcd;
+            e = hipLaunchKernel(v->fn[d.n_w == 2][f32], dim3((unsigned)per_xcd * kXcds), dim3(64 * v->waves), params,
                                 (size_t)v->lds, (hipStream_t)stream);
         }
         if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
