@@ -99,18 +99,20 @@ struct Mul<e4m3w> {
 // 2^x on the instruction
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// x / 2 * (1 + erf(x / sqrt 2)): erf by the rational approximation 7.1.26 of Abramowitz and Stegun, off by at
-// most 1.5e-7: a fifth of erff()'s instructions, which an epilogue on the matrix cores' heels would feel.
+// x / 2 * (1 + erf(x / sqrt 2)) = x P(x), P the normal distribution's function: as x / (1 + 2^(-x p(x^2))), where p is fitted to
+// log2(P / (1 - P)) / x so that the largest error of P, anywhere, is least: 2.9e-8 with seven terms.  Two instructions on the
+// transcendental unit and ten others; with the rational approximation 7.1.26 of Abramowitz and Stegun (1.5e-7) it is two
+// and fifteen, and erff() several times that, which an epilogue at the matrix cores' heels feels.
 __device__ __forceinline__ float gelu_erf(float x)
 {
-    const float z = fabsf(x) * 0.70710678f;
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f));
-    float p = fmaf(1.061405429f, t, -1.453152027f);
-    p = fmaf(p, t, 1.421413741f);
-    p = fmaf(p, t, -0.284496736f);
-    p = fmaf(p, t, 0.254829592f);
-    const float q = p * t * exp2_fast(z * z * -1.44269504f);  // 1 - erf(z)
-    return 0.5f * x * (x < 0.f ? q : 2.f - q);
+    const float t = x * x;
+    float p = fmaf(t, -5.067244690e-09f, 3.816315040e-07f);
+    p = fmaf(p, t, -1.143983534e-05f);
+    p = fmaf(p, t, 1.595799422e-04f);
+    p = fmaf(p, t, 9.404923028e-05f);
+    p = fmaf(p, t, -1.048351218e-01f);
+    p = fmaf(p, t, -2.302209292e+00f);
+    return x * __builtin_amdgcn_rcpf(1.f + exp2_fast(x * p));
 }
 
 template <int ACT>
@@ -386,12 +388,160 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const ActAr
                                                    &cols[1][wn * BS * NB], (float *)smem + wv * (BS * MP * SR), lane);
 }
 
+// The same for the persistent kernels, in an area of its own beside the ring (the ring goes on loading meanwhile): 32 rows x 32
+// output channels at a time (16 rows in fp32), in the output's type.  The residual comes the same way in, one or two passes
+// ahead, and its sum is rounded once.
+constexpr int kPassBytes = 2304;  // of a wavefront
+template <typename T, int MB, int NB, bool GATED, typename TO, bool SCALED, int ACT, bool RES>
+__device__ __forceinline__ void epilogue_beside(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], int64_t m0, int c0,
+                                                const float *bias, const float *wscale, unsigned char *stage, int lane)
+{
+    using M = Mul<T>;
+    constexpr int BS = M::BS, NO = GATED ? 2 : 1, ES = (int)sizeof(TO);
+    constexpr int ROWS = 64 / ES > 16 ? 32 : 16, MP = ROWS / BS, NP = 32 * NO / BS;  // of a pass
+    static_assert(MP >= 1 && MB % MP == 0 && NB % NP == 0, "whole passes");
+    constexpr int SB = 32 * ES + (ES == 2 ? 8 : 16);  // bytes of a staged row
+    static_assert(ROWS * SB <= kPassBytes, "the staging area holds a pass");
+    constexpr int PER = 16 / ES, CPR = 32 / PER, IT = ROWS * CPR / 64;  // channels of a piece, pieces of a row, of a lane
+    constexpr int PASSES = (MB / MP) * (NB / NP), AHEAD = GATED && SCALED ? 1 : 2;
+    typedef TO Piece __attribute__((ext_vector_type(PER)));
+    typedef TO Quad __attribute__((ext_vector_type(4)));
+    typedef uint32_t Half __attribute__((ext_vector_type(2)));
+    const int rl = lane % BS, cq = 4 * (lane / BS);
+    const bool whole = a.Cout % PER == 0;
+    // this lane's piece `it` of a pass: row and channel within it, and their place from the part's first number on
+    auto row_of = [&](int it) __attribute__((always_inline)) { return (lane + 64 * it) / CPR; };
+    const int ch = lane % CPR * PER;
+    const int left_rows = (int)min(a.M - m0, (int64_t)(BS * MB)), left = a.Cout - c0;
+    auto row_at = [&](int pass) __attribute__((always_inline)) { return pass / (NB / NP) * ROWS; };
+    auto channel_at = [&](int pass) __attribute__((always_inline)) { return pass % (NB / NP) * 32; };
+    const int64_t base = m0 * a.Cout + c0;
+    auto there = [&](int pass, int it) __attribute__((always_inline)) {
+        return row_at(pass) + row_of(it) < left_rows && channel_at(pass) + ch < left;
+    };
+    auto offset = [&](int pass, int it) __attribute__((always_inline)) {
+        return (uint32_t)((row_at(pass) + row_of(it)) * a.Cout + channel_at(pass) + ch);
+    };
+    Piece r[AHEAD][IT];
+    auto fetch = [&](int pass) __attribute__((always_inline)) {
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            Piece x{};
+            if (there(pass, it)) {
+                const TO *from = (const TO *)a.R + base + offset(pass, it);
+                if (whole) {
+                    x = *(const Piece *)from;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        if (channel_at(pass) + ch + e < left) x[e] = from[e];
+                }
+            }
+            r[pass % AHEAD][it] = x;
+        }
+    };
+    // (8-byte accesses: a staged row of bf16 is 72 bytes)
+    auto put_piece = [&](unsigned char *at, const Piece &x) __attribute__((always_inline)) {
+        if constexpr (ES == 2) {
+            const i32x4 w = __builtin_bit_cast(i32x4, x);
+            *(Half *)at = Half{(uint32_t)w[0], (uint32_t)w[1]};
+            *(Half *)(at + 8) = Half{(uint32_t)w[2], (uint32_t)w[3]};
+        } else {
+            *(Piece *)at = x;
+        }
+    };
+    auto get_piece = [&](const unsigned char *at) __attribute__((always_inline)) {
+        if constexpr (ES == 2) {
+            const Half lo = *(const Half *)at, hi = *(const Half *)(at + 8);
+            return __builtin_bit_cast(Piece, (i32x4){(int)lo[0], (int)lo[1], (int)hi[0], (int)hi[1]});
+        } else {
+            return *(const Piece *)at;
+        }
+    };
+    if constexpr (RES) {
+#pragma unroll
+        for (int p = 0; p < AHEAD && p < PASSES; ++p) fetch(p);
+    }
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+        const int ip = pass / (NB / NP) * MP, jp = pass % (NB / NP) * NP;
+        float xs[MP];
+        if constexpr (SCALED) {
+#pragma unroll
+            for (int i = 0; i < MP; ++i) {
+                const int64_t m = m0 + BS * (ip + i) + rl;
+                xs[i] = a.xs ? a.xs[m < a.M ? m : a.M - 1] : 1.f;
+            }
+        }
+        if constexpr (RES) {
+#pragma unroll
+            for (int it = 0; it < IT; ++it) put_piece(stage + row_of(it) * SB + ch * ES, r[pass % AHEAD][it]);
+            wave_sync();
+            if (pass + AHEAD < PASSES) fetch(pass + AHEAD);
+        }
+#pragma unroll
+        for (int j = 0; j < NP; j += NO)
+#pragma unroll
+            for (int q = 0; q < M::QUADS; ++q) {
+                f32x4 b[NO], s[NO];
+#pragma unroll
+                for (int k = 0; k < NO; ++k) {
+                    const int at = BS * (jp + j + k) + 8 * q + cq;
+                    b[k] = *(const f32x4 *)(bias + at);
+                    if constexpr (SCALED) s[k] = *(const f32x4 *)(wscale + at);
+                }
+#pragma unroll
+                for (int i = 0; i < MP; ++i) {
+                    f32x4 y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float z[NO];
+#pragma unroll
+                        for (int k = 0; k < NO; ++k) {
+                            z[k] = acc[ip + i][jp + j + k][4 * q + e];
+                            if constexpr (SCALED) z[k] *= xs[i] * s[k][e];
+                            z[k] += b[k][e];
+                        }
+                        y[e] = act_fast<ACT>(z[0]);
+                        if constexpr (GATED) y[e] *= z[1];
+                    }
+                    unsigned char *at = stage + (BS * i + rl) * SB + (BS * j / NO + 8 * q + cq) * ES;
+                    Quad t;
+                    if constexpr (RES) {
+                        t = *(const Quad *)at;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] += (float)t[e];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t[e] = (TO)y[e];
+                    *(Quad *)at = t;
+                }
+            }
+        wave_sync();
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            const Piece x = get_piece(stage + row_of(it) * SB + ch * ES);
+            if (there(pass, it)) {
+                TO *to = (TO *)a.Y + base + offset(pass, it);
+                if (whole) {
+                    *(Piece *)to = x;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        if (channel_at(pass) + ch + e < left) to[e] = x[e];
+                }
+            }
+        }
+        wave_sync();
+    }
+}
+
 // Large products: persistent workgroups of eight wavefronts (two per SIMD), at most one per compute unit, on 256 x 256 tiles.
 // The stages of successive tiles are one stream through two LDS slots: while a tile's last stage is multiplied out, the
 // next tile's first one is on its way into the other slot.  A wavefront's part is MB x NB blocks; its multiplies run in
 // halves (X blocks [0, HB), then [HB, MB)) so that one set of fragments, refilled in place under the multiplies, is
 // enough beside the accumulators: LDS reads and the next stage's loads sit between the matrix instructions by hand.
-template <typename T, int MB, int NB, bool GATED, typename TO>
+template <typename T, int MB, int NB, bool GATED, typename TO, int ACT>
 __global__ __launch_bounds__(512, 2) void act_stream_kernel(const ActArgs a)
 {
     using M = Mul<T>;
@@ -401,13 +551,11 @@ __global__ __launch_bounds__(512, 2) void act_stream_kernel(const ActArgs a)
     static_assert(BM == 256 && BN == 256, "tiles of 256 x 256");
     constexpr int GA = BM / 8 / NW, GB = BN / 8 / NW, NL = GA + GB;
     constexpr int ABYTES = BM * kRow, BUF = (BM + BN) * kRow;
-    // the epilogue's staging area, 32 rows x 64 channels of every wavefront: the slot that the tile's last stage has
-    // left, and the gap between the slots
-    constexpr int CHP = BS * NB / (GATED ? 2 : 1), MP = 32 / BS, NP = 64 * NB / CHP, SR = 64 + 4;
-    static_assert(CHP % 64 == 0, "passes of 64 channels");
-    constexpr int STAGING = NW * 32 * SR * 4, GAP = STAGING > BUF ? STAGING - BUF : 0, SLOT = BUF + GAP;
+    constexpr int SLOT = BUF, CHP = BS * NB / (GATED ? 2 : 1), COLS = BS * NB;  // output channels, columns of the part
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    float *cols = (float *)(smem + SLOT + BUF);  // [2][BN]: bias and scale of the tile's columns
+    // behind the ring, of each wavefront: the epilogue's staging area; bias and scale of its columns
+    unsigned char *own = smem + 2 * SLOT + (threadIdx.x >> 6) * (kPassBytes + 2 * COLS * 4);
+    float *cols = (float *)(own + kPassBytes);
 
     // workgroup -> tiles: XCD x (= blockIdx % 8) owns tiles [x * per_xcd, (x + 1) * per_xcd), which its workgroups take in
     // turn; column tiles are numbered in panels of a.panel of them, row tile by row tile (see act_panel())
@@ -592,8 +740,9 @@ __global__ __launch_bounds__(512, 2) void act_stream_kernel(const ActArgs a)
         const int64_t m0 = (int64_t)place.mt * BM;
         const int n0 = (place.first + place.c) * BO;
         // the tile's biases and scales: fetched now, put into LDS before the epilogue
-        float cb = 0.f, csc = 1.f;
-        if (threadIdx.x < BN) column<BS, GATED, SCALED>(a, n0, (int)threadIdx.x, cb, csc);
+        float cb[COLS / 64], csc[COLS / 64];
+#pragma unroll
+        for (int u = 0; u < COLS / 64; ++u) column<BS, GATED, SCALED>(a, n0, wn * COLS + lane + 64 * u, cb[u], csc[u]);
         for (int ks = 0; ks < stages; ++ks, ++cs) {
             const unsigned char *bufc = smem + (cs & 1) * SLOT, *bufn = smem + ((cs + 1) & 1) * SLOT;
             // (the younger of two wavefronts on a SIMD goes first here, so that they draw apart)
@@ -610,33 +759,29 @@ __global__ __launch_bounds__(512, 2) void act_stream_kernel(const ActArgs a)
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
-            // (after a tile's last stage the slot just left is the staging area: its loads wait for the epilogue)
-            half2(bufn, 0, 0, ks + 1 < stages);
+            half2(bufn, 0, 0, true);
         }
         int le = lane;
         asm volatile("" : "+v"(le));  // (or the epilogue's addresses are kept alive through the main loop)
-        if (threadIdx.x < BN) {
-            cols[threadIdx.x] = cb;
-            if constexpr (SCALED) cols[BN + threadIdx.x] = csc;
+#pragma unroll
+        for (int u = 0; u < COLS / 64; ++u) {
+            cols[le + 64 * u] = cb[u];
+            if constexpr (SCALED) cols[COLS + le + 64 * u] = csc[u];
         }
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        float *stage = (float *)(smem + (((cs - 1) & 1) ? SLOT + BUF - STAGING : 0)) + wv * (32 * SR);
-        epilogue<T, MB, NB, MP, NP, GATED, TO, SCALED>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, cols + wn * BS * NB,
-                                                       cols + BN + wn * BS * NB, stage, le);
+        wave_sync();
+        if (a.R)
+            epilogue_beside<T, MB, NB, GATED, TO, SCALED, ACT, true>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, cols, cols + COLS,
+                                                                     own, le);
+        else
+            epilogue_beside<T, MB, NB, GATED, TO, SCALED, ACT, false>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, cols, cols + COLS,
+                                                                      own, le);
         tile += nper;
         if (tile >= t_end) break;
         step(place);
         clear_acc();
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_barrier();  // everybody has left the staging area and the columns
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        issue_tail_loads();
     }
 }
-constexpr int kStreamLds = 2 * 65536 + (8 * 32 * 68 * 4 - 65536) + 2 * 256 * 4;
+constexpr int kStreamLds = 2 * 512 * kRow + 8 * (kPassBytes + 2 * 128 * 4);
 
 }  // namespace
 }  // namespace dsattn

@@ -90,7 +90,12 @@ namespace {
 struct ActVariant {
     int rows, cols, waves, lds;  // tile (rows of X, rows of W of both sets), wavefronts, bytes of dynamic LDS
     const void *fn[2][2];        // gated, fp32 output
-    bool stream = false;         // persistent workgroups
+};
+
+// The persistent kernels, by gate, output and activation.
+constexpr int kActs = DSATTN_ACT_SILU + 1;
+struct StreamVariant {
+    const void *fn[2][2][kActs];
 };
 #define DSATTN_ACT_TILE(T, MB, NB, WVM, WVN)                                                                        \
     {Mul<T>::BS * MB * WVM, Mul<T>::BS * NB * WVN, WVM * WVN,                                                       \
@@ -110,40 +115,47 @@ struct ActVariant {
     {16 * MB * WVM, 16 * NB * WVN, WVM * WVN, 2 * (16 * MB * WVM + 16 * NB * WVN) * kRow,                           \
      {{nullptr, (const void *)&act_tile_kernel<float, MB, NB, WVM, WVN, false, float>},                             \
       {nullptr, (const void *)&act_tile_kernel<float, MB, NB, WVM, WVN, true, float>}}}
-const ActVariant kBf16Variants[] = {
-    {256, 256, 8, kStreamLds,
-     {{(const void *)&act_stream_kernel<__bf16, 4, 8, false, __bf16>, (const void *)&act_stream_kernel<__bf16, 4, 8, false, float>},
-      {(const void *)&act_stream_kernel<__bf16, 4, 8, true, __bf16>, (const void *)&act_stream_kernel<__bf16, 4, 8, true, float>}},
-     true},
-    DSATTN_ACT_TILE(__bf16, 2, 4, 4, 2), DSATTN_ACT_TILE(__bf16, 2, 2, 2, 2)};
+const ActVariant kBf16Variants[] = {DSATTN_ACT_TILE(__bf16, 2, 4, 4, 2), DSATTN_ACT_TILE(__bf16, 2, 2, 2, 2)};
 const ActVariant kF32Variants[] = {DSATTN_ACT_TILE_F32(2, 4, 4, 2), DSATTN_ACT_TILE_F32(2, 2, 2, 2)};
-const ActVariant kE4m3Variants[] = {
-    {256, 256, 8, kStreamLds,
-     {{(const void *)&act_stream_kernel<e4m3, 2, 4, false, __bf16>, nullptr},
-      {(const void *)&act_stream_kernel<e4m3, 2, 4, true, __bf16>, nullptr}},
-     true},
-    DSATTN_ACT_TILE_E4M3(1, 2, 4, 2), DSATTN_ACT_TILE_E4M3(1, 2, 2, 1)};
+const ActVariant kE4m3Variants[] = {DSATTN_ACT_TILE_E4M3(1, 2, 4, 2), DSATTN_ACT_TILE_E4M3(1, 2, 2, 1)};
 
-const ActVariant *act_pick(const dsattn_linear_act_desc &d, int64_t es)
+#define DSATTN_ACT_STREAM(T, MB, NB, G, TO)                                                       \
+    {                                                                                             \
+        (const void *)&act_stream_kernel<T, MB, NB, G, TO, DSATTN_ACT_NONE>,                      \
+            (const void *)&act_stream_kernel<T, MB, NB, G, TO, DSATTN_ACT_RELU>,                  \
+            (const void *)&act_stream_kernel<T, MB, NB, G, TO, DSATTN_ACT_GELU>,                  \
+            (const void *)&act_stream_kernel<T, MB, NB, G, TO, DSATTN_ACT_GELU_TANH>,             \
+            (const void *)&act_stream_kernel<T, MB, NB, G, TO, DSATTN_ACT_SILU>                   \
+    }
+const StreamVariant kBf16Stream = {{{DSATTN_ACT_STREAM(__bf16, 4, 8, false, __bf16), DSATTN_ACT_STREAM(__bf16, 4, 8, false, float)},
+                                    {DSATTN_ACT_STREAM(__bf16, 4, 8, true, __bf16), DSATTN_ACT_STREAM(__bf16, 4, 8, true, float)}}};
+const StreamVariant kE4m3Stream = {{{DSATTN_ACT_STREAM(e4m3, 2, 4, false, __bf16), {}}, {DSATTN_ACT_STREAM(e4m3, 2, 4, true, __bf16), {}}}};
+
+// How a product runs; fn null: the vector kernel.
+struct ActLaunch {
+    const void *fn = nullptr;
+    int rows, cols, waves, lds;
+    bool stream;
+};
+ActLaunch act_pick(const dsattn_linear_act_desc &d, int64_t es)
 {
     const int64_t rowbytes = d.c_in * es;
     // rows are whole 16-byte chunks, and a tile's are addressed with 32-bit offsets
-    if (rowbytes % 16 != 0 || rowbytes * 256 >= ((int64_t)1 << 31) || (d.flags & DSATTN_FLAG_FORCE_GENERIC)) return nullptr;
-    const bool f32 = d.out_dtype == DSATTN_F32;
-    const int64_t cols = (int64_t)d.c_out * d.n_w;
-    auto tiles = [&](const ActVariant &t) { return (d.rows + t.rows - 1) / t.rows * ((cols + t.cols - 1) / t.cols); };
-    const ActVariant *v, *best;
-    if (d.io_dtype == DSATTN_F32) {
-        v = kF32Variants;
-    } else {
-        v = d.io_dtype == DSATTN_BF16 ? kBf16Variants : kE4m3Variants;
-        // (tiles are numbered with 32 bits)
-        if (v->fn[d.n_w == 2][f32] && tiles(*v) >= 256 && tiles(*v) < (1 << 30)) return v;
-        ++v;
-    }
-    best = tiles(v[0]) >= 384 ? &v[0] : &v[1];
+    if (rowbytes % 16 != 0 || rowbytes * 256 >= ((int64_t)1 << 31) || d.c_out >= 1 << 22 || (d.flags & DSATTN_FLAG_FORCE_GENERIC))
+        return {};
+    const bool f32 = d.out_dtype == DSATTN_F32, gated = d.n_w == 2;
+    const int64_t n = (int64_t)d.c_out * d.n_w;
+    auto tiles = [&](int rows, int cols) { return (d.rows + rows - 1) / rows * ((n + cols - 1) / cols); };
+    const int64_t large = tiles(256, 256);
+    const StreamVariant *sv = d.io_dtype == DSATTN_BF16 ? &kBf16Stream : &kE4m3Stream;
+    // (tiles are numbered with 32 bits)
+    if (d.io_dtype != DSATTN_F32 && sv->fn[gated][f32][d.act] && large >= 256 && large < (1 << 30))
+        return {sv->fn[gated][f32][d.act], 256, 256, 8, kStreamLds, true};
+    const ActVariant *v = d.io_dtype == DSATTN_F32 ? kF32Variants : d.io_dtype == DSATTN_BF16 ? kBf16Variants : kE4m3Variants;
+    if (tiles(v[0].rows, v[0].cols) < 384) ++v;
     // (a launch has less than 2^32 threads)
-    return tiles(*best) < ((int64_t)1 << 32) / (64 * best->waves) - kXcds ? best : nullptr;
+    if (tiles(v->rows, v->cols) >= ((int64_t)1 << 32) / (64 * v->waves) - kXcds) return {};
+    return {v->fn[gated][f32], v->rows, v->cols, v->waves, v->lds, false};
 }
 
 // Column tiles that are numbered together.  An XCD's 32 tiles in flight are this many wide and 32 / width row tiles high,
@@ -175,25 +187,6 @@ bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
 {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
     return a && b && x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
-}
-
-// The default cap on dynamic LDS is 64 KB.
-template <size_t N>
-hipError_t raise_lds(const ActVariant (&table)[N])
-{
-    for (const ActVariant &v : table)
-        for (const auto &gated : v.fn)
-            for (const void *fn : gated) {
-                const hipError_t e = fn ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, v.lds) : hipSuccess;
-                if (e != hipSuccess) return e;
-            }
-    return hipSuccess;
-}
-hipError_t act_prepare()
-{
-    hipError_t e = raise_lds(kBf16Variants);
-    if (e == hipSuccess) e = raise_lds(kF32Variants);
-    return e == hipSuccess ? raise_lds(kE4m3Variants) : e;
 }
 
 int64_t dtype_bytes(int32_t t) { return t == DSATTN_F32 ? 4 : t == DSATTN_BF16 ? 2 : 1; }
@@ -256,25 +249,21 @@ extern "C" int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void 
     if (residual != Y && overlap(Y, yn, residual, yn))
         return fail(DSATTN_EINVAL, "%s: Y overlaps the residual without being it", who);
     const bool f32 = d.out_dtype == DSATTN_F32;
-    if (const ActVariant *v = act_pick(d, es)) {
-        static std::atomic<uint64_t> prepared;  // devices whose kernels may use all of the LDS
-        int dev = 0;
-        hipError_t e = hipGetDevice(&dev);
-        if (e == hipSuccess && (dev >= 64 || !(prepared.load(std::memory_order_acquire) >> dev & 1))) {
-            e = act_prepare();
-            if (e == hipSuccess && dev < 64) prepared.fetch_or((uint64_t)1 << dev, std::memory_order_release);
-        }
-        if (e == hipSuccess) {
-            const int cols = v->cols / d.n_w;
-            a.tiles_n = (d.c_out + cols - 1) / cols;
-            a.tiles = (int32_t)((d.rows + v->rows - 1) / v->rows) * a.tiles_n;
-            a.per_xcd = (a.tiles + kXcds - 1) / kXcds;
-            a.panel = act_panel(a.tiles_n);
-            void *params[] = {&a};
-            const int per_xcd = v->stream ? std::min(a.per_xcd, (compute_units(dev) + kXcds - 1) / kXcds) : a.per_xcd;
-            e = hipLaunchKernel(v->fn[d.n_w == 2][f32], dim3((unsigned)per_xcd * kXcds), dim3(64 * v->waves), params,
-                                (size_t)v->lds, (hipStream_t)stream);
-        }
+    const ActLaunch v = act_pick(d, es);
+    if (v.fn) {
+        const int cols = v.cols / d.n_w;
+        a.tiles_n = (d.c_out + cols - 1) / cols;
+        a.tiles = (int32_t)((d.rows + v.rows - 1) / v.rows) * a.tiles_n;
+        a.per_xcd = (a.tiles + kXcds - 1) / kXcds;
+        a.panel = act_panel(a.tiles_n);
+        int dev = 0, per_xcd = a.per_xcd;
+        hipError_t e = v.stream ? hipGetDevice(&dev) : hipSuccess;
+        if (v.stream) per_xcd = std::min(per_xcd, (compute_units(dev) + kXcds - 1) / kXcds);
+        // the default cap on dynamic LDS is 64 KB
+        if (e == hipSuccess && v.lds > 64 << 10) e = hipFuncSetAttribute(v.fn, hipFuncAttributeMaxDynamicSharedMemorySize, v.lds);
+        void *params[] = {&a};
+        if (e == hipSuccess)
+            e = hipLaunchKernel(v.fn, dim3((unsigned)per_xcd * kXcds), dim3(64 * v.waves), params, (size_t)v.lds, (hipStream_t)stream);
         if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
         return DSATTN_OK;
     }
