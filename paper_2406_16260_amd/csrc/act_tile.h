@@ -38,6 +38,7 @@ struct Mul {
     using Frag = std::conditional_t<sizeof(T) == 4, f32x4, bf16x8>;
     static __device__ __forceinline__ int offset(int lane, int kk) { return (((4 * kk) | (lane >> 4)) ^ (lane & 7)) * 16; }
     static __device__ __forceinline__ Frag read(const unsigned char *row, int off) { return *(const Frag *)(row + off); }
+    static __device__ __forceinline__ Frag from(const i32x4 &a) { return __builtin_bit_cast(Frag, a); }
     static __device__ __forceinline__ Acc mul(const Frag &w, const Frag &x, Acc c)
     {
         if constexpr (sizeof(T) == 4) {
@@ -73,10 +74,10 @@ struct Mul<e4m3w> {
     using Acc = f32x4;
     struct Frag { bf16x8 half[2]; };
     static __device__ __forceinline__ int offset(int lane, int kk) { return Mul<__bf16>::offset(lane, kk); }
-    static __device__ __forceinline__ Frag read(const unsigned char *row, int off)
+    static __device__ __forceinline__ Frag read(const unsigned char *row, int off) { return from(*(const i32x4 *)(row + off)); }
+    static __device__ __forceinline__ Frag from(const i32x4 &a)
     {
         typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        const i32x4 a = *(const i32x4 *)(row + off);
         Frag f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -265,6 +266,8 @@ __device__ __forceinline__ void column(const ActArgs &a, int n0, int r, float &b
     if constexpr (SCALED) scale = !s ? 1.f : c < a.Cout ? s[c] : 0.f;
 }
 
+constexpr uint32_t kOob = 0xfffffff0u;
+
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *p, int64_t row, int64_t rows, int rowbytes)
 {
     const int64_t left = max((int64_t)0, (rows - row) * rowbytes);
@@ -272,7 +275,115 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *p, int64
                                              (int)min(left, (int64_t)0x7fffffff), 0x00020000);
 }
 
-constexpr uint32_t kOob = 0xfffffff0u;
+// Small products: 32 rows of X by 32 rows of W a workgroup, whose eight wavefronts share the contraction: a wavefront takes
+// every eighth stage through two LDS slots of its own, waits for nobody, and the eight sums are added up in LDS at the
+// end, in an order that does not change.  What such a call takes is latency, an eighth of a row's length of it.  (Fetched in
+// the operands' layout, straight into registers, 16 neighbouring lanes are on 16 rows, and the first-level cache serves
+// them one by one: 160 x 1,280 x 1,280 7.6 us, 1 x 5,120 x 1,280 13 us.)
+constexpr int kSmallLds = 8 * 2 * 64 * kRow;
+template <typename T, bool GATED, typename TO>
+__global__ __launch_bounds__(512, 2) void act_small_kernel(const ActArgs a)
+{
+    using M = Mul<T>;
+    constexpr int BS = M::BS, NW = 8, SR = 36, SLOT = 64 * kRow;
+    constexpr bool SCALED = sizeof(T) == 1;
+    static_assert(BS == 16, "two blocks of 16 rows of either");
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    constexpr int BO = GATED ? 16 : 32;
+    const int mt = (int)blockIdx.x / a.tiles_n;
+    const int64_t m0 = (int64_t)mt * 32;
+    const int n0 = ((int)blockIdx.x - mt * a.tiles_n) * BO;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rowbytes = a.Cin * (int)sizeof(T);
+    // rows past the end read as zeros through the descriptors' range checks
+    const __amdgpu_buffer_rsrc_t xres = rows_from(a.X, m0, a.M, rowbytes);
+    const __amdgpu_buffer_rsrc_t wres0 = rows_from(a.W[0], n0, a.Cout, rowbytes);
+    const __amdgpu_buffer_rsrc_t wres1 = GATED ? rows_from(a.W[1], n0, a.Cout, rowbytes) : wres0;
+    unsigned char *mem = smem + wv * (2 * SLOT);
+    const int lr = lane >> 3, lc = (lane & 7) ^ lr;
+    const uint32_t off = (uint32_t)(lr * rowbytes + lc * 16), next = (uint32_t)(8 * rowbytes);
+    const int stages = (rowbytes + kRow - 1) / kRow;
+    auto issue = [&](int ks, int slot) __attribute__((always_inline)) {
+        const bool live = ks * kRow + lc * 16 < rowbytes;
+        const uint32_t o = off + (uint32_t)(ks * kRow);
+#pragma unroll
+        for (int l = 0; l < 4; ++l) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xres, (__attribute__((address_space(3))) void *)(mem + slot * SLOT + l * 1024), 16,
+                                                     live ? o + l * next : kOob, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(GATED && l >= 2 ? wres1 : wres0,
+                                                     (__attribute__((address_space(3))) void *)(mem + slot * SLOT + 4096 + l * 1024), 16,
+                                                     live ? o + (GATED ? l & 1 : l) * next : kOob, 0, 0, 0);
+        }
+    };
+    f32x4 acc[2][2] = {};
+    int koff[2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) koff[kk] = M::offset(lane, kk);
+    if (wv < stages) issue(wv, 0);
+    int slot = 0;
+    for (int ks = wv; ks < stages; ks += NW) {
+        const bool more = ks + NW < stages;
+        if (more) issue(ks + NW, slot ^ 1);
+        asm volatile("" ::: "memory");
+        if (more)
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(8));  // all but the stage just asked for have landed
+        else
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        const unsigned char *buf = mem + slot * SLOT + l16 * kRow;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            typename M::Frag x[2], w[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                x[i] = M::read(buf + i * (16 * kRow), koff[kk]);
+                w[i] = M::read(buf + 4096 + i * (16 * kRow), koff[kk]);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[i][j] = M::mul(w[j], x[i], acc[i][j]);
+        }
+        // the slot's reads are done before it is asked to be filled again
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // (LDS operations only)
+        asm volatile("" ::: "memory");
+        slot ^= 1;
+    }
+    // the sums, in the place of the wavefront's slots
+    float(*sums)[32][SR] = (float(*)[32][SR])smem;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *(f32x4 *)&sums[wv][16 * i + l16][16 * j + 4 * lg] = acc[i][j];
+    __syncthreads();
+    const int row = (int)threadIdx.x >> 4, c = (int)threadIdx.x & 15;
+    const int64_t m = m0 + row;
+    if (m >= a.M) return;
+    const float xs = SCALED && a.xs ? a.xs[m] : 1.f;
+#pragma unroll
+    for (int o = 0; o < BO / 16; ++o) {
+        const int ch = n0 + c + 16 * o;
+        if (ch >= a.Cout) continue;
+        float z[GATED ? 2 : 1];
+#pragma unroll
+        for (int k = 0; k < (GATED ? 2 : 1); ++k) {
+            z[k] = 0.f;
+#pragma unroll
+            for (int v = 0; v < NW; ++v) z[k] += sums[v][row][c + 16 * (GATED ? k : o)];
+            if (SCALED) z[k] *= a.ws[k] ? xs * a.ws[k][ch] : xs;
+            if (a.bias[k]) z[k] += a.bias[k][ch];
+        }
+        float y = 0.f;
+        with_act(a.act, [&](auto act) __attribute__((always_inline)) { y = act_fast<decltype(act)::value>(z[0]); });
+        if constexpr (GATED) y *= z[1];
+        if (a.R) y += (float)((const TO *)a.R)[m * a.Cout + ch];
+        ((TO *)a.Y)[m * a.Cout + ch] = (TO)y;
+    }
+}
 
 // One tile a workgroup: two LDS slots, two to four workgroups on a compute unit, whose loads and barriers hide behind each
 // other's multiplies.  A workgroup of WVM x WVN wavefronts computes a (BS MB WVM) x (BS NB WVN) tile.
@@ -394,7 +505,8 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const ActAr
 constexpr int kPassBytes = 2304;  // of a wavefront
 template <typename T, int MB, int NB, bool GATED, typename TO, bool SCALED, int ACT, bool RES>
 __device__ __forceinline__ void epilogue_beside(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], int64_t m0, int c0,
-                                                const float *bias, const float *wscale, unsigned char *stage, int lane)
+                                                const float *bias, const float *wscale, const float (&xscale)[MB],
+                                                unsigned char *stage, int lane)
 {
     using M = Mul<T>;
     constexpr int BS = M::BS, NO = GATED ? 2 : 1, ES = (int)sizeof(TO);
@@ -465,14 +577,6 @@ __device__ __forceinline__ void epilogue_beside(const ActArgs &a, const typename
 #pragma unroll
     for (int pass = 0; pass < PASSES; ++pass) {
         const int ip = pass / (NB / NP) * MP, jp = pass % (NB / NP) * NP;
-        float xs[MP];
-        if constexpr (SCALED) {
-#pragma unroll
-            for (int i = 0; i < MP; ++i) {
-                const int64_t m = m0 + BS * (ip + i) + rl;
-                xs[i] = a.xs ? a.xs[m < a.M ? m : a.M - 1] : 1.f;
-            }
-        }
         if constexpr (RES) {
 #pragma unroll
             for (int it = 0; it < IT; ++it) put_piece(stage + row_of(it) * SB + ch * ES, r[pass % AHEAD][it]);
@@ -499,7 +603,7 @@ __device__ __forceinline__ void epilogue_beside(const ActArgs &a, const typename
 #pragma unroll
                         for (int k = 0; k < NO; ++k) {
                             z[k] = acc[ip + i][jp + j + k][4 * q + e];
-                            if constexpr (SCALED) z[k] *= xs[i] * s[k][e];
+                            if constexpr (SCALED) z[k] *= xscale[ip + i] * s[k][e];
                             z[k] += b[k][e];
                         }
                         y[e] = act_fast<ACT>(z[0]);
@@ -743,6 +847,13 @@ __global__ __launch_bounds__(512, 2) void act_stream_kernel(const ActArgs a)
         float cb[COLS / 64], csc[COLS / 64];
 #pragma unroll
         for (int u = 0; u < COLS / 64; ++u) column<BS, GATED, SCALED>(a, n0, wn * COLS + lane + 64 * u, cb[u], csc[u]);
+        // (and the scales of its rows: a load in the epilogue would be waited for behind the stores)
+        float xs[MB];
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+            const int64_t m = m0 + BS * (wm * MB + i) + lane % BS;
+            xs[i] = SCALED && a.xs ? a.xs[m < a.M ? m : a.M - 1] : 1.f;
+        }
         for (int ks = 0; ks < stages; ++ks, ++cs) {
             const unsigned char *bufc = smem + (cs & 1) * SLOT, *bufn = smem + ((cs + 1) & 1) * SLOT;
             // (the younger of two wavefronts on a SIMD goes first here, so that they draw apart)
@@ -771,10 +882,10 @@ __global__ __launch_bounds__(512, 2) void act_stream_kernel(const ActArgs a)
         wave_sync();
         if (a.R)
             epilogue_beside<T, MB, NB, GATED, TO, SCALED, ACT, true>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, cols, cols + COLS,
-                                                                     own, le);
+                                                                     xs, own, le);
         else
             epilogue_beside<T, MB, NB, GATED, TO, SCALED, ACT, false>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, cols, cols + COLS,
-                                                                      own, le);
+                                                                      xs, own, le);
         tile += nper;
         if (tile >= t_end) break;
         step(place);

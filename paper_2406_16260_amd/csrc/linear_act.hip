@@ -119,6 +119,15 @@ const ActVariant kBf16Variants[] = {DSATTN_ACT_TILE(__bf16, 2, 4, 4, 2), DSATTN_
 const ActVariant kF32Variants[] = {DSATTN_ACT_TILE_F32(2, 4, 4, 2), DSATTN_ACT_TILE_F32(2, 2, 2, 2)};
 const ActVariant kE4m3Variants[] = {DSATTN_ACT_TILE_E4M3(1, 2, 4, 2), DSATTN_ACT_TILE_E4M3(1, 2, 2, 1)};
 
+// The kernels of small products: gated, fp32 output.
+#define DSATTN_ACT_SMALL(T, F32)                                                                  \
+    {F32 ? (const void *)&act_small_kernel<T, false, float> : (const void *)&act_small_kernel<T, false, __bf16>, \
+     F32 ? (const void *)&act_small_kernel<T, true, float> : (const void *)&act_small_kernel<T, true, __bf16>}
+const void *const kSmall[3][2][2] = {  // by type of the operands, fp32 output, gate
+    {{nullptr, nullptr}, DSATTN_ACT_SMALL(float, true)},
+    {DSATTN_ACT_SMALL(__bf16, false), DSATTN_ACT_SMALL(__bf16, true)},
+    {DSATTN_ACT_SMALL(e4m3w, false), DSATTN_ACT_SMALL(e4m3w, true)}};
+
 #define DSATTN_ACT_STREAM(T, MB, NB, G, TO)                                                       \
     {                                                                                             \
         (const void *)&act_stream_kernel<T, MB, NB, G, TO, DSATTN_ACT_NONE>,                      \
@@ -131,11 +140,51 @@ const StreamVariant kBf16Stream = {{{DSATTN_ACT_STREAM(__bf16, 4, 8, false, __bf
                                     {DSATTN_ACT_STREAM(__bf16, 4, 8, true, __bf16), DSATTN_ACT_STREAM(__bf16, 4, 8, true, float)}}};
 const StreamVariant kE4m3Stream = {{{DSATTN_ACT_STREAM(e4m3, 2, 4, false, __bf16), {}}, {DSATTN_ACT_STREAM(e4m3, 2, 4, true, __bf16), {}}}};
 
+// Whether the small kernel is faster than 64 x 64 tiles, by estimates in us: rounds of workgroups on the 256 compute units, and
+// the time of a stage (of all of a row's in the tile kernel, of its eighth in the small one).  Measured us in a captured graph,
+// small and 64 x 64, rows x c_in x c_out:
+//                                       bf16            fp32            e4m3
+//       1 x   320 x 1,280            2.9   3.5       4.2   8.0       3.0   3.4
+//       1 x 5,120 x 1,280            7.1  21.7      23.8  96.6       6.1  13.7
+//     160 x 1,280 x 1,280            4.1   7.5       8.8  26.7       4.0   5.9
+//     320 x 1,280 x 1,280            6.7   7.7      15.5  27.5       6.4   6.0
+//     640 x   640 x   640            5.5   5.1      10.0  14.9       5.4   4.5
+//     100 x 4,096 x 4,096           17.0  32.0      46.5  79.5      12.3  17.6
+//     640 x 1,280 x 1,280           12.3   8.8      30.0  28.0      11.6   6.3
+bool small_is_faster(int32_t type, int64_t small_tiles, int64_t stages)
+{
+    static const double small_stage[] = {0.17, 0.07, 0.1}, tile_stage[] = {0.6, 0.27, 0.35};  // by dsattn_dtype
+    const double rounds = (double)((small_tiles + 255) / 256);
+    return 1.5 + rounds * (1.2 + small_stage[type] * (double)stages) < 2.0 + tile_stage[type] * (double)stages;
+}
+
+// Estimated us of `tiles` tiles of 256 x 256 (persistent), 128 x 128 or 64 x 64 and `stages` stages, bf16 or 8 bits: a start,
+// and per round on the compute units the stages of a tile and what its start and end cost (two workgroups of the 128 x 128
+// kernel share a unit, so that a round of it is 512 tiles).  Measured us in a captured graph, bf16 and e4m3, rows x c_in x c_out:
+//                                  64 x 64       128 x 128     256 x 256
+//      2,560 x 1,280 x 1,280     17.8  10.3     18.1   9.7    27.9  17.0
+//      5,120 x 1,280 x 1,280     29.8  18.6     23.8  15.5    30.0  19.1
+//     10,240 x 1,280 x 1,280     55.8  30.8     43.1  26.7    34.0  21.4
+//     16,000 x 1,280 x 1,280     79.8  46.1     60.5  35.1    57.6  35.2
+//     20,000 x 1,280 x   320     29.0  18.9     23.3  15.8    28.9  19.4
+//     40,960 x   320 x   320     19.2  17.4     17.6  14.4    22.4  19.7
+//      8,000 x   640 x   640     13.5  10.8     13.1  10.1    17.9  12.8
+double tile_estimate(int size, int64_t tiles, int64_t stages)
+{
+    const double st = (double)stages, n = (double)tiles;
+    const int64_t full = tiles / 512, rest = tiles - 512 * full, rounds = (tiles + 255) / 256;
+    if (size == 256) return 3.0 + (double)rounds * (1.22 * st + 5.0);
+    if (size == 128)
+        return 3.0 + (double)full * (0.95 * st + 2.0) + (rest > 256 ? 0.82 * st + 2.6 : rest > 0 ? 0.61 * st + 2.9 : 0.0);
+    static const double stage[] = {0.25, 0.3, 0.41, 0.61};
+    return 4.0 + 1.3e-3 * n + st * (rounds > 4 ? std::max(1.0, 8.2e-4 * n) : stage[rounds - 1]);
+}
+
 // How a product runs; fn null: the vector kernel.
 struct ActLaunch {
     const void *fn = nullptr;
     int rows, cols, waves, lds;
-    bool stream;
+    bool stream, small;
 };
 ActLaunch act_pick(const dsattn_linear_act_desc &d, int64_t es)
 {
@@ -146,16 +195,23 @@ ActLaunch act_pick(const dsattn_linear_act_desc &d, int64_t es)
     const bool f32 = d.out_dtype == DSATTN_F32, gated = d.n_w == 2;
     const int64_t n = (int64_t)d.c_out * d.n_w;
     auto tiles = [&](int rows, int cols) { return (d.rows + rows - 1) / rows * ((n + cols - 1) / cols); };
-    const int64_t large = tiles(256, 256);
-    const StreamVariant *sv = d.io_dtype == DSATTN_BF16 ? &kBf16Stream : &kE4m3Stream;
-    // (tiles are numbered with 32 bits)
-    if (d.io_dtype != DSATTN_F32 && sv->fn[gated][f32][d.act] && large >= 256 && large < (1 << 30))
-        return {sv->fn[gated][f32][d.act], 256, 256, 8, kStreamLds, true};
+    const int64_t stages = (rowbytes + kRow - 1) / kRow, large = tiles(256, 256);
+    if (small_is_faster(d.io_dtype, tiles(32, 32), stages))
+        return {kSmall[d.io_dtype][f32][gated], 32, 32, 8, kSmallLds, false, true};
     const ActVariant *v = d.io_dtype == DSATTN_F32 ? kF32Variants : d.io_dtype == DSATTN_BF16 ? kBf16Variants : kE4m3Variants;
-    if (tiles(v[0].rows, v[0].cols) < 384) ++v;
+    if (d.io_dtype == DSATTN_F32) {
+        if (tiles(128, 128) < 384) ++v;
+    } else {
+        const double us128 = tile_estimate(128, tiles(128, 128), stages), us64 = tile_estimate(64, tiles(64, 64), stages);
+        const StreamVariant *sv = d.io_dtype == DSATTN_BF16 ? &kBf16Stream : &kE4m3Stream;
+        // (tiles are numbered with 32 bits)
+        if (sv->fn[gated][f32][d.act] && large < (1 << 30) && tile_estimate(256, large, stages) < std::min(us128, us64))
+            return {sv->fn[gated][f32][d.act], 256, 256, 8, kStreamLds, true, false};
+        if (us64 < us128) ++v;
+    }
     // (a launch has less than 2^32 threads)
     if (tiles(v->rows, v->cols) >= ((int64_t)1 << 32) / (64 * v->waves) - kXcds) return {};
-    return {v->fn[gated][f32], v->rows, v->cols, v->waves, v->lds, false};
+    return {v->fn[gated][f32], v->rows, v->cols, v->waves, v->lds, false, false};
 }
 
 // Column tiles that are numbered together.  An XCD's 32 tiles in flight are this many wide and 32 / width row tiles high,
@@ -263,7 +319,7 @@ extern "C" int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void 
         if (e == hipSuccess && v.lds > 64 << 10) e = hipFuncSetAttribute(v.fn, hipFuncAttributeMaxDynamicSharedMemorySize, v.lds);
         void *params[] = {&a};
         if (e == hipSuccess)
-            e = hipLaunchKernel(v.fn, dim3((unsigned)per_xcd * kXcds), dim3(64 * v.waves), params, (size_t)v.lds, (hipStream_t)stream);
+            e = hipLaunchKernel(v.fn, dim3(v.small ? (unsigned)a.tiles : (unsigned)per_xcd * kXcds), dim3(64 * v.waves), params, (size_t)v.lds, (hipStream_t)stream);
         if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
         return DSATTN_OK;
     }
