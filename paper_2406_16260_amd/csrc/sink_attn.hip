@@ -362,7 +362,7 @@ int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, cons
         // the default cap on dynamic LDS is 64 KB
         if (k.tile.lds > 64 << 10) e = hipFuncSetAttribute(k.tile.fn, hipFuncAttributeMaxDynamicSharedMemorySize, k.tile.lds);
         if (e == hipSuccess)
-            e = hipLaunchKernel(k.tile.fn, dim3((unsigned)a.per_xcd * 8u), dim3(256), params, (size_t)k.tile.lds, st);
+            e = hipLaunchKernel(k.tile.fn, dim3((unsigned)a.per_xcd * 8u), dim3(64u * k.tile.waves), params, (size_t)k.tile.lds, st);
     } else {
         // (a launch has less than 2^32 threads)
         const int64_t blocks = ((int64_t)a.B * a.T * a.P * a.h + 3) / 4;

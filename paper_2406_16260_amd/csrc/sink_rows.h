@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256) void sink_rows_kernel(const SinkArgs a)
 #pragma unroll
             for (int c = 0; c < PV; ++c) {
                 k[i][c] = v[i][c] = Piece{};
-                if (LG * PV * V == D || (c * LG + li) * V < D) {
+                if (PV > 1 || (c * LG + li) * V < D) {
                     k[i][c] = *(const Piece *)(kp + c * (LG * V));
                     v[i][c] = *(const Piece *)(vp + c * (LG * V));
                 }
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256) void sink_rows_kernel(const SinkArgs a)
                 const int64_t to = fr.slot(a, f[i]) * row;
 #pragma unroll
                 for (int c = 0; c < PV; ++c)
-                    if (LG * PV * V == D || (c * LG + li) * V < D) {
+                    if (PV > 1 || (c * LG + li) * V < D) {
                         *(Piece *)(Kc + to + c * (LG * V)) = k[i][c];
                         *(Piece *)(Vc + to + c * (LG * V)) = v[i][c];
                     }

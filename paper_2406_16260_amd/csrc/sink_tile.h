@@ -5,10 +5,10 @@
 // walks the frames that they see between them in tiles of KT with a running maximum:
 //   S^T = K Q^T   keys on M, queries on N, both operands 16-byte pieces of rows: lane l has piece l / 16 of row l % 16
 //   O^T = V^T P^T a lane's weights are the operand as they stand (any order of the keys contracts the same); bf16: V^T by
-//                 transposing LDS reads, weights rounded to bf16 (2^-9 each, as far from the output's own rounding as
-//                 their mean; the sum that they are divided by is of the unrounded ones); fp32: 16x16x4 on both
-// K and V pass through LDS in rows padded by 16 bytes.  Two ways to share them:
-//   SHARED   the four wavefronts of a workgroup have neighbouring rows of one unit and one tile of 64 or 32 frames, which is
+//                 transposing LDS reads, weights rounded to bf16, and divided by the sum of the rounded ones: an error of 2^-8 each
+//                 at most, which their weighted mean makes smaller than the output's own; fp32: 16x16x4 on both
+// K and V pass through LDS.  Two ways to share them:
+//   SHARED   the wavefronts of a workgroup have neighbouring rows of one unit and one tile of 64 or 32 frames, which is
 //            double-buffered: long windows, bound by the matrix cores and the exponentials
 //   else     a wavefront has LDS of its own, and a unit or a part of its frames (`splits`) of its own: short windows,
 //            bound by memory, and few rows over a long window
@@ -42,28 +42,44 @@ __device__ __forceinline__ float over_quarters(float x)
     return MAX ? fmaxf(z0, z1) : z0 + z1;
 }
 
-// LDS row of NB 64-byte blocks, padded so that the rows spread over the banks
-constexpr int tile_row_bytes(int NB) { return 64 * NB + 16; }
-constexpr int tile_lds_bytes(int NB, int KT, bool SHARED) { return (SHARED ? 2 : 4) * 2 * KT * tile_row_bytes(NB); }
+// LDS rows of NB 64-byte blocks.  K is read by 16-byte pieces: the 16 lanes that are served together are on rows 0 - 3 and
+// 12 - 15 of one piece and 4 - 11 of the next, which are in different banks where a row is 2 pieces more than a multiple
+// of four.  V by 8 bytes of four rows of a group of 16 lanes (bf16): a row is an odd number of blocks; or by 4 bytes of
+// rows four apart (fp32): one piece more than whole blocks.  (Both one piece more than whole blocks: 61 % of the LDS's
+// busy cycles were conflicts, and it was busy 90 % of the time.)
+constexpr int k_row_bytes(int NB) { return 64 * NB + 32; }
+constexpr int v_row_bytes(bool F32, int NB) { return F32 ? 64 * NB + 16 : NB % 2 ? 64 * NB : 64 * NB + 64; }
+constexpr int tile_bytes(bool F32, int NB, int KT) { return KT * (k_row_bytes(NB) + v_row_bytes(F32, NB)); }
+constexpr int tile_lds_bytes(bool F32, int NB, int KT, bool SHARED) { return (SHARED ? 2 : 4) * tile_bytes(F32, NB, KT); }
 
-// Blocks of 16 rows of a wavefront and frames of a tile, as many as leave a wavefront its registers (bf16, head_dim 160:
-// 40 registers of sums a block of rows, 20 of queries, and 40 of rows on their way for every 16 or 64 frames).
-constexpr int tile_blocks(bool F32, int NB, bool SHARED, bool many) { return F32 || NB > 5 || (!SHARED && (!many || NB > 4)) ? 1 : 2; }
-constexpr int tile_frames(bool F32, int NB, bool SHARED) { return SHARED ? (F32 || NB == 5 ? 32 : 64) : F32 ? 16 : 32; }
+// Blocks of 16 rows of a wavefront, frames of a tile and wavefronts of a workgroup, as many as leave a wavefront its registers
+// (bf16, head_dim 160: 40 registers of sums a block of rows, 20 of queries, and what is on its way of the next tile).
+constexpr int tile_blocks(bool F32, int NB, bool SHARED, bool many) { return F32 || (!SHARED && !many) || NB > 4 ? 1 : 2; }
+constexpr int tile_frames(bool F32, int NB, bool SHARED) { return SHARED ? (F32 ? 32 : 64) : F32 ? 16 : 32; }
+constexpr int tile_group(bool F32, int NB, bool SHARED) { return SHARED && !F32 && NB > 4 ? 8 : 4; }
+// Numbers of blocks that kernels are compiled for, and how many of them every head that a kernel takes fills.
+constexpr int round_blocks(int NB) { return NB <= 6 ? NB : NB <= 8 ? 8 : NB <= 10 ? 10 : NB <= 12 ? 12 : 16; }
+constexpr int full_blocks(int NB) { return NB <= 6 ? NB - 1 : NB == 8 ? 6 : NB == 10 ? 8 : NB == 12 ? 10 : 12; }
 // Wavefronts per SIMD that the registers have to leave room for.
-constexpr int tile_waves(int NB, int RB, bool SHARED) { return NB > 8 || (NB > 6 && !SHARED) ? 1 : SHARED || NB * RB > 4 ? 2 : 3; }
+constexpr int tile_waves(int NB, int RB, bool SHARED, int WV)
+{
+    if (SHARED && WV == 8) return 2;
+    return NB > 8 || (NB > 6 && !SHARED) ? 1 : SHARED || NB * RB > 4 ? 2 : 3;
+}
 
 // NB = 64-byte blocks of a head's row, rounded up.
-template <typename T, int NB, int RB, int KT, bool SHARED>
-__global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_kernel(const SinkArgs a)
+template <typename T, int NB, int RB, int KT, bool SHARED, int WV>
+__global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_tile_kernel(const SinkArgs a)
 {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int V = 16 / (int)sizeof(T), DB = 4 * V;  // numbers of a piece, of a block
-    constexpr int RS = tile_row_bytes(NB), TILE = KT * RS;
+    constexpr int RK = k_row_bytes(NB), RV = v_row_bytes(F32, NB), TILE = tile_bytes(F32, NB, KT);  // K, behind it V
     constexpr int KB = KT / 16;                           // blocks of 16 keys
-    constexpr int PASS = SHARED ? 64 : 16;                // rows that the threads fetch at a time, four lanes a row
-    constexpr int NP = (KT + PASS - 1) / PASS;
-    constexpr int ROWS = 16 * RB * (SHARED ? 4 : 1);      // rows of a task
+    // threads that fetch a tile, LPR neighbouring lanes a row (64 bytes at least), in PASSES of RP rows, NP pieces a lane and row
+    constexpr int THREADS = SHARED ? 64 * WV : 64, LPR = THREADS / KT > 4 ? THREADS / KT : 4;
+    constexpr int RP = THREADS / LPR, PASSES = KT / RP, NP = (4 * NB + LPR - 1) / LPR;
+    static_assert(PASSES * RP == KT, "whole passes");
+    constexpr int ROWS = 16 * RB * (SHARED ? WV : 1);     // rows of a task
     typedef T Piece __attribute__((ext_vector_type(V)));
     using Frag = std::conditional_t<F32, f32x4, bf16x8>;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -72,17 +88,20 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = a.h / a.hk, D = a.D;
     // workgroup -> tasks: XCD x (= blockIdx % 8) takes a contiguous run of them
-    const int64_t wg = (int64_t)(blockIdx.x % 8u) * a.per_xcd + blockIdx.x / 8u;
-    int64_t id = SHARED ? wg : wg * 4 + wv;
-    if (id >= a.tasks) return;  // shared: the whole workgroup; else nobody waits for anybody
+    // (32-bit divisions: a 64-bit one is some hundred scalar instructions)
+    const uint32_t wg = (blockIdx.x % 8u) * (uint32_t)a.per_xcd + blockIdx.x / 8u;
+    uint32_t id = SHARED ? wg : wg * 4u + (uint32_t)wv;
+    if (id >= (uint32_t)a.tasks) return;  // shared: the whole workgroup; else nobody waits for anybody
     // heads are neighbours (they share memory pages and lines), then the row tiles of a unit (they share frames)
-    const int split = (int)(id % a.splits);
-    id /= a.splits;
-    const int kvh = (int)(id % a.hk);
-    id /= a.hk;
-    const int rt = (int)(id % a.row_tiles);
-    id /= a.row_tiles;
-    const int p = (int)(id % a.P), b = (int)(id / a.P);
+    uint32_t rest = a.splits > 1 ? id / (uint32_t)a.splits : id;
+    const int split = a.splits > 1 ? (int)(id - rest * a.splits) : 0;
+    id = rest;
+    rest = id / (uint32_t)a.hk;
+    const int kvh = (int)(id - rest * a.hk);
+    id = rest;
+    rest = id / (uint32_t)a.row_tiles;
+    const int rt = (int)(id - rest * a.row_tiles);
+    const int b = (int)(rest / (uint32_t)a.P), p = (int)(rest - (uint32_t)b * a.P);
     const Stream st = stream_of(a, b);
     const int rows = st.count * g, first = rt * ROWS;
     if (first >= rows) return;  // (the same for all wavefronts of a task)
@@ -114,47 +133,60 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
     const int lw_all = st.start + max(rz, 0) / g - a.window - shift, lw_any = st.start + ra - a.window - shift;
     const int hi_any = r0 < rows ? st.start + max(rz, 0) / g - shift : -1;
 
-    // ---- K and V into LDS: four lanes a row, each a piece of every block
+    // ---- K and V into LDS: LPR neighbouring lanes a row, every LPR-th piece each
     const int tid = SHARED ? (int)threadIdx.x : lane;
-    const int lrow = tid >> 2, lc = tid & 3;
-    unsigned char *mem = smem + (SHARED ? 0 : wv * 2 * TILE);
-    const int64_t frow = (int64_t)a.P * a.hk * D, at = ((int64_t)p * a.hk + kvh) * D + V * lc;
-    const int64_t fresh0 = (int64_t)b * a.T * frow + at, cache0 = (int64_t)b * (a.sinks + a.ring) * frow + at;
-    Piece kr[NP][NB], vr[NP][NB];
+    const int lrow = tid / LPR, lc = tid % LPR;
+    unsigned char *mem = smem + (SHARED ? 0 : wv * TILE);
+    const int64_t frow = (int64_t)a.P * a.hk * D, at = ((int64_t)p * a.hk + kvh) * D;
+    // (kept in registers: a choice between arguments is otherwise a load by every lane, which the loop then waits for)
+    typedef const __attribute__((address_space(1))) T *Rows;
+    Rows kf = (Rows)a.K + (int64_t)b * a.T * frow + at, vf = (Rows)a.V + (int64_t)b * a.T * frow + at;
+    Rows kc = (Rows)a.Kc + (int64_t)b * (a.sinks + a.ring) * frow + at, vc = (Rows)a.Vc + (int64_t)b * (a.sinks + a.ring) * frow + at;
+    asm volatile("" : "+s"(kf), "+s"(vf), "+s"(kc), "+s"(vc));
+    // (unconditional loads: behind a branch each would be waited for at its end; past the head the row's first piece)
+    auto in_row = [&](int i) __attribute__((always_inline)) { return LPR * i + LPR <= 4 * NB || LPR * i + lc < 4 * NB; };
+    auto within = [&](int i) __attribute__((always_inline)) {
+        return LPR * i + LPR <= 4 * full_blocks(NB) || (LPR * i + lc) * V < D;
+    };
+    Piece kr[PASSES][NP], vr[PASSES][NP];
     auto fetch = [&](int tile) __attribute__((always_inline)) {
+        typedef const __attribute__((address_space(1))) Piece *Pieces;
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
-            const int j = min(tile * KT + n * PASS + lrow, fr.n - 1), f = fr.frame(j);
+        for (int n = 0; n < PASSES; ++n) {
+            const int j = min(tile * KT + n * RP + lrow, fr.n - 1), f = fr.frame(j);
             const bool fresh = f >= st.start;
-            const int64_t off = fresh ? fresh0 + (f - st.start) * frow : cache0 + fr.slot(a, f) * frow;
-            const T *kp = (const T *)(fresh ? a.K : a.Kc) + off, *vp = (const T *)(fresh ? a.V : a.Vc) + off;
+            const int64_t off = (fresh ? f - st.start : fr.slot(a, f)) * frow;
+            const Rows kp = (fresh ? kf : kc) + off, vp = (fresh ? vf : vc) + off;
 #pragma unroll
-            for (int kb = 0; kb < NB; ++kb) {
-                kr[n][kb] = vr[n][kb] = Piece{};
-                if ((KT % PASS == 0 || n * PASS + lrow < KT) && DB * kb + V * lc < D) {
-                    kr[n][kb] = *(const Piece *)(kp + DB * kb);
-                    vr[n][kb] = *(const Piece *)(vp + DB * kb);
-                }
+            for (int i = 0; i < NP; ++i) {
+                const int c = within(i) ? (LPR * i + lc) * V : 0;
+                kr[n][i] = *(Pieces)(kp + c);
+                vr[n][i] = *(Pieces)(vp + c);
             }
         }
     };
-    // (pieces past the head are zeros: what K has there is multiplied with Q's zeros)
+    // (K's pieces past the head are zeros, as Q's are; V's are never stored)
     auto put = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
-            if (KT % PASS != 0 && n * PASS + lrow >= KT) continue;
-            unsigned char *to = mem + (SHARED ? buf * 2 * TILE : 0) + (n * PASS + lrow) * RS + 16 * lc;
+        for (int n = 0; n < PASSES; ++n) {
+            unsigned char *tok = mem + (SHARED ? buf * TILE : 0) + (n * RP + lrow) * RK + 16 * lc;
+            unsigned char *tov = mem + (SHARED ? buf * TILE : 0) + KT * RK + (n * RP + lrow) * RV + 16 * lc;
 #pragma unroll
-            for (int kb = 0; kb < NB; ++kb) {
-                *(Piece *)(to + 64 * kb) = kr[n][kb];
-                *(Piece *)(to + TILE + 64 * kb) = vr[n][kb];
+            for (int i = 0; i < NP; ++i) {
+                if (!in_row(i)) continue;
+                *(Piece *)(tok + 16 * LPR * i) = within(i) ? kr[n][i] : Piece{};
+                *(Piece *)(tov + 16 * LPR * i) = vr[n][i];
             }
         }
     };
 
     constexpr int OB = F32 ? NB : 2 * NB;  // blocks of 16 channels
     f32x4 o[RB][OB] = {};
-    float m[RB], l[RB];
+    float m[RB], l[RB];  // the row's maximum; fp32: this lane's part of the sum
+    f32x4 ls[RB] = {};   // bf16: the sum, of the rounded weights, in every element: a row of ones times P^T
+    bf16x8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
 #pragma unroll
     for (int i = 0; i < RB; ++i) m[i] = -INFINITY, l[i] = 0.f;
 
@@ -162,7 +194,7 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
         const int j0 = tile * KT;
         // no row of this wavefront sees a frame of the tile
         if (j0 > hi_any || (j0 + KT - 1 <= lw_any && j0 >= always)) return;
-        const unsigned char *vs = ks + TILE;
+        const unsigned char *vs = ks + KT * RK;
         f32x4 s[RB][KB];
 #pragma unroll
         for (int k = 0; k < KB; ++k)
@@ -172,7 +204,7 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
             for (int k = 0; k < KB; ++k) {
-                const Frag kf = *(const Frag *)(ks + (16 * k + l16) * RS + 64 * kb + 16 * lg);
+                const Frag kf = *(const Frag *)(ks + (16 * k + l16) * RK + 64 * kb + 16 * lg);
 #pragma unroll
                 for (int i = 0; i < RB; ++i) {
                     if constexpr (F32) {
@@ -185,16 +217,28 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
             }
         // hidden keys: key 16 k + 4 lg + e of the tile
         if (j0 + KT - 1 > hi_all || (j0 <= lw_all && j0 + KT - 1 >= always)) {
+            if (j0 >= always) {  // behind the sinks a row sees the keys from lw + 1 to hi
 #pragma unroll
-            for (int i = 0; i < RB; ++i)
+                for (int i = 0; i < RB; ++i) {
+                    const uint32_t span = (uint32_t)max(hi[i] - lw[i], 0);
+                    const int from = j0 + 4 * lg - lw[i] - 1;
 #pragma unroll
-                for (int k = 0; k < KB; ++k)
+                    for (int k = 0; k < KB; ++k)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int j = j0 + 16 * k + 4 * lg + e;
-                        const bool sees = j <= hi[i] && (j > lw[i] || j < always);
-                        s[i][k][e] = sees ? s[i][k][e] : -INFINITY;
-                    }
+                        for (int e = 0; e < 4; ++e) s[i][k][e] = (uint32_t)(from + 16 * k + e) < span ? s[i][k][e] : -INFINITY;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < RB; ++i)
+#pragma unroll
+                    for (int k = 0; k < KB; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int j = j0 + 16 * k + 4 * lg + e;
+                            const bool sees = j <= hi[i] && (j > lw[i] || j < always);
+                            s[i][k][e] = sees ? s[i][k][e] : -INFINITY;
+                        }
+            }
         }
         float shiftv[RB];
 #pragma unroll
@@ -209,6 +253,7 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
             if (__any(top > m[i])) {
                 const float old = __builtin_amdgcn_exp2f(m[i] - shiftv[i]);
                 l[i] *= old;
+                ls[i] *= old;
 #pragma unroll
                 for (int c = 0; c < OB; ++c) o[i][c] *= old;
             }
@@ -218,7 +263,7 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     s[i][k][e] = __builtin_amdgcn_exp2f(fmaf(s[i][k][e], a.sc, -shiftv[i]));
-                    l[i] += s[i][k][e];
+                    if constexpr (F32) l[i] += s[i][k][e];
                 }
         }
         if constexpr (F32) {
@@ -228,7 +273,7 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
                     for (int c = 0; c < OB; ++c) {
-                        const float vf = *(const float *)(vs + (16 * k + 4 * lg + e) * RS + 64 * c + 4 * l16);
+                        const float vf = *(const float *)(vs + (16 * k + 4 * lg + e) * RV + 64 * c + 4 * l16);
 #pragma unroll
                         for (int i = 0; i < RB; ++i) o[i][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf, s[i][k][e], o[i][c], 0, 0, 0);
                     }
@@ -243,6 +288,8 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
                         w[i][e] = (__bf16)s[i][k][e];
                         w[i][4 + e] = (__bf16)s[i][k + 1][e];
                     }
+#pragma unroll
+                for (int i = 0; i < RB; ++i) ls[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, w[i], ls[i], 0, 0, 0);
                 // V^T: within a group of 16 lanes the transposing read hands lane i element i % 4 of the 8 bytes
                 // that lanes i / 4, 4 + i / 4, 8 + i / 4 and 12 + i / 4 point at.  Lane i points at key 4 lg + i / 4,
                 // channels 8 (i % 4) + 4 x .. of the block, and so gets keys 4 lg .. 4 lg + 3 of channel
@@ -253,7 +300,7 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
                         r[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (__attribute__((address_space(3))) s16x4 *)(vs + (16 * (k + t) + 4 * lg + (l16 >> 2)) * RS +
+                            (__attribute__((address_space(3))) s16x4 *)(vs + (16 * (k + t) + 4 * lg + (l16 >> 2)) * RV +
                                                                         64 * (c / 2) + 16 * (l16 & 3) + 8 * (c & 1)));
                     const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(r[0], r[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
@@ -272,7 +319,7 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
             put(t & 1);
             if (t + 1 < tiles) fetch(t + 1);
             __syncthreads();  // everybody's part of tile t is there, and tile t - 1, whose buffer is next, is done with
-            multiply(t, mem + (t & 1) * 2 * TILE);
+            multiply(t, mem + (t & 1) * TILE);
         }
     } else {
         const int per = (tiles + a.splits - 1) / a.splits, t0 = split * per, t1 = min(tiles, t0 + per);
@@ -288,7 +335,7 @@ __global__ __launch_bounds__(256, tile_waves(NB, RB, SHARED)) void sink_tile_ker
 
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
-        const float sum = over_quarters<false>(l[i]);
+        const float sum = F32 ? over_quarters<false>(l[i]) : ls[i][0];
         const int r = r0 + 16 * i + l16;
         if (!SHARED && a.splits > 1) {
             if (r >= rows) continue;
@@ -346,7 +393,8 @@ const void *tile_kernel_of(int NB)
 {
     constexpr bool F32 = sizeof(T) == 4;
 #define DSATTN_TILE(nb) \
-    if (NB == nb) return (const void *)&sink_tile_kernel<T, nb, tile_blocks(F32, nb, SHARED, MANY), tile_frames(F32, nb, SHARED), SHARED>
+    if (NB == nb) return (const void *)&sink_tile_kernel<T, nb, tile_blocks(F32, nb, SHARED, MANY), tile_frames(F32, nb, SHARED), SHARED, \
+                                                    tile_group(F32, nb, SHARED)>
     DSATTN_TILE(1);
     DSATTN_TILE(2);
     DSATTN_TILE(3);
@@ -366,7 +414,7 @@ const void *tile_kernel_of(int NB)
 // The launch on the matrix cores; fn null: none.
 struct TileLaunch {
     const void *fn;
-    int row_tiles, splits, lds;
+    int row_tiles, splits, lds, waves;
     int64_t tasks, workgroups;
 };
 TileLaunch tile_launch(const dsattn_sink_desc &d)
@@ -375,13 +423,13 @@ TileLaunch tile_launch(const dsattn_sink_desc &d)
     const bool f32 = d.io_dtype == DSATTN_F32;
     const int V = f32 ? 4 : 8;
     if (d.head_dim % V != 0 || d.head_dim > 256) return k;
-    int NB = (d.head_dim + 4 * V - 1) / (4 * V);
-    NB = NB <= 6 ? NB : NB <= 8 ? 8 : NB <= 10 ? 10 : NB <= 12 ? 12 : 16;
+    const int NB = round_blocks((d.head_dim + 4 * V - 1) / (4 * V));
     const int64_t rows = (int64_t)d.frames * (d.heads / d.kv_heads), units = (int64_t)d.streams * d.spatial * d.kv_heads;
     const bool shared = rows >= 64 && (int64_t)d.sinks + d.window >= 128;
     const bool many = rows > 16;
     const int RB = tile_blocks(f32, NB, shared, many), KT = tile_frames(f32, NB, shared);
-    const int per = 16 * RB * (shared ? 4 : 1);
+    k.waves = tile_group(f32, NB, shared);
+    const int per = 16 * RB * (shared ? k.waves : 1);
     if ((rows + per - 1) / per > 0x7fffffff) return k;
     k.row_tiles = (int)((rows + per - 1) / per);
     k.tasks = units * k.row_tiles;
@@ -394,7 +442,7 @@ TileLaunch tile_launch(const dsattn_sink_desc &d)
     }
     k.workgroups = shared ? k.tasks : (k.tasks + 3) / 4;
     if (k.workgroups > 0xffffff - 8) return TileLaunch{};
-    k.lds = tile_lds_bytes(NB, KT, shared);
+    k.lds = tile_lds_bytes(f32, NB, KT, shared);
     k.fn = f32 ? (shared ? tile_kernel_of<float, true, true>(NB) : tile_kernel_of<float, false, true>(NB))
                : (shared ? tile_kernel_of<__bf16, true, true>(NB)
                   : many ? tile_kernel_of<__bf16, false, true>(NB)

@@ -153,7 +153,7 @@ def run(c, seed=0, scale=0.0, flags=0):
     return s, O
 
 
-DIMS = [1, 5, 8, 16, 24, 32, 40, 48, 64, 80, 96, 100, 128, 160, 192, 256, 264, 512]
+DIMS = [1, 5, 8, 16, 24, 32, 40, 48, 64, 72, 80, 96, 100, 104, 128, 136, 160, 176, 192, 200, 216, 232, 256, 264, 512]
 
 
 @pytest.mark.gpu
@@ -168,6 +168,8 @@ def test_one_frame_of_every_head_dim(D, dtype):
 @pytest.mark.parametrize("D", DIMS)
 def test_many_frames_of_every_head_dim(D, dtype):
     run(case(dtype, T=70, P=2, h=2, D=D, sinks=3, window=21, start=13), D)
+    run(case(dtype, T=70, P=2, h=2, D=D, sinks=3, window=130, start=150), D)
+    run(case(dtype, T=9, P=2, h=2, D=D, sinks=1, window=12, start=40), D)
 
 
 @pytest.mark.gpu
