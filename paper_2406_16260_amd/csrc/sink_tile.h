@@ -92,15 +92,20 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
     const uint32_t wg = (blockIdx.x % 8u) * (uint32_t)a.per_xcd + blockIdx.x / 8u;
     uint32_t id = SHARED ? wg : wg * 4u + (uint32_t)wv;
     if (id >= (uint32_t)a.tasks) return;  // shared: the whole workgroup; else nobody waits for anybody
-    // heads are neighbours (they share memory pages and lines), then the row tiles of a unit (they share frames)
-    uint32_t rest = a.splits > 1 ? id / (uint32_t)a.splits : id;
-    const int split = a.splits > 1 ? (int)(id - rest * a.splits) : 0;
+    // Shared: the row tiles of a unit are neighbours, the longest first.  (A unit's K and V stay in one XCD's L2, and the short
+    // ones at a stream's start are spread over the XCDs.)  Else the heads are (they share memory pages and lines), then the
+    // row tiles of a unit (they share frames).
+    const uint32_t parts = SHARED ? 1u : (uint32_t)a.splits, inner = (uint32_t)(SHARED ? a.row_tiles : a.hk);
+    const uint32_t outer = (uint32_t)(SHARED ? a.hk : a.row_tiles);
+    uint32_t rest = parts > 1 ? id / parts : id;
+    const int split = parts > 1 ? (int)(id - rest * parts) : 0;
     id = rest;
-    rest = id / (uint32_t)a.hk;
-    const int kvh = (int)(id - rest * a.hk);
+    rest = id / inner;
+    const int in = (int)(id - rest * inner);
     id = rest;
-    rest = id / (uint32_t)a.row_tiles;
-    const int rt = (int)(id - rest * a.row_tiles);
+    rest = id / outer;
+    const int out = (int)(id - rest * outer);
+    const int kvh = SHARED ? out : in, rt = SHARED ? a.row_tiles - 1 - in : out;
     const int b = (int)(rest / (uint32_t)a.P), p = (int)(rest - (uint32_t)b * a.P);
     const Stream st = stream_of(a, b);
     const int rows = st.count * g, first = rt * ROWS;
@@ -266,6 +271,8 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
                     if constexpr (F32) l[i] += s[i][k][e];
                 }
         }
+        // (while the other wavefront of the SIMD is elsewhere: 330 -> 315 us, 2 prompts of 8,192, 16 heads on 4 x 128, window 2,048)
+        if constexpr (SHARED) __builtin_amdgcn_s_setprio(1);
         if constexpr (F32) {
 #pragma unroll
             for (int k = 0; k < KB; ++k)
@@ -318,6 +325,7 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
         for (int t = 0; t < tiles; ++t) {
             put(t & 1);
             if (t + 1 < tiles) fetch(t + 1);
+            __builtin_amdgcn_s_setprio(0);
             __syncthreads();  // everybody's part of tile t is there, and tile t - 1, whose buffer is next, is done with
             multiply(t, mem + (t & 1) * TILE);
         }
