@@ -55,7 +55,8 @@ constexpr int tile_lds_bytes(bool F32, int NB, int KT, bool SHARED) { return (SH
 // Blocks of 16 rows of a wavefront, frames of a tile and wavefronts of a workgroup, as many as leave a wavefront its registers
 // (bf16, head_dim 160: 40 registers of sums a block of rows, 20 of queries, and what is on its way of the next tile).
 constexpr int tile_blocks(bool F32, int NB, bool SHARED, bool many) { return F32 || (!SHARED && !many) || NB > 4 ? 1 : 2; }
-constexpr int tile_frames(bool F32, int NB, bool SHARED) { return SHARED ? (F32 ? 32 : 64) : F32 ? 16 : 32; }
+constexpr int tile_frames(bool F32, bool SHARED, bool many) { return SHARED ? (F32 || !many ? 32 : 64) : F32 ? 16 : 32; }
+// (many: of rows, more than 16; shared: of frames, a window of 128 or more)
 constexpr int tile_group(bool F32, int NB, bool SHARED) { return SHARED && !F32 && NB > 4 ? 8 : 4; }
 // Numbers of blocks that kernels are compiled for, and how many of them every head that a kernel takes fills.
 constexpr int round_blocks(int NB) { return NB <= 6 ? NB : NB <= 8 ? 8 : NB <= 10 ? 10 : NB <= 12 ? 12 : 16; }
@@ -64,7 +65,7 @@ constexpr int full_blocks(int NB) { return NB <= 6 ? NB - 1 : NB == 8 ? 6 : NB =
 constexpr int tile_waves(int NB, int RB, bool SHARED, int WV)
 {
     if (SHARED && WV == 8) return 2;
-    return NB > 8 || (NB > 6 && !SHARED) ? 1 : SHARED || NB * RB > 4 ? 2 : 3;
+    return NB > 8 || (NB > 6 && !SHARED) ? 1 : SHARED || NB >= 4 || NB * RB > 4 ? 2 : 3;
 }
 
 // NB = 64-byte blocks of a head's row, rounded up.
@@ -401,7 +402,7 @@ const void *tile_kernel_of(int NB)
 {
     constexpr bool F32 = sizeof(T) == 4;
 #define DSATTN_TILE(nb) \
-    if (NB == nb) return (const void *)&sink_tile_kernel<T, nb, tile_blocks(F32, nb, SHARED, MANY), tile_frames(F32, nb, SHARED), SHARED, \
+    if (NB == nb) return (const void *)&sink_tile_kernel<T, nb, tile_blocks(F32, nb, SHARED, MANY), tile_frames(F32, SHARED, MANY), SHARED, \
                                                     tile_group(F32, nb, SHARED)>
     DSATTN_TILE(1);
     DSATTN_TILE(2);
@@ -433,9 +434,15 @@ TileLaunch tile_launch(const dsattn_sink_desc &d)
     if (d.head_dim % V != 0 || d.head_dim > 256) return k;
     const int NB = round_blocks((d.head_dim + 4 * V - 1) / (4 * V));
     const int64_t rows = (int64_t)d.frames * (d.heads / d.kv_heads), units = (int64_t)d.streams * d.spatial * d.kv_heads;
-    const bool shared = rows >= 64 && (int64_t)d.sinks + d.window >= 128;
-    const bool many = rows > 16;
-    const int RB = tile_blocks(f32, NB, shared, many), KT = tile_frames(f32, NB, shared);
+    // Row tiles that share their frames, us apart (32 rows a wavefront) and shared, in tiles of 32 and of 64 frames:
+    //   128 frames x 640 positions, 8 x 80, 4 sinks, window 32      126.5  108.7  115.4
+    //   256 frames x 160 positions, 8 x 128, 4 sinks, window 64      87.0   85.0   88.5
+    //   256 frames x 160 positions, 8 x 128, 4 sinks, window 130            89.6   86.4
+    //   64 frames x 2,560 positions, 8 x 40, 4 sinks, window 16     132.1  149.2  168.0
+    const int64_t sees = (int64_t)d.sinks + d.window;
+    const bool shared = rows >= 64 && sees >= 32;
+    const bool many = shared ? sees >= 128 : rows > 16;
+    const int RB = tile_blocks(f32, NB, shared, many), KT = tile_frames(f32, shared, many);
     k.waves = tile_group(f32, NB, shared);
     const int per = 16 * RB * (shared ? k.waves : 1);
     if ((rows + per - 1) / per > 0x7fffffff) return k;
@@ -452,9 +459,8 @@ TileLaunch tile_launch(const dsattn_sink_desc &d)
     if (k.workgroups > 0xffffff - 8) return TileLaunch{};
     k.lds = tile_lds_bytes(f32, NB, KT, shared);
     k.fn = f32 ? (shared ? tile_kernel_of<float, true, true>(NB) : tile_kernel_of<float, false, true>(NB))
-               : (shared ? tile_kernel_of<__bf16, true, true>(NB)
-                  : many ? tile_kernel_of<__bf16, false, true>(NB)
-                         : tile_kernel_of<__bf16, false, false>(NB));
+           : shared ? (many ? tile_kernel_of<__bf16, true, true>(NB) : tile_kernel_of<__bf16, true, false>(NB))
+                    : (many ? tile_kernel_of<__bf16, false, true>(NB) : tile_kernel_of<__bf16, false, false>(NB));
     return k;
 }
 
