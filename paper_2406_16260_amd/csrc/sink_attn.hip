@@ -22,7 +22,7 @@ struct SinkArgs {
     const int32_t *start, *counts;  // or null
     int32_t B, T, P, h, hk, D, sinks, window, ring;
     float sc;  // softmax scale * log2(e)
-    int32_t U, splits, fused;  // see sink_rows.h: units of a wavefront; parts of a row's frames; new frames are put into the cache
+    int32_t U, splits, fused;  // see sink_rows.h: units of a wavefront; parts of a row's frames; see puts_frames()
     float *parts;              // partial results of the splits
     int32_t per_xcd, row_tiles;  // see sink_tile.h: workgroups of an XCD, row tiles of a unit, tasks in all
     int64_t tasks;
@@ -41,6 +41,16 @@ __device__ __forceinline__ Stream stream_of(const SinkArgs &a, int b)
     s.start = a.start ? min(max(a.start[b], 0), 0x7fffffff - a.T) : 0;
     s.count = a.counts ? min(max(a.counts[b], 0), a.T) : a.T;
     return s;
+}
+
+// Whether the attention itself puts a stream's new frames into the cache, rather than a kernel after it: where none of them
+// takes a slot whose frame a query of the call still reads.  `fused`: 1, the ring has room for both (or nothing is cached
+// yet, for all streams); 2, where the stream has nothing cached yet; 0, never.
+__device__ __forceinline__ bool puts_frames(const SinkArgs &a, const Stream &s) { return a.fused == 1 || (a.fused == 2 && s.start == 0); }
+// Whether new frame f stays in the cache when the call is done: of several with one slot the last one does.
+__device__ __forceinline__ bool stays(const SinkArgs &a, const Stream &s, int f)
+{
+    return f < a.sinks || s.start + s.count - 1 - f < a.ring;
 }
 
 // slot of a frame in the cache
@@ -157,11 +167,11 @@ __global__ __launch_bounds__(256) void sink_append_kernel(const SinkArgs a, int6
 {
     const int b = (int)(blockIdx.z >> 1);
     const Stream s = stream_of(a, b);
+    if (puts_frames(a, s)) return;
     const bool v = blockIdx.z & 1;
     for (int t = (int)blockIdx.y; t < s.count; t += (int)gridDim.y) {
         const int f = s.start + t;
-        // (of several frames with one slot the last one stays)
-        if (f >= a.sinks && s.count - t > a.ring) continue;
+        if (!stays(a, s, f)) continue;
         const U *from = (const U *)(v ? a.V : a.K) + ((int64_t)b * a.T + t) * units;
         U *to = (U *)(v ? a.Vc : a.Kc) + ((int64_t)b * (a.sinks + a.ring) + slot_of(a, f)) * units;
         for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < units; i += (int64_t)gridDim.x * 256) to[i] = from[i];
@@ -348,10 +358,10 @@ int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, cons
     a.splits = k.splits;
     a.parts = (float *)workspace;
     hipError_t e = hipSuccess;
+    if ((k.rows.fn || k.tile.fn) && Kcache && d.window >= 1)  // (without a window a query does not see its own frame)
+        a.fused = !start || d.ring >= (int64_t)d.window + d.frames - 1 ? 1 : 2;
     if (k.rows.fn) {
         a.U = k.rows.U;
-        // (a frame that goes into the cache must not take a slot that another query of the call still reads)
-        a.fused = Kcache && d.window >= 1 && d.ring >= (int64_t)d.window + d.frames - 1;
         void *params[] = {&a};
         e = hipLaunchKernel(k.rows.fn, dim3((unsigned)k.rows.blocks), dim3(256), params, (size_t)k.rows.lds, st);
     } else if (k.tile.fn) {
@@ -381,12 +391,13 @@ int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, cons
             hipLaunchKernelGGL((sink_join_kernel<__bf16>), dim3(blocks), dim3(256), 0, st, a);
         e = hipGetLastError();
     }
-    if (e == hipSuccess && Kcache && !a.fused) {
+    if (e == hipSuccess && Kcache && a.fused != 1) {
         // in units that divide a frame's row
         const bool wide = row * es % 16 == 0;
         const int64_t units = wide ? row * es / 16 : row;
-        const unsigned x = (unsigned)std::min<int64_t>((units + 255) / 256, 256);
-        const dim3 grid(x, (unsigned)std::min(a.T, 65535), 2u * a.B);
+        // some 4,096 workgroups, of which those of streams that have theirs already end at once
+        const int64_t per = std::max<int64_t>(1, 4096 / (2 * a.B)), x = std::min<int64_t>((units + 255) / 256, per);
+        const dim3 grid((unsigned)x, (unsigned)std::min<int64_t>(a.T, std::max<int64_t>(1, per / x)), 2u * a.B);
         if (wide)
             hipLaunchKernelGGL((sink_append_kernel<uint4>), grid, dim3(256), 0, st, a, units);
         else if (es == 4)

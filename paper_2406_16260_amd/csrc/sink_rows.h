@@ -104,7 +104,7 @@ __global__ __launch_bounds__(256) void sink_rows_kernel(const SinkArgs a)
     T *Kc = (T *)a.Kc + (int64_t)b * (a.sinks + a.ring) * row + at, *Vc = (T *)a.Vc + (int64_t)b * (a.sinks + a.ring) * row + at;
     const int all = groups * 4 * a.splits, me = (split * 4 + wv) * groups + fg;
     const int steps = (fr.n + all * kFrames - 1) / (all * kFrames);
-    const bool masked = a.T > 1;
+    const bool masked = a.T > 1, fuse = puts_frames(a, st);
     Running<N> run[R];
     for (int step = 0; step < steps; ++step) {
         const int j0 = (step * all + me) * kFrames;
@@ -126,8 +126,8 @@ __global__ __launch_bounds__(256) void sink_rows_kernel(const SinkArgs a)
                 }
             }
             // a new frame goes into the cache from here: one group has it
-            if (a.fused && fresh && j0 + i < fr.n && mine) {
-                const int64_t to = fr.slot(a, f[i]) * row;
+            if (fuse && fresh && j0 + i < fr.n && mine && stays(a, st, f[i])) {
+                const int64_t to = slot_of(a, f[i]) * row;
 #pragma unroll
                 for (int c = 0; c < PV; ++c)
                     if (PV > 1 || (c * LG + li) * V < D) {

@@ -147,7 +147,8 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
     // (kept in registers: a choice between arguments is otherwise a load by every lane, which the loop then waits for)
     typedef const __attribute__((address_space(1))) T *Rows;
     Rows kf = (Rows)a.K + (int64_t)b * a.T * frow + at, vf = (Rows)a.V + (int64_t)b * a.T * frow + at;
-    Rows kc = (Rows)a.Kc + (int64_t)b * (a.sinks + a.ring) * frow + at, vc = (Rows)a.Vc + (int64_t)b * (a.sinks + a.ring) * frow + at;
+    typedef __attribute__((address_space(1))) T *Cache;
+    Cache kc = (Cache)a.Kc + (int64_t)b * (a.sinks + a.ring) * frow + at, vc = (Cache)a.Vc + (int64_t)b * (a.sinks + a.ring) * frow + at;
     asm volatile("" : "+s"(kf), "+s"(vf), "+s"(kc), "+s"(vc));
     // (unconditional loads: behind a branch each would be waited for at its end; past the head the row's first piece)
     auto in_row = [&](int i) __attribute__((always_inline)) { return LPR * i + LPR <= 4 * NB || LPR * i + lc < 4 * NB; };
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
             const int j = min(tile * KT + n * RP + lrow, fr.n - 1), f = fr.frame(j);
             const bool fresh = f >= st.start;
             const int64_t off = (fresh ? f - st.start : fr.slot(a, f)) * frow;
-            const Rows kp = (fresh ? kf : kc) + off, vp = (fresh ? vf : vc) + off;
+            const Rows kp = (fresh ? kf : (Rows)kc) + off, vp = (fresh ? vf : (Rows)vc) + off;
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const int c = within(i) ? (LPR * i + lc) * V : 0;
@@ -172,7 +173,25 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
         }
     };
     // (K's pieces past the head are zeros, as Q's are; V's are never stored)
-    auto put = [&](int buf) __attribute__((always_inline)) {
+    // The task's own new frames go into the cache on the way (each is fetched by one part of the task's frames).
+    const int own_first = st.start + first / g, own_last = st.start + last / g;
+    const bool puts = puts_frames(a, st);
+    auto put = [&](int tile, int buf) __attribute__((always_inline)) {
+        if (puts && tile * KT + KT - 1 + (fr.lo - fr.ns) >= own_first) {
+            typedef __attribute__((address_space(1))) Piece *Slots;
+#pragma unroll
+            for (int n = 0; n < PASSES; ++n) {
+                const int j = tile * KT + n * RP + lrow, f = fr.frame(j);
+                if (j >= fr.n || f < own_first || f > own_last || !stays(a, st, f)) continue;
+                const int64_t off = slot_of(a, f) * frow;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    if (!in_row(i) || !within(i)) continue;
+                    *(Slots)(kc + off + (LPR * i + lc) * V) = kr[n][i];
+                    *(Slots)(vc + off + (LPR * i + lc) * V) = vr[n][i];
+                }
+            }
+        }
 #pragma unroll
         for (int n = 0; n < PASSES; ++n) {
             unsigned char *tok = mem + (SHARED ? buf * TILE : 0) + (n * RP + lrow) * RK + 16 * lc;
@@ -324,7 +343,7 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
         // are none (frames_of() leaves them out)
         if (tiles > 0) fetch(0);
         for (int t = 0; t < tiles; ++t) {
-            put(t & 1);
+            put(t, t & 1);
             if (t + 1 < tiles) fetch(t + 1);
             __builtin_amdgcn_s_setprio(0);
             __syncthreads();  // everybody's part of tile t is there, and tile t - 1, whose buffer is next, is done with
@@ -335,7 +354,7 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
         if (t0 < t1) fetch(t0);
         for (int t = t0; t < t1; ++t) {
             wave_lds_sync();
-            put(0);
+            put(t, 0);
             wave_lds_sync();
             if (t + 1 < t1) fetch(t + 1);
             multiply(t, mem);
