@@ -83,7 +83,7 @@ __device__ __forceinline__ Frames frames_of(const SinkArgs &a, const Stream &s, 
 }
 
 // A split's partial result for row r of a unit: maximum, sum, two unused numbers, weighted sum.
-constexpr int kPartHead = 4;
+constexpr int kPartHead = 4, kMaxSplits = 64;
 __device__ __forceinline__ float *part_of(const SinkArgs &a, int b, int64_t unit, int r, int rows, int split)
 {
     const int64_t row = (((int64_t)b * a.P * a.hk + unit) * rows + r) * a.splits + split;
@@ -187,38 +187,60 @@ __global__ __launch_bounds__(256) void sink_append_kernel(const SinkArgs a, int6
 namespace dsattn {
 namespace {
 
-// Joins the splits of a row: a wavefront a row, lane l has channels l, l + 64, ...
+// Joins the splits of a row (64 at most): a workgroup a row, lane l of a wavefront has split l's maximum and sum, and then
+// channels l, l + 64, ... of every fourth split, four of them in flight.
 template <typename T>
 __global__ __launch_bounds__(256) void sink_join_kernel(const SinkArgs a)
 {
-    const int g = a.h / a.hk, rows = a.T * g, lane = threadIdx.x & 63, D = a.D;
-    const int64_t all = (int64_t)a.B * a.P * a.hk * rows, id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (id >= all) return;
-    const int r = (int)(id % rows);
-    const int64_t unit = id / rows % ((int64_t)a.P * a.hk);
-    const int b = (int)(id / rows / ((int64_t)a.P * a.hk)), t = r / g;
+    constexpr int R = kMaxDim / 64, U = 4;
+    __shared__ float sums[3][kMaxDim];
+    const int g = a.h / a.hk, rows = a.T * g, D = a.D;
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int64_t id = blockIdx.x, units = (int64_t)a.P * a.hk;
+    const int r = (int)(id % rows), t = r / g;
+    const int64_t unit = id / rows % units;
+    const int b = (int)(id / rows / units);
     if (t >= stream_of(a, b).count) return;
     const float *parts = part_of(a, b, unit, r, rows, 0);
     const int stride = D + kPartHead;
-    float top = -INFINITY;
-    for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, parts[s * stride]);
+    const bool mine = lane < a.splits;
+    const float m = mine ? parts[lane * stride] : -INFINITY;
+    float l = mine ? parts[lane * stride + 1] : 0.f, top = m;
     for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
-    const float shift = top == -INFINITY ? 0.f : top;
-    constexpr int R = kMaxDim / 64;
-    float l = 0.f, o[R] = {};
-    for (int s = 0; s < a.splits; ++s) {
-        const float *from = parts + s * stride;
-        const float f = __builtin_amdgcn_exp2f(from[0] - shift);
-        l = fmaf(from[1], f, l);
+    const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
+    l = wave_sum(l * f);
+    float o[R] = {};
+    for (int s0 = wv; s0 < a.splits; s0 += 4 * U) {
+        float x[U][R];
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-            if (lane + 64 * i < D) o[i] = fmaf(from[kPartHead + lane + 64 * i], f, o[i]);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const int s = min(s0 + 4 * u, a.splits - 1);
+                x[u][i] = lane + 64 * i < D ? parts[s * stride + kPartHead + lane + 64 * i] : 0.f;
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = s0 + 4 * u;
+            const float fs = __shfl(f, min(s, a.splits - 1));
+#pragma unroll
+            for (int i = 0; i < R; ++i) o[i] = s < a.splits ? fmaf(x[u][i], fs, o[i]) : o[i];
+        }
     }
+    if (wv > 0)
+#pragma unroll
+        for (int i = 0; i < R; ++i) sums[wv - 1][lane + 64 * i] = o[i];
+    __syncthreads();
+    if (wv > 0) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int p = (int)(unit / a.hk), head = (int)(unit % a.hk) * g + r % g;
     bool nan = false;
 #pragma unroll
-    for (int i = 0; i < R; ++i) nan = nan || o[i] * inv != o[i] * inv;
+    for (int i = 0; i < R; ++i) {
+        for (int w = 0; w < 3; ++w) o[i] += sums[w][lane + 64 * i];
+        o[i] *= inv;
+        nan = nan || o[i] != o[i];
+    }
+    const int p = (int)(unit / a.hk), head = (int)(unit % a.hk) * g + r % g;
     if (__any(nan)) {  // (a hidden frame's infinity times its weight of zero)
         vector_row<T>(a, b, stream_of(a, b), t, p, head, lane);
         return;
@@ -226,7 +248,7 @@ __global__ __launch_bounds__(256) void sink_join_kernel(const SinkArgs a)
     T *to = (T *)a.O + (((int64_t)b * a.T + t) * a.P + p) * a.h * D + (int64_t)head * D;
 #pragma unroll
     for (int i = 0; i < R; ++i)
-        if (lane + 64 * i < D) to[lane + 64 * i] = (T)(o[i] * inv);
+        if (lane + 64 * i < D) to[lane + 64 * i] = (T)o[i];
 }
 
 bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
@@ -384,7 +406,7 @@ int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, cons
         e = hipGetLastError();
     }
     if (e == hipSuccess && k.splits > 1) {
-        const unsigned blocks = (unsigned)(((int64_t)a.B * a.T * a.P * a.h + 3) / 4);
+        const unsigned blocks = (unsigned)((int64_t)a.B * a.T * a.P * a.h);
         if (f32)
             hipLaunchKernelGGL((sink_join_kernel<float>), dim3(blocks), dim3(256), 0, st, a);
         else

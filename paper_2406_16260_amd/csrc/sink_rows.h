@@ -250,12 +250,8 @@ const void *rows_kernel_of(int LG, int PV)
     if constexpr (R == 1) {
         DSATTN_ROWS(1, 3);
         DSATTN_ROWS(2, 3);
-        DSATTN_ROWS(4, 3);
-        DSATTN_ROWS(8, 3);
         DSATTN_ROWS(1, 5);
         DSATTN_ROWS(2, 5);
-        DSATTN_ROWS(4, 5);
-        DSATTN_ROWS(8, 5);
     }
 #undef DSATTN_ROWS
     return nullptr;
@@ -277,23 +273,28 @@ RowsLaunch rows_launch(const dsattn_sink_desc &d)
     const int pieces = d.head_dim / V;
     if (pieces > 64) return k;
     k.R = rows > 2 ? 4 : rows;
-    // lanes of a unit: the power of two in its pieces, where three or five a lane are left of them and one row's
-    // sums leave the registers for it; else as many as there are pieces, up to a power of two
-    int two = pieces & -pieces;
-    const int odd = pieces / two;
+    // Lanes of a unit: as many as there are pieces, up to a power of two; or three or five pieces a lane where one or two
+    // lanes then hold a unit and one row's sums leave the registers for it.  One frame over 4 first and some last ones, us in
+    // a captured graph, pieces a lane and idle lanes: 640 positions, 8 x 80, 32 frames 15.3 and 17.5; 2,560 positions, 8 x 40,
+    // 16 frames 18.0 and 19.9; but four lanes: 160 positions, 8 x 160, 60 frames 14.7 and 13.6, 300 positions, 8 x 96, 150
+    // frames 33.1 and 30.7.
+    const int two = pieces & -pieces, odd = pieces / two;
     k.PV = 1;
     for (k.LG = 1; k.LG < pieces;) k.LG *= 2;
-    if (k.R == 1 && (odd == 3 || odd == 5) && two <= 8) {
+    if (k.R == 1 && (odd == 3 || odd == 5) && two <= 2) {
         k.LG = two;
         k.PV = odd;
     }
-    // Units of a wavefront, and workgroups for one unit's frames, so that about 2,048 wavefronts have work, of a step's
-    // frames a group of lanes at least (of 32 where another kernel has to join the workgroups').
+    // Units of a wavefront: as many as leave about 512 wavefronts (2,048: 640 positions, 8 x 80, 21.1 us instead of 15.3), of a
+    // step's frames a group of lanes at least.  Then workgroups for one unit's frames, up to 2,048 wavefronts, of eight
+    // frames a group at least, or of 64 where there are 512 wavefronts already: a kernel joins them (16 streams over 16,384
+    // frames, 32 heads on 8 x 128: 688 us by one, 228 by four; one token of 32 heads on 8 x 128 over 4,096: 39 us by 8 workgroups a unit,
+    // 20 by 32; 160 positions, 8 x 128, over 64: 11.2 us by one, 15.8 by two).
     const int64_t units = (int64_t)d.spatial * d.kv_heads, n = (int64_t)d.sinks + d.window + d.frames;
     auto waves = [&](int U) { return d.streams * ((units + U - 1) / U) * 4; };
-    for (k.U = 64 / k.LG; k.U > 1 && (waves(k.U) < 2048 || k.U / 2 >= units) && n / (4 * 64 / (k.LG * k.U)) > step_frames(k.PV);) k.U /= 2;
+    for (k.U = 64 / k.LG; k.U > 1 && (waves(k.U) < 512 || k.U / 2 >= units) && n / (4 * 64 / (k.LG * k.U)) > step_frames(k.PV);) k.U /= 2;
     const int64_t groups = 4 * 64 / (k.LG * k.U);
-    k.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(2048 + waves(k.U) - 1) / waves(k.U), n / (groups * 32), 64}));
+    k.splits = (int)std::max<int64_t>(1, std::min<int64_t>({2048 / waves(k.U), n / (groups * (waves(k.U) < 512 ? 8 : 64)), kMaxSplits}));
     k.blocks = waves(k.U) / 4 * k.splits;
     if (k.blocks > 0xffffff) return RowsLaunch{};
     k.lds = 3 * k.R * (V * k.PV + 2) * k.LG * k.U * 4;

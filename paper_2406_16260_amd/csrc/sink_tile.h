@@ -469,9 +469,10 @@ TileLaunch tile_launch(const dsattn_sink_desc &d)
     k.tasks = units * k.row_tiles;
     k.splits = 1;
     if (!shared) {
-        // few wavefronts: up to 2,048 with parts of the frames each, of four tiles at least
+        // few wavefronts: up to 1,024 with parts of the frames each, of four tiles at least (16 streams of 4 tokens, 32 heads on
+        // 8 x 128, over 8,192: 129 us up to 2,048, 122 up to 1,024; 4 streams of 8 tokens over 4,096: 26.5 and 26.6)
         const int64_t n = std::min<int64_t>((int64_t)d.sinks + d.window + d.frames, 1 << 24), tiles = (n + KT - 1) / KT;
-        k.splits = (int)std::max<int64_t>(1, std::min<int64_t>({2048 / std::max<int64_t>(k.tasks, 1), tiles / 4, 64}));
+        k.splits = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / std::max<int64_t>(k.tasks, 1), tiles / 4, kMaxSplits}));
         k.tasks *= k.splits;
     }
     k.workgroups = shared ? k.tasks : (k.tasks + 3) / 4;
