@@ -250,13 +250,16 @@ def _stream(stream):
 # checks below, which accept what may be accepted and say what is wrong with the rest.  Nothing is
 # remembered about a tensor from one call to the next.
 _torch = None
+_current_device = None
 _DTYPES = {}
 _I32 = "int32"  # (in the place of a dtype code, for index tensors)
 
 
 def _setup_torch():
-    global _torch
+    global _torch, _current_device
     import torch
+    # (without the checks of torch.cuda.current_device(), which a tensor on a device has already passed)
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _DTYPES.update({DSATTN_F32: torch.float32, DSATTN_BF16: torch.bfloat16,
                     DSATTN_E4M3: torch.float8_e4m3fn, _I32: torch.int32})
     _torch = torch
@@ -284,7 +287,7 @@ def _device_of(t):
     if _torch is None:
         _setup_torch()
     dev = t.get_device() if isinstance(t, _torch.Tensor) else -1
-    return dev if dev >= 0 and dev == _torch.cuda.current_device() else -2
+    return dev if dev >= 0 and dev == _current_device() else -2
 
 
 def _raw_stream(stream):
@@ -292,7 +295,7 @@ def _raw_stream(stream):
     if stream is None:
         raw = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
         if raw is not None:
-            return raw(_torch.cuda.current_device())
+            return raw(_current_device())
     return _stream(stream)
 
 
