@@ -26,7 +26,8 @@ __device__ __forceinline__ void wave_lds_sync()
     __builtin_amdgcn_wave_barrier();
 }
 
-// maximum / sum over the lanes l, l ^ 16, l ^ 32, l ^ 48
+// maximum (NaN where one is: fmaxf() takes an instruction more for each of its operands, to drop it) / sum over the lanes
+// l, l ^ 16, l ^ 32, l ^ 48
 template <bool MAX>
 __device__ __forceinline__ float over_quarters(float x)
 {
@@ -34,12 +35,12 @@ __device__ __forceinline__ float over_quarters(float x)
     const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
     const unsigned r0 = r[0], r1 = r[1];
     const float y0 = __builtin_bit_cast(float, r0), y1 = __builtin_bit_cast(float, r1);
-    x = MAX ? fmaxf(y0, y1) : y0 + y1;
+    x = MAX ? __builtin_elementwise_maximum(y0, y1) : y0 + y1;
     a = __builtin_bit_cast(unsigned, x);
     const auto s = __builtin_amdgcn_permlane32_swap(a, a, false, false);
     const unsigned s0 = s[0], s1 = s[1];
     const float z0 = __builtin_bit_cast(float, s0), z1 = __builtin_bit_cast(float, s1);
-    return MAX ? fmaxf(z0, z1) : z0 + z1;
+    return MAX ? __builtin_elementwise_maximum(z0, z1) : z0 + z1;
 }
 
 // LDS rows of NB 64-byte blocks.  K is read by 16-byte pieces: the 16 lanes that are served together are on rows 0 - 3 and
@@ -272,8 +273,8 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
 #pragma unroll
             for (int k = 0; k < KB; ++k)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][k][e]);
-            top = fmaxf(m[i], over_quarters<true>(top) * a.sc);
+                for (int e = 0; e < 4; ++e) top = __builtin_elementwise_maximum(top, s[i][k][e]);
+            top = __builtin_elementwise_maximum(m[i], over_quarters<true>(top) * a.sc);
             shiftv[i] = top == -INFINITY ? 0.f : top;
             if (__any(top > m[i])) {
                 const float old = __builtin_amdgcn_exp2f(m[i] - shiftv[i]);
