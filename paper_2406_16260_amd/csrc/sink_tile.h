@@ -97,7 +97,7 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
     // Shared: the row tiles of a unit are neighbours, the longest first.  (A unit's K and V stay in one XCD's L2, and the short
     // ones at a stream's start are spread over the XCDs.)  Else the heads are (they share memory pages and lines), then the
     // row tiles of a unit (they share frames).
-    const uint32_t parts = SHARED ? 1u : (uint32_t)a.splits, inner = (uint32_t)(SHARED ? a.row_tiles : a.hk);
+    const uint32_t parts = (uint32_t)a.splits, inner = (uint32_t)(SHARED ? a.row_tiles : a.hk);
     const uint32_t outer = (uint32_t)(SHARED ? a.hk : a.row_tiles);
     uint32_t rest = parts > 1 ? id / parts : id;
     const int split = parts > 1 ? (int)(id - rest * parts) : 0;
@@ -338,20 +338,19 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
         }
     };
 
-    const int tiles = (fr.n + KT - 1) / KT;
+    // this task's tiles: all, or a part of them
+    const int tiles = (fr.n + KT - 1) / KT, per = (tiles + a.splits - 1) / a.splits;
+    const int t0 = split * per, t1 = min(tiles, t0 + per);
     if constexpr (SHARED) {
-        // tiles that no row of the workgroup sees: between the sinks in their window and the next row's window there
-        // are none (frames_of() leaves them out)
-        if (tiles > 0) fetch(0);
-        for (int t = 0; t < tiles; ++t) {
+        if (t0 < t1) fetch(t0);
+        for (int t = t0; t < t1; ++t) {
             put(t, t & 1);
-            if (t + 1 < tiles) fetch(t + 1);
+            if (t + 1 < t1) fetch(t + 1);
             __builtin_amdgcn_s_setprio(0);
             __syncthreads();  // everybody's part of tile t is there, and tile t - 1, whose buffer is next, is done with
             multiply(t, mem + (t & 1) * TILE);
         }
     } else {
-        const int per = (tiles + a.splits - 1) / a.splits, t0 = split * per, t1 = min(tiles, t0 + per);
         if (t0 < t1) fetch(t0);
         for (int t = t0; t < t1; ++t) {
             wave_lds_sync();
@@ -366,7 +365,7 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
     for (int i = 0; i < RB; ++i) {
         const float sum = F32 ? over_quarters<false>(l[i]) : ls[i][0];
         const int r = r0 + 16 * i + l16;
-        if (!SHARED && a.splits > 1) {
+        if (a.splits > 1) {
             if (r >= rows) continue;
             float *to = part_of(a, b, (int64_t)p * a.hk + kvh, r, a.T * g, split);
             if (lg == 0) {
@@ -468,14 +467,18 @@ TileLaunch tile_launch(const dsattn_sink_desc &d)
     if ((rows + per - 1) / per > 0x7fffffff) return k;
     k.row_tiles = (int)((rows + per - 1) / per);
     k.tasks = units * k.row_tiles;
-    k.splits = 1;
-    if (!shared) {
-        // few wavefronts: up to 1,024 with parts of the frames each, of four tiles at least (16 streams of 4 tokens, 32 heads on
-        // 8 x 128, over 8,192: 129 us up to 2,048, 122 up to 1,024; 4 streams of 8 tokens over 4,096: 26.5 and 26.6)
-        const int64_t n = std::min<int64_t>((int64_t)d.sinks + d.window + d.frames, 1 << 24), tiles = (n + KT - 1) / KT;
-        k.splits = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / std::max<int64_t>(k.tasks, 1), tiles / 4, kMaxSplits}));
-        k.tasks *= k.splits;
-    }
+    // Few tasks: parts of the frames each, of four tiles at least, up to 1,024 wavefronts apart (16 streams of 4 tokens, 32 heads
+    // on 8 x 128, over 8,192: 129 us up to 2,048, 122 up to 1,024; 4 streams of 8 tokens over 4,096: 26.5 and 26.6) or 512
+    // workgroups shared.
+    const int64_t n = std::min<int64_t>((int64_t)d.sinks + d.window + (shared ? per / (d.heads / d.kv_heads) : d.frames), 1 << 24);
+    const int64_t tiles = (n + KT - 1) / KT;
+    k.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(shared ? 512 : 1024) / k.tasks, tiles / 4, kMaxSplits}));
+    // What the join costs, 5 us and 1.5 ns a row, against what the parts save, 1.6 us a shared tile (fp32 2.5).  Measured us, whole
+    // and in parts: 384 tokens, 8 heads on 2 x 32, window 3,372, 53.9 and 21.3; 512, 16 on 4 x 128, 4,096, 109 and 53; 1,035,
+    // 20 on 5 x 40, 911, 24.1 and 54.9; 2,048, 16 on 4 x 128, 4,096, 57.6 and 96.3.
+    const double tile_us = f32 ? 2.5 : 1.6, join_us = 5.0 + 1.5e-3 * (double)d.streams * d.frames * d.spatial * d.heads;
+    if (shared && (double)(tiles - (tiles + k.splits - 1) / k.splits) * tile_us < join_us) k.splits = 1;
+    k.tasks *= k.splits;
     k.workgroups = shared ? k.tasks : (k.tasks + 3) / 4;
     if (k.workgroups > 0xffffff - 8) return TileLaunch{};
     k.lds = tile_lds_bytes(f32, NB, KT, shared);
