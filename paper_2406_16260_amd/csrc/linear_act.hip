@@ -1,6 +1,15 @@
 // Token-wise product with bias, activation, gate and residual in its epilogue (dsattn_linear_act).
 //
 //   z_k = (X W_k^T) x_scale w_scale_k + b_k,   Y = act(z_0) [* z_1] + R
+//
+// Bound by the matrix cores where there are many rows, by latency where there are few.  Four kernels on the matrix cores and a
+// vector kernel for rows that are not whole 16-byte pieces; estimates of their times choose (act_pick()).  us and TFLOP/s:
+//   25,920 x 5,120 x 1,280, residual, bf16             270   1,260   (elementary fp32 operations 2,560; a library product
+//                                                                     without bias and residual 251)
+//   40,960 x 640 x 5,120, bias, bf16                   232   1,157   (library product 308 to 348)
+//   40,960 x 640 x 2 x 2,560, GELU gate, bf16          257   1,045
+//   61,440 x 1,280 x 2 x 5,120, GELU gate, 8 bits      790   2,040   (16,384 x 5,120 x 16,384: 2,790 to 2,860)
+//   160 x 1,280 x 1,280, bf16                          4.1           in a captured graph
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
