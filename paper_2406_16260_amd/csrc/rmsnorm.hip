@@ -142,8 +142,8 @@ __global__ __launch_bounds__(L <= 256 ? 256 : L) void rms_vec_kernel(const RmsAr
     }
 }
 
-// The kernel of a shape: the fewest lanes that hold the row in four pieces each (eight where its numbers go one by
-// one, in rows that are not whole 16-byte pieces); null: longer than 1,024 lanes hold.
+// The kernel of a shape: pieces of as many numbers as divide the row, up to 16 bytes, and the fewest lanes that hold the row in
+// four pieces each (eight of one or two numbers); null: longer than 1,024 lanes hold.
 struct RmsKernel {
     const void *fn;
     int lanes;
@@ -167,17 +167,17 @@ RmsKernel rms_pick_of(int C)
     if (pieces <= 16) return {(const void *)&rms_vec_kernel<T, V, 16, 1, E8>, 16};
     if (pieces <= 32) return {(const void *)&rms_vec_kernel<T, V, 32, 1, E8>, 32};
     if (pieces <= 256) return {rms_kernel_of<T, V, E8, 64>((pieces + 63) / 64), 64};
-    if (V == 1 && pieces <= 512) return {(const void *)&rms_vec_kernel<T, V, 64, 8, E8>, 64};
+    if (V <= 2 && pieces <= 512) return {(const void *)&rms_vec_kernel<T, V, 64, 8, E8>, 64};
     if (pieces <= 1024) return {rms_kernel_of<T, V, E8, 256>((pieces + 255) / 256), 256};
-    if (V == 1 && pieces <= 2048) return {(const void *)&rms_vec_kernel<T, V, 256, 8, E8>, 256};
+    if (V <= 2 && pieces <= 2048) return {(const void *)&rms_vec_kernel<T, V, 256, 8, E8>, 256};
     if (pieces <= 4096) return {rms_kernel_of<T, V, E8, 1024>((pieces + 1023) / 1024), 1024};
     return {nullptr, 0};
 }
 template <typename T, bool E8>
 RmsKernel rms_pick(int C)
 {
-    constexpr int V = 16 / (int)sizeof(T);
-    return C % V == 0 ? rms_pick_of<T, V, E8>(C) : rms_pick_of<T, 1, E8>(C);
+    if (sizeof(T) == 2 && C % 8 == 0) return rms_pick_of<T, 16 / (int)sizeof(T), E8>(C);
+    return C % 4 == 0 ? rms_pick_of<T, 4, E8>(C) : C % 2 == 0 ? rms_pick_of<T, 2, E8>(C) : rms_pick_of<T, 1, E8>(C);
 }
 
 // Rows longer than that: a workgroup a row, two passes over it.

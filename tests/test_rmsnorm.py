@@ -73,7 +73,7 @@ def run(rows, C, dtype, out, seed, residual=True, affine=True, want_sum=True, ep
 
 
 ROWS_C = [(1, 1), (3, 7), (5, 8), (2, 31), (17, 40), (1000, 64), (33, 80), (129, 96), (66, 128), (7, 160), (5, 250),
-          (9, 320), (3, 636), (31, 640), (40, 1280), (2, 1284), (11, 2560), (6, 4096), (4, 5120), (3, 8192), (2, 9999),
+          (9, 320), (3, 636), (70, 12), (33, 36), (5, 130), (4, 530), (3, 1030), (3, 1866), (2, 3996), (2, 4098), (2, 10004), (1, 16396), (31, 640), (40, 1280), (2, 1284), (11, 2560), (6, 4096), (4, 5120), (3, 8192), (2, 9999),
           (3, 16384), (2, 20000), (1, 65536)]
 
 
