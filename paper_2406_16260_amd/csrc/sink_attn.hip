@@ -9,7 +9,7 @@
 //   16 streams, a token of 32 heads on 8 x 128 over 16,388      225   93 %
 //   a frame of 160 positions, 8 x 160, over 64                 12.8   82 %
 //   128 frames of 640 positions, 8 x 80, window 32, cached      129   74 %
-//   2 prompts of 8,192, 16 heads on 4 x 128, window 2,048       288   54 %
+//   2 prompts of 8,192, 16 heads on 4 x 128, window 2,048       277   57 %
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

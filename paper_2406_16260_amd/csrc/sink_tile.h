@@ -241,6 +241,17 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
                     }
                 }
             }
+        // Eight pieces of K on their way ahead of the multiplies, all the time (by itself the compiler reads two and waits for them:
+        // 287 -> 277 us, 2 prompts of 8,192, 16 heads on 4 x 128, window 2,048).
+        if constexpr (!F32 && SHARED && KB == 4 && RB == 2) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
+#pragma unroll
+            for (int x = 0; x < 4 * NB - 8; x += 2) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 2 * RB, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 8 * RB, 1);
+        }
         // hidden keys: key 16 k + 4 lg + e of the tile
         if (j0 + KT - 1 > hi_all || (j0 <= lw_all && j0 + KT - 1 >= always)) {
             if (j0 >= always) {  // behind the sinks a row sees the keys from lw + 1 to hi
