@@ -268,8 +268,9 @@ RowsLaunch rows_launch(const dsattn_sink_desc &d)
 {
     RowsLaunch k{};
     const bool f32 = d.io_dtype == DSATTN_F32;
-    const int V = f32 ? 4 : 8, rows = d.frames * (d.heads / d.kv_heads);
-    if (d.frames > 4 || rows > 4 || d.head_dim % V != 0) return k;
+    const int V = f32 ? 4 : 8;
+    if (d.frames > 4 || d.heads / d.kv_heads > 4 / d.frames || d.head_dim % V != 0) return k;
+    const int rows = d.frames * (d.heads / d.kv_heads);
     const int pieces = d.head_dim / V;
     if (pieces > 64) return k;
     k.R = rows > 2 ? 4 : rows;

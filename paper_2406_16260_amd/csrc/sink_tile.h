@@ -178,7 +178,7 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
     const int own_first = st.start + first / g, own_last = st.start + last / g;
     const bool puts = puts_frames(a, st);
     auto put = [&](int tile, int buf) __attribute__((always_inline)) {
-        if (puts && tile * KT + KT - 1 + (fr.lo - fr.ns) >= own_first) {
+        if (puts && tile * KT + KT - 1 >= own_first - shift) {  // (a frame's number past the last one's may not fit)
             typedef __attribute__((address_space(1))) Piece *Slots;
 #pragma unroll
             for (int n = 0; n < PASSES; ++n) {
@@ -475,7 +475,7 @@ TileLaunch tile_launch(const dsattn_sink_desc &d)
     const int RB = tile_blocks(f32, NB, shared, many), KT = tile_frames(f32, shared, many);
     k.waves = tile_group(f32, NB, shared);
     const int per = 16 * RB * (shared ? k.waves : 1);
-    if ((rows + per - 1) / per > 0x7fffffff) return k;
+    if (rows > 0x7fffff00) return k;  // (numbered with 32 bits)
     k.row_tiles = (int)((rows + per - 1) / per);
     k.tasks = units * k.row_tiles;
     // Few tasks: parts of the frames each, of four tiles at least, up to 1,024 wavefronts apart (16 streams of 4 tokens, 32 heads

@@ -318,16 +318,18 @@ def test_starts_and_counts_outside_their_ranges_count_as_the_nearest():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T", [1, 3, 40])
-def test_the_largest_frame_numbers(T):
-    c = case("bf16", T=T, P=2, h=2, D=64, sinks=2, window=6, ring=17)
-    s, at = Stream(case("bf16", T=T, P=2, h=2, D=64, sinks=2, window=6, ring=17, start=0x7fffffff - T - 1000), 5), 0x7fffffff - T
+@pytest.mark.parametrize("T,ring", [(1, 17), (3, 17), (40, 17), (40, 100), (90, 97)])
+def test_the_largest_frame_numbers(T, ring):
+    c = case("bf16", T=T, P=2, h=2, D=64, sinks=2, window=6, ring=ring)
+    s, at = Stream(case("bf16", T=T, P=2, h=2, D=64, sinks=2, window=6, ring=ring, start=0x7fffffff - T - 1000), 5), 0x7fffffff - T
     s.start = [at]
     O = torch.zeros(1, T, 2, 128, dtype=torch.bfloat16, device=DEV)
     rng = torch.Generator().manual_seed(1)
     s.Kc, s.Vc = (torch.randn(s.Kc.shape, generator=rng).to(torch.bfloat16) for _ in range(2))
-    forward(s, c, O, s.Kc.to(DEV), s.Vc.to(DEV))
+    Kc, Vc = s.Kc.to(DEV), s.Vc.to(DEV)
+    forward(s, c, O, Kc, Vc)
     torch.cuda.synchronize()
+    assert all(same_bits(got, want) for got, want in zip((Kc, Vc), s.caches()))
     frames = [0, 1] + list(range(at - 5, at + T))
     for t in range(T):
         a = at + t
