@@ -7,8 +7,8 @@
 //   25,920 x 5,120 x 1,280, residual, bf16             270   1,260   (elementary fp32 operations 2,560; a library product
 //                                                                     without bias and residual 251)
 //   40,960 x 640 x 5,120, bias, bf16                   232   1,157   (library product 308 to 348)
-//   40,960 x 640 x 2 x 2,560, GELU gate, bf16          257   1,045
-//   61,440 x 1,280 x 2 x 5,120, GELU gate, 8 bits      790   2,040   (16,384 x 5,120 x 16,384: 2,790 to 2,860)
+//   40,960 x 640 x 2 x 2,560, GELU gate, bf16          249 to 264   1,020 to 1,080
+//   61,440 x 1,280 x 2 x 5,120, GELU gate, 8 bits      783 to 814   1,980 to 2,060   (16,384 x 5,120 x 16,384: 2,790 to 2,860)
 //   160 x 1,280 x 1,280, bf16                          4.1           in a captured graph
 #include <hip/hip_runtime.h>
 #include <stdint.h>
