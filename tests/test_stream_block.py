@@ -189,3 +189,25 @@ def test_calls_run_on_the_stream_they_are_given():
     t = {"X": y, "W": [a.w["q"]], "sx": None, "sw": None, "b": None, "R": None}
     want, tol = L.reference(t, "none", "bf16")
     assert ((a.q.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,P,h,hk,D,sinks,window,hidden", [SHAPES[1], SHAPES[3], (1, 1, 8, 2, 128, 4, 3000, 512)])
+def test_two_streams_at_once(T, P, h, hk, D, sinks, window, hidden):
+    """Two blocks with buffers and workspaces of their own, on two streams, nothing waiting between their calls."""
+    both = [Block(T, P, h, hk, D, sinks, window, hidden, True, s) for s in (1, 2)]
+    alone = [Block(T, P, h, hk, D, sinks, window, hidden, True, s) for s in (1, 2)]
+    xs = frames(both[0], 9, 10)
+    side = [torch.cuda.Stream() for _ in both]
+    torch.cuda.synchronize()
+    for x in xs:
+        for blk, s in zip(both, side):
+            with torch.cuda.stream(s):
+                blk.step(x)
+    torch.cuda.synchronize()
+    for blk, ref in zip(both, alone):
+        for x in xs:
+            ref.step(x)
+        torch.cuda.synchronize()
+        for name in ("y", "a", "f", "Kc", "Vc"):
+            assert S.same_bits(getattr(blk, name), getattr(ref, name)), name
