@@ -7,7 +7,6 @@ namespace dsattn {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -33,7 +32,7 @@ __host__ __device__ constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4
 // of the block of W rows and row l % BS of the block of X rows (q = 0 only where BS is 16).
 template <typename T>
 struct Mul {
-    static constexpr int BS = 16, QUADS = 1, kk_bytes = 64;
+    static constexpr int BS = 16, QUADS = 1;
     using Acc = f32x4;
     using Frag = std::conditional_t<sizeof(T) == 4, f32x4, bf16x8>;
     static __device__ __forceinline__ int offset(int lane, int kk) { return (((4 * kk) | (lane >> 4)) ^ (lane & 7)) * 16; }
@@ -52,7 +51,7 @@ struct Mul {
 };
 template <>
 struct Mul<e4m3> {
-    static constexpr int BS = 32, QUADS = 4, kk_bytes = 64;
+    static constexpr int BS = 32, QUADS = 4;
     using Acc = f32x16;
     using Frag = i32x8;
     // (position p of row r holds chunk p ^ r % 8: the second chunk is two further on, another bit of the position.  Half of these
@@ -72,7 +71,7 @@ struct Mul<e4m3> {
 
 template <>
 struct Mul<e4m3w> {
-    static constexpr int BS = 16, QUADS = 1, kk_bytes = 64;
+    static constexpr int BS = 16, QUADS = 1;
     using Acc = f32x4;
     struct Frag { bf16x8 half[2]; };
     static __device__ __forceinline__ int offset(int lane, int kk) { return Mul<__bf16>::offset(lane, kk); }
@@ -144,12 +143,6 @@ __device__ __forceinline__ void with_act(int act, F &&f)
     default: f(std::integral_constant<int, DSATTN_ACT_NONE>{}); break;
     }
 }
-
-// What the epilogue wants of a wavefront's channels, in LDS: bias and scale of each column of its part (gated: of
-// the gate's columns and the value's).
-struct ColumnLds {
-    float *bias, *scale;
-};
 
 // The column of W behind row r of a column tile: set, and channel from the tile's first on.  Gated, blocks of BS
 // rows of the gate and of the value alternate, so that a lane holds both of a channel.

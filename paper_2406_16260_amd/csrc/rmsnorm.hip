@@ -151,8 +151,9 @@ struct RmsKernel {
 template <typename T, int V, bool E8, int L>
 const void *rms_kernel_of(int nv)
 {
+    if constexpr (L == 64)  // (with more lanes a row is longer than one piece each)
+        if (nv == 1) return (const void *)&rms_vec_kernel<T, V, L, 1, E8>;
     switch (nv) {
-    case 1: return (const void *)&rms_vec_kernel<T, V, L, 1, E8>;
     case 2: return (const void *)&rms_vec_kernel<T, V, L, 2, E8>;
     case 3: return (const void *)&rms_vec_kernel<T, V, L, 3, E8>;
     case 4: return (const void *)&rms_vec_kernel<T, V, L, 4, E8>;

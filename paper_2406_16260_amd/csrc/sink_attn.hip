@@ -117,7 +117,7 @@ constexpr int kMaxDim = 512;
 template <typename T>
 __device__ __forceinline__ void vector_row(const SinkArgs &a, int b, const Stream &s, int t, int p, int g, int lane)
 {
-    const int frame = s.start + t, D = a.D;
+    const int D = a.D;
     const int64_t id = (((int64_t)b * a.T + t) * a.P + p) * a.h + g;
     const T *q = (const T *)a.Q + id * D;
     const int64_t at = ((int64_t)p * a.hk + g / (a.h / a.hk)) * D;  // within a frame of K and V
