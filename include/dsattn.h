@@ -412,6 +412,11 @@ typedef struct dsattn_linear_act_desc {
     uint32_t flags;    /* DSATTN_FLAG_FORCE_GENERIC or 0 */
 } dsattn_linear_act_desc;
 
+/* The launch dsattn_linear_act would make (host only): kernel 1 = matrix cores (tiles of 32 x 32 share a
+ * contraction between wavefronts, those of 256 x 256 are walked by persistent workgroups), 0 = the
+ * vector kernel; tile_n counts rows of all W_k, n_blocks output tiles (the vector kernel: workgroups). */
+int dsattn_linear_act_info(const dsattn_linear_act_desc *desc, dsattn_conv_info *info);
+
 /*
  *   X        : device, [rows, c_in] of io_dtype, 16-byte aligned
  *   x_scales : device, [rows] fp32; with DSATTN_E4M3, NULL for 1

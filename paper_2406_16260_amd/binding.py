@@ -39,7 +39,7 @@ EXPORTS = (
     "dsattn_groupnorm", "dsattn_temporal_conv_info", "dsattn_temporal_conv", "dsattn_linear_info",
     "dsattn_linear", "dsattn_groupnorm_static", "dsattn_groupnorm_static_max_bytes",
     "dsattn_temporal_layer_workspace", "dsattn_temporal_layer", "dsattn_rmsnorm", "dsattn_linear_act",
-    "dsattn_sink_workspace", "dsattn_sink_forward",
+    "dsattn_linear_act_info", "dsattn_sink_workspace", "dsattn_sink_forward",
 )
 
 
@@ -200,6 +200,8 @@ def load():
     lib.dsattn_linear_act.restype = ctypes.c_int
     lib.dsattn_linear_act.argtypes = [ctypes.POINTER(DsattnLinearActDesc), vp, vp, ctypes.POINTER(vp),
                                       ctypes.POINTER(vp), ctypes.POINTER(vp), vp, vp, vp]
+    lib.dsattn_linear_act_info.restype = ctypes.c_int
+    lib.dsattn_linear_act_info.argtypes = [ctypes.POINTER(DsattnLinearActDesc), ctypes.POINTER(DsattnConvInfo)]
     lib.dsattn_sink_workspace.restype = ctypes.c_int
     lib.dsattn_sink_workspace.argtypes = [ctypes.POINTER(DsattnSinkDesc), ctypes.POINTER(ctypes.c_size_t)]
     lib.dsattn_sink_forward.restype = ctypes.c_int
@@ -709,6 +711,14 @@ def dsattn_rmsnorm(rows, channels, X, Y, residual=None, gamma=None, sum_out=None
                     (Y, "Y", n, out), (scales, "scales", rows, DSATTN_F32)], "current")
     _check(load().dsattn_rmsnorm(ctypes.byref(desc), _ptr(X), _ptr(residual), _ptr(gamma), _ptr(sum_out),
                                  _ptr(Y), _ptr(scales), _stream(stream)), "dsattn_rmsnorm")
+
+
+def dsattn_linear_act_info(rows, c_in, c_out, n_w=1, act=DSATTN_ACT_NONE, io_dtype=DSATTN_BF16, out_dtype=None,
+                           flags=0) -> dict:
+    out = (DSATTN_BF16 if io_dtype == DSATTN_E4M3 else io_dtype) if out_dtype is None else out_dtype
+    desc, info = DsattnLinearActDesc(rows, c_in, c_out, n_w, act, io_dtype, out, flags), DsattnConvInfo()
+    _check(load().dsattn_linear_act_info(ctypes.byref(desc), ctypes.byref(info)), "dsattn_linear_act_info")
+    return info.as_dict()
 
 
 def dsattn_linear_act(rows, c_in, c_out, X, Ws, Y, biases=None, residual=None, x_scales=None, w_scales=None,

@@ -256,16 +256,8 @@ bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
 
 int64_t dtype_bytes(int32_t t) { return t == DSATTN_F32 ? 4 : t == DSATTN_BF16 ? 2 : 1; }
 
-}  // namespace
-}  // namespace dsattn
-
-using namespace dsattn;
-
-extern "C" int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void *X, const float *x_scales,
-                                 const void *const *W, const float *const *w_scales,
-                                 const float *const *bias, const void *residual, void *Y, void *stream)
+int act_validate(const dsattn_linear_act_desc *desc, const char *who)
 {
-    const char *who = "dsattn_linear_act";
     if (!desc) return fail(DSATTN_EINVAL, "%s: null descriptor", who);
     const dsattn_linear_act_desc &d = *desc;
     if (d.rows < 1 || d.rows > 0x7fffffffLL || d.c_in < 1 || d.c_out < 1)
@@ -279,6 +271,52 @@ extern "C" int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void 
         return fail(DSATTN_EINVAL, "%s: the output is fp32, or bf16 of inputs of 16 or 8 bits", who);
     if (d.flags & ~DSATTN_FLAG_FORCE_GENERIC)
         return fail(DSATTN_EINVAL, "%s: unknown flag bits 0x%x", who, d.flags);
+    return DSATTN_OK;
+}
+
+}  // namespace
+}  // namespace dsattn
+
+using namespace dsattn;
+
+extern "C" {
+
+int dsattn_linear_act_info(const dsattn_linear_act_desc *desc, dsattn_conv_info *info)
+{
+    const int rc = act_validate(desc, "dsattn_linear_act_info");
+    if (rc != DSATTN_OK) return rc;
+    if (!info) return fail(DSATTN_EINVAL, "dsattn_linear_act_info: null output");
+    const dsattn_linear_act_desc &d = *desc;
+    const int64_t es = dtype_bytes(d.io_dtype), os = dtype_bytes(d.out_dtype), n = (int64_t)d.c_out * d.n_w;
+    *info = dsattn_conv_info{};
+    const ActLaunch v = act_pick(d, es);
+    if (v.fn) {
+        info->kernel = 1;
+        info->tile_m = v.rows;
+        info->tile_n = v.cols;
+        info->tile_k = (int32_t)(kRow / es);
+        info->n_blocks = (int32_t)((d.rows + v.rows - 1) / v.rows * ((n + v.cols - 1) / v.cols));
+        info->block_threads = 64 * v.waves;
+        info->lds_bytes = v.lds;
+    } else {
+        info->tile_n = 1;
+        info->tile_k = 1;
+        info->n_blocks = (int32_t)std::min<int64_t>((d.rows * d.c_out + 255) / 256, 0x7fffffff);
+        info->block_threads = 256;
+    }
+    info->useful_flops = 2 * d.rows * d.c_in * n;
+    info->algorithmic_bytes = (d.rows + n) * d.c_in * es + d.rows * d.c_out * os;
+    return DSATTN_OK;
+}
+
+int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void *X, const float *x_scales,
+                      const void *const *W, const float *const *w_scales, const float *const *bias,
+                      const void *residual, void *Y, void *stream)
+{
+    const char *who = "dsattn_linear_act";
+    const int rc = act_validate(desc, who);
+    if (rc != DSATTN_OK) return rc;
+    const dsattn_linear_act_desc &d = *desc;
     if (!X || !W || !Y) return fail(DSATTN_EINVAL, "%s: null pointer", who);
     const int64_t es = dtype_bytes(d.io_dtype), os = dtype_bytes(d.out_dtype);
     const int64_t xn = d.rows * d.c_in * es, wn = (int64_t)d.c_out * d.c_in * es, yn = d.rows * d.c_out * os;
@@ -344,3 +382,5 @@ extern "C" int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void 
     if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
     return DSATTN_OK;
 }
+
+}  // extern "C"
