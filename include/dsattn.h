@@ -467,6 +467,22 @@ typedef struct dsattn_sink_desc {
 /* Bytes of device workspace dsattn_sink_forward needs for this shape; may be 0. */
 int dsattn_sink_workspace(const dsattn_sink_desc *desc, size_t *bytes);
 
+/* The launch dsattn_sink_forward would make for this shape (host only). */
+typedef struct dsattn_sink_info {
+    int32_t kernel;        /* 0 = vector kernel; 1 = lanes stream the cache (few queries of a head of K
+                              and V); on the matrix cores, tiles of frames that 2 = a wavefront has for
+                              itself, 3 = a workgroup shares */
+    int32_t splits;        /* parts of a query's frames, joined by a kernel of its own; 1: whole */
+    int32_t tile_rows;     /* kernels 2 and 3: queries of a task, 0 for the others */
+    int32_t tile_frames;   /* likewise: frames of a tile */
+    int32_t n_blocks;      /* workgroups */
+    int32_t block_threads;
+    int32_t lds_bytes;     /* dynamic LDS of a workgroup */
+    int32_t reserved;
+} dsattn_sink_info;
+
+int dsattn_sink_forward_info(const dsattn_sink_desc *desc, dsattn_sink_info *info);
+
 /*
  *   start     : device, [streams] int32 in [0, 2^31 - 1 - frames] (values outside count as the
  *               nearest inside): the index of each stream's first new frame; NULL: 0 for all.

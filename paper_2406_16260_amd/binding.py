@@ -39,7 +39,8 @@ EXPORTS = (
     "dsattn_groupnorm", "dsattn_temporal_conv_info", "dsattn_temporal_conv", "dsattn_linear_info",
     "dsattn_linear", "dsattn_groupnorm_static", "dsattn_groupnorm_static_max_bytes",
     "dsattn_temporal_layer_workspace", "dsattn_temporal_layer", "dsattn_rmsnorm", "dsattn_linear_act",
-    "dsattn_linear_act_info", "dsattn_sink_workspace", "dsattn_sink_forward",
+    "dsattn_linear_act_info", "dsattn_sink_workspace", "dsattn_sink_forward_info",
+    "dsattn_sink_forward",
 )
 
 
@@ -99,6 +100,17 @@ class DsattnSinkDesc(ctypes.Structure):
         ("sinks", ctypes.c_int32), ("window", ctypes.c_int32), ("ring", ctypes.c_int32),
         ("io_dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("flags", ctypes.c_uint32),
     ]
+
+
+class DsattnSinkInfo(ctypes.Structure):
+    _fields_ = [
+        ("kernel", ctypes.c_int32), ("splits", ctypes.c_int32), ("tile_rows", ctypes.c_int32),
+        ("tile_frames", ctypes.c_int32), ("n_blocks", ctypes.c_int32), ("block_threads", ctypes.c_int32),
+        ("lds_bytes", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+    def as_dict(self):
+        return {name: int(getattr(self, name)) for name, _ in self._fields_ if name != "reserved"}
 
 
 class DsattnConvInfo(ctypes.Structure):
@@ -204,6 +216,8 @@ def load():
     lib.dsattn_linear_act_info.argtypes = [ctypes.POINTER(DsattnLinearActDesc), ctypes.POINTER(DsattnConvInfo)]
     lib.dsattn_sink_workspace.restype = ctypes.c_int
     lib.dsattn_sink_workspace.argtypes = [ctypes.POINTER(DsattnSinkDesc), ctypes.POINTER(ctypes.c_size_t)]
+    lib.dsattn_sink_forward_info.restype = ctypes.c_int
+    lib.dsattn_sink_forward_info.argtypes = [ctypes.POINTER(DsattnSinkDesc), ctypes.POINTER(DsattnSinkInfo)]
     lib.dsattn_sink_forward.restype = ctypes.c_int
     lib.dsattn_sink_forward.argtypes = [ctypes.POINTER(DsattnSinkDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                         ctypes.c_size_t, vp]
@@ -765,6 +779,15 @@ def dsattn_sink_workspace(streams, frames, spatial, heads, kv_heads, head_dim, s
     out = ctypes.c_size_t()
     _check(load().dsattn_sink_workspace(ctypes.byref(desc), ctypes.byref(out)), "dsattn_sink_workspace")
     return int(out.value)
+
+
+def dsattn_sink_forward_info(streams, frames, spatial, heads, kv_heads, head_dim, sinks, window, ring=None,
+                             io_dtype=DSATTN_BF16, scale=0.0, flags=0) -> dict:
+    desc = DsattnSinkDesc(streams, frames, spatial, heads, kv_heads, head_dim, sinks, window,
+                          max(window, 1) if ring is None else ring, io_dtype, scale, flags)
+    info = DsattnSinkInfo()
+    _check(load().dsattn_sink_forward_info(ctypes.byref(desc), ctypes.byref(info)), "dsattn_sink_forward_info")
+    return info.as_dict()
 
 
 def dsattn_sink_forward(streams, frames, spatial, heads, kv_heads, head_dim, sinks, window, ring, Q, K, V, O,

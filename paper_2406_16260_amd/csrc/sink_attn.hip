@@ -333,6 +333,33 @@ int dsattn_sink_workspace(const dsattn_sink_desc *desc, size_t *bytes)
     return DSATTN_OK;
 }
 
+int dsattn_sink_forward_info(const dsattn_sink_desc *desc, dsattn_sink_info *info)
+{
+    const int rc = sink_validate(desc, "dsattn_sink_forward_info");
+    if (rc != DSATTN_OK) return rc;
+    if (!info) return fail(DSATTN_EINVAL, "dsattn_sink_forward_info: null output");
+    const dsattn_sink_desc &d = *desc;
+    const SinkLaunch k = sink_launch(d);
+    *info = dsattn_sink_info{};
+    info->splits = k.splits;
+    info->block_threads = 256;
+    if (k.rows.fn) {
+        info->kernel = 1;
+        info->n_blocks = (int32_t)k.rows.blocks;
+        info->lds_bytes = k.rows.lds;
+    } else if (k.tile.fn) {
+        info->kernel = k.tile.shared ? 3 : 2;
+        info->tile_rows = k.tile.rows;
+        info->tile_frames = k.tile.frames;
+        info->n_blocks = (int32_t)((k.tile.workgroups + 7) / 8 * 8);
+        info->block_threads = 64 * k.tile.waves;
+        info->lds_bytes = k.tile.lds;
+    } else {
+        info->n_blocks = (int32_t)std::min<int64_t>(((int64_t)d.streams * d.frames * d.spatial * d.heads + 3) / 4, 0x7fffffff);
+    }
+    return DSATTN_OK;
+}
+
 int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, const int32_t *counts,
                         const void *Q, const void *K, const void *V, void *Kcache, void *Vcache, void *O,
                         void *workspace, size_t workspace_bytes, void *stream)

@@ -454,6 +454,8 @@ const void *tile_kernel_of(int NB)
 struct TileLaunch {
     const void *fn;
     int row_tiles, splits, lds, waves;
+    int rows, frames;  // of a task, of a tile
+    bool shared;
     int64_t tasks, workgroups;
 };
 TileLaunch tile_launch(const dsattn_sink_desc &d)
@@ -474,8 +476,11 @@ TileLaunch tile_launch(const dsattn_sink_desc &d)
     const bool many = shared ? sees >= 128 : rows > 16;
     const int RB = tile_blocks(f32, NB, shared, many), KT = tile_frames(f32, shared, many);
     k.waves = tile_group(f32, NB, shared);
+    k.shared = shared;
+    k.frames = KT;
     const int per = 16 * RB * (shared ? k.waves : 1);
     if (rows > 0x7fffff00) return k;  // (numbered with 32 bits)
+    k.rows = per;
     k.row_tiles = (int)((rows + per - 1) / per);
     k.tasks = units * k.row_tiles;
     // Few tasks: parts of the frames each, of four tiles at least, up to 1,024 wavefronts apart (16 streams of 4 tokens, 32 heads
