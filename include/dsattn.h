@@ -360,8 +360,9 @@ int dsattn_temporal_layer(const dsattn_plan_t *plan, const void *X, const void *
  *   y = s / sqrt(mean(s^2) + eps) * gamma     from the unrounded s, rounded once
  * With out_dtype DSATTN_E4M3 a row gets a scale of its own, max(max|y| / 448, 2^-126), which is
  * written to `scales`, and Y receives y / scale in 8 bits (to nearest, ties to even): the X and
- * x_scales of a dsattn_linear_act.  A row that holds an infinity or a NaN has a NaN scale.  The sum
- * of squares is an fp32 number: rows of a norm beyond 1.8 * 10^19 are not normalised.
+ * x_scales of a dsattn_linear_act.  A row that holds an infinity or a NaN has a NaN scale.  Rows of
+ * every size are normalised: one whose squares are beyond fp32's numbers, at either end, is
+ * multiplied with a power of two first.  A row of zeros is NaN (0 / 0) with eps 0, zeros otherwise.
  */
 typedef struct dsattn_rms_desc {
     int64_t rows;      /* >= 1, at most 2^31 - 1: tokens, or tokens times heads for a norm per head */

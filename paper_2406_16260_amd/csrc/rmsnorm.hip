@@ -39,6 +39,17 @@ __device__ __forceinline__ uint8_t to_e4m3(float y)
 // The maximum of two numbers, NaN if one is: what fmaxf() would drop.
 __device__ __forceinline__ float max_or_nan(float a, float b) { return a > b || a != a ? a : b; }
 
+// A power of two that brings a row's squares into fp32's range, 1 where they are there (a row of ordinary size, and every one
+// where eps is far above the squares that are lost).  Sums of squares below 2^-100 are of numbers below 2^-50 and times 2^100
+// at least 2^-49 and below 2^50; one of 2^128 or more has a number beyond 2^54, and 2^20 squares of numbers below 2^53 fit.  The
+// factor is exact, so that a row's result has the same error at every size, but for what it pushes below 2^-126: numbers
+// below 2^-51 in a row of a norm of 2^64 or more.  (A sum that is infinite for an infinity stays so.)
+__device__ __forceinline__ float row_unit(float ss, float eps)
+{
+    if (ss < 0x1p-100f && eps < 0x1p-80f) return 0x1p100f;
+    return ss == INFINITY ? 0x1p-75f : 1.f;
+}
+
 // The scale of a row whose largest |s gamma| is top.
 __device__ __forceinline__ float row_scale(float top, float rstd)
 {
@@ -61,47 +72,63 @@ __global__ __launch_bounds__(L <= 256 ? 256 : L) void rms_vec_kernel(const RmsAr
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = at + i * (L * V);
-        x[i] = r[i] = Piece{};
+        x[i] = Piece{};
+        r[i] = -Piece{};  // (-0, which leaves every x as it is)
         if (c < C) {
             x[i] = *(const Piece *)((const T *)a.X + base + c);
             if (a.R) r[i] = *(const Piece *)((const T *)a.R + base + c);
         }
     }
     Floats s[NV], g[NV];
-    float ss = 0.f, top = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = at + i * (L * V);
         g[i] = Floats{} + 1.f;
         if (a.gamma && c < C) g[i] = *(const Floats *)(a.gamma + c);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            s[i][e] = a.R ? (float)x[i][e] + (float)r[i][e] : (float)x[i][e];
-            ss = fmaf(s[i][e], s[i][e], ss);
-            if constexpr (E8) top = max_or_nan(top, fabsf(s[i][e] * g[i][e]));
-        }
     }
 #pragma unroll
-    for (int w = 1; w < (L < 64 ? L : 64); w *= 2) {
-        ss += __shfl_xor(ss, w);
-        if constexpr (E8) top = max_or_nan(top, __shfl_xor(top, w));
-    }
-    if constexpr (L > 64) {
-        __shared__ float part[2][NW];
-        if ((threadIdx.x & 63) == 0) {
-            part[0][threadIdx.x >> 6] = ss;
-            part[1][threadIdx.x >> 6] = top;
-        }
-        __syncthreads();
-        ss = part[0][0];
-        top = part[1][0];
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int w = 1; w < NW; ++w) {
-            ss += part[0][w];
-            top = max_or_nan(top, part[1][w]);
+        for (int e = 0; e < V; ++e) s[i][e] = (float)x[i][e] + (float)r[i][e];
+    float ss, top;
+    auto moments = [&](float unit) __attribute__((always_inline)) {
+        ss = top = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float su = s[i][e] * unit;
+                ss = fmaf(su, su, ss);
+                if constexpr (E8) top = max_or_nan(top, fabsf(su * g[i][e]));
+            }
+#pragma unroll
+        for (int w = 1; w < (L < 64 ? L : 64); w *= 2) {
+            ss += __shfl_xor(ss, w);
+            if constexpr (E8) top = max_or_nan(top, __shfl_xor(top, w));
         }
+        if constexpr (L > 64) {
+            __shared__ float part[2][NW];
+            if ((threadIdx.x & 63) == 0) {
+                part[0][threadIdx.x >> 6] = ss;
+                part[1][threadIdx.x >> 6] = top;
+            }
+            __syncthreads();
+            ss = part[0][0];
+            top = part[1][0];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) {
+                ss += part[0][w];
+                top = max_or_nan(top, part[1][w]);
+            }
+        }
+    };
+    moments(1.f);
+    const float unit = row_unit(ss, a.eps);
+    if (unit != 1.f) {  // (the same for all lanes of a row, which a workgroup's barrier is for)
+        if constexpr (L > 64) __syncthreads();
+        moments(unit);
     }
-    const float rstd = 1.f / sqrtf(ss / (float)C + a.eps);
+    const float rstd = 1.f / sqrtf(ss / (float)C + a.eps * unit * unit);
     const float scale = E8 ? row_scale(top, rstd) : 1.f, inv = 1.f / scale;  // (its product with rstd may overflow)
     if (!there) return;
     if (E8 && at == 0) a.scales[row] = scale;
@@ -117,7 +144,7 @@ __global__ __launch_bounds__(L <= 256 ? 256 : L) void rms_vec_kernel(const RmsAr
         }
         Floats y;
 #pragma unroll
-        for (int e = 0; e < V; ++e) y[e] = s[i][e] * g[i][e] * rstd;
+        for (int e = 0; e < V; ++e) y[e] = s[i][e] * unit * g[i][e] * rstd;
         if constexpr (E8) {
             uint8_t *to = (uint8_t *)a.Y + base + c;
             if constexpr (V % 4 == 0) {
@@ -189,33 +216,41 @@ __global__ __launch_bounds__(256) void rms_row_kernel(const RmsArgs a)
     const int64_t row = blockIdx.x;
     const int C = a.C;
     const T *x = (const T *)a.X + row * C, *r = a.R ? (const T *)a.R + row * C : nullptr;
-    float ss = 0.f, top = 0.f;
-    for (int c = threadIdx.x; c < C; c += 256) {
-        const float s = (float)x[c] + (r ? (float)r[c] : 0.f);
-        ss = fmaf(s, s, ss);
-        top = max_or_nan(top, fabsf(a.gamma ? s * a.gamma[c] : s));
+    float ss, unit = 1.f;
+    for (;;) {
+        float top = 0.f;
+        ss = 0.f;
+        for (int c = threadIdx.x; c < C; c += 256) {
+            const float s = ((float)x[c] + (r ? (float)r[c] : 0.f)) * unit;
+            ss = fmaf(s, s, ss);
+            top = max_or_nan(top, fabsf(a.gamma ? s * a.gamma[c] : s));
+        }
+        for (int w = 32; w > 0; w >>= 1) {
+            ss += __shfl_xor(ss, w);
+            top = max_or_nan(top, __shfl_xor(top, w));
+        }
+        if ((threadIdx.x & 63) == 0) {
+            part[0][threadIdx.x >> 6] = ss;
+            part[1][threadIdx.x >> 6] = top;
+        }
+        __syncthreads();
+        ss = part[0][0] + part[0][1] + part[0][2] + part[0][3];
+        if (unit != 1.f) break;
+        unit = row_unit(ss, a.eps);
+        if (unit == 1.f) break;
+        __syncthreads();  // (the second turn, at most, is the last)
     }
-    for (int w = 32; w > 0; w >>= 1) {
-        ss += __shfl_xor(ss, w);
-        top = max_or_nan(top, __shfl_xor(top, w));
-    }
-    if ((threadIdx.x & 63) == 0) {
-        part[0][threadIdx.x >> 6] = ss;
-        part[1][threadIdx.x >> 6] = top;
-    }
-    __syncthreads();
-    ss = part[0][0] + part[0][1] + part[0][2] + part[0][3];
-    const float rstd = 1.f / sqrtf(ss / (float)C + a.eps);
+    const float rstd = 1.f / sqrtf(ss / (float)C + a.eps * unit * unit);
     float scale = 1.f;
     if constexpr (E8) {
-        top = max_or_nan(max_or_nan(part[1][0], part[1][1]), max_or_nan(part[1][2], part[1][3]));
+        const float top = max_or_nan(max_or_nan(part[1][0], part[1][1]), max_or_nan(part[1][2], part[1][3]));
         scale = row_scale(top, rstd);
         if (threadIdx.x == 0) a.scales[row] = scale;
     }
     const float inv = 1.f / scale;  // (its product with rstd may overflow)
     for (int c = threadIdx.x; c < C; c += 256) {
-        const float s = (float)x[c] + (r ? (float)r[c] : 0.f);
-        const float y = (a.gamma ? s * a.gamma[c] : s) * rstd * inv;
+        const float s = (float)x[c] + (r ? (float)r[c] : 0.f), su = s * unit;
+        const float y = (a.gamma ? su * a.gamma[c] : su) * rstd * inv;
         if (a.S) ((T *)a.S)[row * C + c] = (T)s;
         if constexpr (E8)
             ((uint8_t *)a.Y)[row * C + c] = to_e4m3(y);
