@@ -208,7 +208,7 @@ __device__ __forceinline__ void epilogue(const ActArgs &a, const typename Mul<T>
 #pragma unroll
                                 for (int k = 0; k < NO; ++k) {
                                     z[k] = acc[ip + i][jp + j + k][4 * q + e];
-                                    if constexpr (SCALED) z[k] *= xs[i] * s[k][e];
+                                    if constexpr (SCALED) z[k] = z[k] * xs[i] * s[k][e];  // (in this order: the scales' product may overflow)
                                     z[k] += b[k][e];
                                 }
                                 y[e] = act_fast<ACT>(z[0]);
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(512, 2) void act_small_kernel(const ActArgs a)
             z[k] = 0.f;
 #pragma unroll
             for (int v = 0; v < NW; ++v) z[k] += sums[v][row][c + 16 * (GATED ? k : o)];
-            if (SCALED) z[k] *= a.ws[k] ? xs * a.ws[k][ch] : xs;
+            if (SCALED) z[k] = a.ws[k] ? z[k] * xs * a.ws[k][ch] : z[k] * xs;
             if (a.bias[k]) z[k] += a.bias[k][ch];
         }
         float y = 0.f;
@@ -598,7 +598,7 @@ __device__ __forceinline__ void epilogue_beside(const ActArgs &a, const typename
 #pragma unroll
                         for (int k = 0; k < NO; ++k) {
                             z[k] = acc[ip + i][jp + j + k][4 * q + e];
-                            if constexpr (SCALED) z[k] *= xscale[ip + i] * s[k][e];
+                            if constexpr (SCALED) z[k] = z[k] * xscale[ip + i] * s[k][e];
                             z[k] += b[k][e];
                         }
                         y[e] = act_fast<ACT>(z[0]);
