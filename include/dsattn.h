@@ -66,6 +66,9 @@ typedef enum dsattn_dtype {
                                          already sees, as a visible local key or as an earlier
                                          global entry, is dropped, so that no frame counts twice */
 
+#define DSATTN_FLAG_FP32_SUMS 16u     /* dsattn_linear_act: sums of products of 8-bit operands in fp32 at
+                                         every size, at less than half the rate of large ones */
+
 /* Problem statement, in the paper's terms. */
 typedef struct dsattn_desc {
     int32_t clip_len;   /* F_clip >= 1                              (Section 4) */
@@ -392,7 +395,14 @@ int dsattn_rmsnorm(const dsattn_rms_desc *desc, const void *X, const void *resid
  *   z_k = (X W_k^T) * x_scale[row] * w_scale_k[channel] + b_k       (scales with DSATTN_E4M3 only)
  *   Y   = act(z_0) + residual              n_w = 1
  *   Y   = act(z_0) * z_1 + residual        n_w = 2, a gate and its value (W_0 is the gate)
- * Products are accumulated in fp32, the epilogue is computed in fp32 and rounded once.
+ * Products are accumulated in fp32, the epilogue is computed in fp32 and rounded once.  There is one
+ * exception: operands in DSATTN_E4M3 with a DSATTN_BF16 output run, unless few tiles make the call a
+ * small one, on matrix instructions for 8 bits, which line up the products of neighbouring channels
+ * with the largest of them and drop what is more than 13 bits below it: every product loses less than
+ * 2^-13 of the largest |x w| among the 64 channels 64 i .. 64 i + 63 that it is one of (1.3 * 10^-5 of
+ * the 2-norm of Y for normal numbers, 1/130 of its rounding).  What is left where products of outlier
+ * channels cancel may be lost so, and a row may come out otherwise with more rows beside it, as these
+ * choose the kernel.  DSATTN_FLAG_FP32_SUMS keeps the sums in fp32 there too; it changes nothing else.
  */
 typedef enum dsattn_act {
     DSATTN_ACT_NONE = 0,
@@ -410,7 +420,7 @@ typedef struct dsattn_linear_act_desc {
     int32_t act;       /* dsattn_act */
     int32_t io_dtype;  /* dsattn_dtype of X and W */
     int32_t out_dtype; /* of Y and residual: DSATTN_F32, or DSATTN_BF16 unless io_dtype is DSATTN_F32 */
-    uint32_t flags;    /* DSATTN_FLAG_FORCE_GENERIC or 0 */
+    uint32_t flags;    /* DSATTN_FLAG_FORCE_GENERIC, DSATTN_FLAG_FP32_SUMS */
 } dsattn_linear_act_desc;
 
 /* The launch dsattn_linear_act would make (host only): kernel 1 = matrix cores (tiles of 32 x 32 share a

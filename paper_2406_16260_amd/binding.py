@@ -31,6 +31,7 @@ DSATTN_ACT_SILU = 4
 DSATTN_FLAG_FORCE_GENERIC = 1
 DSATTN_FLAG_SLIDING_WINDOW = 2
 DSATTN_FLAG_DEDUP_GLOBAL = 4
+DSATTN_FLAG_FP32_SUMS = 16
 
 EXPORTS = (
     "dsattn_plan", "dsattn_plan_destroy", "dsattn_plan_ctx_max", "dsattn_plan_ctx_indices",
@@ -738,7 +739,8 @@ def dsattn_linear_act_info(rows, c_in, c_out, n_w=1, act=DSATTN_ACT_NONE, io_dty
 def dsattn_linear_act(rows, c_in, c_out, X, Ws, Y, biases=None, residual=None, x_scales=None, w_scales=None,
                       act=DSATTN_ACT_NONE, io_dtype=DSATTN_BF16, out_dtype=None, flags=0, stream=None):
     """Ws: one weight set, or two (gate, value); biases and w_scales: None, or as many entries (each a
-    tensor or None).  residual may be Y.  out_dtype: bf16 for operands in 8 bits unless given."""
+    tensor or None).  residual may be Y.  out_dtype: bf16 for operands in 8 bits unless given; sums of
+    those are fp32 sums with flags = DSATTN_FLAG_FP32_SUMS (see dsattn.h for what they are otherwise)."""
     n = len(Ws)
     if n not in (1, 2) or any(s is not None and len(s) != n for s in (biases, w_scales)):
         raise ValueError("dsattn_linear_act: one or two weight sets, and as many biases and scales, expected")

@@ -25,9 +25,11 @@ __host__ __device__ constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4
 //   e4m3  v_mfma_f32_32x32x64_f8f6f4, two a stage: chunks 4 kk + lane / 32 and two further on, of row lane % 32.
 //         (16x16x128, one a stage, has the same rate and needs twice the fragments at a time.)  The instructions on
 //         8 bits, of every shape, line the products of a group up with its largest one and drop what is more than 13
-//         bits below it: 1.3e-5 of the result's 2-norm at 64 to 1,280 channels of normal numbers, 1/130 of a bf16
-//         output's own rounding.  So these serve a bf16 output; for an fp32 output
-//   e4m3w the numbers are converted to bf16, exactly, and multiplied with 16x16x32: fp32 sums at half the rate
+//         bits below it (the accumulator keeps its fp32): 1.3e-5 of the result's 2-norm at 64 to 1,280 channels of
+//         normal numbers, 1/130 of a bf16 output's own rounding, but what large products that cancel leave may be
+//         lost.  So these serve a bf16 output, unless the caller asks for fp32 sums; for those and for an fp32 output
+//   e4m3w the numbers are converted to bf16, exactly, and multiplied with 16x16x32: fp32 sums at half the rate (gated
+//         61,440 x 1,280 x 5,120 785 and 1,682 us, 16,384 x 5,120 x 16,384 1,068 and 2,525)
 // Block: rows of a fragment, BS; the accumulator's element 4 q + e of lane l is channel 8 q + 4 (l / BS) + e
 // of the block of W rows and row l % BS of the block of X rows (q = 0 only where BS is 16).
 template <typename T>

@@ -113,13 +113,11 @@ struct StreamVariant {
        (const void *)&act_tile_kernel<T, MB, NB, WVM, WVN, false, float>},                                          \
       {(const void *)&act_tile_kernel<T, MB, NB, WVM, WVN, true, __bf16>,                                           \
        (const void *)&act_tile_kernel<T, MB, NB, WVM, WVN, true, float>}}}
-// (16-row blocks to the fp32 output's kernel, 32-row ones to the other)
+// (8 bits: bf16 outputs only)
 #define DSATTN_ACT_TILE_E4M3(MB, NB, WVM, WVN)                                                                      \
     {32 * MB * WVM, 32 * NB * WVN, WVM * WVN, 2 * (32 * MB * WVM + 32 * NB * WVN) * kRow,                           \
-     {{(const void *)&act_tile_kernel<e4m3, MB, NB, WVM, WVN, false, __bf16>,                                       \
-       (const void *)&act_tile_kernel<e4m3w, 2 * MB, 2 * NB, WVM, WVN, false, float>},                              \
-      {(const void *)&act_tile_kernel<e4m3, MB, NB, WVM, WVN, true, __bf16>,                                        \
-       (const void *)&act_tile_kernel<e4m3w, 2 * MB, 2 * NB, WVM, WVN, true, float>}}}
+     {{(const void *)&act_tile_kernel<e4m3, MB, NB, WVM, WVN, false, __bf16>, nullptr},                             \
+      {(const void *)&act_tile_kernel<e4m3, MB, NB, WVM, WVN, true, __bf16>, nullptr}}}
 #define DSATTN_ACT_TILE_F32(MB, NB, WVM, WVN)                                                                       \
     {16 * MB * WVM, 16 * NB * WVN, WVM * WVN, 2 * (16 * MB * WVM + 16 * NB * WVN) * kRow,                           \
      {{nullptr, (const void *)&act_tile_kernel<float, MB, NB, WVM, WVN, false, float>},                             \
@@ -127,6 +125,7 @@ struct StreamVariant {
 const ActVariant kBf16Variants[] = {DSATTN_ACT_TILE(__bf16, 2, 4, 4, 2), DSATTN_ACT_TILE(__bf16, 2, 2, 2, 2)};
 const ActVariant kF32Variants[] = {DSATTN_ACT_TILE_F32(2, 4, 4, 2), DSATTN_ACT_TILE_F32(2, 2, 2, 2)};
 const ActVariant kE4m3Variants[] = {DSATTN_ACT_TILE_E4M3(1, 2, 4, 2), DSATTN_ACT_TILE_E4M3(1, 2, 2, 1)};
+const ActVariant kE4m3WideVariants[] = {DSATTN_ACT_TILE(e4m3w, 2, 4, 4, 2), DSATTN_ACT_TILE(e4m3w, 2, 4, 2, 1)};
 
 // The kernels of small products: gated, fp32 output.
 #define DSATTN_ACT_SMALL(T, F32)                                                                  \
@@ -207,14 +206,19 @@ ActLaunch act_pick(const dsattn_linear_act_desc &d, int64_t es)
     const int64_t stages = (rowbytes + kRow - 1) / kRow, large = tiles(256, 256);
     if (small_is_faster(d.io_dtype, tiles(32, 32), stages))
         return {kSmall[d.io_dtype][f32][gated], 32, 32, 8, kSmallLds, false, true};
-    const ActVariant *v = d.io_dtype == DSATTN_F32 ? kF32Variants : d.io_dtype == DSATTN_BF16 ? kBf16Variants : kE4m3Variants;
+    // sums of 8-bit operands in fp32: for an fp32 output, and where the caller wants them
+    const bool wide = d.io_dtype == DSATTN_E4M3 && (f32 || (d.flags & DSATTN_FLAG_FP32_SUMS));
+    const ActVariant *v = d.io_dtype == DSATTN_F32    ? kF32Variants
+                          : d.io_dtype == DSATTN_BF16 ? kBf16Variants
+                          : wide                      ? kE4m3WideVariants
+                                                      : kE4m3Variants;
     if (d.io_dtype == DSATTN_F32) {
         if (tiles(128, 128) < 384) ++v;
     } else {
         const double us128 = tile_estimate(128, tiles(128, 128), stages), us64 = tile_estimate(64, tiles(64, 64), stages);
         const StreamVariant *sv = d.io_dtype == DSATTN_BF16 ? &kBf16Stream : &kE4m3Stream;
         // (tiles are numbered with 32 bits)
-        if (sv->fn[gated][f32][d.act] && large < (1 << 30) && tile_estimate(256, large, stages) < std::min(us128, us64))
+        if (!wide && large < (1 << 30) && tile_estimate(256, large, stages) < std::min(us128, us64))
             return {sv->fn[gated][f32][d.act], 256, 256, 8, kStreamLds, true, false};
         if (us64 < us128) ++v;
     }
@@ -269,7 +273,7 @@ int act_validate(const dsattn_linear_act_desc *desc, const char *who)
         return fail(DSATTN_EINVAL, "%s: unknown input dtype", who);
     if (d.out_dtype != DSATTN_F32 && (d.out_dtype != DSATTN_BF16 || d.io_dtype == DSATTN_F32))
         return fail(DSATTN_EINVAL, "%s: the output is fp32, or bf16 of inputs of 16 or 8 bits", who);
-    if (d.flags & ~DSATTN_FLAG_FORCE_GENERIC)
+    if (d.flags & ~(DSATTN_FLAG_FORCE_GENERIC | DSATTN_FLAG_FP32_SUMS))
         return fail(DSATTN_EINVAL, "%s: unknown flag bits 0x%x", who, d.flags);
     return DSATTN_OK;
 }
