@@ -12,8 +12,13 @@ _BINDING_NAMES = (
     "dsattn_plan_launch_info", "dsattn_gather_context", "dsattn_forward", "dsattn_forward_ctx",
     "dsattn_copy_probe", "dsattn_strerror", "dsattn_last_error", "dsattn_groupnorm",
     "dsattn_groupnorm_workspace", "Plan", "DsattnError",
-    "dsattn_rmsnorm", "dsattn_linear_act", "dsattn_sink_workspace", "dsattn_sink_forward", "DSATTN_E4M3",
-    "DSATTN_F32", "DSATTN_BF16", "DSATTN_FLAG_FORCE_GENERIC", "DSATTN_FLAG_SLIDING_WINDOW",
+    "dsattn_groupnorm_static", "dsattn_groupnorm_static_max_bytes", "dsattn_temporal_conv",
+    "dsattn_temporal_conv_info", "dsattn_linear", "dsattn_linear_info", "dsattn_temporal_layer",
+    "dsattn_temporal_layer_workspace", "dsattn_rmsnorm", "dsattn_linear_act", "dsattn_linear_act_info",
+    "dsattn_sink_workspace", "dsattn_sink_forward", "dsattn_sink_forward_info",
+    "DSATTN_F32", "DSATTN_BF16", "DSATTN_E4M3", "DSATTN_ACT_NONE", "DSATTN_ACT_RELU", "DSATTN_ACT_GELU",
+    "DSATTN_ACT_GELU_TANH", "DSATTN_ACT_SILU", "DSATTN_FLAG_FORCE_GENERIC", "DSATTN_FLAG_SLIDING_WINDOW",
+    "DSATTN_FLAG_DEDUP_GLOBAL", "DSATTN_FLAG_FP32_SUMS",
 )
 
 
