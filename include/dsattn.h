@@ -413,7 +413,7 @@ typedef enum dsattn_act {
 } dsattn_act;
 
 typedef struct dsattn_linear_act_desc {
-    int64_t rows;      /* M >= 1 tokens, at most 2^31 - 1 */
+    int64_t rows;      /* M >= 1 tokens, at most 2^31 - 1; no tensor has more than 2^46 numbers */
     int32_t c_in;      /* >= 1 */
     int32_t c_out;     /* >= 1: channels of Y and of every W_k */
     int32_t n_w;       /* 1, or 2: gated */

@@ -266,6 +266,9 @@ int act_validate(const dsattn_linear_act_desc *desc, const char *who)
     const dsattn_linear_act_desc &d = *desc;
     if (d.rows < 1 || d.rows > 0x7fffffffLL || d.c_in < 1 || d.c_out < 1)
         return fail(DSATTN_EINVAL, "%s: sizes must be positive (rows at most 2^31 - 1)", who);
+    // (2^46 numbers a tensor, so that their bytes are counted in 64 bits)
+    const int64_t most = (int64_t)1 << 46, widest = std::max(d.c_in, d.c_out);
+    if (d.rows > most / widest || (int64_t)d.c_in > most / d.c_out) return fail(DSATTN_EINVAL, "%s: problem too large", who);
     if (d.n_w < 1 || d.n_w > 2) return fail(DSATTN_EINVAL, "%s: n_w %d is neither 1 nor 2", who, d.n_w);
     if (d.act < DSATTN_ACT_NONE || d.act > DSATTN_ACT_SILU)
         return fail(DSATTN_EINVAL, "%s: unknown activation", who);
@@ -308,7 +311,7 @@ int dsattn_linear_act_info(const dsattn_linear_act_desc *desc, dsattn_conv_info 
         info->n_blocks = (int32_t)std::min<int64_t>((d.rows * d.c_out + 255) / 256, 0x7fffffff);
         info->block_threads = 256;
     }
-    info->useful_flops = 2 * d.rows * d.c_in * n;
+    info->useful_flops = (int64_t)std::min(2.0 * (double)(d.rows * d.c_in) * (double)n, 0x1p62);
     info->algorithmic_bytes = (d.rows + n) * d.c_in * es + d.rows * d.c_out * os;
     return DSATTN_OK;
 }

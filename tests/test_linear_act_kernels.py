@@ -111,3 +111,14 @@ def test_info_refuses_what_the_call_refuses():
         assert lib.dsattn_linear_act_info(ctypes.byref(L._desc(**kw)), ctypes.byref(info)) == B.DSATTN_EINVAL, kw
     with pytest.raises(B.DsattnError):
         B.dsattn_linear_act_info(0, 64, 32)
+
+
+@pytest.mark.parametrize("kw", [dict(rows=(1 << 31) - 1, c_in=(1 << 31) - 1), dict(rows=(1 << 31) - 1, c_out=1 << 16),
+                                dict(c_in=1 << 30, c_out=1 << 17), dict(rows=1 << 24, c_in=(1 << 31) - 1, c_out=1)])
+def test_sizes_whose_bytes_pass_64_bits_are_refused(kw):
+    lib, info = B.load(), B.DsattnConvInfo()
+    d = L._desc(**{"io_dtype": B.DSATTN_F32, "out_dtype": B.DSATTN_F32, **kw})
+    assert lib.dsattn_linear_act_info(ctypes.byref(d), ctypes.byref(info)) == B.DSATTN_EINVAL
+    assert lib.dsattn_linear_act(ctypes.byref(d), 0x10000, None, L._vps(0x20000), None, None, None, 0x40000, None) == B.DSATTN_EINVAL
+    big = L._desc(rows=(1 << 31) - 1, c_in=1 << 14, c_out=1 << 14, n_w=2)
+    assert lib.dsattn_linear_act_info(ctypes.byref(big), ctypes.byref(info)) == B.DSATTN_OK and info.useful_flops > 0
