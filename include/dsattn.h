@@ -471,7 +471,7 @@ typedef struct dsattn_sink_desc {
     int32_t window;    /* >= 0 latest frames that a query sees, its own included */
     int32_t ring;      /* >= max(window, 1): frames that the cache holds besides the sinks */
     int32_t io_dtype;  /* DSATTN_F32 or DSATTN_BF16 of all tensors; accumulation is fp32 */
-    float scale;       /* softmax scale; <= 0 selects 1/sqrt(head_dim) */
+    float scale;       /* softmax scale, below 2.3 * 10^38; <= 0 selects 1/sqrt(head_dim) */
     uint32_t flags;    /* DSATTN_FLAG_FORCE_GENERIC or 0 */
 } dsattn_sink_desc;
 

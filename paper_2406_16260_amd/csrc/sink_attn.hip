@@ -264,6 +264,8 @@ bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
     return a && b && x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
 }
 
+constexpr float kLog2e = 1.44269504f;
+
 int sink_validate(const dsattn_sink_desc *d, const char *who)
 {
     if (!d) return fail(DSATTN_EINVAL, "%s: null descriptor", who);
@@ -278,7 +280,8 @@ int sink_validate(const dsattn_sink_desc *d, const char *who)
         return fail(DSATTN_EINVAL, "%s: a ring of %d frames does not hold a window of %d", who, d->ring, d->window);
     if (d->io_dtype != DSATTN_F32 && d->io_dtype != DSATTN_BF16)
         return fail(DSATTN_EINVAL, "%s: unknown dtype", who);
-    if (!std::isfinite(d->scale)) return fail(DSATTN_EINVAL, "%s: scale is not finite", who);
+    if (!std::isfinite(d->scale) || std::isinf(std::max(d->scale, 0.f) * kLog2e))
+        return fail(DSATTN_EINVAL, "%s: scale is not finite, or is not times log2(e)", who);
     if (d->flags & ~DSATTN_FLAG_FORCE_GENERIC)
         return fail(DSATTN_EINVAL, "%s: unknown flag bits 0x%x", who, d->flags);
     // 2^24 frames, 2^20 channels, 2^40 numbers a tensor at most
@@ -407,7 +410,7 @@ int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, cons
     a.sinks = d.sinks;
     a.window = d.window;
     a.ring = d.ring;
-    a.sc = (d.scale > 0.f ? d.scale : 1.f / sqrtf((float)d.head_dim)) * 1.44269504f;
+    a.sc = (d.scale > 0.f ? d.scale : 1.f / sqrtf((float)d.head_dim)) * kLog2e;
     const hipStream_t st = (hipStream_t)stream;
     const SinkLaunch k = sink_launch(d);
     const bool f32 = d.io_dtype == DSATTN_F32;

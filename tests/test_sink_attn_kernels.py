@@ -132,3 +132,11 @@ def test_info_refuses_what_the_call_refuses():
         assert lib.dsattn_sink_forward_info(ctypes.byref(S._desc(**kw)), ctypes.byref(out)) == B.DSATTN_EINVAL, kw
     with pytest.raises(B.DsattnError):
         B.dsattn_sink_forward_info(1, 1, 1, 3, 2, 64, 0, 4)
+
+
+@pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
+def test_a_scale_beyond_fp32_in_powers_of_two_is_refused(scale):
+    lib, out = B.load(), B.DsattnSinkInfo()
+    assert lib.dsattn_sink_forward_info(ctypes.byref(S._desc(scale=scale)), ctypes.byref(out)) == B.DSATTN_EINVAL
+    for good in (2.3e38, -3.4e38, 0.0):  # (the last two select 1 / sqrt(head_dim))
+        assert lib.dsattn_sink_forward_info(ctypes.byref(S._desc(scale=good)), ctypes.byref(out)) == B.DSATTN_OK
