@@ -391,7 +391,10 @@ int dsattn_rmsnorm(const dsattn_rms_desc *desc, const void *X, const void *resid
                    const float *gamma, void *sum, void *Y, float *scales, void *stream);
 
 /*
- * Token-wise product with everything that follows it in a transformer block done in its epilogue:
+ * Token-wise product with everything that follows it in a transformer block done in its epilogue
+ * (dsattn_linear has neither activation, gate and residual nor 8 bits, but several outputs of one X in
+ * a launch; of a plain product, which either does, it is the faster one for fp32 operands of more than
+ * some thousand rows, and this one for fewer):
  *   z_k = (X W_k^T) * x_scale[row] * w_scale_k[channel] + b_k       (scales with DSATTN_E4M3 only)
  *   Y   = act(z_0) + residual              n_w = 1
  *   Y   = act(z_0) * z_1 + residual        n_w = 2, a gate and its value (W_0 is the gate)
@@ -453,8 +456,12 @@ int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void *X, const f
  * most `frames`; the query of frame a sees frame f, at its own position and head, iff
  *   0 <= f <= a  and  (f < sinks  or  a - f < window)
  * and O = softmax(scale * q.k) v over those, 0 where there is none (or none with a score above
- * -infinity).  Query head i reads head
- * i / (heads / kv_heads) of K and V.
+ * -infinity).  Query head i reads head i / (heads / kv_heads) of K and V.  Scores, maxima and sums are
+ * fp32 numbers.  The weights too, but for DSATTN_BF16 tensors with more than four queries a call and head
+ * of K and V (frames * heads / kv_heads > 4; head_dim a multiple of 8 up to 256): those round a weight
+ * to bf16 for its product with v and divide by the sum of the rounded ones, so that O is off by up to
+ * 2^-7 of the weighted mean of |v| (measured 1.9 to 2.3 * 10^-3 of its 2-norm, of which its own rounding
+ * is 1.5 to 1.7), and a frame's result among others may differ from its result alone by as much.
  *
  * The cache holds sinks + ring frames per stream: frame f < sinks at slot f, any other at slot
  * sinks + (f - sinks) % ring.  A call reads frames before `start` from it, its own frames from K
