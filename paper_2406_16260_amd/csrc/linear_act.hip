@@ -4,11 +4,13 @@
 //
 // Bound by the matrix cores where there are many rows, by latency where there are few.  Four kernels on the matrix cores and a
 // vector kernel for rows that are not whole 16-byte pieces; estimates of their times choose (act_pick()).  us and TFLOP/s:
-//   25,920 x 5,120 x 1,280, residual, bf16             270   1,260   (elementary fp32 operations 2,560; a library product
-//                                                                     without bias and residual 251)
+//   25,920 x 5,120 x 1,280, residual, bf16             270 to 283   1,200 to 1,260   (elementary fp32 operations 2,560; a
+//                                                                     library product without bias and residual 251)
 //   40,960 x 640 x 5,120, bias, bf16                   232   1,157   (library product 308 to 348)
-//   40,960 x 640 x 2 x 2,560, GELU gate, bf16          249 to 264   1,020 to 1,080
-//   61,440 x 1,280 x 2 x 5,120, GELU gate, 8 bits      783 to 814   1,980 to 2,060   (16,384 x 5,120 x 16,384: 2,790 to 2,860)
+//   40,960 x 640 x 2 x 2,560, GELU gate, bf16          249 to 272   990 to 1,080
+//   61,440 x 1,280 x 2 x 5,120, GELU gate, 8 bits      783 to 831   1,940 to 2,060   (16,384 x 5,120 x 16,384: 2,440 to 2,860)
+//       the same with fp32 sums                        1,682 to 1,833   880 to 960   (16,384 x 5,120 x 16,384: 1,010 to 1,090)
+//   8,192 x 4,096 x 4,096, bias, fp32                  1,917 to 1,931   143
 //   160 x 1,280 x 1,280, bf16                          4.1           in a captured graph
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -148,8 +150,8 @@ const StreamVariant kBf16Stream = {{{DSATTN_ACT_STREAM(__bf16, 4, 8, false, __bf
                                     {DSATTN_ACT_STREAM(__bf16, 4, 8, true, __bf16), DSATTN_ACT_STREAM(__bf16, 4, 8, true, float)}}};
 const StreamVariant kE4m3Stream = {{{DSATTN_ACT_STREAM(e4m3, 2, 4, false, __bf16), {}}, {DSATTN_ACT_STREAM(e4m3, 2, 4, true, __bf16), {}}}};
 
-// Whether the small kernel is faster than 64 x 64 tiles, by estimates in us: rounds of workgroups on the 256 compute units, and
-// the time of a stage (of all of a row's in the tile kernel, of its eighth in the small one).  Measured us in a captured graph,
+// Whether the small kernel is faster than 64 x 64 tiles, by estimates in us: rounds of workgroups on a whole card's 256 compute
+// units (on a part of one the choice is the same, the result too), and the time of a stage (of all of a row's in the tile kernel, of its eighth in the small one).  Measured us in a captured graph,
 // small and 64 x 64, rows x c_in x c_out:
 //                                       bf16            fp32            e4m3
 //       1 x   320 x 1,280            2.9   3.5       4.2   8.0       3.0   3.4

@@ -6,8 +6,8 @@
 // registers between the sum of its squares and its output: L lanes have it, NV pieces of V numbers each, and a
 // wavefront has 64 / L rows (L <= 64) or a workgroup one (L = 256 or 1,024).  The largest |y|, which a scale is
 // made of, is max|s gamma| times the row's factor, and so comes with the sum of squares.
-// 368,640 x 1,280 bf16 with residual and sum into 8 bits, 3.3 GB: 577 us, 5.7 TB/s (a large copy 5.1; a workgroup a row in two
-// passes 1,755 us).  40 x 1,280: 7.3 us, of which 6 are the host's.
+// 368,640 x 1,280 bf16 with residual and sum into 8 bits, 3.3 GB: 567 to 577 us, 5.8 TB/s (a large copy 5.1; a workgroup a row
+// in two passes 1,755 us).  40 x 1,280: 7.0 us, of which 6 are the host's.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

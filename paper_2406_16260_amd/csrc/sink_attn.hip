@@ -7,9 +7,10 @@
 // Few queries of a head of K and V are a stream of the cache (sink_rows.h), more of them matrix products (sink_tile.h); head
 // sizes that are neither have a wavefront a query.  us, and of a large copy's or library product's rate:
 //   16 streams, a token of 32 heads on 8 x 128 over 16,388      225   93 %
-//   a frame of 160 positions, 8 x 160, over 64                 12.8   82 %
-//   128 frames of 640 positions, 8 x 80, window 32, cached      129   74 %
-//   2 prompts of 8,192, 16 heads on 4 x 128, window 2,048       277   57 %
+//   a frame of 160 positions, 8 x 160, over 64                 12.8   82 %   (fp32 19.5)
+//   128 frames of 640 positions, 8 x 80, window 32, cached      130   74 %   (fp32 311; on a full ring of 32, which a kernel
+//                                                                     after it fills, 150 and 320)
+//   2 prompts of 8,192, 16 heads on 4 x 128, window 2,048       276 to 295   53 to 57 %   (fp32 2,000)
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

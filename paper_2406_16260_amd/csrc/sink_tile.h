@@ -242,7 +242,7 @@ __global__ __launch_bounds__(64 * WV, tile_waves(NB, RB, SHARED, WV)) void sink_
                 }
             }
         // Eight pieces of K on their way ahead of the multiplies, all the time (by itself the compiler reads two and waits for them:
-        // 287 -> 277 us, 2 prompts of 8,192, 16 heads on 4 x 128, window 2,048).
+        // 287 -> 277 us on one card, 295 -> 287 on another, 2 prompts of 8,192, 16 heads on 4 x 128, window 2,048).
         if constexpr (!F32 && SHARED && KB == 4 && RB == 2) {
             __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
 #pragma unroll
@@ -483,7 +483,7 @@ TileLaunch tile_launch(const dsattn_sink_desc &d)
     k.rows = per;
     k.row_tiles = (int)((rows + per - 1) / per);
     k.tasks = units * k.row_tiles;
-    // Few tasks: parts of the frames each, of four tiles at least, up to 1,024 wavefronts apart (16 streams of 4 tokens, 32 heads
+    // Few tasks (on 256 compute units; the workspace follows from the shape alone): parts of the frames each, of four tiles at least, up to 1,024 wavefronts apart (16 streams of 4 tokens, 32 heads
     // on 8 x 128, over 8,192: 129 us up to 2,048, 122 up to 1,024; 4 streams of 8 tokens over 4,096: 26.5 and 26.6) or 512
     // workgroups shared.
     const int64_t n = std::min<int64_t>((int64_t)d.sinks + d.window + (shared ? per / (d.heads / d.kv_heads) : d.frames), 1 << 24);
