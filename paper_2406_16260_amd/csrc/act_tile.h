@@ -210,7 +210,7 @@ __device__ __forceinline__ void epilogue(const ActArgs &a, const typename Mul<T>
 #pragma unroll
                                 for (int k = 0; k < NO; ++k) {
                                     z[k] = acc[ip + i][jp + j + k][4 * q + e];
-                                    if constexpr (SCALED) z[k] = z[k] * xs[i] * s[k][e];  // (in this order: the scales' product may overflow)
+                                    if constexpr (SCALED) z[k] = z[k] * xs[i] * s[k][e];  // (the scales' product may overflow)
                                     z[k] += b[k][e];
                                 }
                                 y[e] = act_fast<ACT>(z[0]);

@@ -151,8 +151,8 @@ const StreamVariant kBf16Stream = {{{DSATTN_ACT_STREAM(__bf16, 4, 8, false, __bf
 const StreamVariant kE4m3Stream = {{{DSATTN_ACT_STREAM(e4m3, 2, 4, false, __bf16), {}}, {DSATTN_ACT_STREAM(e4m3, 2, 4, true, __bf16), {}}}};
 
 // Whether the small kernel is faster than 64 x 64 tiles, by estimates in us: rounds of workgroups on a whole card's 256 compute
-// units (on a part of one the choice is the same, the result too), and the time of a stage (of all of a row's in the tile kernel, of its eighth in the small one).  Measured us in a captured graph,
-// small and 64 x 64, rows x c_in x c_out:
+// units (on a part of one the choice is the same, and the result), and the time of a stage (of all of a row's in the tile
+// kernel, of its eighth in the small one).  Measured us in a captured graph, small and 64 x 64, rows x c_in x c_out:
 //                                       bf16            fp32            e4m3
 //       1 x   320 x 1,280            2.9   3.5       4.2   8.0       3.0   3.4
 //       1 x 5,120 x 1,280            7.1  21.7      23.8  96.6       6.1  13.7

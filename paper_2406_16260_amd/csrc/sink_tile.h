@@ -483,9 +483,9 @@ TileLaunch tile_launch(const dsattn_sink_desc &d)
     k.rows = per;
     k.row_tiles = (int)((rows + per - 1) / per);
     k.tasks = units * k.row_tiles;
-    // Few tasks (on 256 compute units; the workspace follows from the shape alone): parts of the frames each, of four tiles at least, up to 1,024 wavefronts apart (16 streams of 4 tokens, 32 heads
-    // on 8 x 128, over 8,192: 129 us up to 2,048, 122 up to 1,024; 4 streams of 8 tokens over 4,096: 26.5 and 26.6) or 512
-    // workgroups shared.
+    // Few tasks (for a card's 256 compute units: the workspace has to follow from the shape alone): parts of the frames each, of
+    // four tiles at least, up to 1,024 wavefronts apart (16 streams of 4 tokens, 32 heads on 8 x 128, over 8,192: 129 us up to
+    // 2,048, 122 up to 1,024; 4 streams of 8 tokens over 4,096: 26.5 and 26.6) or 512 workgroups shared.
     const int64_t n = std::min<int64_t>((int64_t)d.sinks + d.window + (shared ? per / (d.heads / d.kv_heads) : d.frames), 1 << 24);
     const int64_t tiles = (n + KT - 1) / KT;
     k.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(shared ? 512 : 1024) / k.tasks, tiles / 4, kMaxSplits}));
