@@ -448,6 +448,36 @@ int dsattn_linear_act(const dsattn_linear_act_desc *desc, const void *X, const f
                       const void *const *W, const float *const *w_scales,
                       const float *const *bias, const void *residual, void *Y, void *stream);
 
+/* Bytes of device workspace dsattn_linear_act_backward needs for this shape; may be 0. */
+int dsattn_linear_act_backward_workspace(const dsattn_linear_act_desc *desc, size_t *bytes);
+
+/*
+ * Gradients of dsattn_linear_act from its inputs, for a DSATTN_F32 or DSATTN_BF16 io_dtype that is the
+ * out_dtype too; nothing of the forward pass needs to be kept.  With dy the gradient of Y
+ *   dz_0 = dy * act'(z_0)                       n_w = 1
+ *   dz_0 = dy * z_1 * act'(z_0),  dz_1 = dy * act(z_0)        n_w = 2
+ *   dX = sum_k dz_k W_k,   dW_k = dz_k^T X,   dbias_k = sum of dz_k over the rows
+ * The residual's gradient is dy itself.  z and dz are computed in fp32 and sums are fp32, rounded once.
+ * With DSATTN_BF16 dz is rounded to bf16 on the way into the two products (the matrix instructions'
+ * operand), so that dX and dW are off by up to 2^-8 of the sum of |dz w| or |dz x| beside their own
+ * rounding (2.4 * 10^-3 of the 2-norm, of which their own rounding is 1.7).  relu'(0) is 0.  Sums are in an order
+ * that the shape alone decides: the same call gives the same bits.
+ *   X, W, bias : as in the forward call
+ *   dY         : device, [rows, c_out], 16-byte aligned
+ *   dX         : device, like X, or NULL: not wanted
+ *   dW         : NULL, or HOST array of n_w device pointers, each like W or NULL
+ *   dbias      : NULL, or HOST array of n_w device pointers, each [c_out] fp32 or NULL
+ *   workspace  : device, at least dsattn_linear_act_backward_workspace() bytes, 16-byte aligned; NULL
+ *                if those are 0.  Contents are overwritten; calls that share a workspace must not
+ *                overlap in time
+ * Outputs overlap neither inputs nor each other.  The pointer arrays are read during the call only.
+ * Runs on the current device; enqueues up to five kernels on `stream`; allocates nothing.
+ * Errors: EINVAL, EUNSUPPORTED (too large), EHIP.
+ */
+int dsattn_linear_act_backward(const dsattn_linear_act_desc *desc, const void *X, const void *const *W,
+                               const float *const *bias, const void *dY, void *dX, void *const *dW, float *const *dbias,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 /*
  * Attention of a stream of frames over a window of the latest ones and a few first ones that stay
  * visible (sinks), with the cache that it reads and keeps up to date: the streaming counterpart of
@@ -522,6 +552,126 @@ int dsattn_sink_forward_info(const dsattn_sink_desc *desc, dsattn_sink_info *inf
 int dsattn_sink_forward(const dsattn_sink_desc *desc, const int32_t *start, const int32_t *counts,
                         const void *Q, const void *K, const void *V, void *Kcache, void *Vcache,
                         void *O, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Layer norm with the residual's addition, the other norm of transformer blocks.  For each row
+ *   s = x + residual                                 in fp32; `sum` receives s rounded once
+ *   n = (s - mean(s)) / sqrt(var(s) + eps)           var: the mean of the squared differences
+ *   y = n * gamma + beta                             from the unrounded s, rounded once
+ * 8-bit outputs and their scales, infinities and NaN, and rows beyond fp32's range as in
+ * dsattn_rmsnorm.  A row of equal numbers is beta, NaN (0 / 0) with eps 0.
+ */
+typedef struct dsattn_ln_desc {
+    int64_t rows;      /* >= 1, at most 2^31 - 1 */
+    int32_t channels;  /* >= 1, at most 2^20 */
+    int32_t io_dtype;  /* DSATTN_F32 or DSATTN_BF16, of X, residual and sum */
+    int32_t out_dtype; /* of Y: io_dtype or DSATTN_E4M3 (dsattn_layernorm only) */
+    float eps;         /* >= 0 */
+} dsattn_ln_desc;
+
+/*
+ *   beta     : device, [channels] fp32, 16-byte aligned, or NULL for 0
+ * The others, what may be in whose place, and the errors as in dsattn_rmsnorm.
+ */
+int dsattn_layernorm(const dsattn_ln_desc *desc, const void *X, const void *residual, const float *gamma,
+                     const float *beta, void *sum, void *Y, float *scales, void *stream);
+
+/* Bytes of device workspace dsattn_layernorm_backward needs for the gradients of gamma and beta. */
+int dsattn_layernorm_backward_workspace(const dsattn_ln_desc *desc, size_t *bytes);
+
+/*
+ * Gradients of dsattn_layernorm, from its inputs: mean and variance are computed again.  With
+ * e = dy * gamma,
+ *   dx     = (e - mean(e) - n * mean(e * n)) / sqrt(var(s) + eps) + dsum,   rounded once
+ *   dgamma = sum of dy * n over the rows,  dbeta = sum of dy                in fp32
+ * dx is the gradient of x and of the residual alike.  Sums are in an order of their own that the
+ * shape alone decides: the same call gives the same bits.
+ *   X, residual, gamma : as in the forward call (X = its `sum` and no residual is its result within the
+ *               sum's rounding)
+ *   dY        : device, [rows, channels] of io_dtype, 16-byte aligned
+ *   dsum      : device, like dY: the gradient that arrives at `sum` by other ways, or NULL for 0
+ *   dX        : device, like dY; may be dY, dsum, X or residual itself (with more than 2,048 pieces of 8, 4, 2 or 1
+ *               channels, as many as divide `channels`, 4 at most in fp32: only dsum, unless dgamma
+ *               and dbeta are NULL)
+ *   dgamma,
+ *   dbeta     : device, [channels] fp32, or NULL: not wanted
+ *   workspace : device, at least dsattn_layernorm_backward_workspace() bytes, 16-byte aligned; may be
+ *               NULL if dgamma and dbeta are.  Contents are overwritten; calls that share a
+ *               workspace must not overlap in time
+ * Outputs overlap the inputs in no other way, and not each other.  Runs on the current device;
+ * enqueues one to three kernels on `stream`; allocates nothing.  Errors: EINVAL, EUNSUPPORTED, EHIP.
+ */
+int dsattn_layernorm_backward(const dsattn_ln_desc *desc, const void *X, const void *residual, const float *gamma,
+                              const void *dY, const void *dsum, void *dX, float *dgamma, float *dbeta, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/*
+ * Gated linear recurrence over the frames of a stream, a temporal module whose state has one size
+ * however long the stream: at every position and channel by itself
+ *   a_t = 1 / (1 + exp(-g_t)),   h_t = a_t * h_(t-1) + w(a_t) * x_t,   y_t = h_t rounded once
+ * with w by `mode`.  States are fp32 throughout.  Frames are [streams, frames, P, channels] as in
+ * dsattn_sink_forward; a stream goes on in a later call with the state that it left, one frame a
+ * call or many.  Many frames of few channels are cut into chunks and joined, so that a
+ * stream's last bits depend on how it is cut into calls.  An infinite state stays infinite or is NaN.
+ */
+#define DSATTN_SCAN_FRAMES 16 /* frames between two of the states kept for the backward pass */
+
+typedef enum dsattn_scan_mode {
+    DSATTN_SCAN_SUM = 0,  /* w = 1 */
+    DSATTN_SCAN_MEAN = 1, /* w = 1 - a: a weighted mean of the inputs so far */
+    DSATTN_SCAN_NORM = 2  /* w = sqrt(1 - a^2): inputs of variance 1 keep states of variance 1 */
+} dsattn_scan_mode;
+
+typedef struct dsattn_scan_desc {
+    int32_t streams;  /* B >= 1 */
+    int32_t frames;   /* T >= 1 */
+    int32_t spatial;  /* P >= 1 positions */
+    int32_t channels; /* >= 1; no tensor has more than 2^46 numbers */
+    int32_t mode;     /* dsattn_scan_mode */
+    int32_t io_dtype; /* DSATTN_F32 or DSATTN_BF16 of X, G, Y and their gradients */
+} dsattn_scan_desc;
+
+/* Bytes of device workspace either direction needs for this shape; may be 0. */
+int dsattn_gated_scan_workspace(const dsattn_scan_desc *desc, size_t *bytes);
+
+/*
+ *   counts      : device, [streams] int32 in [0, frames] (values outside count as the nearest inside):
+ *                 frames of each stream; NULL: `frames` for all.  Rows behind a stream's last frame are
+ *                 neither read nor written
+ *   X, G        : device, [streams, frames, P, channels] of io_dtype: inputs, and gates as logits
+ *   start_state : device, [streams, P, channels] fp32; NULL: 0
+ *   Y           : device, like X; may be X or G itself
+ *   end_state   : device, like start_state, which it may be itself: h behind the last frame (the
+ *                 start state of a stream of 0 frames); NULL: not wanted
+ *   states      : device, [streams, ceil(frames / DSATTN_SCAN_FRAMES), P, channels] fp32: the state in
+ *                 front of frames 0, 16, 32 .., for dsattn_gated_scan_backward (those behind a stream's
+ *                 end are not written); NULL: not wanted
+ *   workspace   : device, at least dsattn_gated_scan_workspace() bytes; NULL if those are 0.  Contents
+ *                 are overwritten; calls that share a workspace must not overlap in time
+ * All 16-byte aligned (counts: 4).  Outputs overlap the inputs in no other way, and not each other.  Runs
+ * on the current device; enqueues one or three kernels on `stream`; allocates nothing.
+ * Errors: EINVAL, EUNSUPPORTED (too large), EHIP.
+ */
+int dsattn_gated_scan(const dsattn_scan_desc *desc, const int32_t *counts, const void *X, const void *G,
+                      const float *start_state, void *Y, float *end_state, float *states, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
+/*
+ * Gradients of dsattn_gated_scan: with D_t = dy_t + a_(t+1) D_(t+1) (behind the last frame a D is
+ * the end state's gradient)
+ *   dx_t = w(a_t) D_t,   dg_t = D_t * (a_t (1 - a_t) h_(t-1) + w'(a_t) a_t (1 - a_t) x_t)
+ * in fp32, each rounded once; the states h are run again from `states`, in fp32.
+ *   X, G, counts : as in the forward call
+ *   states       : what it left
+ *   dY           : device, like Y
+ *   dend_state   : device, [streams, P, channels] fp32; NULL: 0
+ *   dX, dG       : device, like X; either may be X, G or dY itself
+ *   dstart_state : device, like dend_state, which it may be itself; NULL: not wanted
+ * The rest as there.
+ */
+int dsattn_gated_scan_backward(const dsattn_scan_desc *desc, const int32_t *counts, const void *X, const void *G,
+                               const float *states, const void *dY, const float *dend_state, void *dX, void *dG,
+                               float *dstart_state, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Static description of a status code; never NULL. */
 const char *dsattn_strerror(int code);

@@ -16,6 +16,10 @@ _BINDING_NAMES = (
     "dsattn_temporal_conv_info", "dsattn_linear", "dsattn_linear_info", "dsattn_temporal_layer",
     "dsattn_temporal_layer_workspace", "dsattn_rmsnorm", "dsattn_linear_act", "dsattn_linear_act_info",
     "dsattn_sink_workspace", "dsattn_sink_forward", "dsattn_sink_forward_info",
+    "dsattn_layernorm", "dsattn_layernorm_backward_workspace", "dsattn_layernorm_backward",
+    "dsattn_gated_scan_workspace", "dsattn_gated_scan", "dsattn_gated_scan_backward",
+    "dsattn_linear_act_backward_workspace", "dsattn_linear_act_backward",
+    "DSATTN_SCAN_SUM", "DSATTN_SCAN_MEAN", "DSATTN_SCAN_NORM", "DSATTN_SCAN_FRAMES",
     "DSATTN_F32", "DSATTN_BF16", "DSATTN_E4M3", "DSATTN_ACT_NONE", "DSATTN_ACT_RELU", "DSATTN_ACT_GELU",
     "DSATTN_ACT_GELU_TANH", "DSATTN_ACT_SILU", "DSATTN_FLAG_FORCE_GENERIC", "DSATTN_FLAG_SLIDING_WINDOW",
     "DSATTN_FLAG_DEDUP_GLOBAL", "DSATTN_FLAG_FP32_SUMS",

@@ -28,6 +28,10 @@ DSATTN_ACT_RELU = 1
 DSATTN_ACT_GELU = 2
 DSATTN_ACT_GELU_TANH = 3
 DSATTN_ACT_SILU = 4
+DSATTN_SCAN_SUM = 0
+DSATTN_SCAN_MEAN = 1
+DSATTN_SCAN_NORM = 2
+DSATTN_SCAN_FRAMES = 16
 DSATTN_FLAG_FORCE_GENERIC = 1
 DSATTN_FLAG_SLIDING_WINDOW = 2
 DSATTN_FLAG_DEDUP_GLOBAL = 4
@@ -41,7 +45,9 @@ EXPORTS = (
     "dsattn_linear", "dsattn_groupnorm_static", "dsattn_groupnorm_static_max_bytes",
     "dsattn_temporal_layer_workspace", "dsattn_temporal_layer", "dsattn_rmsnorm", "dsattn_linear_act",
     "dsattn_linear_act_info", "dsattn_sink_workspace", "dsattn_sink_forward_info",
-    "dsattn_sink_forward",
+    "dsattn_sink_forward", "dsattn_layernorm", "dsattn_layernorm_backward_workspace",
+    "dsattn_layernorm_backward", "dsattn_gated_scan_workspace", "dsattn_gated_scan",
+    "dsattn_gated_scan_backward", "dsattn_linear_act_backward_workspace", "dsattn_linear_act_backward",
 )
 
 
@@ -100,6 +106,20 @@ class DsattnSinkDesc(ctypes.Structure):
         ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
         ("sinks", ctypes.c_int32), ("window", ctypes.c_int32), ("ring", ctypes.c_int32),
         ("io_dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("flags", ctypes.c_uint32),
+    ]
+
+
+class DsattnLnDesc(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64), ("channels", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+    ]
+
+
+class DsattnScanDesc(ctypes.Structure):
+    _fields_ = [
+        ("streams", ctypes.c_int32), ("frames", ctypes.c_int32), ("spatial", ctypes.c_int32),
+        ("channels", ctypes.c_int32), ("mode", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
     ]
 
 
@@ -222,6 +242,25 @@ def load():
     lib.dsattn_sink_forward.restype = ctypes.c_int
     lib.dsattn_sink_forward.argtypes = [ctypes.POINTER(DsattnSinkDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                         ctypes.c_size_t, vp]
+    sizep = ctypes.POINTER(ctypes.c_size_t)
+    lib.dsattn_layernorm.restype = ctypes.c_int
+    lib.dsattn_layernorm.argtypes = [ctypes.POINTER(DsattnLnDesc)] + [vp] * 8
+    lib.dsattn_layernorm_backward_workspace.restype = ctypes.c_int
+    lib.dsattn_layernorm_backward_workspace.argtypes = [ctypes.POINTER(DsattnLnDesc), sizep]
+    lib.dsattn_layernorm_backward.restype = ctypes.c_int
+    lib.dsattn_layernorm_backward.argtypes = [ctypes.POINTER(DsattnLnDesc)] + [vp] * 9 + [ctypes.c_size_t, vp]
+    lib.dsattn_gated_scan_workspace.restype = ctypes.c_int
+    lib.dsattn_gated_scan_workspace.argtypes = [ctypes.POINTER(DsattnScanDesc), sizep]
+    lib.dsattn_gated_scan.restype = ctypes.c_int
+    lib.dsattn_gated_scan.argtypes = [ctypes.POINTER(DsattnScanDesc)] + [vp] * 8 + [ctypes.c_size_t, vp]
+    lib.dsattn_gated_scan_backward.restype = ctypes.c_int
+    lib.dsattn_gated_scan_backward.argtypes = [ctypes.POINTER(DsattnScanDesc)] + [vp] * 10 + [ctypes.c_size_t, vp]
+    lib.dsattn_linear_act_backward_workspace.restype = ctypes.c_int
+    lib.dsattn_linear_act_backward_workspace.argtypes = [ctypes.POINTER(DsattnLinearActDesc), sizep]
+    lib.dsattn_linear_act_backward.restype = ctypes.c_int
+    lib.dsattn_linear_act_backward.argtypes = [ctypes.POINTER(DsattnLinearActDesc), vp, ctypes.POINTER(vp),
+                                               ctypes.POINTER(vp), vp, vp, ctypes.POINTER(vp), ctypes.POINTER(vp),
+                                               vp, ctypes.c_size_t, vp]
     lib.dsattn_strerror.restype = ctypes.c_char_p
     lib.dsattn_strerror.argtypes = [ctypes.c_int]
     lib.dsattn_last_error.restype = ctypes.c_char_p
@@ -828,3 +867,142 @@ def dsattn_sink_forward(streams, frames, spatial, heads, kv_heads, head_dim, sin
     _check(load().dsattn_sink_forward(ctypes.byref(desc), _ptr(start), _ptr(counts), _ptr(Q), _ptr(K), _ptr(V),
                                       _ptr(Kcache), _ptr(Vcache), _ptr(O), _ptr(workspace), nbytes,
                                       _stream(stream)), "dsattn_sink_forward")
+
+
+def _addresses(who, dev, items):
+    """The addresses of (tensor or None, name, numel, dtype code): the path of an ordinary call, and the general checks."""
+    out = []
+    for t, _, numel, code in items:
+        p = None if t is None else _addr(t, numel, code, dev)
+        if p is None and t is not None:
+            _check_tensors(who, items, "current")
+            return [_ptr(s[0]) for s in items]
+        out.append(p)
+    return out
+
+
+def _space(who, workspace, dev):
+    """Address and bytes of a workspace: a byte tensor on the call's device, or None."""
+    if workspace is None:
+        return None, 0
+    if _torch is not None and isinstance(workspace, _torch.Tensor) and workspace.element_size() == 1 \
+            and workspace.get_device() == dev and workspace.is_contiguous():
+        return workspace.data_ptr(), workspace.numel()
+    if not hasattr(workspace, "data_ptr") or workspace.element_size() != 1:
+        raise ValueError(f"{who}: workspace: a byte tensor (uint8) expected")
+    _check_tensors(who, [(workspace, "workspace", ("min", 0), None)], "current")
+    return _ptr(workspace), workspace.numel()
+
+
+def _workspace_bytes(name, desc):
+    out = ctypes.c_size_t()
+    _check(getattr(load(), name)(ctypes.byref(desc), ctypes.byref(out)), name)
+    return int(out.value)
+
+
+def dsattn_layernorm(rows, channels, X, Y, residual=None, gamma=None, beta=None, sum_out=None, scales=None,
+                     io_dtype=DSATTN_BF16, out_dtype=None, eps=1e-6, stream=None):
+    """sum_out receives X + residual (which it may be itself), scales the rows' scales of an output in
+    8 bits (out_dtype = DSATTN_E4M3; Y is then a torch.float8_e4m3fn tensor)."""
+    out = io_dtype if out_dtype is None else out_dtype
+    desc = DsattnLnDesc(rows, channels, io_dtype, out, eps)
+    dev, n = _device_of(X), rows * channels
+    x, r, g, b, t, y, s = _addresses("dsattn_layernorm", dev, (
+        (X, "X", n, io_dtype), (residual, "residual", n, io_dtype), (gamma, "gamma", channels, DSATTN_F32),
+        (beta, "beta", channels, DSATTN_F32), (sum_out, "sum_out", n, io_dtype), (Y, "Y", n, out),
+        (scales, "scales", rows, DSATTN_F32)))
+    _check((_lib or load()).dsattn_layernorm(ctypes.byref(desc), x, r, g, b, t, y, s, _raw_stream(stream)),
+           "dsattn_layernorm")
+
+
+def dsattn_layernorm_backward_workspace(rows, channels, io_dtype=DSATTN_BF16) -> int:
+    """Bytes of device workspace dsattn_layernorm_backward needs for the gradients of gamma and beta."""
+    return _workspace_bytes("dsattn_layernorm_backward_workspace", DsattnLnDesc(rows, channels, io_dtype, io_dtype, 0.0))
+
+
+def dsattn_layernorm_backward(rows, channels, X, dY, dX, residual=None, gamma=None, dsum=None, dgamma=None, dbeta=None,
+                              workspace=None, io_dtype=DSATTN_BF16, eps=1e-6, stream=None):
+    """dsum: the gradient that arrives at X + residual by other ways, added to dX.  workspace: a uint8 device tensor of at
+    least dsattn_layernorm_backward_workspace() bytes, or None without dgamma and dbeta."""
+    who = "dsattn_layernorm_backward"
+    desc = DsattnLnDesc(rows, channels, io_dtype, io_dtype, eps)
+    dev, n = _device_of(X), rows * channels
+    x, r, g, dy, ds, dx, dg, db = _addresses(who, dev, (
+        (X, "X", n, io_dtype), (residual, "residual", n, io_dtype), (gamma, "gamma", channels, DSATTN_F32),
+        (dY, "dY", n, io_dtype), (dsum, "dsum", n, io_dtype), (dX, "dX", n, io_dtype),
+        (dgamma, "dgamma", channels, DSATTN_F32), (dbeta, "dbeta", channels, DSATTN_F32)))
+    w, nw = _space(who, workspace, dev)
+    _check((_lib or load()).dsattn_layernorm_backward(ctypes.byref(desc), x, r, g, dy, ds, dx, dg, db, w, nw,
+                                                      _raw_stream(stream)), who)
+
+
+def dsattn_gated_scan_workspace(streams, frames, spatial, channels, io_dtype=DSATTN_BF16) -> int:
+    """Bytes of device workspace either direction of the recurrence needs for this shape (may be 0)."""
+    return _workspace_bytes("dsattn_gated_scan_workspace",
+                            DsattnScanDesc(streams, frames, spatial, channels, DSATTN_SCAN_SUM, io_dtype))
+
+
+def dsattn_gated_scan(streams, frames, spatial, channels, X, G, Y, mode=DSATTN_SCAN_MEAN, start_state=None,
+                      end_state=None, states=None, counts=None, workspace=None, io_dtype=DSATTN_BF16, stream=None):
+    """states: an fp32 tensor [streams, ceil(frames / DSATTN_SCAN_FRAMES), spatial, channels] for the backward pass, or
+    None; workspace: a uint8 device tensor of at least dsattn_gated_scan_workspace() bytes, or None where that is 0."""
+    who = "dsattn_gated_scan"
+    desc = DsattnScanDesc(streams, frames, spatial, channels, mode, io_dtype)
+    dev, n = _device_of(X), streams * spatial * channels
+    c, x, g, h, y, e, s = _addresses(who, dev, (
+        (counts, "counts", streams, _I32), (X, "X", n * frames, io_dtype), (G, "G", n * frames, io_dtype),
+        (start_state, "start_state", n, DSATTN_F32), (Y, "Y", n * frames, io_dtype),
+        (end_state, "end_state", n, DSATTN_F32),
+        (states, "states", n * ((frames + DSATTN_SCAN_FRAMES - 1) // DSATTN_SCAN_FRAMES), DSATTN_F32)))
+    w, nw = _space(who, workspace, dev)
+    _check((_lib or load()).dsattn_gated_scan(ctypes.byref(desc), c, x, g, h, y, e, s, w, nw, _raw_stream(stream)), who)
+
+
+def dsattn_gated_scan_backward(streams, frames, spatial, channels, X, G, states, dY, dX, dG, mode=DSATTN_SCAN_MEAN,
+                               dend_state=None, dstart_state=None, counts=None, workspace=None, io_dtype=DSATTN_BF16,
+                               stream=None):
+    """states: what dsattn_gated_scan left of the same inputs; workspace as there."""
+    who = "dsattn_gated_scan_backward"
+    desc = DsattnScanDesc(streams, frames, spatial, channels, mode, io_dtype)
+    dev, n = _device_of(X), streams * spatial * channels
+    c, x, g, s, dy, de, dx, dg, ds = _addresses(who, dev, (
+        (counts, "counts", streams, _I32), (X, "X", n * frames, io_dtype), (G, "G", n * frames, io_dtype),
+        (states, "states", n * ((frames + DSATTN_SCAN_FRAMES - 1) // DSATTN_SCAN_FRAMES), DSATTN_F32),
+        (dY, "dY", n * frames, io_dtype), (dend_state, "dend_state", n, DSATTN_F32), (dX, "dX", n * frames, io_dtype),
+        (dG, "dG", n * frames, io_dtype), (dstart_state, "dstart_state", n, DSATTN_F32)))
+    w, nw = _space(who, workspace, dev)
+    _check((_lib or load()).dsattn_gated_scan_backward(ctypes.byref(desc), c, x, g, s, dy, de, dx, dg, ds, w, nw,
+                                                       _raw_stream(stream)), who)
+
+
+def dsattn_linear_act_backward_workspace(rows, c_in, c_out, n_w=1, act=DSATTN_ACT_NONE, io_dtype=DSATTN_BF16,
+                                         flags=0) -> int:
+    """Bytes of device workspace dsattn_linear_act_backward needs for this shape (may be 0)."""
+    return _workspace_bytes("dsattn_linear_act_backward_workspace",
+                            DsattnLinearActDesc(rows, c_in, c_out, n_w, act, io_dtype, io_dtype, flags))
+
+
+def dsattn_linear_act_backward(rows, c_in, c_out, X, Ws, dY, dX=None, dWs=None, dbiases=None, biases=None,
+                               act=DSATTN_ACT_NONE, workspace=None, io_dtype=DSATTN_BF16, flags=0, stream=None):
+    """Ws: one weight set, or two (gate, value); biases, dWs and dbiases: None, or as many entries (each a tensor or None).
+    workspace: a uint8 device tensor of at least dsattn_linear_act_backward_workspace() bytes, or None where that is 0."""
+    who, n = "dsattn_linear_act_backward", len(Ws)
+    if n not in (1, 2) or any(s is not None and len(s) != n for s in (biases, dWs, dbiases)):
+        raise ValueError(f"{who}: one or two weight sets, and as many biases and gradients, expected")
+    desc = DsattnLinearActDesc(rows, c_in, c_out, n, act, io_dtype, io_dtype, flags)
+    dev, nw = _device_of(X), c_out * c_in
+    items = [(X, "X", rows * c_in, io_dtype), (dY, "dY", rows * c_out, io_dtype), (dX, "dX", rows * c_in, io_dtype)]
+    items += [(w, f"W[{k}]", nw, io_dtype) for k, w in enumerate(Ws)]
+    lists = [(biases, "bias", c_out, DSATTN_F32), (dWs, "dW", nw, io_dtype), (dbiases, "dbias", c_out, DSATTN_F32)]
+    for some, name, numel, code in lists:
+        if some is not None:
+            items += [(t, f"{name}[{k}]", numel, code) for k, t in enumerate(some)]
+    at = _addresses(who, dev, items)
+    vp, start = ctypes.c_void_p * n, 3 + n
+    arrays = []
+    for some, _, _, _ in lists:
+        arrays.append(None if some is None else vp(*at[start:start + n]))
+        start += 0 if some is None else n
+    w, nbytes = _space(who, workspace, dev)
+    _check((_lib or load()).dsattn_linear_act_backward(ctypes.byref(desc), at[0], vp(*at[3:3 + n]), arrays[0], at[1], at[2],
+                                                       arrays[1], arrays[2], w, nbytes, _raw_stream(stream)), who)

@@ -16,7 +16,8 @@ LIB = os.path.join(HERE, "libdsattn.so")
 SOURCES = ["mfma_d40.hip", "mfma_d32.hip", "mfma_d96.hip", "mfma_d80.hip", "mfma_d64.hip",
            "mfma_d160.hip", "mfma_d128.hip", "dsattn_api.hip", "kernels_generic.hip",
            "kernel_mfma.hip", "tile_attn.hip", "groupnorm.hip", "tconv.hip", "rmsnorm.hip",
-           "linear_act.hip", "sink_attn.hip"]
+           "linear_act.hip", "sink_attn.hip", "layernorm.hip", "gated_scan.hip",
+           "linear_act_grad.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -1,0 +1,548 @@
+// Gated linear recurrence over frames and its backward pass (dsattn_gated_scan, dsattn_gated_scan_backward).
+//
+//   a_t = sigmoid(g_t),  h_t = a_t h_(t-1) + w(a_t) x_t            w = 1, 1 - a or sqrt(1 - a^2)
+//   D_t = dy_t + a_(t+1) D_(t+1),  dx_t = w D_t,  dg_t = D_t (a (1 - a) h_(t-1) + x_t dw/dg)
+//
+// Bound by memory.  Positions and channels are independent and lie next to each other: a lane has four bytes of a frame (two
+// bf16 or one fp32 channel) and walks the frames, those ahead already on their way.  Where that makes too few wavefronts the
+// frames are cut into chunks: a first pass finds what each chunk does to a state (its product of gates A and its result H
+// from 0), one kernel joins these, and the chunks run again from their states.  The backward pass does the same from the end; it
+// needs the states h, which it runs again, in 32 bits, from those that the forward pass left every 16 frames.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+#include <utility>
+
+#include "dsattn.h"
+#include "plan.h"
+#include "rows.h"
+
+namespace dsattn {
+namespace {
+
+constexpr int kStep = DSATTN_SCAN_FRAMES;
+
+struct ScanArgs {
+    const void *X, *G, *dY;
+    const float *states_in;   // backward: [B][steps][n]
+    const float *carry_in;    // start state, or the end state's gradient; null: 0
+    const int32_t *counts;    // or null
+    void *Y;                  // Y, or dX
+    void *dG;
+    float *carry_out;         // end state, or the start state's gradient; null: not wanted
+    float *states_out;        // forward: [B][steps][n] or null
+    float *A, *H;             // of chunks: [B][chunks][n]; after the join H is what each chunk starts from
+    int64_t n;                // P * channels
+    int32_t B, T, steps;      // steps: ceil(T / kStep)
+    int32_t chunk, chunks;    // frames of a chunk (a multiple of kStep), chunks of a stream
+};
+
+// e^-|g|, within an ulp or so: the product with log2(e) in two parts
+__device__ __forceinline__ float exp_minus_abs(float g)
+{
+    const float x = -fabsf(g), hi = x * 1.44269504f;
+    const float lo = fmaf(x, 1.44269504f, -hi) + x * 1.92596299e-8f;
+    const float e = __builtin_amdgcn_exp2f(hi);
+    return fmaf(e, lo * 0.693147181f, e);
+}
+
+// What a gate keeps, a = sigmoid(g), and what it leaves, 1 - a: each with a small relative error.
+struct Gate {
+    float keep, leave;
+};
+__device__ __forceinline__ Gate gate_of(float g)
+{
+    const float e = exp_minus_abs(g), big = 1.f / (1.f + e), small = e * big;
+    return g >= 0.f ? Gate{big, small} : Gate{small, big};  // (a NaN: both are)
+}
+// sqrt((1 - a) f), f of ordinary size: the root of what is left, e^-g / (1 + e^-g), by e^(-g / 2), which does not underflow
+// until the root does
+__device__ __forceinline__ float root_left(const Gate &q, float g, float f)
+{
+    return g >= 0.f ? exp_minus_abs(0.5f * g) * sqrtf(q.keep * f) : sqrtf(q.leave * f);
+}
+template <int MODE>
+__device__ __forceinline__ float weight_of(const Gate &q, float g)
+{
+    if constexpr (MODE == DSATTN_SCAN_MEAN) return q.leave;
+    if constexpr (MODE == DSATTN_SCAN_NORM) return root_left(q, g, 1.f + q.keep);
+    return 1.f;
+}
+// dw / dg
+template <int MODE>
+__device__ __forceinline__ float weight_slope_of(const Gate &q, float g)
+{
+    if constexpr (MODE == DSATTN_SCAN_MEAN) return -q.keep * q.leave;
+    if constexpr (MODE == DSATTN_SCAN_NORM) return -q.keep * q.keep * root_left(q, g, 1.f / (1.f + q.keep));
+    return 0.f;
+}
+
+template <typename T, int V>
+struct Lane {
+    typedef T Piece __attribute__((ext_vector_type(V)));
+};
+
+// This lane's first channel, stream and frames.  (Grid: channels, chunks, streams.)
+template <int V>
+struct Place {
+    int64_t c;
+    int b, j, t0, t1;  // frames [t0, t1): none where the stream is over
+    __device__ __forceinline__ Place(const ScanArgs &a)
+    {
+        c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
+        j = (int)blockIdx.y;
+        b = (int)blockIdx.z;
+        const int count = a.counts ? min(max(a.counts[b], 0), a.T) : a.T;
+        t0 = min(j * a.chunk, count);
+        t1 = min(j * a.chunk + a.chunk, count);
+    }
+};
+
+// f(0), f(1), .. of the frames [t, end), kStep of them at most; a whole step without conditions.  (Constants, so that what f
+// indexes with them stays in registers.)
+template <bool BACK, typename F, int... I>
+__device__ __forceinline__ void frames_each(int left, F &f, std::integer_sequence<int, I...>)
+{
+    if (left >= kStep) {
+        (f(std::integral_constant<int, BACK ? kStep - 1 - I : I>{}), ...);
+    } else {
+        (((BACK ? kStep - 1 - I : I) < left ? f(std::integral_constant<int, BACK ? kStep - 1 - I : I>{}) : (void)0), ...);
+    }
+}
+template <typename F>
+__device__ __forceinline__ void frames_of(int t, int end, F f) { frames_each<false>(end - t, f, std::make_integer_sequence<int, kStep>{}); }
+// the same from the last on
+template <typename F>
+__device__ __forceinline__ void frames_back(int t, int end, F f) { frames_each<true>(end - t, f, std::make_integer_sequence<int, kStep>{}); }
+
+// Steps of kStep frames, the next one's on their way meanwhile.  With STORE the states and Y are written, else A and H of the chunk.
+template <typename T, int V, int MODE, bool STORE>
+__global__ __launch_bounds__(256) void scan_kernel(const ScanArgs a)
+{
+    using Piece = typename Lane<T, V>::Piece;
+    const Place<V> p(a);
+    if (p.c >= a.n) return;
+    const int64_t base = (int64_t)p.b * a.T * a.n + p.c, part = ((int64_t)p.b * a.chunks + p.j) * a.n + p.c;
+    const T *X = (const T *)a.X + base, *G = (const T *)a.G + base;
+    float h[V], prod[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        prod[v] = 1.f;
+        h[v] = 0.f;
+        if constexpr (STORE) h[v] = a.chunks > 1 ? a.H[part + v] : a.carry_in ? a.carry_in[(int64_t)p.b * a.n + p.c + v] : 0.f;
+    }
+    Piece x[kStep], g[kStep];
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) {
+            const int64_t at = (int64_t)min(t + i, p.t1 - 1) * a.n;  // (past the end: the last one again, not used)
+            x[i] = *(const Piece *)(X + at);
+            g[i] = *(const Piece *)(G + at);
+        }
+    };
+    if (p.t1 > p.t0) fetch(p.t0);
+    for (int t = p.t0; t < p.t1; t += kStep) {
+        Piece xc[kStep], gc[kStep];
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) {
+            xc[i] = x[i];
+            gc[i] = g[i];
+        }
+        if (t + kStep < p.t1) fetch(t + kStep);
+        if constexpr (STORE) {
+            if (a.states_out) {
+                float *to = a.states_out + ((int64_t)p.b * a.steps + t / kStep) * a.n + p.c;
+#pragma unroll
+                for (int v = 0; v < V; ++v) to[v] = h[v];
+            }
+        }
+        frames_of(t, p.t1, [&](auto at) __attribute__((always_inline)) {
+            constexpr int i = decltype(at)::value;
+            Piece y;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Gate q = gate_of((float)gc[i][v]);
+                h[v] = fmaf(q.keep, h[v], weight_of<MODE>(q, (float)gc[i][v]) * (float)xc[i][v]);
+                if constexpr (STORE)
+                    y[v] = (T)h[v];
+                else
+                    prod[v] *= q.keep;
+            }
+            if constexpr (STORE) *(Piece *)((T *)a.Y + base + (int64_t)(t + i) * a.n) = y;
+        });
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        if constexpr (!STORE) {
+            a.A[part + v] = prod[v];
+            a.H[part + v] = h[v];
+        } else if (a.chunks == 1 && a.carry_out) {
+            a.carry_out[(int64_t)p.b * a.n + p.c + v] = h[v];
+        }
+    }
+}
+
+// The same from the end: c is a_(t+1) D_(t+1), what frame t gets of the later ones.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void scan_back_parts_kernel(const ScanArgs a)
+{
+    using Piece = typename Lane<T, V>::Piece;
+    const Place<V> p(a);
+    if (p.c >= a.n) return;
+    const int64_t base = (int64_t)p.b * a.T * a.n + p.c, part = ((int64_t)p.b * a.chunks + p.j) * a.n + p.c;
+    const T *G = (const T *)a.G + base, *dY = (const T *)a.dY + base;
+    float c[V], prod[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        prod[v] = 1.f;
+        c[v] = 0.f;
+    }
+    for (int t = p.t0 + (p.t1 - p.t0 - 1) / kStep * kStep; p.t1 > p.t0 && t >= p.t0; t -= kStep) {
+        Piece g[kStep], dy[kStep];
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) {
+            const int64_t at = (int64_t)min(t + i, p.t1 - 1) * a.n;  // (past the end: the last one again, not used)
+            g[i] = *(const Piece *)(G + at);
+            dy[i] = *(const Piece *)(dY + at);
+        }
+        frames_back(t, p.t1, [&](auto at) __attribute__((always_inline)) {
+            constexpr int i = decltype(at)::value;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float keep = gate_of((float)g[i][v]).keep;
+                c[v] = keep * (c[v] + (float)dy[i][v]);
+                prod[v] *= keep;
+            }
+        });
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        a.A[part + v] = prod[v];
+        a.H[part + v] = c[v];
+    }
+}
+
+template <typename T, int V, int MODE>
+__global__ __launch_bounds__(256) void scan_back_kernel(const ScanArgs a)
+{
+    using Piece = typename Lane<T, V>::Piece;
+    const Place<V> p(a);
+    if (p.c >= a.n) return;
+    const int64_t base = (int64_t)p.b * a.T * a.n + p.c, part = ((int64_t)p.b * a.chunks + p.j) * a.n + p.c;
+    const T *X = (const T *)a.X + base, *G = (const T *)a.G + base, *dY = (const T *)a.dY + base;
+    const float *S = a.states_in + (int64_t)p.b * a.steps * a.n + p.c;
+    float c[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        c[v] = a.chunks > 1 ? a.H[part + v] : a.carry_in ? a.carry_in[(int64_t)p.b * a.n + p.c + v] : 0.f;
+    Piece x[kStep], g[kStep], dy[kStep];
+    float s[V];
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) s[v] = S[(int64_t)(t / kStep) * a.n + v];
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) {
+            const int64_t at = (int64_t)min(t + i, p.t1 - 1) * a.n;  // (past the end: the last one again, not used)
+            x[i] = *(const Piece *)(X + at);
+            g[i] = *(const Piece *)(G + at);
+            dy[i] = *(const Piece *)(dY + at);
+        }
+    };
+    int t = p.t0 + (p.t1 - p.t0 - 1) / kStep * kStep;
+    if (p.t1 > p.t0) fetch(t);
+    for (; p.t1 > p.t0 && t >= p.t0; t -= kStep) {
+        Piece xc[kStep], gc[kStep], dc[kStep];
+        float h[kStep][V];  // the state in front of each frame
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) {
+            xc[i] = x[i];
+            gc[i] = g[i];
+            dc[i] = dy[i];
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[0][v] = s[v];
+        if (t - kStep >= p.t0) fetch(t - kStep);
+#pragma unroll
+        for (int i = 0; i + 1 < kStep; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Gate q = gate_of((float)gc[i][v]);
+                h[i + 1][v] = fmaf(q.keep, h[i][v], weight_of<MODE>(q, (float)gc[i][v]) * (float)xc[i][v]);  // (past the end: not used)
+            }
+        frames_back(t, p.t1, [&](auto at) __attribute__((always_inline)) {
+            constexpr int i = decltype(at)::value;
+            Piece dx, dg;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Gate q = gate_of((float)gc[i][v]);
+                const float d = c[v] + (float)dc[i][v];
+                dx[v] = (T)(d * weight_of<MODE>(q, (float)gc[i][v]));
+                if constexpr (MODE == DSATTN_SCAN_MEAN)  // the two slopes differ in sign only
+                    dg[v] = (T)(d * (q.keep * q.leave) * (h[i][v] - (float)xc[i][v]));
+                else
+                    dg[v] = (T)(d * fmaf(q.keep * q.leave, h[i][v], weight_slope_of<MODE>(q, (float)gc[i][v]) * (float)xc[i][v]));
+                c[v] = q.keep * d;
+            }
+            *(Piece *)((T *)a.Y + base + (int64_t)(t + i) * a.n) = dx;
+            *(Piece *)((T *)a.dG + base + (int64_t)(t + i) * a.n) = dg;
+        });
+    }
+    if (a.chunks == 1 && a.carry_out) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) a.carry_out[(int64_t)p.b * a.n + p.c + v] = c[v];
+    }
+}
+
+// What each chunk starts from: 16 channels a workgroup, 64 threads to each, which have runs of chunks.  BACK: from the last on.
+template <bool BACK>
+__global__ __launch_bounds__(1024) void scan_join_kernel(const ScanArgs a)
+{
+    __shared__ float As[64][17], Hs[64][17];
+    const int l = threadIdx.x & 15, w = threadIdx.x >> 4, b = (int)blockIdx.y;
+    const int64_t c = (int64_t)blockIdx.x * 16 + l;
+    const bool there = c < a.n;
+    const int per = (a.chunks + 63) / 64, first = min(w * per, a.chunks), end = min(first + per, a.chunks);
+    auto at = [&](int j) __attribute__((always_inline)) {
+        return ((int64_t)b * a.chunks + (BACK ? a.chunks - 1 - j : j)) * a.n + c;
+    };
+    // (read before anything is written: the state that there is may be where the last one goes)
+    const float start = there && a.carry_in ? a.carry_in[(int64_t)b * a.n + c] : 0.f;
+    float A = 1.f, H = 0.f;
+    if (there)
+        for (int j = first; j < end; ++j) {
+            const float aj = a.A[at(j)];
+            H = fmaf(aj, H, a.H[at(j)]);
+            A *= aj;
+        }
+    if (w == 0) {  // the first run begins with the state that there is
+        if (a.carry_in) H = fmaf(A, start, H);
+        A = 0.f;
+    }
+    for (int span = 1; span < 64; span *= 2) {
+        As[w][l] = A;
+        Hs[w][l] = H;
+        __syncthreads();
+        if (w >= span) {
+            H = fmaf(A, Hs[w - span][l], H);
+            A *= As[w - span][l];
+        }
+        __syncthreads();
+    }
+    Hs[w][l] = H;
+    __syncthreads();
+    if (!there) return;
+    H = w ? Hs[w - 1][l] : start;
+    for (int j = first; j < end; ++j) {
+        const float hj = a.H[at(j)], aj = a.A[at(j)];
+        a.H[at(j)] = H;
+        H = fmaf(aj, H, hj);
+    }
+    if (a.carry_out && w == 63) a.carry_out[(int64_t)b * a.n + c] = Hs[63][l];
+}
+
+int scan_validate(const dsattn_scan_desc *desc, const char *who)
+{
+    if (!desc) return fail(DSATTN_EINVAL, "%s: null descriptor", who);
+    const dsattn_scan_desc &d = *desc;
+    if (d.streams < 1 || d.frames < 1 || d.spatial < 1 || d.channels < 1)
+        return fail(DSATTN_EINVAL, "%s: sizes must be positive", who);
+    if (d.frames > 0x7fffffff - 2 * kStep) return fail(DSATTN_EINVAL, "%s: too many frames", who);
+    const int64_t most = (int64_t)1 << 46, n = (int64_t)d.spatial * d.channels;
+    if (n > most / d.streams || n * d.streams > most / d.frames) return fail(DSATTN_EINVAL, "%s: problem too large", who);
+    if (d.mode < DSATTN_SCAN_SUM || d.mode > DSATTN_SCAN_NORM) return fail(DSATTN_EINVAL, "%s: unknown mode", who);
+    if (d.io_dtype != DSATTN_F32 && d.io_dtype != DSATTN_BF16) return fail(DSATTN_EINVAL, "%s: unknown dtype", who);
+    return DSATTN_OK;
+}
+
+// Channels of a lane: four bytes, or one where a frame is an odd number of 16-bit ones.
+int scan_lane(const dsattn_scan_desc &d)
+{
+    return d.io_dtype == DSATTN_BF16 && (int64_t)d.spatial * d.channels % 2 == 0 ? 2 : 1;
+}
+
+// Chunks of a stream: as many as make 2,048 wavefronts, of at least 64 frames each.
+void scan_chunks(const dsattn_scan_desc &d, int32_t &chunk, int32_t &chunks)
+{
+    const int64_t n = (int64_t)d.spatial * d.channels, lanes = (n + scan_lane(d) - 1) / scan_lane(d);
+    const int64_t waves = std::max<int64_t>(1, (lanes + 63) / 64 * d.streams), want = std::min<int64_t>(2048 / waves, d.frames / 64);
+    chunk = d.frames;
+    chunks = 1;
+    if (want >= 4) {
+        chunk = (int32_t)(((d.frames + want - 1) / want + kStep - 1) / kStep * kStep);
+        chunks = (d.frames + chunk - 1) / chunk;
+    }
+}
+
+size_t scan_bytes(const dsattn_scan_desc &d)
+{
+    int32_t chunk, chunks;
+    scan_chunks(d, chunk, chunks);
+    return chunks == 1 ? 0 : (size_t)d.streams * chunks * d.spatial * d.channels * 2 * sizeof(float);
+}
+
+enum { kPartsPass, kRunPass, kBackPartsPass, kBackPass };
+
+template <typename T, int V, int MODE>
+const void *scan_kernel_of(int pass)
+{
+    switch (pass) {
+    case kPartsPass: return (const void *)&scan_kernel<T, V, MODE, false>;
+    case kRunPass: return (const void *)&scan_kernel<T, V, MODE, true>;
+    case kBackPartsPass: return (const void *)&scan_back_parts_kernel<T, V>;
+    default: return (const void *)&scan_back_kernel<T, V, MODE>;
+    }
+}
+template <typename T, int V>
+const void *scan_kernel_of(int mode, int pass)
+{
+    switch (mode) {
+    case DSATTN_SCAN_MEAN: return scan_kernel_of<T, V, DSATTN_SCAN_MEAN>(pass);
+    case DSATTN_SCAN_NORM: return scan_kernel_of<T, V, DSATTN_SCAN_NORM>(pass);
+    default: return scan_kernel_of<T, V, DSATTN_SCAN_SUM>(pass);
+    }
+}
+
+// Checks what both directions share and fills a; then the launches.
+int scan_setup(const dsattn_scan_desc &d, const char *who, ScanArgs &a, void *workspace, size_t workspace_bytes)
+{
+    a.n = (int64_t)d.spatial * d.channels;
+    a.B = d.streams;
+    a.T = d.frames;
+    a.steps = (d.frames + kStep - 1) / kStep;
+    scan_chunks(d, a.chunk, a.chunks);
+    const size_t need = scan_bytes(d);
+    if (need && (!workspace || workspace_bytes < need)) return fail(DSATTN_EINVAL, "%s: workspace of %zu bytes needed", who, need);
+    if ((uintptr_t)workspace & 15u) return fail(DSATTN_EINVAL, "%s: pointers must be 16-byte aligned", who);
+    a.A = need ? (float *)workspace : nullptr;
+    a.H = need ? a.A + (int64_t)a.B * a.chunks * a.n : nullptr;
+    const int64_t lanes = (a.n + scan_lane(d) - 1) / scan_lane(d);
+    // (a launch has less than 2^32 threads, and less than 2^16 in the grid's other dimensions)
+    if (a.B > 65535 || a.chunks > 65535 || (lanes + 255) / 256 * a.chunks * a.B > 0xffffff ||
+        (a.chunks > 1 && (a.n + 15) / 16 * a.B > 0x3fffff))
+        return fail(DSATTN_EUNSUPPORTED, "%s: too large for one launch", who);
+    return DSATTN_OK;
+}
+
+int scan_launch(const dsattn_scan_desc &d, const char *who, ScanArgs &a, bool back, hipStream_t st)
+{
+    const int V = scan_lane(d), parts = back ? kBackPartsPass : kPartsPass, run = back ? kBackPass : kRunPass;
+    auto fn = [&](int pass) {
+        return d.io_dtype == DSATTN_F32 ? scan_kernel_of<float, 1>(d.mode, pass)
+               : V == 2                 ? scan_kernel_of<__bf16, 2>(d.mode, pass)
+                                        : scan_kernel_of<__bf16, 1>(d.mode, pass);
+    };
+    const dim3 grid((unsigned)(((a.n + V - 1) / V + 255) / 256), (unsigned)a.chunks, (unsigned)a.B);
+    void *params[] = {&a};
+    hipError_t e = hipSuccess;
+    if (a.chunks > 1) {
+        e = hipLaunchKernel(fn(parts), grid, dim3(256), params, 0, st);
+        const void *join = back ? (const void *)&scan_join_kernel<true> : (const void *)&scan_join_kernel<false>;
+        if (e == hipSuccess) e = hipLaunchKernel(join, dim3((unsigned)((a.n + 15) / 16), (unsigned)a.B), dim3(1024), params, 0, st);
+    }
+    if (e == hipSuccess) e = hipLaunchKernel(fn(run), grid, dim3(256), params, 0, st);
+    if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
+    return DSATTN_OK;
+}
+
+struct Span {
+    const void *p;
+    int64_t n;
+};
+
+// Outputs (the first `n_in_place` of which may be one of the first `n_taken` inputs) against inputs and each other.
+int scan_overlaps(const char *who, const Span *in, int n_in, int n_taken, const Span *out, int n_out, int n_in_place, bool carry_in_place)
+{
+    for (int o = 0; o < n_out; ++o) {
+        for (int i = 0; i < n_in; ++i) {
+            const bool same = in[i].p == out[o].p && in[i].n == out[o].n &&
+                              ((o < n_in_place && i < n_taken) || (carry_in_place && o == n_in_place && i == n_taken));
+            if (!same && overlap(out[o].p, out[o].n, in[i].p, in[i].n)) return fail(DSATTN_EINVAL, "%s: an output overlaps an input", who);
+        }
+        for (int q = 0; q < o; ++q)
+            if (overlap(out[o].p, out[o].n, out[q].p, out[q].n)) return fail(DSATTN_EINVAL, "%s: two outputs overlap", who);
+    }
+    return DSATTN_OK;
+}
+
+}  // namespace
+}  // namespace dsattn
+
+using namespace dsattn;
+
+extern "C" {
+
+int dsattn_gated_scan_workspace(const dsattn_scan_desc *desc, size_t *bytes)
+{
+    const int rc = scan_validate(desc, "dsattn_gated_scan_workspace");
+    if (rc != DSATTN_OK) return rc;
+    if (!bytes) return fail(DSATTN_EINVAL, "dsattn_gated_scan_workspace: null output");
+    *bytes = scan_bytes(*desc);
+    return DSATTN_OK;
+}
+
+int dsattn_gated_scan(const dsattn_scan_desc *desc, const int32_t *counts, const void *X, const void *G,
+                      const float *start_state, void *Y, float *end_state, float *states, void *workspace,
+                      size_t workspace_bytes, void *stream)
+{
+    const char *who = "dsattn_gated_scan";
+    int rc = scan_validate(desc, who);
+    if (rc != DSATTN_OK) return rc;
+    const dsattn_scan_desc &d = *desc;
+    if (!X || !G || !Y) return fail(DSATTN_EINVAL, "%s: null pointer", who);
+    if (((uintptr_t)X | (uintptr_t)G | (uintptr_t)Y | (uintptr_t)start_state | (uintptr_t)end_state | (uintptr_t)states) & 15u)
+        return fail(DSATTN_EINVAL, "%s: pointers must be 16-byte aligned", who);
+    if ((uintptr_t)counts & 3u) return fail(DSATTN_EINVAL, "%s: counts must be 4-byte aligned", who);
+    ScanArgs a{};
+    rc = scan_setup(d, who, a, workspace, workspace_bytes);
+    if (rc != DSATTN_OK) return rc;
+    const int64_t rows = (int64_t)d.streams * d.frames * a.n * (d.io_dtype == DSATTN_F32 ? 4 : 2), state = 4 * d.streams * a.n;
+    const Span in[] = {{X, rows}, {G, rows}, {start_state, state}, {counts, 4 * (int64_t)d.streams}},
+               out[] = {{Y, rows}, {end_state, state}, {states, state * a.steps}, {a.A, (int64_t)scan_bytes(d)}};
+    rc = scan_overlaps(who, in, 4, 2, out, 4, 1, true);
+    if (rc != DSATTN_OK) return rc;
+    a.X = X;
+    a.G = G;
+    a.counts = counts;
+    a.carry_in = start_state;
+    a.carry_out = end_state;
+    a.states_out = states;
+    a.Y = Y;
+    return scan_launch(d, who, a, false, (hipStream_t)stream);
+}
+
+int dsattn_gated_scan_backward(const dsattn_scan_desc *desc, const int32_t *counts, const void *X, const void *G,
+                               const float *states, const void *dY, const float *dend_state, void *dX, void *dG,
+                               float *dstart_state, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *who = "dsattn_gated_scan_backward";
+    int rc = scan_validate(desc, who);
+    if (rc != DSATTN_OK) return rc;
+    const dsattn_scan_desc &d = *desc;
+    if (!X || !G || !states || !dY || !dX || !dG) return fail(DSATTN_EINVAL, "%s: null pointer", who);
+    if (((uintptr_t)X | (uintptr_t)G | (uintptr_t)dY | (uintptr_t)dX | (uintptr_t)dG | (uintptr_t)states | (uintptr_t)dend_state |
+         (uintptr_t)dstart_state) & 15u)
+        return fail(DSATTN_EINVAL, "%s: pointers must be 16-byte aligned", who);
+    if ((uintptr_t)counts & 3u) return fail(DSATTN_EINVAL, "%s: counts must be 4-byte aligned", who);
+    ScanArgs a{};
+    rc = scan_setup(d, who, a, workspace, workspace_bytes);
+    if (rc != DSATTN_OK) return rc;
+    const int64_t rows = (int64_t)d.streams * d.frames * a.n * (d.io_dtype == DSATTN_F32 ? 4 : 2), state = 4 * d.streams * a.n;
+    const Span in[] = {{X, rows}, {G, rows}, {dY, rows}, {dend_state, state}, {states, state * a.steps}, {counts, 4 * (int64_t)d.streams}},
+               out[] = {{dX, rows}, {dG, rows}, {dstart_state, state}, {a.A, (int64_t)scan_bytes(d)}};
+    rc = scan_overlaps(who, in, 6, 3, out, 4, 2, true);
+    if (rc != DSATTN_OK) return rc;
+    a.X = X;
+    a.G = G;
+    a.dY = dY;
+    a.counts = counts;
+    a.states_in = states;
+    a.carry_in = dend_state;
+    a.carry_out = dstart_state;
+    a.Y = dX;
+    a.dG = dG;
+    return scan_launch(d, who, a, true, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,677 @@
+// Layer norm with the residual's addition and its backward pass (dsattn_layernorm, dsattn_layernorm_backward).
+//
+//   s = x + r,  n = (s - mean s) * rsqrt(var s + eps),  y = n * gamma + beta,  optionally y / scale in 8 bits
+//   e = dy * gamma,  dx = rsqrt(var s + eps) * (e - mean e - n * mean(e n)) + dsum,  dgamma = sum dy n,  dbeta = sum dy
+//
+// Bound by memory: a row stays in registers from its only read to its output, in L lanes with NV pieces of V numbers each.
+// The mean is taken off twice, the second time that of the differences: what the first left of it by rounding (a row whose
+// mean is 1,000 times its spread would lose ten bits of the spread to that) is gone, and the variance comes with it.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "dsattn.h"
+#include "plan.h"
+#include "rows.h"
+
+namespace dsattn {
+namespace {
+
+struct LnArgs {
+    const void *X, *R;
+    const float *gamma, *beta;
+    void *S, *Y;
+    float *scales;
+    int64_t rows;
+    int32_t C;
+    float eps;
+};
+
+struct LnBackArgs {
+    const void *X, *R, *dY, *dS;
+    const float *gamma;
+    void *dX;
+    float *partial;  // [groups][2][C]: sums of dy n and of dy; null where neither is wanted
+    struct RowStats *stats;  // long rows only
+    int64_t rows;
+    int32_t C;
+    float eps;
+};
+
+// n = ((s * unit - mean) * gain - rest) * rstd, and 1 / sqrt(var + eps) = unit * gain * rstd.  unit is 1, or 2^-75 for a row
+// whose squares are beyond fp32's numbers (2^20 numbers of up to 2^53 stay within them then); gain is 1, or 2^100 for one whose
+// differences have squares below 2^-100 (and eps far less): both exact, so that rows of every size are normalised alike.
+struct RowStats {
+    float unit, gain, mean, rest, rstd;
+    __device__ __forceinline__ float norm(float s) const { return ((s * unit - mean) * gain - rest) * rstd; }
+    // (one after the other: their product may be infinite where d is 0)
+    __device__ __forceinline__ float slope(float d) const { return d * rstd * gain * unit; }
+};
+
+// Sums of N numbers over the L lanes of a row; part: LDS of a workgroup, for rows of several wavefronts.
+template <int L, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*part)[N])
+{
+#pragma unroll
+    for (int w = 1; w < (L < 64 ? L : 64); w *= 2)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], w);
+    if constexpr (L > 64) {
+        __syncthreads();  // the sums before have been read
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int k = 0; k < N; ++k) part[threadIdx.x >> 6][k] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = part[0][k];
+#pragma unroll
+            for (int w = 1; w < L / 64; ++w) v[k] += part[w][k];
+        }
+    }
+}
+
+// each(f) calls f(s) for the lane's numbers of the row, sums(v) adds v over the row's lanes: whether another turn is needed
+// depends on sums only, which all lanes of a row have.
+template <typename Each, typename Sums>
+__device__ __forceinline__ RowStats row_stats(int C, float eps, Each each, Sums sums)
+{
+    RowStats t{1.f, 1.f, 0.f, 0.f, 0.f};
+    const float inv = 1.f / (float)C;
+    float var = 0.f;
+    for (int turn = 0;; ++turn) {
+        float v[2] = {0.f, 0.f};
+        each([&](float s) __attribute__((always_inline)) { v[0] = fmaf(s, t.unit, v[0]); });
+        sums(v);
+        t.mean = v[0] * inv;
+        v[0] = v[1] = 0.f;
+        each([&](float s) __attribute__((always_inline)) {
+            const float d = (s * t.unit - t.mean) * t.gain;
+            v[0] += d;
+            v[1] = fmaf(d, d, v[1]);
+        });
+        sums(v);
+        t.rest = v[0] * inv;
+        var = fmaf(-t.rest, t.rest, v[1] * inv);
+        if (turn == 1) break;
+        if (!(v[1] < INFINITY))
+            t.unit = 0x1p-75f;
+        else if (v[1] < 0x1p-100f && eps < 0x1p-80f)
+            t.gain = 0x1p100f;
+        else
+            break;
+    }
+    // (var is not below 0 but by rounding; a NaN stays)
+    const float g = t.unit * t.gain;
+    t.rstd = 1.f / sqrtf((var < 0.f ? 0.f : var) + eps * g * g);
+    return t;
+}
+
+template <typename T, int V>
+struct Row {
+    typedef T Piece __attribute__((ext_vector_type(V)));
+    typedef float Floats __attribute__((ext_vector_type(V)));
+};
+
+// x + r of a row's pieces, in fp32; 0 behind its end.
+template <typename T, int V, int L, int NV>
+__device__ __forceinline__ void row_load(const void *X, const void *R, int64_t base, int at, int C, typename Row<T, V>::Floats (&s)[NV])
+{
+    using Piece = typename Row<T, V>::Piece;
+    Piece x[NV], r[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = at + i * (L * V);
+        x[i] = Piece{};
+        r[i] = -Piece{};  // (-0, which leaves every x as it is)
+        if (c < C) {
+            x[i] = *(const Piece *)((const T *)X + base + c);
+            if (R) r[i] = *(const Piece *)((const T *)R + base + c);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[i][e] = (float)x[i][e] + (float)r[i][e];
+}
+
+template <typename T, int V, int L, int NV, bool E8>
+__global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_vec_kernel(const LnArgs a)
+{
+    using Piece = typename Row<T, V>::Piece;
+    using Floats = typename Row<T, V>::Floats;
+    constexpr int THREADS = L <= 256 ? 256 : L, NW = L > 64 ? L / 64 : 1;
+    __shared__ float part[NW][2];
+    const int64_t row = (int64_t)blockIdx.x * (THREADS / L) + threadIdx.x / L;
+    const int C = a.C, at = (int)(threadIdx.x % L) * V;
+    const bool there = row < a.rows;
+    const int64_t base = (there ? row : a.rows - 1) * C;
+    Floats s[NV];
+    row_load<T, V, L, NV>(a.X, a.R, base, at, C, s);
+    Floats g[NV], b[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = at + i * (L * V);
+        g[i] = Floats{} + 1.f;
+        b[i] = Floats{};
+        if (a.gamma && c < C) g[i] = *(const Floats *)(a.gamma + c);
+        if (a.beta && c < C) b[i] = *(const Floats *)(a.beta + c);
+    }
+    const RowStats t = row_stats(
+        C, a.eps,
+        [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (at + i * (L * V) < C)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) f(s[i][e]);
+        },
+        [&](float (&v)[2]) __attribute__((always_inline)) { row_sums<L, 2>(v, part); });
+    Floats y[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[i][e] = fmaf(t.norm(s[i][e]), g[i][e], b[i][e]);
+    float inv = 1.f;
+    if constexpr (E8) {
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (at + i * (L * V) < C)
+#pragma unroll
+                for (int e = 0; e < V; ++e) top = max_or_nan(top, fabsf(y[i][e]));
+#pragma unroll
+        for (int w = 1; w < (L < 64 ? L : 64); w *= 2) top = max_or_nan(top, __shfl_xor(top, w));
+        if constexpr (L > 64) {
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6][0] = top;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < NW; ++w) top = max_or_nan(top, part[w][0]);
+        }
+        float scale = top / 448.f;
+        scale = scale < 0x1p-126f ? 0x1p-126f : scale;  // (a NaN stays)
+        if (there && at == 0) a.scales[row] = scale;
+        inv = 1.f / scale;
+    }
+    if (!there) return;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = at + i * (L * V);
+        if (c >= C) continue;
+        if (a.S) {
+            Piece p;
+#pragma unroll
+            for (int e = 0; e < V; ++e) p[e] = (T)s[i][e];
+            *(Piece *)((T *)a.S + base + c) = p;
+        }
+        if constexpr (E8) {
+            uint8_t *to = (uint8_t *)a.Y + base + c;
+            if constexpr (V % 4 == 0) {
+                typedef int Words __attribute__((ext_vector_type(V / 4)));
+                Words w;
+#pragma unroll
+                for (int q = 0; q < V / 4; ++q) {
+                    w[q] = __builtin_amdgcn_cvt_pk_fp8_f32(y[i][4 * q] * inv, y[i][4 * q + 1] * inv, 0, false);
+                    w[q] = __builtin_amdgcn_cvt_pk_fp8_f32(y[i][4 * q + 2] * inv, y[i][4 * q + 3] * inv, w[q], true);
+                }
+                *(Words *)to = w;
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e) to[e] = to_e4m3(y[i][e] * inv);
+            }
+        } else {
+            Piece p;
+#pragma unroll
+            for (int e = 0; e < V; ++e) p[e] = (T)y[i][e];
+            *(Piece *)((T *)a.Y + base + c) = p;
+        }
+    }
+}
+
+// A workgroup's loop over a row that is longer than its registers: f(column, x + r).
+template <typename T, typename F>
+__device__ __forceinline__ void long_row(const T *x, const T *r, int C, F f)
+{
+    for (int c = threadIdx.x; c < C; c += 256) f(c, (float)x[c] + (r ? (float)r[c] : -0.f));
+}
+
+template <typename T>
+__device__ __forceinline__ RowStats long_row_stats(const T *x, const T *r, int C, float eps, float (*part)[2])
+{
+    return row_stats(
+        C, eps,
+        [&](auto f) __attribute__((always_inline)) { long_row(x, r, C, [&](int, float s) __attribute__((always_inline)) { f(s); }); },
+        [&](float (&v)[2]) __attribute__((always_inline)) { row_sums<256, 2>(v, part); });
+}
+
+template <typename T, bool E8>
+__global__ __launch_bounds__(256) void ln_row_kernel(const LnArgs a)
+{
+    __shared__ float part[4][2];
+    const int64_t row = blockIdx.x;
+    const int C = a.C;
+    const T *x = (const T *)a.X + row * C, *r = a.R ? (const T *)a.R + row * C : nullptr;
+    const RowStats t = long_row_stats(x, r, C, a.eps, part);
+    auto y_of = [&](int c, float s) __attribute__((always_inline)) {
+        return fmaf(t.norm(s), a.gamma ? a.gamma[c] : 1.f, a.beta ? a.beta[c] : 0.f);
+    };
+    float inv = 1.f;
+    if constexpr (E8) {
+        float top = 0.f;
+        long_row(x, r, C, [&](int c, float s) __attribute__((always_inline)) { top = max_or_nan(top, fabsf(y_of(c, s))); });
+        for (int w = 32; w > 0; w >>= 1) top = max_or_nan(top, __shfl_xor(top, w));
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6][0] = top;
+        __syncthreads();
+        top = max_or_nan(max_or_nan(part[0][0], part[1][0]), max_or_nan(part[2][0], part[3][0]));
+        float scale = top / 448.f;
+        scale = scale < 0x1p-126f ? 0x1p-126f : scale;
+        if (threadIdx.x == 0) a.scales[row] = scale;
+        inv = 1.f / scale;
+    }
+    // (each number is read before its place is written, by the same thread: outputs may be the inputs)
+    long_row(x, r, C, [&](int c, float s) __attribute__((always_inline)) {
+        const float y = y_of(c, s) * inv;
+        if (a.S) ((T *)a.S)[row * C + c] = (T)s;
+        if constexpr (E8)
+            ((uint8_t *)a.Y)[row * C + c] = to_e4m3(y);
+        else
+            ((T *)a.Y)[row * C + c] = (T)y;
+    });
+}
+
+// A workgroup takes rows blockIdx.x, + gridDim.x, .. (times the rows that it has at once); a lane has the same channels of all of
+// them, adds up their dgamma and dbeta in registers, and the workgroup's sums go to `partial`: no atomics, one order.
+template <typename T, int V, int L, int NV>
+__global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_back_vec_kernel(const LnBackArgs a)
+{
+    using Piece = typename Row<T, V>::Piece;
+    using Floats = typename Row<T, V>::Floats;
+    constexpr int THREADS = L <= 256 ? 256 : L, NW = L > 64 ? L / 64 : 1, PER = THREADS / L;
+    __shared__ float part[NW][2];
+    const int C = a.C, at = (int)(threadIdx.x % L) * V, mine = threadIdx.x / L;
+    const float inv = 1.f / (float)C;
+    Floats g[NV], dg[NV], db[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = at + i * (L * V);
+        g[i] = Floats{} + 1.f;
+        dg[i] = db[i] = Floats{};
+        if (a.gamma && c < C) g[i] = *(const Floats *)(a.gamma + c);
+    }
+    for (int64_t first = (int64_t)blockIdx.x * PER; first < a.rows; first += (int64_t)gridDim.x * PER) {
+        const bool there = first + mine < a.rows;
+        const int64_t base = (there ? first + mine : a.rows - 1) * C;
+        Piece dyp[NV], dsp[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = at + i * (L * V);
+            dyp[i] = dsp[i] = Piece{};
+            if (c < C) {
+                dyp[i] = *(const Piece *)((const T *)a.dY + base + c);
+                if (a.dS) dsp[i] = *(const Piece *)((const T *)a.dS + base + c);
+            }
+        }
+        Floats s[NV];
+        row_load<T, V, L, NV>(a.X, a.R, base, at, C, s);
+        const RowStats t = row_stats(
+            C, a.eps,
+            [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (at + i * (L * V) < C)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) f(s[i][e]);
+            },
+            [&](float (&v)[2]) __attribute__((always_inline)) { row_sums<L, 2>(v, part); });
+        float v[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                s[i][e] = t.norm(s[i][e]);
+                if (at + i * (L * V) < C) {  // (behind the row's end dy is 0, but n may be infinite)
+                    const float de = (float)dyp[i][e] * g[i][e];
+                    v[0] += de;
+                    v[1] = fmaf(de, s[i][e], v[1]);
+                }
+            }
+        row_sums<L, 2>(v, part);
+        if (!there) continue;  // (rows of several wavefronts: PER is 1, and all of the workgroup are there)
+        const float m0 = v[0] * inv, m1 = v[1] * inv;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = at + i * (L * V);
+            if (c >= C) continue;
+            Piece p;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float dy = (float)dyp[i][e], n = s[i][e];
+                dg[i][e] = fmaf(dy, n, dg[i][e]);
+                db[i][e] += dy;
+                const float dx = t.slope(fmaf(dy, g[i][e], -m0) - n * m1);
+                p[e] = (T)(a.dS ? dx + (float)dsp[i][e] : dx);
+            }
+            *(Piece *)((T *)a.dX + base + c) = p;
+        }
+    }
+    if (!a.partial) return;
+    float *to = a.partial + (int64_t)blockIdx.x * 2 * C;
+    if constexpr (PER > 1) {
+        __shared__ Floats sums[256];
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                __syncthreads();
+                sums[threadIdx.x] = k ? db[i] : dg[i];
+                __syncthreads();
+                const int c = at + i * (L * V);
+                if (mine == 0 && c < C) {
+                    Floats v = sums[threadIdx.x];
+#pragma unroll
+                    for (int w = 1; w < PER; ++w) v += sums[threadIdx.x + w * L];
+                    *(Floats *)(to + (int64_t)k * C + c) = v;
+                }
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = at + i * (L * V);
+            if (c >= C) continue;
+            *(Floats *)(to + c) = dg[i];
+            *(Floats *)(to + (int64_t)C + c) = db[i];
+        }
+    }
+}
+
+// Longer rows: a workgroup a row for dX, which leaves the row's mean and deviation, and a thread a column of every 64 rows
+// for the sums.
+template <typename T>
+__global__ __launch_bounds__(256) void ln_back_row_kernel(const LnBackArgs a)
+{
+    __shared__ float part[4][2];
+    const int64_t row = blockIdx.x;
+    const int C = a.C;
+    const T *x = (const T *)a.X + row * C, *r = a.R ? (const T *)a.R + row * C : nullptr;
+    const T *dy = (const T *)a.dY + row * C, *ds = a.dS ? (const T *)a.dS + row * C : nullptr;
+    const RowStats t = long_row_stats(x, r, C, a.eps, part);
+    float v[2] = {0.f, 0.f};
+    long_row(x, r, C, [&](int c, float s) __attribute__((always_inline)) {
+        const float e = (float)dy[c] * (a.gamma ? a.gamma[c] : 1.f);
+        v[0] += e;
+        v[1] = fmaf(e, t.norm(s), v[1]);
+    });
+    row_sums<256, 2>(v, part);
+    const float inv = 1.f / (float)C, m0 = v[0] * inv, m1 = v[1] * inv;
+    if (threadIdx.x == 0 && a.stats) a.stats[row] = t;
+    long_row(x, r, C, [&](int c, float s) __attribute__((always_inline)) {
+        const float e = (float)dy[c] * (a.gamma ? a.gamma[c] : 1.f);
+        const float dx = t.slope(e - m0 - t.norm(s) * m1);
+        ((T *)a.dX)[row * C + c] = (T)(ds ? dx + (float)ds[c] : dx);
+    });
+}
+
+constexpr int kLongRows = 64;  // rows of a partial sum
+template <typename T>
+__global__ __launch_bounds__(256) void ln_back_col_kernel(const LnBackArgs a)
+{
+    const int C = a.C, c = (int)blockIdx.x * 256 + threadIdx.x;
+    if (c >= C) return;
+    const int64_t first = (int64_t)blockIdx.y * kLongRows, end = min(first + kLongRows, a.rows);
+    float dg = 0.f, db = 0.f;
+    for (int64_t row = first; row < end; ++row) {
+        const int64_t i = row * C + c;
+        const float s = (float)((const T *)a.X)[i] + (a.R ? (float)((const T *)a.R)[i] : -0.f), dy = (float)((const T *)a.dY)[i];
+        dg = fmaf(dy, a.stats[row].norm(s), dg);
+        db += dy;
+    }
+    a.partial[((int64_t)blockIdx.y * 2) * C + c] = dg;
+    a.partial[((int64_t)blockIdx.y * 2 + 1) * C + c] = db;
+}
+
+// The partial sums of `groups` workgroups added up: 16 columns a workgroup, 64 threads to each.
+__global__ __launch_bounds__(1024) void ln_join_kernel(const float *partial, int groups, int C, float *dgamma, float *dbeta)
+{
+    __shared__ float sums[64][17];
+    const int c = (int)blockIdx.x * 16 + (threadIdx.x & 15), g0 = threadIdx.x >> 4, which = blockIdx.y;
+    float *to = which ? dbeta : dgamma;
+    if (!to) return;
+    float v = 0.f;
+    if (c < C) {
+        const float *from = partial + (int64_t)which * C + c;
+#pragma unroll 4
+        for (int g = g0; g < groups; g += 64) v += from[(int64_t)g * 2 * C];
+    }
+    sums[g0][threadIdx.x & 15] = v;
+    __syncthreads();
+    for (int w = 32; w > 0; w >>= 1) {
+        if (g0 < w) sums[g0][threadIdx.x & 15] += sums[g0 + w][threadIdx.x & 15];
+        __syncthreads();
+    }
+    if (g0 == 0 && c < C) to[c] = sums[0][threadIdx.x & 15];
+}
+
+// The kernel of a shape: pieces of as many numbers as divide the row, up to 16 bytes, and the fewest lanes that hold the row in
+// four pieces each (1,024 lanes: in two); null: longer.  The backward pass holds a row four times, which leaves 1,024 lanes
+// too few registers.
+struct LnKernel {
+    const void *fn;
+    int lanes;
+};
+template <typename K, int L>
+const void *ln_of(int nv)
+{
+    if constexpr (L == 64)
+        if (nv == 1) return K::template of<L, 1>();
+    if (nv <= 2) return K::template of<L, 2>();
+    if constexpr (L < 1024) {
+        if (nv == 3) return K::template of<L, 3>();
+        if (nv == 4) return K::template of<L, 4>();
+    }
+    return nullptr;
+}
+template <typename K>
+LnKernel ln_pick_of(int C)
+{
+    const int pieces = (C + K::V - 1) / K::V;
+    if (pieces <= 8) return {K::template of<8, 1>(), 8};
+    if (pieces <= 16) return {K::template of<16, 1>(), 16};
+    if (pieces <= 32) return {K::template of<32, 1>(), 32};
+    if (pieces <= 256) return {ln_of<K, 64>((pieces + 63) / 64), 64};
+    if (pieces <= 1024) return {ln_of<K, 256>((pieces + 255) / 256), 256};
+    if (pieces <= 2048) return {ln_of<K, K::WIDE>((pieces + K::WIDE - 1) / K::WIDE), K::WIDE};
+    return {nullptr, 0};
+}
+template <typename T, int VV, bool E8>
+struct LnForward {
+    static constexpr int V = VV, WIDE = 1024;
+    template <int L, int NV>
+    static const void *of() { return (const void *)&ln_vec_kernel<T, V, L, NV, E8>; }
+};
+template <typename T, int VV>
+struct LnBackward {
+    static constexpr int V = VV, WIDE = 512;
+    template <int L, int NV>
+    static const void *of() { return (const void *)&ln_back_vec_kernel<T, V, L, NV>; }
+};
+template <typename T, bool E8>
+LnKernel ln_pick(int C)
+{
+    if (sizeof(T) == 2 && C % 8 == 0) return ln_pick_of<LnForward<T, 16 / (int)sizeof(T), E8>>(C);
+    return C % 4 == 0   ? ln_pick_of<LnForward<T, 4, E8>>(C)
+           : C % 2 == 0 ? ln_pick_of<LnForward<T, 2, E8>>(C)
+                        : ln_pick_of<LnForward<T, 1, E8>>(C);
+}
+template <typename T>
+LnKernel ln_back_pick(int C)
+{
+    if (sizeof(T) == 2 && C % 8 == 0) return ln_pick_of<LnBackward<T, 16 / (int)sizeof(T)>>(C);
+    return C % 4 == 0   ? ln_pick_of<LnBackward<T, 4>>(C)
+           : C % 2 == 0 ? ln_pick_of<LnBackward<T, 2>>(C)
+                        : ln_pick_of<LnBackward<T, 1>>(C);
+}
+
+int ln_validate(const dsattn_ln_desc *desc, const char *who)
+{
+    if (!desc) return fail(DSATTN_EINVAL, "%s: null descriptor", who);
+    const dsattn_ln_desc &d = *desc;
+    if (d.rows < 1 || d.rows > 0x7fffffffLL || d.channels < 1 || d.channels > (1 << 20))
+        return fail(DSATTN_EINVAL, "%s: rows outside [1, 2^31 - 1] or channels outside [1, 2^20]", who);
+    if (d.io_dtype != DSATTN_F32 && d.io_dtype != DSATTN_BF16)
+        return fail(DSATTN_EINVAL, "%s: unknown input dtype", who);
+    if (d.out_dtype != d.io_dtype && d.out_dtype != DSATTN_E4M3)
+        return fail(DSATTN_EINVAL, "%s: the output is of the input's dtype or in 8 bits", who);
+    if (!(d.eps >= 0.f) || std::isinf(d.eps)) return fail(DSATTN_EINVAL, "%s: eps must be finite and >= 0", who);
+    return DSATTN_OK;
+}
+
+// How a backward pass runs: workgroups of the sums, and whether its rows are long ones.
+struct LnBackLaunch {
+    const void *fn;
+    int threads, groups;
+    size_t bytes;
+};
+LnBackLaunch ln_back_launch(const dsattn_ln_desc &d)
+{
+    const LnKernel k = d.io_dtype == DSATTN_F32 ? ln_back_pick<float>(d.channels) : ln_back_pick<__bf16>(d.channels);
+    LnBackLaunch l{k.fn, 256, 0, 0};
+    if (k.fn) {
+        const int per = k.lanes <= 256 ? 256 / k.lanes : 1;
+        l.threads = k.lanes <= 256 ? 256 : k.lanes;
+        l.groups = (int)std::min<int64_t>((d.rows + per - 1) / per, k.lanes <= 256 ? 1024 : 512);
+    } else {
+        l.groups = (int)((d.rows + kLongRows - 1) / kLongRows);
+    }
+    l.bytes = (size_t)l.groups * 2 * (size_t)d.channels * sizeof(float);
+    if (!k.fn) l.bytes += (size_t)d.rows * sizeof(RowStats);
+    return l;
+}
+
+}  // namespace
+}  // namespace dsattn
+
+using namespace dsattn;
+
+extern "C" {
+
+int dsattn_layernorm(const dsattn_ln_desc *desc, const void *X, const void *residual, const float *gamma,
+                     const float *beta, void *sum, void *Y, float *scales, void *stream)
+{
+    const char *who = "dsattn_layernorm";
+    const int rc = ln_validate(desc, who);
+    if (rc != DSATTN_OK) return rc;
+    const dsattn_ln_desc &d = *desc;
+    const bool e8 = d.out_dtype == DSATTN_E4M3;
+    if (!X || !Y || (e8 && !scales)) return fail(DSATTN_EINVAL, "%s: null pointer", who);
+    if (!e8 && scales) return fail(DSATTN_EINVAL, "%s: scales without an output in 8 bits", who);
+    if (((uintptr_t)X | (uintptr_t)residual | (uintptr_t)gamma | (uintptr_t)beta | (uintptr_t)sum | (uintptr_t)Y) & 15u)
+        return fail(DSATTN_EINVAL, "%s: pointers must be 16-byte aligned", who);
+    if ((uintptr_t)scales & 3u) return fail(DSATTN_EINVAL, "%s: scales must be 4-byte aligned", who);
+    const int64_t n = d.rows * d.channels, in = n * (d.io_dtype == DSATTN_BF16 ? 2 : 4), cn = 4 * (int64_t)d.channels;
+    const int64_t out = e8 ? n : in;
+    const struct { const void *p; int64_t n; } inputs[] = {{X, in}, {residual, in}, {gamma, cn}, {beta, cn}},
+                                               outputs[] = {{sum, in}, {Y, out}, {scales, 4 * d.rows}};
+    for (int o = 0; o < 3; ++o) {
+        for (int i = 0; i < 4; ++i) {
+            const bool same = i < 2 && outputs[o].p == inputs[i].p && (o == 0 || (o == 1 && !e8));
+            if (!same && overlap(outputs[o].p, outputs[o].n, inputs[i].p, inputs[i].n))
+                return fail(DSATTN_EINVAL, "%s: an output overlaps an input", who);
+        }
+        for (int q = 0; q < o; ++q)
+            if (overlap(outputs[o].p, outputs[o].n, outputs[q].p, outputs[q].n))
+                return fail(DSATTN_EINVAL, "%s: two outputs overlap", who);
+    }
+    const LnArgs a{X, residual, gamma, beta, sum, Y, scales, d.rows, d.channels, d.eps};
+    const bool f32 = d.io_dtype == DSATTN_F32;
+    const LnKernel k = f32 ? (e8 ? ln_pick<float, true>(d.channels) : ln_pick<float, false>(d.channels))
+                           : (e8 ? ln_pick<__bf16, true>(d.channels) : ln_pick<__bf16, false>(d.channels));
+    const void *fn = k.fn;
+    unsigned groups = (unsigned)d.rows, threads = 256;
+    if (fn) {
+        const int per = k.lanes <= 256 ? 256 / k.lanes : 1;  // rows of a workgroup
+        groups = (unsigned)((d.rows + per - 1) / per);
+        threads = k.lanes <= 256 ? 256u : (unsigned)k.lanes;
+    } else {
+        fn = f32 ? (e8 ? (const void *)&ln_row_kernel<float, true> : (const void *)&ln_row_kernel<float, false>)
+                 : (e8 ? (const void *)&ln_row_kernel<__bf16, true> : (const void *)&ln_row_kernel<__bf16, false>);
+    }
+    // (a launch has less than 2^32 threads)
+    if ((uint64_t)groups * threads > 0xffffffffull)
+        return fail(DSATTN_EUNSUPPORTED, "%s: too many rows for one launch", who);
+    void *params[] = {(void *)&a};
+    const hipError_t e = hipLaunchKernel(fn, dim3(groups), dim3(threads), params, 0, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
+    return DSATTN_OK;
+}
+
+int dsattn_layernorm_backward_workspace(const dsattn_ln_desc *desc, size_t *bytes)
+{
+    const int rc = ln_validate(desc, "dsattn_layernorm_backward_workspace");
+    if (rc != DSATTN_OK) return rc;
+    if (!bytes) return fail(DSATTN_EINVAL, "dsattn_layernorm_backward_workspace: null output");
+    *bytes = ln_back_launch(*desc).bytes;
+    return DSATTN_OK;
+}
+
+int dsattn_layernorm_backward(const dsattn_ln_desc *desc, const void *X, const void *residual, const float *gamma,
+                              const void *dY, const void *dsum, void *dX, float *dgamma, float *dbeta, void *workspace,
+                              size_t workspace_bytes, void *stream)
+{
+    const char *who = "dsattn_layernorm_backward";
+    const int rc = ln_validate(desc, who);
+    if (rc != DSATTN_OK) return rc;
+    const dsattn_ln_desc &d = *desc;
+    if (d.out_dtype != d.io_dtype) return fail(DSATTN_EINVAL, "%s: gradients are of the input's dtype", who);
+    if (!X || !dY || !dX) return fail(DSATTN_EINVAL, "%s: null pointer", who);
+    if (((uintptr_t)X | (uintptr_t)residual | (uintptr_t)gamma | (uintptr_t)dY | (uintptr_t)dsum | (uintptr_t)dX | (uintptr_t)workspace) & 15u)
+        return fail(DSATTN_EINVAL, "%s: pointers must be 16-byte aligned", who);
+    if (((uintptr_t)dgamma | (uintptr_t)dbeta) & 3u) return fail(DSATTN_EINVAL, "%s: gradients of weights must be 4-byte aligned", who);
+    const LnBackLaunch l = ln_back_launch(d);
+    const bool sums = dgamma || dbeta;
+    if (sums && (!workspace || workspace_bytes < l.bytes)) return fail(DSATTN_EINVAL, "%s: workspace of %zu bytes needed", who, l.bytes);
+    const int64_t n = d.rows * d.channels * (d.io_dtype == DSATTN_BF16 ? 2 : 4), cn = 4 * (int64_t)d.channels;
+    const struct { const void *p; int64_t n; } inputs[] = {{X, n}, {residual, n}, {dY, n}, {dsum, n}, {gamma, cn}},
+                                               outputs[] = {{dX, n}, {dgamma, cn}, {dbeta, cn}, {sums ? workspace : nullptr, (int64_t)l.bytes}};
+    for (int o = 0; o < 4; ++o) {
+        for (int i = 0; i < 5; ++i) {
+            // (dX in the place of an input: not where rows are long and their columns are read again for the sums)
+            const bool same = o == 0 && i < 4 && outputs[o].p == inputs[i].p && (l.fn || !sums || i == 3);
+            if (!same && overlap(outputs[o].p, outputs[o].n, inputs[i].p, inputs[i].n))
+                return fail(DSATTN_EINVAL, "%s: an output overlaps an input", who);
+        }
+        for (int q = 0; q < o; ++q)
+            if (overlap(outputs[o].p, outputs[o].n, outputs[q].p, outputs[q].n))
+                return fail(DSATTN_EINVAL, "%s: two outputs overlap", who);
+    }
+    LnBackArgs a{X, residual, dY, dsum, gamma, dX, sums ? (float *)workspace : nullptr, nullptr, d.rows, d.channels, d.eps};
+    const bool f32 = d.io_dtype == DSATTN_F32;
+    const hipStream_t st = (hipStream_t)stream;
+    void *params[] = {&a};
+    hipError_t e;
+    if (l.fn) {
+        e = hipLaunchKernel(l.fn, dim3((unsigned)l.groups), dim3((unsigned)l.threads), params, 0, st);
+    } else {
+        if ((uint64_t)d.rows * 256 > 0xffffffffull || l.groups > 65535)
+            return fail(DSATTN_EUNSUPPORTED, "%s: too many rows of this length", who);
+        if (sums) a.stats = (RowStats *)((char *)workspace + (size_t)l.groups * 2 * (size_t)d.channels * sizeof(float));
+        const void *fn = f32 ? (const void *)&ln_back_row_kernel<float> : (const void *)&ln_back_row_kernel<__bf16>;
+        e = hipLaunchKernel(fn, dim3((unsigned)d.rows), dim3(256), params, 0, st);
+        fn = f32 ? (const void *)&ln_back_col_kernel<float> : (const void *)&ln_back_col_kernel<__bf16>;
+        if (e == hipSuccess && sums)
+            e = hipLaunchKernel(fn, dim3((unsigned)(d.channels + 255) / 256, (unsigned)l.groups), dim3(256), params, 0, st);
+    }
+    if (e == hipSuccess && sums) {
+        const float *partial = a.partial;
+        int groups = l.groups, C = d.channels;
+        void *args[] = {&partial, &groups, &C, &dgamma, &dbeta};
+        e = hipLaunchKernel((const void *)&ln_join_kernel, dim3((unsigned)(C + 15) / 16, 2), dim3(1024), args, 0, st);
+    }
+    if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
+    return DSATTN_OK;
+}
+
+}  // extern "C"

@@ -16,6 +16,7 @@
 
 #include "dsattn.h"
 #include "plan.h"
+#include "rows.h"
 
 namespace dsattn {
 namespace {
@@ -29,15 +30,6 @@ struct RmsArgs {
     int32_t C;
     float eps;
 };
-
-// y in 8 bits, to nearest, ties to even
-__device__ __forceinline__ uint8_t to_e4m3(float y)
-{
-    return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false) & 255);
-}
-
-// The maximum of two numbers, NaN if one is: what fmaxf() would drop.
-__device__ __forceinline__ float max_or_nan(float a, float b) { return a > b || a != a ? a : b; }
 
 // A power of two that brings a row's squares into fp32's range, 1 where they are there (a row of ordinary size, and every one
 // where eps is far above the squares that are lost).  Sums of squares below 2^-100 are of numbers below 2^-50 and times 2^100
@@ -257,12 +249,6 @@ __global__ __launch_bounds__(256) void rms_row_kernel(const RmsArgs a)
         else
             ((T *)a.Y)[row * C + c] = (T)y;
     }
-}
-
-bool overlap(const void *a, int64_t an, const void *b, int64_t bn)
-{
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return a && b && x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
 }
 
 }  // namespace

@@ -1,0 +1,337 @@
+"""dsattn_gated_scan and its backward pass: refusals on the host, the formulas against differences, and parity with them in 64 bits.
+
+Tolerances, u = 2^-24.  A gate, what it leaves and the weight are off by 8 u of themselves (the exponential's two, sum,
+quotient, product and root).  An exponential below 2^-126 counts as 0, so that a gate, what it leaves, a weight and their
+products are off by 2^-125 at most beside that, LOW times what each is multiplied with.  With M_t = a_t M_(t-1) + w |x_t|, the sizes of what the
+state is a sum of, a step adds 12 u M_t to the state's error, in whatever order chunks are joined; the same for D with
+N_t = |dy_t| + a_(t+1) N_(t+1).  The gradients are products of these with eight roundings more, and an output's own."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2406_16260_amd import binding as B
+
+DEV = "cuda:0"
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
+CODE = {"f32": B.DSATTN_F32, "bf16": B.DSATTN_BF16}
+MODES = {"sum": B.DSATTN_SCAN_SUM, "mean": B.DSATTN_SCAN_MEAN, "norm": B.DSATTN_SCAN_NORM}
+U, LOW, STEP = 2.0 ** -24, 2.0 ** -125, B.DSATTN_SCAN_FRAMES
+
+
+def gates(g, mode):
+    g = g.double()
+    a, i = torch.sigmoid(g), torch.sigmoid(-g)
+    if mode == "mean":
+        return a, i, i, -a * i
+    if mode == "norm":
+        return a, i, torch.sqrt(i * (1 + a)), -a * a * torch.sqrt(i / (1 + a))
+    return a, i, torch.ones_like(a), torch.zeros_like(a)
+
+
+def forward(x, g, h0, mode, count):
+    """States behind each of one stream's frames, [count + 1, ...] from the start on, and their tolerances."""
+    a, _, w, _ = gates(g, mode)
+    h, m, e = h0.double(), h0.double().abs(), torch.zeros_like(h0, dtype=torch.float64)
+    out = [(h, e, m)]
+    for t in range(count):
+        h = a[t] * h + w[t] * x[t].double()
+        e = e + LOW * (m + x[t].double().abs())
+        m = a[t] * m + w[t] * x[t].double().abs()
+        e = a[t] * e + 12 * U * m + LOW
+        out.append((h, e, m))
+    return [torch.stack([o[k] for o in out]) for k in range(3)]
+
+
+def backward(x, g, h0, mode, count, dy, dend):
+    """(dx, dg, dh0) of one stream with their tolerances in fp32."""
+    a, i, w, dw = gates(g, mode)
+    h, eh, m = forward(x, g, h0, mode, count)
+    c, n, e = dend.double(), dend.double().abs(), torch.zeros_like(dend, dtype=torch.float64)
+    res = {k: torch.zeros(x.shape, dtype=torch.float64) for k in ("dx", "edx", "dg", "edg")}
+    for t in reversed(range(count)):
+        d, n = c + dy[t].double(), n + dy[t].double().abs()
+        e = e + 12 * U * n + LOW
+        ai, xt = a[t] * i[t], x[t].double()
+        res["dx"][t], res["edx"][t] = d * w[t], e * w[t] + 8 * U * n * w[t] + LOW * (n + 1)
+        size = ai * m[t] + dw[t].abs() * xt.abs()
+        res["dg"][t] = d * (ai * h[t] + dw[t] * xt)
+        res["edg"][t] = e * size + n * (ai * eh[t] + 24 * U * size + LOW * (m[t] + xt.abs())) + LOW
+        c, n, e = a[t] * d, a[t] * n, a[t] * e + 12 * U * a[t] * n + LOW * n
+    return (res["dx"], res["edx"]), (res["dg"], res["edg"]), (c, e)
+
+
+def inputs(Bs, T, P, C, dtype, seed, spread=6.0):
+    gen = torch.Generator().manual_seed(seed)
+    t = TORCH[dtype]
+
+    def rand(*s):
+        return torch.randn(*s, generator=gen)
+
+    x, dy = rand(Bs, T, P, C).to(t), rand(Bs, T, P, C).to(t)
+    g = (spread * torch.rand(C, generator=gen) - 0.5 + 1.5 * rand(Bs, T, P, C)).to(t)
+    return x, g, rand(Bs, P, C), dy, rand(Bs, P, C)
+
+
+def near(got, want, tol, dtype, what):
+    half = torch.finfo(torch.bfloat16).eps / 2 if dtype == "bf16" else U
+    off, tol = (got.cpu().double() - want).abs(), tol * (1 + half) + half * want.abs()
+    assert (off <= tol).all(), f"{what}: {(off / tol).max().item()} of the tolerance"
+
+
+def space(Bs, T, P, C, dtype):
+    n = B.dsattn_gated_scan_workspace(Bs, T, P, C, io_dtype=CODE[dtype])
+    return torch.full((n,), 255, dtype=torch.uint8, device=DEV) if n else None  # (NaN, read before written)
+
+
+def run(Bs, T, P, C, dtype, mode, counts=None, start=True, seed=1, back=True, spread=6.0):
+    x, g, h0, dy, dend = inputs(Bs, T, P, C, dtype, seed + T + C, spread)
+    shape, n = (Bs, T, P, C), x.numel()
+    steps = -(-T // STEP)
+    print(f"[case] gated_scan {shape} {dtype} {mode} counts {counts} start {start}", flush=True)
+    if not start:
+        h0 = torch.zeros_like(h0)
+    dev = [t.to(DEV) for t in (x, g, h0, dy, dend)]
+    cnt = None if counts is None else torch.tensor(counts, dtype=torch.int32, device=DEV)
+    guard = torch.full((3, n + 64), 7.0, device=DEV).to(TORCH[dtype])
+    Y, dX, dG = (guard[k, :n].view(shape) for k in range(3)) if n % 8 == 0 else (torch.full(shape, 7.0, device=DEV).to(TORCH[dtype]) for _ in range(3))
+    hT, dh0 = (torch.full((Bs, P, C), float("nan"), device=DEV) for _ in range(2))
+    S = torch.full((Bs, steps, P, C), float("nan"), device=DEV)
+    B.dsattn_gated_scan(*shape, dev[0], dev[1], Y, mode=MODES[mode], start_state=dev[2] if start else None, end_state=hT, states=S,
+                        counts=cnt, workspace=space(*shape, dtype), io_dtype=CODE[dtype])
+    torch.cuda.synchronize()
+    lens = [T if counts is None else min(max(c, 0), T) for c in (counts or [T] * Bs)]
+    for b, c in enumerate(lens):
+        h, e, _ = forward(x[b], g[b], h0[b], mode, c)
+        near(Y[b, :c].float(), h[1:], e[1:], dtype, "Y")
+        near(hT[b], h[-1], e[-1], "f32", "end")
+        k = -(-c // STEP)
+        near(S[b, :k], h[:-1:STEP] if c else h[:0], e[:-1:STEP] if c else e[:0], "f32", "states")
+        assert (Y[b, c:] == 7.0).all() and S[b, k:].isnan().all(), "rows behind the end"
+    if not back:
+        return
+    B.dsattn_gated_scan_backward(*shape, dev[0], dev[1], S, dev[3], dX, dG, mode=MODES[mode], dend_state=dev[4], dstart_state=dh0,
+                                 counts=cnt, workspace=space(*shape, dtype), io_dtype=CODE[dtype])
+    torch.cuda.synchronize()
+    for b, c in enumerate(lens):
+        rx, rg, r0 = backward(x[b], g[b], h0[b], mode, c, dy[b], dend[b])
+        near(dX[b, :c].float(), rx[0][:c], rx[1][:c], dtype, "dX")
+        near(dG[b, :c].float(), rg[0][:c], rg[1][:c], dtype, "dG")
+        near(dh0[b], r0[0], r0[1], "f32", "dstart")
+        assert (dX[b, c:] == 7.0).all() and (dG[b, c:] == 7.0).all(), "rows behind the end"
+    assert (guard[:, n:] == 7.0).all(), "written past the end"
+
+
+SHAPES = [(1, 1, 1, 1), (1, 1, 5, 8), (2, 2, 3, 40), (1, 15, 1, 7), (1, 16, 4, 24), (3, 17, 1, 320), (1, 31, 9, 33), (2, 33, 7, 64),
+          (1, 48, 2, 130), (1, 100, 40, 80), (1, 250, 1, 1280), (2, 256, 1, 8), (1, 257, 3, 5), (1, 300, 1, 1), (5, 511, 1, 66),
+          (1, 1000, 1, 640), (1, 3000, 1, 24), (2, 2049, 1, 129)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Bs,T,P,C", SHAPES)
+def test_against_the_formula(Bs, T, P, C, dtype, mode):
+    run(Bs, T, P, C, dtype, mode)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,mode", [("f32", "norm"), ("bf16", "mean"), ("bf16", "sum")])
+@pytest.mark.parametrize("T,P,C,counts", [
+    (1, 3, 40, [1, 0, 1]), (40, 3, 40, [0, 1, 40, 16, 17, 39]), (300, 1, 64, [300, 0, 255, 64, 65, 1]), (1000, 1, 33, [999, 16, 1000, -5]),
+    (700, 1, 6, [10, 2000, 0, 321])])
+def test_streams_of_different_lengths(T, P, C, counts, dtype, mode):
+    run(len(counts), T, P, C, dtype, mode, counts)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,P,C", [(20, 3, 40), (600, 1, 40)])
+@pytest.mark.parametrize("mode", list(MODES))
+def test_without_states(T, P, C, mode):
+    run(2, T, P, C, "bf16", mode, start=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("T", [40, 600])
+def test_far_gates(T, mode):
+    """Logits of -120 to 120: gates of 0 and of 1."""
+    x, g, h0, dy, dend = inputs(1, T, 1, 64, "f32", 3)
+    g = torch.linspace(-120, 120, 64).expand(1, T, 1, 64).contiguous()
+    dev = [t.to(DEV) for t in (x, g, h0, dy, dend)]
+    Y, dX, dG = (torch.empty_like(dev[0]) for _ in range(3))
+    S, hT = torch.empty(1, -(-T // STEP), 1, 64, device=DEV), torch.empty_like(dev[2])
+    ws = space(1, T, 1, 64, "f32")
+    kw = dict(mode=MODES[mode], workspace=ws, io_dtype=B.DSATTN_F32)
+    B.dsattn_gated_scan(1, T, 1, 64, dev[0], dev[1], Y, start_state=dev[2], end_state=hT, states=S, **kw)
+    B.dsattn_gated_scan_backward(1, T, 1, 64, dev[0], dev[1], S, dev[3], dX, dG, dend_state=dev[4], **kw)
+    torch.cuda.synchronize()
+    h, e, _ = forward(x[0], g[0], h0[0], mode, T)
+    near(Y[0], h[1:], e[1:], "f32", "Y")
+    rx, rg, _ = backward(x[0], g[0], h0[0], mode, T, dy[0], dend[0])
+    near(dX[0], *rx, "f32", "dX")
+    near(dG[0], *rg, "f32", "dG")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Bs,T,P,C", [(1, 1, 160, 320), (2, 50, 9, 40), (1, 900, 1, 64)])
+def test_in_place_and_frame_by_frame(Bs, T, P, C, dtype):
+    """Y in the place of X and of G, the state in the place of the one before, gradients in the place of their inputs; and one
+    frame a call, which a chunk's last bits differ from."""
+    x, g, h0, dy, dend = inputs(Bs, T, P, C, dtype, 9)
+    t = [v.to(DEV) for v in (x, g, h0, dy, dend)]
+    shape, ws, code = (Bs, T, P, C), space(Bs, T, P, C, dtype), CODE[dtype]
+    Y, hT, S = torch.empty_like(t[0]), torch.empty_like(t[2]), torch.empty(Bs, -(-T // STEP), P, C, device=DEV)
+    B.dsattn_gated_scan(*shape, t[0], t[1], Y, start_state=t[2], end_state=hT, states=S, workspace=ws, io_dtype=code)
+    for into in (0, 1):
+        u = [v.clone() for v in t]
+        B.dsattn_gated_scan(*shape, u[0], u[1], u[into], start_state=u[2], end_state=u[2], workspace=ws, io_dtype=code)
+        assert torch.equal(u[into], Y) and torch.equal(u[2], hT)
+    dX, dG, dh = torch.empty_like(Y), torch.empty_like(Y), torch.empty_like(hT)
+    B.dsattn_gated_scan_backward(*shape, t[0], t[1], S, t[3], dX, dG, dend_state=t[4], dstart_state=dh, workspace=ws, io_dtype=code)
+    for a, b in ((0, 1), (1, 0), (3, 1), (0, 3)):
+        u = [v.clone() for v in t]
+        B.dsattn_gated_scan_backward(*shape, u[0], u[1], S, u[3], u[a], u[b], dend_state=u[4], dstart_state=u[4], workspace=ws,
+                                     io_dtype=code)
+        assert torch.equal(u[a], dX) and torch.equal(u[b], dG) and torch.equal(u[4], dh)
+    h = t[2].clone()
+    y = torch.empty(Bs, 1, P, C, device=DEV, dtype=TORCH[dtype])
+    for f in range(T):
+        B.dsattn_gated_scan(Bs, 1, P, C, t[0][:, f:f + 1].contiguous(), t[1][:, f:f + 1].contiguous(), y, start_state=h, end_state=h,
+                            io_dtype=code)
+    torch.cuda.synchronize()
+    for b in range(Bs):
+        want, e, _ = forward(x[b], g[b], h0[b], "mean", T)
+        near(h[b], want[-1], e[-1], "f32", "state")
+        near(y[b, 0].float(), want[-1], e[-1], dtype, "Y")
+
+
+@pytest.mark.gpu
+def test_infinities_and_nan_behind_the_end_and_in_other_channels():
+    """What is not there or not theirs does not reach a stream or a channel."""
+    for T in (40, 900):
+        x, g, h0, dy, dend = inputs(2, T, 1, 64, "bf16", 4)
+        x[0, 30:], g[0, 30:], dy[0, 30:] = float("nan"), float("inf"), float("nan")
+        x[1, 3, 0, 5], g[1, 7, 0, 9], dy[1, 9, 0, 11] = float("inf"), float("nan"), float("nan")
+        t = [v.to(DEV) for v in (x, g, h0, dy, dend)]
+        cnt = torch.tensor([30, T], dtype=torch.int32, device=DEV)
+        Y, dX, dG = (torch.full_like(t[0], 7.0) for _ in range(3))
+        S, ws = torch.empty(2, -(-T // STEP), 1, 64, device=DEV), space(2, T, 1, 64, "bf16")
+        B.dsattn_gated_scan(2, T, 1, 64, t[0], t[1], Y, start_state=t[2], states=S, counts=cnt, workspace=ws)
+        B.dsattn_gated_scan_backward(2, T, 1, 64, t[0], t[1], S, t[3], dX, dG, dend_state=t[4], counts=cnt, workspace=ws)
+        torch.cuda.synchronize()
+        h, e, _ = forward(x[0], g[0], h0[0], "mean", 30)
+        near(Y[0, :30].float(), h[1:], e[1:], "bf16", "Y")
+        rx, rg, _ = backward(x[0], g[0], h0[0], "mean", 30, dy[0], dend[0])
+        near(dX[0, :30].float(), rx[0][:30], rx[1][:30], "bf16", "dX")
+        near(dG[0, :30].float(), rg[0][:30], rg[1][:30], "bf16", "dG")
+        bad = Y[1].isfinite().logical_not().any(0).any(0)
+        assert bad.nonzero().flatten().tolist() == [5, 9]
+        assert not Y[1, 3:, 0, 5].isfinite().any() and Y[1, 7:, 0, 9].isnan().all()
+        assert dX[1, :10, 0, 11].isnan().all() and dX[1, 10:, 0, 11].isfinite().all()
+        assert set(dX[1].isfinite().logical_not().any(0).any(0).nonzero().flatten().tolist()) <= {5, 9, 11}
+
+
+@pytest.mark.gpu
+def test_the_same_call_gives_the_same_bits_and_streams_stand_alone():
+    shape = (3, 1100, 1, 136)
+    x, g, h0, _, _ = inputs(*shape, "bf16", 8)
+    t = [v.to(DEV) for v in (x, g, h0)]
+    ys = []
+    for _ in range(3):
+        y = torch.empty_like(t[0])
+        B.dsattn_gated_scan(*shape, t[0], t[1], y, start_state=t[2], workspace=space(*shape, "bf16"))
+        ys.append(y)
+    assert all(torch.equal(y, ys[0]) for y in ys)
+
+
+def test_the_formula_against_differences():
+    """In 64 bits: central differences of y . dy + end . dend, whose error is h^2 times third derivatives (h = 1e-4: 1e-7)."""
+    gen = torch.Generator().manual_seed(2)
+    T, C, h = 5, 3, 1e-4
+    x, g, dy = (torch.randn(T, C, generator=gen, dtype=torch.float64) for _ in range(3))
+    h0, dend = (torch.randn(C, generator=gen, dtype=torch.float64) for _ in range(2))
+    for mode in MODES:
+        def loss(x, g, h0):
+            s = forward(x, g, h0, mode, T)[0]
+            return (s[1:] * dy).sum() + (s[-1] * dend).sum()
+
+        def differences(t, f):
+            out = torch.zeros_like(t)
+            for i in range(t.numel()):
+                e = torch.zeros_like(t).view(-1)
+                e[i] = h
+                out.view(-1)[i] = (f(t + e.view_as(t)) - f(t - e.view_as(t))) / (2 * h)
+            return out
+
+        rx, rg, r0 = backward(x, g, h0, mode, T, dy, dend)
+        assert (differences(x, lambda t: loss(t, g, h0)) - rx[0]).abs().max() < 1e-6
+        assert (differences(g, lambda t: loss(x, t, h0)) - rg[0]).abs().max() < 1e-6
+        assert (differences(h0, lambda t: loss(x, g, t)) - r0[0]).abs().max() < 1e-6
+
+
+def _desc(**kw):
+    d = dict(streams=2, frames=40, spatial=3, channels=8, mode=1, io_dtype=B.DSATTN_BF16)
+    d.update(kw)
+    return B.DsattnScanDesc(**d)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(streams=0), dict(frames=0), dict(spatial=0), dict(channels=-1), dict(mode=-1), dict(mode=3), dict(io_dtype=2),
+    dict(io_dtype=-1), dict(frames=0x7fffffff), dict(streams=1 << 20, frames=1 << 20, spatial=1 << 10),
+    dict(spatial=0x7fffffff, channels=0x7fffffff)])
+def test_bad_descriptors_are_refused(kw):
+    lib, d, n = B.load(), _desc(**kw), ctypes.c_size_t()
+    p = [0x100000 * (k + 1) for k in range(9)]
+    assert lib.dsattn_gated_scan(ctypes.byref(d), None, p[0], p[1], None, p[2], None, None, None, 0, None) == B.DSATTN_EINVAL
+    assert lib.dsattn_gated_scan_backward(ctypes.byref(d), None, p[0], p[1], p[2], p[3], None, p[4], p[5], None, None, 0,
+                                          None) == B.DSATTN_EINVAL
+    assert lib.dsattn_gated_scan_workspace(ctypes.byref(d), ctypes.byref(n)) == B.DSATTN_EINVAL
+    assert B.dsattn_last_error()
+
+
+def test_bad_pointers_are_refused():
+    lib, d = B.load(), ctypes.byref(_desc())
+    long = _desc(frames=4000, spatial=1)
+    need = B.dsattn_gated_scan_workspace(2, 4000, 1, 8)
+    assert need > 0 and B.dsattn_gated_scan_workspace(2, 40, 3, 8) == 0
+    p = [0x100000 * (k + 1) for k in range(9)]
+    f = lib.dsattn_gated_scan
+    for args in [(None, None, p[0], p[1], None, p[2], None, None, None, 0), (d, None, None, p[1], None, p[2], None, None, None, 0),
+                 (d, None, p[0], None, None, p[2], None, None, None, 0), (d, None, p[0], p[1], None, None, None, None, None, 0),
+                 (d, p[5] + 2, p[0], p[1], None, p[2], None, None, None, 0), (d, None, p[0] + 8, p[1], None, p[2], None, None, None, 0),
+                 (d, None, p[0], p[1], p[3] + 4, p[2], None, None, None, 0), (d, None, p[0], p[1], None, p[0] + 16, None, None, None, 0),
+                 (d, None, p[0], p[1], p[3], p[2], p[3] + 16, None, None, 0), (d, None, p[0], p[1], p[3], p[2], None, p[3], None, 0),
+                 (d, None, p[0], p[1], None, p[2], p[2], None, None, 0), (d, p[2], p[0], p[1], None, p[2], None, None, None, 0),
+                 (ctypes.byref(long), None, p[0], p[1], None, p[2], None, None, None, 0),
+                 (ctypes.byref(long), None, p[0], p[1], None, p[2], None, None, p[5], need - 1),
+                 (ctypes.byref(long), None, p[0], p[1], None, p[2], None, None, p[5] + 8, need),
+                 (ctypes.byref(long), None, p[0], p[1], None, p[2], None, None, p[1], need)]:
+        assert f(*args, None) == B.DSATTN_EINVAL, args
+    f = lib.dsattn_gated_scan_backward
+    for args in [(None, None, p[0], p[1], p[2], p[3], None, p[4], p[5], None, None, 0),
+                 (d, None, p[0], p[1], None, p[3], None, p[4], p[5], None, None, 0), (d, None, p[0], p[1], p[2], None, None, p[4], p[5], None, None, 0),
+                 (d, None, p[0], p[1], p[2], p[3], None, None, p[5], None, None, 0), (d, None, p[0], p[1], p[2], p[3], None, p[4], None, None, None, 0),
+                 (d, None, p[0], p[1], p[2], p[3], None, p[4], p[4], None, None, 0), (d, None, p[0], p[1], p[2], p[3], None, p[2], p[5], None, None, 0),
+                 (d, None, p[0], p[1], p[2], p[3], p[6], p[4], p[5], p[6] + 16, None, 0),
+                 (d, None, p[0], p[1], p[2] + 4, p[3], None, p[4], p[5], None, None, 0),
+                 (ctypes.byref(long), None, p[0], p[1], p[2], p[3], None, p[4], p[5], None, None, 0)]:
+        assert f(*args, None) == B.DSATTN_EINVAL, args
+
+
+@pytest.mark.gpu
+def test_tensors_that_do_not_fit_are_refused():
+    x = torch.zeros(2, 40, 3, 8, device=DEV, dtype=torch.bfloat16)
+    s = torch.zeros(2, 3, 3, 8, device=DEV)
+    for bad in (x[:1], x.float(), x.cpu(), torch.zeros(2, 40, 3, 16, device=DEV, dtype=torch.bfloat16)[..., ::2]):
+        with pytest.raises(ValueError):
+            B.dsattn_gated_scan(2, 40, 3, 8, x, bad, x.clone())
+        with pytest.raises(ValueError):
+            B.dsattn_gated_scan_backward(2, 40, 3, 8, x, x.clone(), s, bad, x.clone(), x.clone())
+    with pytest.raises(ValueError):
+        B.dsattn_gated_scan(2, 40, 3, 8, x, x.clone(), x.clone(), states=s[:, :2])
+    with pytest.raises(ValueError):
+        B.dsattn_gated_scan(2, 40, 3, 8, x, x.clone(), x.clone(), counts=torch.zeros(2, device=DEV, dtype=torch.int64))
+    with pytest.raises(ValueError):
+        B.dsattn_gated_scan_backward(2, 40, 3, 8, x, x.clone(), s.bfloat16(), x.clone(), x.clone(), x.clone())
