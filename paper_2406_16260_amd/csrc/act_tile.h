@@ -3,8 +3,32 @@
 // from memory into LDS, 16-byte chunks swizzled by their row.
 #pragma once
 
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "dsattn.h"
+
 namespace dsattn {
 namespace {
+
+struct ActArgs {
+    const void *X;
+    const void *W[2];
+    const float *bias[2];      // [c_out] or null
+    const float *xs, *ws[2];   // scales of rows and channels, or null
+    const void *R;             // [M][c_out] or null
+    void *Y;
+    int64_t M;
+    int32_t Cin, Cout, n_w, act;
+    int32_t tiles_n, tiles, per_xcd;  // column tiles; all of them; ceil(tiles / 8)
+    int32_t panel;                    // persistent kernels: column tiles that are numbered together
+    float *sums;                      // gradients: [parts of rows][n_w Cout], column sums; R is dy and Y is dz then
+};
+
+struct e4m3 { uint8_t bits; };
+struct e4m3w { uint8_t bits; };  // the same, to be multiplied in 16 bits
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -107,7 +131,7 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // log2(P / (1 - P)) / x so that the largest error of P, anywhere, is least: 2.9e-8 with seven terms.  Two instructions on the
 // transcendental unit and ten others; with the rational approximation 7.1.26 of Abramowitz and Stegun (1.5e-7) it is two
 // and fifteen, and erff() several times that, which an epilogue at the matrix cores' heels feels.
-__device__ __forceinline__ float gelu_erf(float x)
+__device__ __forceinline__ float gelu_part(float x)
 {
     const float t = x * x;
     float p = fmaf(t, -5.067244690e-09f, 3.816315040e-07f);
@@ -116,8 +140,9 @@ __device__ __forceinline__ float gelu_erf(float x)
     p = fmaf(p, t, 9.404923028e-05f);
     p = fmaf(p, t, -1.048351218e-01f);
     p = fmaf(p, t, -2.302209292e+00f);
-    return x * __builtin_amdgcn_rcpf(1.f + exp2_fast(x * p));
+    return __builtin_amdgcn_rcpf(1.f + exp2_fast(x * p));
 }
+__device__ __forceinline__ float gelu_erf(float x) { return x * gelu_part(x); }
 
 template <int ACT>
 __device__ __forceinline__ float act_fast(float x)
@@ -272,13 +297,166 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *p, int64
                                              (int)min(left, (int64_t)0x7fffffff), 0x00020000);
 }
 
+// Gradients of the activation's argument and of its gate: dz_0 = dy [* z_1] act'(z_0), dz_1 = dy act(z_0).  A wavefront's part as
+// in epilogue(); 16 rows x 32 channels at a time through the wavefront's own kGradBytes, into which dy comes (two passes
+// ahead) and from which dz leaves, as rows of n_w Cout numbers.  The columns' sums over the part's rows, in fp32 of unrounded dz, go
+// to row `part` of a.sums.
+// Both derivatives take x within +-100: beyond, its factor is 0, and 0 * infinity would be NaN.
+template <int ACT>
+__device__ __forceinline__ void act_slope_fast(float x, float &y, float &d)
+{
+    const float c = __builtin_amdgcn_fmed3f(x, -100.f, 100.f);
+    if constexpr (ACT == DSATTN_ACT_RELU) {
+        y = x > 0.f || x != x ? x : 0.f;
+        d = x > 0.f ? 1.f : x != x ? x : 0.f;
+    } else if constexpr (ACT == DSATTN_ACT_GELU) {
+        const float p = gelu_part(x);
+        y = x * p;
+        d = fmaf(c * 0.39894228f, exp2_fast(c * c * -0.72134752f), p);
+    } else if constexpr (ACT == DSATTN_ACT_GELU_TANH) {
+        const float c2 = c * c, p = __builtin_amdgcn_rcpf(1.f + exp2_fast(x * fmaf(x * x, -0.10294324f, -2.3022082f)));
+        y = x * p;
+        d = fmaf(c * p * (1.f - p), fmaf(0.21406550f, c2, 1.5957691f), p);
+    } else if constexpr (ACT == DSATTN_ACT_SILU) {
+        const float p = __builtin_amdgcn_rcpf(1.f + exp2_fast(x * -1.44269504f));
+        y = x * p;
+        d = fmaf(c * p, 1.f - p, p);
+    } else {
+        y = x;
+        d = 1.f;
+    }
+}
+
+template <typename TO, bool GATED>
+constexpr int kGradBytes = (GATED ? 2 : 1) * 16 * (32 * (int)sizeof(TO) + (sizeof(TO) == 2 ? 8 : 16));
+template <typename T, int MB, int NB, bool GATED, typename TO, int ACT>
+__device__ __forceinline__ void epilogue_grad(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], int64_t m0, int c0,
+                                              const float *bias, unsigned char *stage, int lane)
+{
+    constexpr int BS = 16, NO = GATED ? 2 : 1, ES = (int)sizeof(TO), NP = 2 * NO, CP = NB / NP;  // passes of a row block
+    static_assert(Mul<T>::BS == BS && NB % NP == 0, "blocks of 16, whole passes");
+    constexpr int SB = 32 * ES + (ES == 2 ? 8 : 16), PER = 16 / ES, CPR = 32 / PER, IT = 16 * CPR / 64;
+    constexpr int PASSES = MB * CP, AHEAD = 2;
+    typedef TO Piece __attribute__((ext_vector_type(PER)));
+    typedef TO Quad __attribute__((ext_vector_type(4)));
+    typedef uint32_t Half __attribute__((ext_vector_type(2)));
+    const int rl = lane % BS, cq = 4 * (lane / BS), ch = lane % CPR * PER;
+    const int left_rows = (int)min(a.M - m0, (int64_t)(BS * MB)), left = a.Cout - c0;
+    if (left_rows <= 0) return;
+    const bool whole = a.Cout % PER == 0;
+    auto row_of = [&](int it) __attribute__((always_inline)) { return (lane + 64 * it) / CPR; };
+    auto there = [&](int pass, int it) __attribute__((always_inline)) {
+        return pass / CP * BS + row_of(it) < left_rows && pass % CP * 32 + ch < left;
+    };
+    const TO *dy = (const TO *)a.R + m0 * a.Cout + c0;
+    TO *dz = (TO *)a.Y + m0 * NO * a.Cout + c0;
+    Piece r[AHEAD][IT];
+    auto fetch = [&](int pass) __attribute__((always_inline)) {
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            Piece x{};
+            if (there(pass, it)) {
+                const TO *from = dy + (int64_t)(pass / CP * BS + row_of(it)) * a.Cout + pass % CP * 32 + ch;
+                if (whole) {
+                    x = *(const Piece *)from;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        if (pass % CP * 32 + ch + e < left) x[e] = from[e];
+                }
+            }
+            r[pass % AHEAD][it] = x;
+        }
+    };
+    // (8-byte accesses: a staged row of bf16 is 72 bytes)
+    auto put_piece = [&](unsigned char *at, const Piece &x) __attribute__((always_inline)) {
+        const i32x4 w = __builtin_bit_cast(i32x4, x);
+        *(Half *)at = Half{(uint32_t)w[0], (uint32_t)w[1]};
+        *(Half *)(at + 8) = Half{(uint32_t)w[2], (uint32_t)w[3]};
+    };
+    auto get_piece = [&](const unsigned char *at) __attribute__((always_inline)) {
+        const Half lo = *(const Half *)at, hi = *(const Half *)(at + 8);
+        return __builtin_bit_cast(Piece, (i32x4){(int)lo[0], (int)lo[1], (int)hi[0], (int)hi[1]});
+    };
+#pragma unroll
+    for (int p = 0; p < AHEAD && p < PASSES; ++p) fetch(p);
+    f32x4 sum[CP][NP] = {};
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+        const int i = pass / CP, jp = pass % CP * NP;
+#pragma unroll
+        for (int it = 0; it < IT; ++it) put_piece(stage + row_of(it) * SB + ch * ES, r[pass % AHEAD][it]);
+        wave_sync();
+        if (pass + AHEAD < PASSES) fetch(pass + AHEAD);
+        const bool live = BS * i + rl < left_rows;  // (rows past the end: a bias that is infinite would be NaN in the sums)
+#pragma unroll
+        for (int j = 0; j < NP; j += NO) {
+            unsigned char *at = stage + rl * SB + (BS * j / NO + cq) * ES;
+            Quad t0 = *(const Quad *)at, t1{};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float g = live ? (float)t0[e] : 0.f;
+                const float z0 = acc[i][jp + j][e] + bias[BS * (jp + j) + cq + e];
+                float y, d, dz0;
+                act_slope_fast<ACT>(z0, y, d);
+                if constexpr (GATED) {
+                    const float z1 = acc[i][jp + j + 1][e] + bias[BS * (jp + j + 1) + cq + e];
+                    dz0 = g * (z1 * d);
+                    const float dz1 = g * y;
+                    t1[e] = (TO)dz1;
+                    sum[pass % CP][j + 1][e] += live ? dz1 : 0.f;
+                } else {
+                    dz0 = g * d;
+                }
+                t0[e] = (TO)dz0;
+                sum[pass % CP][j][e] += live ? dz0 : 0.f;
+            }
+            *(Quad *)at = t0;
+            if constexpr (GATED) *(Quad *)(at + 16 * SB) = t1;
+        }
+        wave_sync();
+#pragma unroll
+        for (int k = 0; k < NO; ++k)
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                const Piece x = get_piece(stage + k * (16 * SB) + row_of(it) * SB + ch * ES);
+                if (there(pass, it)) {
+                    const int c = pass % CP * 32 + ch;
+                    TO *to = dz + ((int64_t)(BS * i + row_of(it)) * NO + k) * a.Cout + c;
+                    if (whole) {
+                        *(Piece *)to = x;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < PER; ++e)
+                            if (c + e < left) to[e] = x[e];
+                    }
+                }
+            }
+        wave_sync();
+    }
+    if (!a.sums) return;
+    float *to = a.sums + (m0 / (BS * MB)) * NO * a.Cout + c0;
+#pragma unroll
+    for (int p = 0; p < CP; ++p)
+#pragma unroll
+        for (int j = 0; j < NP; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float v = sum[p][j][e];
+#pragma unroll
+                for (int w = 1; w < 16; w *= 2) v += __shfl_xor(v, w);
+                const int c = 32 * p + BS * (j / NO) + cq + e;
+                if (rl == 0 && c < left) to[(j % NO) * a.Cout + c] = v;
+            }
+}
+
 // Small products: 32 rows of X by 32 rows of W a workgroup, whose eight wavefronts share the contraction: a wavefront takes
 // every eighth stage through two LDS slots of its own, waits for nobody, and the eight sums are added up in LDS at the
 // end, in an order that does not change.  What such a call takes is latency, an eighth of a row's length of it.  (Fetched in
 // the operands' layout, straight into registers, 16 neighbouring lanes are on 16 rows, and the first-level cache serves
 // them one by one: 160 x 1,280 x 1,280 7.6 us, 1 x 5,120 x 1,280 13 us.)
 constexpr int kSmallLds = 8 * 2 * 64 * kRow;
-template <typename T, bool GATED, typename TO>
+template <typename T, bool GATED, typename TO, bool GRAD = false>
 __global__ __launch_bounds__(512, 2) void act_small_kernel(const ActArgs a)
 {
     using M = Mul<T>;
@@ -359,6 +537,48 @@ __global__ __launch_bounds__(512, 2) void act_small_kernel(const ActArgs a)
     __syncthreads();
     const int row = (int)threadIdx.x >> 4, c = (int)threadIdx.x & 15;
     const int64_t m = m0 + row;
+    if constexpr (GRAD) {
+        constexpr int NO = GATED ? 2 : 1;
+        float dz[32 / 16];  // of column c + 16 o; gated, of channel c: dz_0 and dz_1
+        const bool live = m < a.M;
+#pragma unroll
+        for (int o = 0; o < BO / 16; ++o) {
+            const int ch = n0 + c + 16 * o;
+            float z[NO];
+#pragma unroll
+            for (int k = 0; k < NO; ++k) {
+                z[k] = 0.f;
+#pragma unroll
+                for (int v = 0; v < NW; ++v) z[k] += sums[v][row][c + 16 * (GATED ? k : o)];
+                if (a.bias[k] && ch < a.Cout) z[k] += a.bias[k][ch];
+            }
+            const float g = live && ch < a.Cout ? (float)((const TO *)a.R)[m * a.Cout + ch] : 0.f;
+            float y = 0.f, d = 0.f;
+            with_act(a.act, [&](auto act) __attribute__((always_inline)) { act_slope_fast<decltype(act)::value>(z[0], y, d); });
+            if constexpr (GATED) {
+                dz[0] = g * (z[1] * d);
+                dz[1] = g * y;
+            } else {
+                dz[o] = g * d;
+            }
+#pragma unroll
+            for (int k = 0; k < NO; ++k)
+                if (live && ch < a.Cout) ((TO *)a.Y)[(m * NO + k) * a.Cout + ch] = (TO)dz[GATED ? k : o];
+        }
+        if (!a.sums) return;
+        __syncthreads();
+#pragma unroll
+        for (int o = 0; o < 2; ++o) sums[0][row][c + 16 * o] = live ? dz[o] : 0.f;
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            float v = 0.f;
+#pragma unroll
+            for (int q = 0; q < 32; ++q) v += sums[0][q][threadIdx.x];
+            const int o = (int)threadIdx.x >> 4, ch = n0 + c + (GATED ? 0 : 16 * o);
+            if (ch < a.Cout) a.sums[((int64_t)mt * NO + (GATED ? o : 0)) * a.Cout + ch] = v;
+        }
+        return;
+    }
     if (m >= a.M) return;
     const float xs = SCALED && a.xs ? a.xs[m] : 1.f;
 #pragma unroll
@@ -384,7 +604,7 @@ __global__ __launch_bounds__(512, 2) void act_small_kernel(const ActArgs a)
 
 // One tile a workgroup: two LDS slots, two to four workgroups on a compute unit, whose loads and barriers hide behind each
 // other's multiplies.  A workgroup of WVM x WVN wavefronts computes a (BS MB WVM) x (BS NB WVN) tile.
-template <typename T, int MB, int NB, int WVM, int WVN, bool GATED, typename TO>
+template <typename T, int MB, int NB, int WVM, int WVN, bool GATED, typename TO, bool GRAD = false>
 __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const ActArgs a)
 {
     using M = Mul<T>;
@@ -487,13 +707,22 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const ActAr
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     constexpr int CHP = BS * NB / (GATED ? 2 : 1);  // output channels of the part
+    if constexpr (GRAD) {
+        static_assert(NW * kGradBytes<TO, GATED> <= 2 * BUF, "the staging area fits in the ring");
+        with_act(a.act, [&](auto act) __attribute__((always_inline)) {
+            epilogue_grad<T, MB, NB, GATED, TO, decltype(act)::value>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, &cols[0][wn * BS * NB],
+                                                                      smem + wv * kGradBytes<TO, GATED>, lane);
+        });
+        return;
+    }
     // all of the part at once, or a block of rows, or half of its channels
     constexpr int per = NW * BS * (CHP + 4) * 4;
     constexpr int MP = MB * per <= 2 * BUF ? MB : 1, NP = MP * per <= 2 * BUF ? NB : NB / 2;
     constexpr int SR = CHP * NP / NB + 4;
     static_assert(NW * BS * MP * SR * 4 <= 2 * BUF, "the staging area fits in the ring");
-    epilogue<T, MB, NB, MP, NP, GATED, TO, SCALED>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, &cols[0][wn * BS * NB],
-                                                   &cols[1][wn * BS * NB], (float *)smem + wv * (BS * MP * SR), lane);
+    if constexpr (!GRAD)
+        epilogue<T, MB, NB, MP, NP, GATED, TO, SCALED>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, &cols[0][wn * BS * NB],
+                                                       &cols[1][wn * BS * NB], (float *)smem + wv * (BS * MP * SR), lane);
 }
 
 // The same for the persistent kernels, in an area of its own beside the ring (the ring goes on loading meanwhile): 32 rows x 32
@@ -642,7 +871,7 @@ __device__ __forceinline__ void epilogue_beside(const ActArgs &a, const typename
 // next tile's first one is on its way into the other slot.  A wavefront's part is MB x NB blocks; its multiplies run in
 // halves (X blocks [0, HB), then [HB, MB)) so that one set of fragments, refilled in place under the multiplies, is
 // enough beside the accumulators: LDS reads and the next stage's loads sit between the matrix instructions by hand.
-template <typename T, int MB, int NB, bool GATED, typename TO, int ACT>
+template <typename T, int MB, int NB, bool GATED, typename TO, int ACT, bool GRAD = false>
 __global__ __launch_bounds__(512, 2) void act_stream_kernel(const ActArgs a)
 {
     using M = Mul<T>;
@@ -877,7 +1106,9 @@ __global__ __launch_bounds__(512, 2) void act_stream_kernel(const ActArgs a)
             if constexpr (SCALED) cols[COLS + le + 64 * u] = csc[u];
         }
         wave_sync();
-        if (a.R)
+        if constexpr (GRAD)
+            epilogue_grad<T, MB, NB, GATED, TO, ACT>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, cols, own, le);
+        else if (a.R)
             epilogue_beside<T, MB, NB, GATED, TO, SCALED, ACT, true>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, cols, cols + COLS,
                                                                      xs, own, le);
         else

@@ -1,0 +1,279 @@
+// The weights' gradient on the matrix cores: dW = dz^T X, a contraction over the rows of both operands, which lie row by row
+// in memory.  A stage is KS rows (64 bf16, 32 fp32) of a tile's columns, straight from memory into LDS; a lane's fragment,
+// consecutive rows of one column, comes out of it transposed: in 16 bits by ds_read_b64_tr_b16, which hands the 4 x 16
+// numbers that 16 lanes read to them column by column; in 32 bits number by number.  16-byte chunks are swizzled by
+// their row so that the rows of a read lie in different banks.
+#pragma once
+
+#include "act_tile.h"
+
+namespace dsattn {
+namespace {
+
+struct GradWArgs {
+    const void *dz, *X;  // [M][No], [M][Cin]
+    void *dW[2];         // [Cout][Cin] each, or null
+    float *partial;      // [splits][No][Cin] where there are several
+    int64_t M;
+    int32_t Cin, Cout, No;               // No: n_w Cout
+    int32_t tiles_n, tiles, items, per_xcd;  // column tiles (of X); all; tiles * splits; ceil(items / 8)
+    int32_t stages;                      // of a split
+};
+
+// Columns of an operand, W of them a tile.
+template <typename T, int W>
+struct Cols {
+    static constexpr int ES = (int)sizeof(T), KS = kRow / ES, RB = W * ES, CPR = RB / 16, PER = 16 / ES;
+    static constexpr int RPI = 64 / CPR;  // rows of a load instruction
+    static_assert(CPR * RPI == 64 && (ES == 2 ? CPR >= 8 : CPR >= 16), "whole rows");
+    using Frag = typename Mul<T>::Frag;
+    // where chunk c of row k lies: position c ^ swizzle(k)
+    static __device__ __forceinline__ int swizzle(int k)
+    {
+        if constexpr (ES == 4) return 4 * ((k >> 2) & 3);
+        return 2 * (CPR >= 16 ? (k & 3) | ((k >> 1) & 4) : k & 3);
+    }
+    // a lane's place within row 0 of a fragment of columns 16 blk .., and the row (of the first read)
+    static __device__ __forceinline__ int row(int lane) { return ES == 4 ? 4 * (lane >> 4) : 8 * (lane >> 4) + ((lane & 15) >> 2); }
+    static __device__ __forceinline__ int place(int lane, int blk)
+    {
+        const int l = lane & 15;
+        if constexpr (ES == 4) return ((4 * blk + (l >> 2)) ^ swizzle(row(lane))) * 16 + (l & 3) * 4;
+        return ((2 * blk + ((l & 3) >> 1)) ^ swizzle(row(lane))) * 16 + (l & 1) * 8;
+    }
+    static __device__ __forceinline__ Frag read(const unsigned char *at)
+    {
+        if constexpr (ES == 4) {
+            Frag f;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) f[s] = *(const float *)(at + s * RB);
+            return f;
+        } else {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 4 * RB));
+            return __builtin_bit_cast(Frag, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+// Rows k.. of columns c0.. of a matrix of `rows` x `cols`: what lies past its last row reads as zeros.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t cols_from(const void *p, int64_t k, int64_t rows, int rowbytes, int c0bytes)
+{
+    const int64_t left = max((int64_t)0, (rows - k) * rowbytes - c0bytes);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)((const unsigned char *)p + k * rowbytes + c0bytes), 0,
+                                             (int)min(left, (int64_t)0x7fffffff), 0x00020000);
+}
+
+// What a lane's accumulator holds goes out: four neighbouring channels of a row.
+template <typename T>
+__device__ __forceinline__ void grad_w_store(const GradWArgs &a, int split, bool parts, int o, int c, const f32x4 &v)
+{
+    if (o >= a.No || c >= a.Cin) return;
+    if (parts) {
+        *(f32x4 *)(a.partial + ((int64_t)split * a.No + o) * a.Cin + c) = v;
+        return;
+    }
+    T *to = (T *)(o < a.Cout ? a.dW[0] : a.dW[1]);
+    if (!to) return;
+    typedef T Quad __attribute__((ext_vector_type(4)));
+    Quad q;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q[e] = (T)v[e];
+    *(Quad *)(to + (int64_t)(o < a.Cout ? o : o - a.Cout) * a.Cin + c) = q;
+}
+
+// One tile of one split a workgroup, two LDS slots, two workgroups on a compute unit.
+template <typename T, int MB, int NB, int WVM, int WVN>
+__global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const GradWArgs a)
+{
+    using M = Mul<T>;
+    constexpr int NW = WVM * WVN, BM = 16 * MB * WVM, BN = 16 * NB * WVN;
+    using A = Cols<T, BM>;
+    using B = Cols<T, BN>;
+    constexpr int KS = A::KS, GA = BM / 8 / NW, GB = BN / 8 / NW;
+    static_assert(GA * 8 * NW == BM && GB * 8 * NW == BN, "the wavefronts share the loads evenly");
+    constexpr int ABYTES = BM * kRow, BUF = (BM + BN) * kRow;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    // workgroup -> split and tile: XCD x (= blockIdx % 8) owns a contiguous run of items, the tiles of a split one after the other
+    const int item = (int)(blockIdx.x % kXcds) * a.per_xcd + (int)(blockIdx.x / kXcds);
+    if (item >= a.items) return;  // whole workgroup: no barrier has been reached yet
+    const int split = item / a.tiles, tile = item - split * a.tiles;
+    const int mt = tile / a.tiles_n, o0 = mt * BM, c0 = (tile - mt * a.tiles_n) * BN;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv / WVN, wn = wv - wm * WVN;
+    const int zbytes = a.No * A::ES, xbytes = a.Cin * B::ES;
+    uint32_t aoff[GA], boff[GB];
+#pragma unroll
+    for (int l = 0; l < GA; ++l) {
+        const int r = lane / A::CPR, c = (lane % A::CPR) ^ A::swizzle((wv * GA + l) * A::RPI + r);
+        aoff[l] = o0 + c * A::PER < a.No ? (uint32_t)(r * zbytes + c * 16) : kOob;
+    }
+#pragma unroll
+    for (int l = 0; l < GB; ++l) {
+        const int r = lane / B::CPR, c = (lane % B::CPR) ^ B::swizzle((wv * GB + l) * B::RPI + r);
+        boff[l] = c0 + c * B::PER < a.Cin ? (uint32_t)(r * xbytes + c * 16) : kOob;
+    }
+    const int64_t first = (int64_t)split * a.stages * KS;
+    const int stages = (int)min((int64_t)a.stages, (a.M - first + KS - 1) / KS);
+    // (without the casts of the offsets the compiler's host pass has no stub of this kernel)
+    auto issue_stage = [&](int ks) __attribute__((always_inline)) {
+        unsigned char *as = smem + (ks & 1) * BUF + wv * (GA * 1024), *bs = smem + (ks & 1) * BUF + ABYTES + wv * (GB * 1024);
+        const int64_t k0 = first + (int64_t)ks * KS;
+#pragma unroll
+        for (int l = 0; l < GA; ++l) {
+            const __amdgpu_buffer_rsrc_t zres = cols_from(a.dz, k0 + (wv * GA + l) * A::RPI, a.M, zbytes, o0 * A::ES);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(zres, (__attribute__((address_space(3))) void *)(as + l * 1024), 16, (uint32_t)aoff[l], 0, 0, 0);
+        }
+#pragma unroll
+        for (int l = 0; l < GB; ++l) {
+            const __amdgpu_buffer_rsrc_t xres = cols_from(a.X, k0 + (wv * GB + l) * B::RPI, a.M, xbytes, c0 * B::ES);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xres, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16, (uint32_t)boff[l], 0, 0, 0);
+        }
+    };
+    typename M::Acc acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = typename M::Acc{};
+    int ap[MB], bp[NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) ap[i] = A::row(lane) * A::RB + A::place(lane, wm * MB + i);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) bp[j] = ABYTES + B::row(lane) * B::RB + B::place(lane, wn * NB + j);
+    issue_stage(0);
+    for (int ks = 0; ks < stages; ++ks) {
+        // This wavefront's loads of stage ks have landed and its reads of stage ks - 1 are done; behind the
+        // barrier everybody's are, and the slot of stage ks - 1 is free.
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if (ks + 1 < stages) issue_stage(ks + 1);
+        const unsigned char *buf = smem + (ks & 1) * BUF;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            typename M::Frag af[MB], bf[NB];
+#pragma unroll
+            for (int i = 0; i < MB; ++i) af[i] = A::read(buf + kk * (KS / 2 * A::RB) + ap[i]);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) bf[j] = B::read(buf + kk * (KS / 2 * B::RB) + bp[j]);
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int i = 0; i < MB; ++i) acc[i][j] = M::mul(bf[j], af[i], acc[i][j]);
+        }
+    }
+    const bool parts = a.items > a.tiles;
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            grad_w_store<T>(a, split, parts, o0 + 16 * (wm * MB + i) + (lane & 15), c0 + 16 * (wn * NB + j) + 4 * (lane >> 4), acc[i][j]);
+}
+
+// The splits' sums added up, in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void grad_w_join_kernel(const GradWArgs a)
+{
+    const int64_t n = (int64_t)a.No * a.Cin, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    const int splits = a.items / a.tiles;
+    f32x4 v = *(const f32x4 *)(a.partial + i);
+#pragma unroll 4
+    for (int s = 1; s < splits; ++s) v += *(const f32x4 *)(a.partial + s * n + i);
+    const int64_t half = (int64_t)a.Cout * a.Cin;
+    T *to = (T *)(i < half ? a.dW[0] : a.dW[1]);
+    if (!to) return;
+    typedef T Quad __attribute__((ext_vector_type(4)));
+    Quad q;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q[e] = (T)v[e];
+    *(Quad *)(to + (i < half ? i : i - half)) = q;
+}
+
+// W_0 and W_1 below each other, transposed: [Cin][n_w Cout].  64 x 64 tiles through LDS.
+template <typename T>
+__global__ __launch_bounds__(256) void grad_turn_kernel(const void *W0, const void *W1, void *Wt, int Cin, int Cout, int No)
+{
+    constexpr int PER = 16 / (int)sizeof(T), CPR = 64 / PER, ROWS = 256 / CPR;
+    typedef T Piece __attribute__((ext_vector_type(PER)));
+    __shared__ T tile[64][64 + 4 / (int)sizeof(T)];
+    const int o0 = (int)blockIdx.x * 64, c0 = (int)blockIdx.y * 64, r = threadIdx.x / CPR, p = threadIdx.x % CPR * PER;
+#pragma unroll
+    for (int i = 0; i < 64; i += ROWS) {
+        const int o = o0 + r + i, c = c0 + p;
+        Piece x{};
+        if (o < No && c < Cin) x = *(const Piece *)((const T *)(o < Cout ? W0 : W1) + (int64_t)(o < Cout ? o : o - Cout) * Cin + c);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) tile[p + e][r + i] = x[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 64; i += ROWS) {
+        const int c = c0 + r + i, o = o0 + p;
+        if (c >= Cin || o >= No) continue;
+        Piece x;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) x[e] = tile[r + i][p + e];
+        *(Piece *)((T *)Wt + (int64_t)c * No + o) = x;
+    }
+}
+
+// Column sums of 256 rows of a matrix, 128 columns a workgroup: part blockIdx.y.
+template <typename T>
+__global__ __launch_bounds__(256) void grad_sums_kernel(const void *dz, int64_t M, int No, float *sums)
+{
+    constexpr int PER = 8, ES = (int)sizeof(T);
+    typedef T Piece __attribute__((ext_vector_type(16 / ES)));
+    __shared__ float part[16][128 + 4];
+    const int l = threadIdx.x & 15, w = threadIdx.x >> 4, c = (int)blockIdx.x * 128 + l * PER;
+    const int64_t first = (int64_t)blockIdx.y * 256;
+    float v[PER] = {};
+    if (c < No)
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) {
+            const int64_t m = first + w + 16 * i;
+            if (m >= M) break;
+#pragma unroll
+            for (int h = 0; h < PER * ES / 16; ++h) {
+                const int at = h * (16 / ES);
+                if (c + at >= No) break;
+                const Piece x = *(const Piece *)((const T *)dz + m * No + c + at);
+#pragma unroll
+                for (int e = 0; e < 16 / ES; ++e) v[at + e] += (float)x[e];
+            }
+        }
+#pragma unroll
+    for (int e = 0; e < PER; ++e) part[w][l * PER + e] = v[e];
+    __syncthreads();
+    const int cc = (int)blockIdx.x * 128 + (int)threadIdx.x;
+    if (threadIdx.x >= 128 || cc >= No) return;
+    float t = 0.f;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) t += part[q][threadIdx.x];
+    sums[(int64_t)blockIdx.y * No + cc] = t;
+}
+
+// The parts' column sums added up: 16 columns a workgroup, 64 threads to each.
+__global__ __launch_bounds__(1024) void grad_join_kernel(const float *sums, int parts, int Cout, int No, float *db0, float *db1)
+{
+    __shared__ float part[64][17];
+    const int l = threadIdx.x & 15, w = threadIdx.x >> 4, c = (int)blockIdx.x * 16 + l;
+    float v = 0.f;
+    if (c < No)
+#pragma unroll 4
+        for (int p = w; p < parts; p += 64) v += sums[(int64_t)p * No + c];
+    part[w][l] = v;
+    __syncthreads();
+    for (int h = 32; h > 0; h >>= 1) {
+        if (w < h) part[w][l] += part[w + h][l];
+        __syncthreads();
+    }
+    float *to = c < Cout ? db0 : db1;
+    if (w == 0 && c < No && to) to[c < Cout ? c : c - Cout] = part[0][l];
+}
+
+}  // namespace
+}  // namespace dsattn

@@ -9,6 +9,8 @@
 
 #include "dsattn.h"
 #include "plan.h"
+#include "act_pick.h"
+#include "grad_tile.h"
 #include "rows.h"
 
 namespace dsattn {
@@ -29,6 +31,7 @@ struct GradArgs {
 // The activation and its derivative.
 __device__ __forceinline__ void act_and_slope(float x, int act, float &y, float &d)
 {
+    const float c = fminf(fmaxf(x, -100.f), 100.f);  // (beyond, its factor is 0, and 0 * infinity would be NaN)
     switch (act) {
     case DSATTN_ACT_RELU:
         y = x > 0.f || x != x ? x : 0.f;
@@ -37,21 +40,21 @@ __device__ __forceinline__ void act_and_slope(float x, int act, float &y, float 
     case DSATTN_ACT_GELU: {
         const float p = 0.5f * erfcf(x * -0.70710678f);
         y = x * p;
-        d = fmaf(x * 0.39894228f, expf(-0.5f * x * x), p);
+        d = fmaf(c * 0.39894228f, expf(-0.5f * c * c), p);
         break;
     }
     case DSATTN_ACT_GELU_TANH: {
         // p = (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)), dp/dx = 2 p (1 - p) du/dx
-        const float x2 = x * x, u = 0.79788456f * x * fmaf(0.044715f, x2, 1.f);
+        const float u = 0.79788456f * x * fmaf(0.044715f, x * x, 1.f);
         const float p = 1.f / (1.f + expf(-2.f * u)), q = 1.f / (1.f + expf(2.f * u));
         y = x * p;
-        d = fmaf(2.f * x * p * q, 0.79788456f * fmaf(0.134145f, x2, 1.f), p);
+        d = fmaf(2.f * c * p * q, 0.79788456f * fmaf(0.134145f, c * c, 1.f), p);
         break;
     }
     case DSATTN_ACT_SILU: {
         const float p = 1.f / (1.f + expf(-x)), q = 1.f / (1.f + expf(x));
         y = x * p;
-        d = fmaf(x * p, q, p);
+        d = fmaf(c * p, q, p);
         break;
     }
     default:
@@ -155,10 +158,205 @@ int grad_validate(const dsattn_linear_act_desc *desc, const char *who)
 // Where the derivative is 1 everywhere dz is dY itself.
 bool grad_is_dy(const dsattn_linear_act_desc &d) { return d.act == DSATTN_ACT_NONE && d.n_w == 1; }
 
-size_t grad_bytes(const dsattn_linear_act_desc &d)
+// How the gradients are computed.  No kernel (fn null) for dz: the vector kernels do everything.
+struct GradLaunch {
+    bool tiles = false;                         // on the matrix cores
+    const void *dz_fn = nullptr;                // kernel of dz; null: dz is dY
+    int dz_rows, dz_cols, dz_waves, dz_lds;     // its tile, wavefronts and bytes of LDS
+    bool dz_stream, dz_small;
+    int part_rows;                              // rows of a part of the column sums
+    const void *w_fn;                           // kernel of dW
+    int w_rows, w_cols, w_waves, w_lds, splits, stages;
+    size_t dz, turned, sums, partial, bytes;    // places in the workspace, and its size
+};
+
+size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
+
+struct GradVariant {
+    int rows, cols, waves, lds, part;  // (part: rows of a wavefront's, which it sums up)
+    const void *fn[2];                 // gated
+};
+#define DSATTN_GRAD_TILE(T, MB, NB, WVM, WVN)                                                               \
+    {16 * MB * WVM, 16 * NB * WVN, WVM * WVN, 2 * (16 * MB * WVM + 16 * NB * WVN) * kRow, 16 * MB,          \
+     {(const void *)&act_tile_kernel<T, MB, NB, WVM, WVN, false, T, true>,                                  \
+      (const void *)&act_tile_kernel<T, MB, NB, WVM, WVN, true, T, true>}}
+const GradVariant kDzTiles[2][2] = {{DSATTN_GRAD_TILE(float, 2, 4, 4, 2), DSATTN_GRAD_TILE(float, 1, 4, 4, 1)},
+                                    {DSATTN_GRAD_TILE(__bf16, 2, 4, 4, 2), DSATTN_GRAD_TILE(__bf16, 1, 4, 4, 1)}};
+const void *const kDzSmall[2][2] = {
+    {(const void *)&act_small_kernel<float, false, float, true>, (const void *)&act_small_kernel<float, true, float, true>},
+    {(const void *)&act_small_kernel<__bf16, false, __bf16, true>, (const void *)&act_small_kernel<__bf16, true, __bf16, true>}};
+#define DSATTN_GRAD_STREAM(G, ACT) (const void *)&act_stream_kernel<__bf16, 4, 8, G, __bf16, ACT, true>
+const void *const kDzStream[2][DSATTN_ACT_SILU + 1] = {
+    {nullptr, DSATTN_GRAD_STREAM(false, DSATTN_ACT_RELU), DSATTN_GRAD_STREAM(false, DSATTN_ACT_GELU),
+     DSATTN_GRAD_STREAM(false, DSATTN_ACT_GELU_TANH), DSATTN_GRAD_STREAM(false, DSATTN_ACT_SILU)},
+    {DSATTN_GRAD_STREAM(true, DSATTN_ACT_NONE), DSATTN_GRAD_STREAM(true, DSATTN_ACT_RELU), DSATTN_GRAD_STREAM(true, DSATTN_ACT_GELU),
+     DSATTN_GRAD_STREAM(true, DSATTN_ACT_GELU_TANH), DSATTN_GRAD_STREAM(true, DSATTN_ACT_SILU)}};
+
+const void *const kWTiles[2][2] = {  // 64 x 64, 128 x 128
+    {(const void *)&grad_w_tile_kernel<float, 2, 2, 2, 2>, (const void *)&grad_w_tile_kernel<float, 2, 4, 4, 2>},
+    {(const void *)&grad_w_tile_kernel<__bf16, 2, 2, 2, 2>, (const void *)&grad_w_tile_kernel<__bf16, 2, 4, 4, 2>}};
+
+GradLaunch grad_pick(const dsattn_linear_act_desc &d)
 {
-    if (grad_is_dy(d)) return 0;
-    return (size_t)d.rows * d.n_w * d.c_out * sizeof(float);
+    GradLaunch g;
+    const bool f32 = d.io_dtype == DSATTN_F32, gated = d.n_w == 2;
+    const int64_t es = f32 ? 4 : 2, No = (int64_t)d.n_w * d.c_out, rowbytes = d.c_in * es;
+    g.dz = g.turned = g.sums = g.partial = g.bytes = 0;
+    // rows are whole 16-byte chunks, and a tile's are addressed with 32-bit offsets
+    const bool fits = rowbytes % 16 == 0 && d.c_out * es % 16 == 0 && rowbytes * 256 < ((int64_t)1 << 31) &&
+                      No * es * 256 < ((int64_t)1 << 31) && No < 1 << 22 && !(d.flags & DSATTN_FLAG_FORCE_GENERIC);
+    auto tiles = [&](int64_t m, int64_t n, int rows, int cols) { return (m + rows - 1) / rows * ((n + cols - 1) / cols); };
+    if (!fits || tiles(d.rows, No, 32, 32) >= (1 << 23) || tiles(No, d.c_in, 64, 64) >= (1 << 20)) {
+        if (!grad_is_dy(d)) g.bytes = (size_t)d.rows * No * sizeof(float);
+        return g;
+    }
+    g.tiles = true;
+    // dz
+    const int64_t stages = (rowbytes + kRow - 1) / kRow;
+    g.dz_stream = g.dz_small = false;
+    g.part_rows = 256;
+    if (!grad_is_dy(d)) {
+        g.part_rows = 32;
+        const GradVariant *v = kDzTiles[!f32];
+        if (small_is_faster(d.io_dtype, tiles(d.rows, No, 32, 32), stages)) {
+            g.dz_small = true;
+            g.dz_fn = kDzSmall[!f32][gated];
+            g.dz_rows = g.dz_cols = 32;
+            g.dz_waves = 8;
+            g.dz_lds = kSmallLds;
+        } else if (!f32 && tile_estimate(256, tiles(d.rows, No, 256, 256), stages) <
+                               std::min(tile_estimate(128, tiles(d.rows, No, 128, 128), stages),
+                                        tile_estimate(64, tiles(d.rows, No, 64, 64), stages))) {
+            g.dz_stream = true;
+            g.dz_fn = kDzStream[gated][d.act];
+            g.dz_rows = g.dz_cols = 256;
+            g.dz_waves = 8;
+            g.dz_lds = kStreamLds;
+            g.part_rows = 64;
+        } else {
+            if (f32 ? tiles(d.rows, No, 128, 128) < 384
+                    : tile_estimate(64, tiles(d.rows, No, 64, 64), stages) < tile_estimate(128, tiles(d.rows, No, 128, 128), stages))
+                ++v;
+            g.dz_fn = v->fn[gated];
+            g.dz_rows = v->rows;
+            g.dz_cols = v->cols;
+            g.dz_waves = v->waves;
+            g.dz_lds = v->lds;
+            g.part_rows = v->part;
+        }
+        g.dz = g.bytes;
+        g.bytes += aligned((size_t)d.rows * No * es);
+    }
+    g.turned = g.bytes;
+    g.bytes += aligned((size_t)No * d.c_in * es);
+    g.sums = g.bytes;
+    g.bytes += aligned((size_t)((d.rows + g.part_rows - 1) / g.part_rows) * No * sizeof(float));
+    // dW
+    const int KS = kRow / (int)es;
+    const int64_t t128 = tiles(No, d.c_in, 128, 128), t64 = tiles(No, d.c_in, 64, 64), all = (d.rows + KS - 1) / KS;
+    const bool wide = t128 * std::max<int64_t>(1, all / 8) >= 384;
+    g.w_rows = g.w_cols = wide ? 128 : 64;
+    g.w_waves = wide ? 8 : 4;
+    g.w_lds = 2 * (g.w_rows + g.w_cols) * kRow;
+    g.w_fn = kWTiles[!f32][wide];
+    const int64_t t = wide ? t128 : t64, want = std::max<int64_t>(1, std::min<int64_t>({512 / t, all / 8, 64}));
+    g.stages = (int)((all + want - 1) / want);
+    g.splits = (int)((all + g.stages - 1) / g.stages);
+    g.partial = g.bytes;
+    if (g.splits > 1) g.bytes += aligned((size_t)g.splits * No * d.c_in * sizeof(float));
+    return g;
+}
+
+// The kernels one after the other: dz with its parts of the column sums, those joined, W turned, dX, dW.
+int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const GradArgs &a, const char *who, char *space, hipStream_t st)
+{
+    const int No = d.n_w * d.c_out;
+    const bool f32 = d.io_dtype == DSATTN_F32, sums = a.db[0] || a.db[1];
+    hipError_t e = hipSuccess;
+    auto launch = [&](const void *fn, dim3 grid, int threads, void **params, int lds) {
+        // the default cap on dynamic LDS is 64 KB
+        if (e == hipSuccess && lds > 64 << 10) e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e == hipSuccess) e = hipLaunchKernel(fn, grid, dim3((unsigned)threads), params, (size_t)lds, st);
+    };
+    float *parts = (float *)(space + g.sums);
+    const int n_parts = (int)((d.rows + g.part_rows - 1) / g.part_rows);
+    if (g.dz_fn) {
+        ActArgs z{};
+        z.X = a.X;
+        z.R = a.dY;
+        z.Y = a.dz;
+        z.M = d.rows;
+        z.Cin = d.c_in;
+        z.Cout = d.c_out;
+        z.n_w = d.n_w;
+        z.act = d.act;
+        z.sums = sums ? parts : nullptr;
+        for (int k = 0; k < d.n_w; ++k) {
+            z.W[k] = a.W[k];
+            z.bias[k] = a.bias[k];
+        }
+        const int cols = g.dz_cols / d.n_w;
+        z.tiles_n = (d.c_out + cols - 1) / cols;
+        z.tiles = (int32_t)((d.rows + g.dz_rows - 1) / g.dz_rows) * z.tiles_n;
+        z.per_xcd = (z.tiles + kXcds - 1) / kXcds;
+        z.panel = act_panel(z.tiles_n);
+        int dev = 0, per_xcd = z.per_xcd;
+        if (g.dz_stream) {
+            e = hipGetDevice(&dev);
+            per_xcd = std::min(per_xcd, (compute_units(dev) + kXcds - 1) / kXcds);
+        }
+        void *params[] = {&z};
+        launch(g.dz_fn, dim3(g.dz_small ? (unsigned)z.tiles : (unsigned)per_xcd * kXcds), 64 * g.dz_waves, params, g.dz_lds);
+    } else if (sums) {
+        const void *dz = a.dz;
+        int64_t M = d.rows;
+        int no = No;
+        void *params[] = {&dz, &M, &no, &parts};
+        launch(f32 ? (const void *)&grad_sums_kernel<float> : (const void *)&grad_sums_kernel<__bf16>,
+               dim3((unsigned)(No + 127) / 128, (unsigned)n_parts), 256, params, 0);
+    }
+    if (sums) {
+        int n = n_parts, Cout = d.c_out, no = No;
+        float *db0 = a.db[0], *db1 = a.db[1];
+        void *params[] = {&parts, &n, &Cout, &no, &db0, &db1};
+        launch((const void *)&grad_join_kernel, dim3((unsigned)(No + 15) / 16), 1024, params, 0);
+    }
+    if (a.dX) {
+        const void *W0 = a.W[0], *W1 = a.W[1];
+        void *Wt = space + g.turned;
+        int Cin = d.c_in, Cout = d.c_out, no = No;
+        void *params[] = {&W0, &W1, &Wt, &Cin, &Cout, &no};
+        launch(f32 ? (const void *)&grad_turn_kernel<float> : (const void *)&grad_turn_kernel<__bf16>,
+               dim3((unsigned)(No + 63) / 64, (unsigned)(Cin + 63) / 64), 256, params, 0);
+        if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
+        const dsattn_linear_act_desc x{d.rows, No, d.c_in, 1, DSATTN_ACT_NONE, d.io_dtype, d.io_dtype, 0};
+        const int rc = dsattn_linear_act(&x, a.dz, nullptr, &Wt, nullptr, nullptr, nullptr, a.dX, st);
+        if (rc != DSATTN_OK) return rc;
+    }
+    if (a.dW[0] || a.dW[1]) {
+        GradWArgs w{};
+        w.dz = a.dz;
+        w.X = a.X;
+        w.dW[0] = a.dW[0];
+        w.dW[1] = a.dW[1];
+        w.partial = (float *)(space + g.partial);
+        w.M = d.rows;
+        w.Cin = d.c_in;
+        w.Cout = d.c_out;
+        w.No = No;
+        w.tiles_n = (d.c_in + g.w_cols - 1) / g.w_cols;
+        w.tiles = (No + g.w_rows - 1) / g.w_rows * w.tiles_n;
+        w.items = w.tiles * g.splits;
+        w.per_xcd = (w.items + kXcds - 1) / kXcds;
+        w.stages = g.stages;
+        void *params[] = {&w};
+        launch(g.w_fn, dim3((unsigned)w.per_xcd * kXcds), 64 * g.w_waves, params, g.w_lds);
+        if (g.splits > 1)
+            launch(f32 ? (const void *)&grad_w_join_kernel<float> : (const void *)&grad_w_join_kernel<__bf16>,
+                   dim3((unsigned)(((int64_t)No * d.c_in / 4 + 255) / 256)), 256, params, 0);
+    }
+    if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
+    return DSATTN_OK;
 }
 
 }  // namespace
@@ -173,7 +371,7 @@ int dsattn_linear_act_backward_workspace(const dsattn_linear_act_desc *desc, siz
     const int rc = grad_validate(desc, "dsattn_linear_act_backward_workspace");
     if (rc != DSATTN_OK) return rc;
     if (!bytes) return fail(DSATTN_EINVAL, "dsattn_linear_act_backward_workspace: null output");
-    *bytes = grad_bytes(*desc);
+    *bytes = grad_pick(*desc).bytes;
     return DSATTN_OK;
 }
 
@@ -188,7 +386,8 @@ int dsattn_linear_act_backward(const dsattn_linear_act_desc *desc, const void *X
     if (!X || !W || !dY) return fail(DSATTN_EINVAL, "%s: null pointer", who);
     const int64_t es = d.io_dtype == DSATTN_F32 ? 4 : 2;
     const int64_t xn = d.rows * d.c_in * es, yn = d.rows * d.c_out * es, wn = (int64_t)d.c_out * d.c_in * es, bn = 4 * (int64_t)d.c_out;
-    const size_t need = grad_bytes(d);
+    const GradLaunch g = grad_pick(d);
+    const size_t need = g.bytes;
     if (need && (!workspace || workspace_bytes < need)) return fail(DSATTN_EINVAL, "%s: workspace of %zu bytes needed", who, need);
     if (((uintptr_t)X | (uintptr_t)dY | (uintptr_t)dX | (uintptr_t)workspace) & 15u)
         return fail(DSATTN_EINVAL, "%s: pointers must be 16-byte aligned", who);
@@ -196,7 +395,7 @@ int dsattn_linear_act_backward(const dsattn_linear_act_desc *desc, const void *X
     a.X = X;
     a.dY = dY;
     a.dX = dX;
-    a.dz = need ? workspace : (void *)dY;
+    a.dz = grad_is_dy(d) ? (void *)dY : (char *)workspace + g.dz;
     a.M = d.rows;
     a.Cin = d.c_in;
     a.Cout = d.c_out;
@@ -224,14 +423,15 @@ int dsattn_linear_act_backward(const dsattn_linear_act_desc *desc, const void *X
     const hipStream_t st = (hipStream_t)stream;
     void *params[] = {&a};
     hipError_t e = hipSuccess;
+    if (g.tiles) return grad_launch(d, g, a, who, (char *)workspace, st);
     // (a launch has less than 2^32 threads)
     auto blocks = [](int64_t n) { return (n + 255) / 256; };
     if (blocks(d.rows * std::max(d.c_out, d.c_in)) > 0xffffff || blocks((int64_t)d.c_out * d.c_in) > 0x7fffff)
         return fail(DSATTN_EUNSUPPORTED, "%s: too large for the generic kernel", who);
-    if (need)
+    if (!grad_is_dy(d))
         e = hipLaunchKernel(f32 ? (const void *)&grad_dz_kernel<float> : (const void *)&grad_dz_kernel<__bf16>,
                             dim3((unsigned)blocks(d.rows * d.c_out)), dim3(256), params, 0, st);
-    const bool wide = f32 || need;  // dz in fp32
+    const bool wide = f32 || !grad_is_dy(d);  // dz in fp32
     if (e == hipSuccess && dX)
         e = hipLaunchKernel(f32    ? (const void *)&grad_dx_kernel<float, float>
                             : wide ? (const void *)&grad_dx_kernel<__bf16, float>
