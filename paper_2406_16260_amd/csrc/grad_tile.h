@@ -18,7 +18,17 @@ struct GradWArgs {
     int32_t Cin, Cout, No;               // No: n_w Cout
     int32_t tiles_n, tiles, items, per_xcd;  // column tiles (of X); all; tiles * splits; ceil(items / 8)
     int32_t stages;                      // of a split
+    int32_t whole, whole_xcd, rest_xcd;  // 256 x 256 tiles: column tiles that are not half empty; items of an XCD of those and of the others
 };
+
+// Four numbers of a column, transposed by the LDS.  (The pointer is restrict for what the compiler makes of it: a read that it
+// knows nothing about waits for all loads into LDS that are on their way, and the kernels' own waits do that where it is needed.)
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ s16x4 read_turned(__attribute__((address_space(3))) s16x4 *__restrict at)
+{
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(at);
+}
 
 // Columns of an operand, W of them a tile.
 template <typename T, int W>
@@ -49,10 +59,8 @@ struct Cols {
             for (int s = 0; s < 4; ++s) f[s] = *(const float *)(at + s * RB);
             return f;
         } else {
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef short s16x8 __attribute__((ext_vector_type(8)));
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 4 * RB));
+            const s16x4 lo = read_turned((__attribute__((address_space(3))) s16x4 *)at);
+            const s16x4 hi = read_turned((__attribute__((address_space(3))) s16x4 *)(at + 4 * RB));
             return __builtin_bit_cast(Frag, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
     }
@@ -106,12 +114,12 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const Gr
     uint32_t aoff[GA], boff[GB];
 #pragma unroll
     for (int l = 0; l < GA; ++l) {
-        const int r = lane / A::CPR, c = (lane % A::CPR) ^ A::swizzle((wv * GA + l) * A::RPI + r);
+        const int r = (wv * GA + l) * A::RPI + lane / A::CPR, c = (lane % A::CPR) ^ A::swizzle(r);
         aoff[l] = o0 + c * A::PER < a.No ? (uint32_t)(r * zbytes + c * 16) : kOob;
     }
 #pragma unroll
     for (int l = 0; l < GB; ++l) {
-        const int r = lane / B::CPR, c = (lane % B::CPR) ^ B::swizzle((wv * GB + l) * B::RPI + r);
+        const int r = (wv * GB + l) * B::RPI + lane / B::CPR, c = (lane % B::CPR) ^ B::swizzle(r);
         boff[l] = c0 + c * B::PER < a.Cin ? (uint32_t)(r * xbytes + c * 16) : kOob;
     }
     const int64_t first = (int64_t)split * a.stages * KS;
@@ -120,16 +128,14 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const Gr
     auto issue_stage = [&](int ks) __attribute__((always_inline)) {
         unsigned char *as = smem + (ks & 1) * BUF + wv * (GA * 1024), *bs = smem + (ks & 1) * BUF + ABYTES + wv * (GB * 1024);
         const int64_t k0 = first + (int64_t)ks * KS;
+        const __amdgpu_buffer_rsrc_t zres = cols_from(a.dz, k0, a.M, zbytes, o0 * A::ES);
+        const __amdgpu_buffer_rsrc_t xres = cols_from(a.X, k0, a.M, xbytes, c0 * B::ES);
 #pragma unroll
-        for (int l = 0; l < GA; ++l) {
-            const __amdgpu_buffer_rsrc_t zres = cols_from(a.dz, k0 + (wv * GA + l) * A::RPI, a.M, zbytes, o0 * A::ES);
+        for (int l = 0; l < GA; ++l)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(zres, (__attribute__((address_space(3))) void *)(as + l * 1024), 16, (uint32_t)aoff[l], 0, 0, 0);
-        }
 #pragma unroll
-        for (int l = 0; l < GB; ++l) {
-            const __amdgpu_buffer_rsrc_t xres = cols_from(a.X, k0 + (wv * GB + l) * B::RPI, a.M, xbytes, c0 * B::ES);
+        for (int l = 0; l < GB; ++l)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(xres, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16, (uint32_t)boff[l], 0, 0, 0);
-        }
     };
     typename M::Acc acc[MB][NB];
 #pragma unroll
@@ -172,6 +178,183 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const Gr
         for (int j = 0; j < NB; ++j)
             grad_w_store<T>(a, split, parts, o0 + 16 * (wm * MB + i) + (lane & 15), c0 + 16 * (wn * NB + j) + 4 * (lane >> 4), acc[i][j]);
 }
+
+// Large ones: 256 x 256 tiles, eight wavefronts (two per SIMD) whose parts are 64 columns of dz by 128 of X.  Two LDS slots; the
+// multiplies of a stage run in halves (columns of dz [0, 32), then [32, 64) of a part) over one set of fragments that is refilled in
+// place, and LDS reads and the loads of the next stage but one sit between the matrix instructions by hand, as in the
+// product's persistent kernel.  Where X has no more than 128 columns left, the four wavefronts of its other half, one
+// of each SIMD, only load, and the tile takes little more than half the time.
+__global__ __launch_bounds__(512, 2) void grad_w_large_kernel(const GradWArgs a)
+{
+    using T = __bf16;
+    using M = Mul<T>;
+    using K = Cols<T, 256>;
+    constexpr int MB = 4, NB = 8, KS = K::KS, G = 4, NL = 2 * G;
+    constexpr int ABYTES = 256 * kRow, SLOT = 2 * ABYTES;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    // workgroup -> item: every XCD has a run of the items of whole tiles, and then one of the others
+    const int xcd = (int)(blockIdx.x % kXcds), idx = (int)(blockIdx.x / kXcds), tiles_m = a.tiles / a.tiles_n;
+    const int splits = a.items / a.tiles;
+    int split, mt, nt;
+    if (idx < a.whole_xcd) {
+        const int item = xcd * a.whole_xcd + idx, per = tiles_m * a.whole;
+        if (item >= per * splits) return;  // whole workgroup: no barrier has been reached yet
+        split = item / per;
+        mt = (item - split * per) / a.whole;
+        nt = item - split * per - mt * a.whole;
+    } else {
+        const int item = xcd * a.rest_xcd + idx - a.whole_xcd;
+        if (item >= tiles_m * splits) return;
+        split = item / tiles_m;
+        mt = item - split * tiles_m;
+        nt = a.whole;
+    }
+    const int o0 = mt * 256, c0 = nt * 256;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv & 3, wn = wv >> 2;
+    const bool busy = c0 + 128 * wn < a.Cin;
+    const int zbytes = a.No * 2, xbytes = a.Cin * 2;
+    uint32_t aoff[G], boff[G];
+#pragma unroll
+    for (int l = 0; l < G; ++l) {
+        const int r = (wv * G + l) * K::RPI + lane / K::CPR, c = (lane % K::CPR) ^ K::swizzle(r);
+        aoff[l] = o0 + c * K::PER < a.No ? (uint32_t)(r * zbytes + c * 16) : kOob;
+        boff[l] = c0 + c * K::PER < a.Cin ? (uint32_t)(r * xbytes + c * 16) : kOob;
+    }
+    const int64_t first = (int64_t)split * a.stages * KS;
+    const int stages = (int)min((int64_t)a.stages, (a.M - first + KS - 1) / KS);
+    // ---- the load side, up to two stages ahead of the multiplies; past the last stage all lanes are out of range
+    int ld = 0;
+    __amdgpu_buffer_rsrc_t zres, xres;
+    unsigned char *ld_to = smem;
+    auto stage_setup = [&]() __attribute__((always_inline)) {
+        const int64_t k = ld < stages ? first + (int64_t)ld * KS : a.M;
+        zres = cols_from(a.dz, k, a.M, zbytes, o0 * 2);
+        xres = cols_from(a.X, k, a.M, xbytes, c0 * 2);
+        ld_to = smem + (ld & 1) * SLOT + wv * (G * 1024);
+        ++ld;
+    };
+    auto issue_one = [&](int l) __attribute__((always_inline)) {
+        if (l < G)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(zres, (__attribute__((address_space(3))) void *)(ld_to + l * 1024), 16,
+                                                     (uint32_t)aoff[l], 0, 0, 0);
+        else
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xres, (__attribute__((address_space(3))) void *)(ld_to + ABYTES + (l - G) * 1024), 16,
+                                                     (uint32_t)boff[l - G], 0, 0, 0);
+    };
+    typename M::Acc acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = typename M::Acc{};
+    // fragment i of a part is 32 i bytes from the first, exclusive-or'd: the swizzle is one of whole fragments
+    const int ap = K::row(lane) * K::RB + K::place(lane, wm * MB), bp = ABYTES + K::row(lane) * K::RB + K::place(lane, wn * NB);
+    constexpr int HB = MB / 2, NMH = HB * NB;
+    typename M::Frag af[MB], bf[NB];
+    constexpr int TAIL = NMH, kSpread = 5 * NMH / 2;
+    auto read_a = [&](int slot, int kk, int i) __attribute__((always_inline)) {
+        af[i] = K::read(smem + (((ap + slot) ^ (32 * i)) + kk * (KS / 2 * K::RB)));
+    };
+    auto read_b = [&](int slot, int kk, int j) __attribute__((always_inline)) {
+        bf[j] = K::read(smem + (((bp + slot) ^ (32 * j)) + kk * (KS / 2 * K::RB)));
+    };
+    auto loads_at = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < NL; ++q)
+            if ((q * kSpread) / NL == g) {
+                issue_one(q);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    };
+    auto half1 = [&](int slot, int kk, int g0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < NMH; ++m) {
+            loads_at(g0 + m);
+#pragma unroll
+            for (int r = 0; r < HB; ++r)
+                if ((r * (NMH / 2)) / HB == m) {
+                    read_a(slot, kk, HB + r);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            const int j = m / HB, i0 = m - j * HB, i = j & 1 ? HB - 1 - i0 : i0;
+            acc[i][j] = M::mul(bf[j], af[i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto half2 = [&](int nslot, int nkk, int g0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < NMH; ++m) {
+            loads_at(g0 + m);
+            const int j = m / HB, i0 = m - j * HB, i = j & 1 ? HB - 1 - i0 : i0;
+            if (i0 == 0 && j > 0) {
+                read_b(nslot, nkk, j - 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (i0 == HB - 1 && j < HB) {
+                read_a(nslot, nkk, j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            acc[HB + i][j] = M::mul(bf[j], af[HB + i], acc[HB + i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        read_b(nslot, nkk, NB - 1);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto issue_tail = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < NL; ++q)
+            if ((q * kSpread) / NL < TAIL) issue_one(q);
+    };
+    auto wait_all = [&]() __attribute__((always_inline)) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    stage_setup();
+#pragma unroll
+    for (int l = 0; l < NL; ++l) issue_one(l);
+    wait_all();
+    stage_setup();
+    issue_tail();
+    if (busy) {
+#pragma unroll
+        for (int i = 0; i < HB; ++i) read_a(0, 0, i);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) read_b(0, 0, j);
+        for (int ks = 0; ks < stages; ++ks) {
+            const int slot = (ks & 1) * SLOT, next = SLOT - slot;
+            if (wv >= 4) __builtin_amdgcn_s_setprio(1);
+            half1(slot, 0, TAIL);
+            half2(slot, 1, TAIL + NMH);
+            __builtin_amdgcn_s_setprio(0);
+            stage_setup();
+            half1(slot, 1, TAIL + 2 * NMH);
+            // this wavefront's loads of the next stage have landed and its reads of this slot are done; behind the barrier
+            // everybody's are
+            wait_all();
+            half2(next, 0, 0);
+        }
+    } else {
+        for (int ks = 0; ks < stages; ++ks) {
+#pragma unroll
+            for (int q = 0; q < NL; ++q)
+                if ((q * kSpread) / NL >= TAIL) issue_one(q);
+            stage_setup();
+            wait_all();
+            issue_tail();
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(0);  // (nothing is on its way into LDS when the workgroup ends)
+    if (!busy) return;
+    const bool parts = splits > 1;
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            grad_w_store<T>(a, split, parts, o0 + 16 * (wm * MB + i) + (lane & 15), c0 + 16 * (wn * NB + j) + 4 * (lane >> 4), acc[i][j]);
+}
+constexpr int kLargeLds = 2 * 512 * kRow;
 
 // The splits' sums added up, in their order.
 template <typename T>

@@ -196,6 +196,23 @@ const void *const kWTiles[2][2] = {  // 64 x 64, 128 x 128
     {(const void *)&grad_w_tile_kernel<float, 2, 2, 2, 2>, (const void *)&grad_w_tile_kernel<float, 2, 4, 4, 2>},
     {(const void *)&grad_w_tile_kernel<__bf16, 2, 2, 2, 2>, (const void *)&grad_w_tile_kernel<__bf16, 2, 4, 4, 2>}};
 
+// Estimated us of the weights' gradient by tiles of a size, tm x tn of them (the last of 256 may be half empty) and splits of
+// `stages` stages: rounds on the compute units (two workgroups of the 128 x 128 kernel and four of the 64 x 64 one share a
+// unit), each of the stages' time and a start and an end.
+double w_estimate(int size, int64_t tm, int64_t tn, int64_t cin, int64_t splits, int64_t stages, bool f32)
+{
+    const double st = (double)stages;
+    if (size == 256) {
+        const int64_t half = cin % 256 != 0 && cin % 256 <= 128 ? 1 : 0, f = (tm * (tn - half) * splits + 7) / 8, h = (tm * half * splits + 7) / 8;
+        const int64_t rounds = (f + 31) / 32, spare = rounds * 32 - f;
+        const double t = (double)rounds + 0.6 * (double)((std::max<int64_t>(0, h - spare) + 31) / 32);
+        return t * (1.3 * st + 7.0);
+    }
+    const int64_t n = tm * tn * splits, fit = size == 128 ? 512 : 1024;
+    const double rounds = (double)(n / fit) + (n % fit ? std::max(0.55, (double)(n % fit) / (double)fit) : 0.0);
+    return rounds * (st * (size == 128 ? (f32 ? 4.0 : 1.25) : (f32 ? 2.1 : 0.75)) + 4.0);
+}
+
 GradLaunch grad_pick(const dsattn_linear_act_desc &d)
 {
     GradLaunch g;
@@ -253,15 +270,26 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
     g.bytes += aligned((size_t)((d.rows + g.part_rows - 1) / g.part_rows) * No * sizeof(float));
     // dW
     const int KS = kRow / (int)es;
-    const int64_t t128 = tiles(No, d.c_in, 128, 128), t64 = tiles(No, d.c_in, 64, 64), all = (d.rows + KS - 1) / KS;
-    const bool wide = t128 * std::max<int64_t>(1, all / 8) >= 384;
-    g.w_rows = g.w_cols = wide ? 128 : 64;
-    g.w_waves = wide ? 8 : 4;
+    const int64_t all = (d.rows + KS - 1) / KS;
+    double us = 1e30;
+    for (int size : {64, 128, 256}) {
+        if (size == 256 && f32) break;
+        const int64_t tm = (No + size - 1) / size, tn = (d.c_in + size - 1) / size;
+        for (int64_t splits = 1; splits <= std::min<int64_t>(64, std::max<int64_t>(1, all / 4)); ++splits) {
+            const int64_t stages = (all + splits - 1) / splits, used = (all + stages - 1) / stages;
+            if (used != splits) continue;
+            const double t = w_estimate(size, tm, tn, d.c_in, splits, stages, f32) +
+                             (splits > 1 ? 3.0 + 8e-6 * (double)(splits * No) * (double)d.c_in / 5.0 : 0.0);
+            if (t >= us) continue;
+            us = t;
+            g.w_rows = g.w_cols = size;
+            g.splits = (int)splits;
+            g.stages = (int)stages;
+        }
+    }
+    g.w_waves = g.w_rows == 64 ? 4 : 8;
     g.w_lds = 2 * (g.w_rows + g.w_cols) * kRow;
-    g.w_fn = kWTiles[!f32][wide];
-    const int64_t t = wide ? t128 : t64, want = std::max<int64_t>(1, std::min<int64_t>({512 / t, all / 8, 64}));
-    g.stages = (int)((all + want - 1) / want);
-    g.splits = (int)((all + g.stages - 1) / g.stages);
+    g.w_fn = g.w_rows == 256 ? (const void *)&grad_w_large_kernel : kWTiles[!f32][g.w_rows == 128];
     g.partial = g.bytes;
     if (g.splits > 1) g.bytes += aligned((size_t)g.splits * No * d.c_in * sizeof(float));
     return g;
@@ -349,8 +377,16 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         w.items = w.tiles * g.splits;
         w.per_xcd = (w.items + kXcds - 1) / kXcds;
         w.stages = g.stages;
+        unsigned groups = (unsigned)w.per_xcd * kXcds;
+        if (g.w_rows == 256) {
+            const int half = d.c_in % 256 != 0 && d.c_in % 256 <= 128 ? 1 : 0, tm = w.tiles / w.tiles_n;
+            w.whole = w.tiles_n - half;
+            w.whole_xcd = (tm * w.whole * g.splits + kXcds - 1) / kXcds;
+            w.rest_xcd = (tm * half * g.splits + kXcds - 1) / kXcds;
+            groups = (unsigned)(w.whole_xcd + w.rest_xcd) * kXcds;
+        }
         void *params[] = {&w};
-        launch(g.w_fn, dim3((unsigned)w.per_xcd * kXcds), 64 * g.w_waves, params, g.w_lds);
+        launch(g.w_fn, dim3(groups), 64 * g.w_waves, params, g.w_lds);
         if (g.splits > 1)
             launch(f32 ? (const void *)&grad_w_join_kernel<float> : (const void *)&grad_w_join_kernel<__bf16>,
                    dim3((unsigned)(((int64_t)No * d.c_in / 4 + 255) / 256)), 256, params, 0);
