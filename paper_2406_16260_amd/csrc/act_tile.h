@@ -329,42 +329,41 @@ __device__ __forceinline__ void act_slope_fast(float x, float &y, float &d)
 
 template <typename TO, bool GATED>
 constexpr int kGradBytes = (GATED ? 2 : 1) * 16 * (32 * (int)sizeof(TO) + (sizeof(TO) == 2 ? 8 : 16));
-template <typename T, int MB, int NB, bool GATED, typename TO, int ACT>
-__device__ __forceinline__ void epilogue_grad(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], int64_t m0, int c0,
-                                              const float *bias, unsigned char *stage, int lane)
+
+// the sum over 16 neighbouring lanes, in all of them
+template <int ROR>
+__device__ __forceinline__ float plus_turned(float v)
+{
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + ROR, 15, 15, false));
+}
+__device__ __forceinline__ float sum_of_16(float v) { return plus_turned<1>(plus_turned<2>(plus_turned<4>(plus_turned<8>(v)))); }
+
+// WHOLE: all of the part's rows and channels are there.  (Rows of Cout numbers are whole 16-byte pieces.)
+template <typename T, int MB, int NB, bool GATED, typename TO, int ACT, bool WHOLE>
+__device__ __forceinline__ void epilogue_grad_part(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], int64_t m0, int c0,
+                                                   const float *bias, unsigned char *stage, int lane)
 {
     constexpr int BS = 16, NO = GATED ? 2 : 1, ES = (int)sizeof(TO), NP = 2 * NO, CP = NB / NP;  // passes of a row block
     static_assert(Mul<T>::BS == BS && NB % NP == 0, "blocks of 16, whole passes");
     constexpr int SB = 32 * ES + (ES == 2 ? 8 : 16), PER = 16 / ES, CPR = 32 / PER, IT = 16 * CPR / 64;
-    constexpr int PASSES = MB * CP, AHEAD = 2;
+    constexpr int PASSES = MB * CP, AHEAD = PASSES < 4 ? PASSES : 4;
     typedef TO Piece __attribute__((ext_vector_type(PER)));
     typedef TO Quad __attribute__((ext_vector_type(4)));
     typedef uint32_t Half __attribute__((ext_vector_type(2)));
-    const int rl = lane % BS, cq = 4 * (lane / BS), ch = lane % CPR * PER;
+    const int rl = lane % BS, cq = 4 * (lane / BS), ch = lane % CPR * PER, row0 = lane / CPR;
     const int left_rows = (int)min(a.M - m0, (int64_t)(BS * MB)), left = a.Cout - c0;
-    if (left_rows <= 0) return;
-    const bool whole = a.Cout % PER == 0;
-    auto row_of = [&](int it) __attribute__((always_inline)) { return (lane + 64 * it) / CPR; };
     auto there = [&](int pass, int it) __attribute__((always_inline)) {
-        return pass / CP * BS + row_of(it) < left_rows && pass % CP * 32 + ch < left;
+        return WHOLE || (pass % MB * BS + row0 + 64 / CPR * it < left_rows && pass / MB * 32 + ch < left);
     };
     const TO *dy = (const TO *)a.R + m0 * a.Cout + c0;
     TO *dz = (TO *)a.Y + m0 * NO * a.Cout + c0;
+    const uint32_t from = (uint32_t)(row0 * a.Cout + ch), to = (uint32_t)(row0 * NO * a.Cout + ch);
     Piece r[AHEAD][IT];
     auto fetch = [&](int pass) __attribute__((always_inline)) {
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
             Piece x{};
-            if (there(pass, it)) {
-                const TO *from = dy + (int64_t)(pass / CP * BS + row_of(it)) * a.Cout + pass % CP * 32 + ch;
-                if (whole) {
-                    x = *(const Piece *)from;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < PER; ++e)
-                        if (pass % CP * 32 + ch + e < left) x[e] = from[e];
-                }
-            }
+            if (there(pass, it)) x = *(const Piece *)(dy + (int64_t)(pass % MB * BS + 64 / CPR * it) * a.Cout + pass / MB * 32 + from);
             r[pass % AHEAD][it] = x;
         }
     };
@@ -379,75 +378,80 @@ __device__ __forceinline__ void epilogue_grad(const ActArgs &a, const typename M
         return __builtin_bit_cast(Piece, (i32x4){(int)lo[0], (int)lo[1], (int)hi[0], (int)hi[1]});
     };
 #pragma unroll
-    for (int p = 0; p < AHEAD && p < PASSES; ++p) fetch(p);
-    f32x4 sum[CP][NP] = {};
+    for (int p = 0; p < AHEAD; ++p) fetch(p);
+    f32x4 sum[NP];
 #pragma unroll
     for (int pass = 0; pass < PASSES; ++pass) {
-        const int i = pass / CP, jp = pass % CP * NP;
+        const int i = pass % MB, jp = pass / MB * NP;  // (the rows of 32 channels one after the other: fewer sums at a time)
+        if (i == 0)
 #pragma unroll
-        for (int it = 0; it < IT; ++it) put_piece(stage + row_of(it) * SB + ch * ES, r[pass % AHEAD][it]);
+            for (int j = 0; j < NP; ++j) sum[j] = f32x4{};
+#pragma unroll
+        for (int it = 0; it < IT; ++it) put_piece(stage + (row0 + 64 / CPR * it) * SB + ch * ES, r[pass % AHEAD][it]);
         wave_sync();
         if (pass + AHEAD < PASSES) fetch(pass + AHEAD);
-        const bool live = BS * i + rl < left_rows;  // (rows past the end: a bias that is infinite would be NaN in the sums)
+        const bool live = WHOLE || BS * i + rl < left_rows;  // (rows past the end: a bias that is infinite would be NaN in the sums)
 #pragma unroll
         for (int j = 0; j < NP; j += NO) {
             unsigned char *at = stage + rl * SB + (BS * j / NO + cq) * ES;
-            Quad t0 = *(const Quad *)at, t1{};
+            const Quad g = *(const Quad *)at;
+            const f32x4 b0 = *(const f32x4 *)(bias + BS * (jp + j) + cq);
+            f32x4 b1{};
+            if constexpr (GATED) b1 = *(const f32x4 *)(bias + BS * (jp + j + 1) + cq);
+            Quad t0, t1{};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float g = live ? (float)t0[e] : 0.f;
-                const float z0 = acc[i][jp + j][e] + bias[BS * (jp + j) + cq + e];
+                const float z0 = acc[i][jp + j][e] + b0[e], gy = (float)g[e];
                 float y, d, dz0;
                 act_slope_fast<ACT>(z0, y, d);
                 if constexpr (GATED) {
-                    const float z1 = acc[i][jp + j + 1][e] + bias[BS * (jp + j + 1) + cq + e];
-                    dz0 = g * (z1 * d);
-                    const float dz1 = g * y;
+                    const float z1 = acc[i][jp + j + 1][e] + b1[e], dz1 = gy * y;
+                    dz0 = gy * (z1 * d);
                     t1[e] = (TO)dz1;
-                    sum[pass % CP][j + 1][e] += live ? dz1 : 0.f;
+                    sum[j + 1][e] += live ? dz1 : 0.f;
                 } else {
-                    dz0 = g * d;
+                    dz0 = gy * d;
                 }
                 t0[e] = (TO)dz0;
-                sum[pass % CP][j][e] += live ? dz0 : 0.f;
+                sum[j][e] += live ? dz0 : 0.f;
             }
             *(Quad *)at = t0;
             if constexpr (GATED) *(Quad *)(at + 16 * SB) = t1;
+#pragma unroll
+            for (int k = 0; k < NO; ++k) asm volatile("" : "+v"(sum[j + k]));  // (added now, not all at the end)
         }
         wave_sync();
 #pragma unroll
         for (int k = 0; k < NO; ++k)
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
-                const Piece x = get_piece(stage + k * (16 * SB) + row_of(it) * SB + ch * ES);
-                if (there(pass, it)) {
-                    const int c = pass % CP * 32 + ch;
-                    TO *to = dz + ((int64_t)(BS * i + row_of(it)) * NO + k) * a.Cout + c;
-                    if (whole) {
-                        *(Piece *)to = x;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < PER; ++e)
-                            if (c + e < left) to[e] = x[e];
-                    }
-                }
+                const Piece x = get_piece(stage + k * (16 * SB) + (row0 + 64 / CPR * it) * SB + ch * ES);
+                if (there(pass, it))
+                    *(Piece *)(dz + ((int64_t)(BS * i + 64 / CPR * it) * NO + k) * a.Cout + pass / MB * 32 + to) = x;
             }
         wave_sync();
-    }
-    if (!a.sums) return;
-    float *to = a.sums + (m0 / (BS * MB)) * NO * a.Cout + c0;
+        if (i == MB - 1 && a.sums) {
+            float *sums = a.sums + (m0 / (BS * MB)) * NO * a.Cout + c0;
 #pragma unroll
-    for (int p = 0; p < CP; ++p)
+            for (int j = 0; j < NP; ++j) {
+                f32x4 v;
 #pragma unroll
-        for (int j = 0; j < NP; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float v = sum[p][j][e];
-#pragma unroll
-                for (int w = 1; w < 16; w *= 2) v += __shfl_xor(v, w);
-                const int c = 32 * p + BS * (j / NO) + cq + e;
-                if (rl == 0 && c < left) to[(j % NO) * a.Cout + c] = v;
+                for (int e = 0; e < 4; ++e) v[e] = sum_of_16(sum[j][e]);
+                const int c = pass / MB * 32 + BS * (j / NO) + cq;
+                if (rl == 0 && c < left) *(f32x4 *)(sums + (j % NO) * a.Cout + c) = v;
             }
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (passes that the compiler draws into each other do not fit the registers)
+    }
+}
+template <typename T, int MB, int NB, bool GATED, typename TO, int ACT>
+__device__ __forceinline__ void epilogue_grad(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], int64_t m0, int c0,
+                                              const float *bias, unsigned char *stage, int lane)
+{
+    if (a.M - m0 >= 16 * MB && a.Cout - c0 >= 16 * NB / (GATED ? 2 : 1))
+        epilogue_grad_part<T, MB, NB, GATED, TO, ACT, true>(a, acc, m0, c0, bias, stage, lane);
+    else if (a.M > m0)
+        epilogue_grad_part<T, MB, NB, GATED, TO, ACT, false>(a, acc, m0, c0, bias, stage, lane);
 }
 
 // Small products: 32 rows of X by 32 rows of W a workgroup, whose eight wavefronts share the contraction: a wavefront takes

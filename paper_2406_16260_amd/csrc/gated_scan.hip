@@ -48,34 +48,36 @@ __device__ __forceinline__ float exp_minus_abs(float g)
     return fmaf(e, lo * 0.693147181f, e);
 }
 
-// What a gate keeps, a = sigmoid(g), and what it leaves, 1 - a: each with a small relative error.
+// What a gate keeps, a = sigmoid(g), what it leaves, 1 - a, and what it lets in, w(a): each with a small relative error.  (The
+// instructions for quotients and roots, an ulp off at most, not the sequences that round them, which took twice the time.)
+// 1 - a^2 is (1 - a) (1 + a), and its root is taken with e^(-|g| / 2) outside, so that it does not underflow before w does.
 struct Gate {
-    float keep, leave;
+    float keep, leave, let;
 };
+template <int MODE>
 __device__ __forceinline__ Gate gate_of(float g)
 {
-    const float e = exp_minus_abs(g), big = 1.f / (1.f + e), small = e * big;
-    return g >= 0.f ? Gate{big, small} : Gate{small, big};  // (a NaN: both are)
-}
-// sqrt((1 - a) f), f of ordinary size: the root of what is left, e^-g / (1 + e^-g), by e^(-g / 2), which does not underflow
-// until the root does
-__device__ __forceinline__ float root_left(const Gate &q, float g, float f)
-{
-    return g >= 0.f ? exp_minus_abs(0.5f * g) * sqrtf(q.keep * f) : sqrtf(q.leave * f);
-}
-template <int MODE>
-__device__ __forceinline__ float weight_of(const Gate &q, float g)
-{
-    if constexpr (MODE == DSATTN_SCAN_MEAN) return q.leave;
-    if constexpr (MODE == DSATTN_SCAN_NORM) return root_left(q, g, 1.f + q.keep);
-    return 1.f;
+    const bool open = g >= 0.f;  // (a NaN: no, and all are NaN)
+    Gate q;
+    if constexpr (MODE == DSATTN_SCAN_NORM) {
+        const float h = exp_minus_abs(0.5f * g), e = h * h, big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
+        q.keep = open ? big : small;
+        q.leave = open ? small : big;
+        q.let = __builtin_amdgcn_sqrtf(fmaf(big, q.keep, big)) * (open ? h : 1.f);
+    } else {
+        const float e = exp_minus_abs(g), big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
+        q.keep = open ? big : small;
+        q.leave = open ? small : big;
+        q.let = MODE == DSATTN_SCAN_MEAN ? q.leave : 1.f;
+    }
+    return q;
 }
 // dw / dg
 template <int MODE>
-__device__ __forceinline__ float weight_slope_of(const Gate &q, float g)
+__device__ __forceinline__ float slope_of(const Gate &q)
 {
     if constexpr (MODE == DSATTN_SCAN_MEAN) return -q.keep * q.leave;
-    if constexpr (MODE == DSATTN_SCAN_NORM) return -q.keep * q.keep * root_left(q, g, 1.f / (1.f + q.keep));
+    if constexpr (MODE == DSATTN_SCAN_NORM) return -q.keep * q.keep * q.let * __builtin_amdgcn_rcpf(1.f + q.keep);
     return 0.f;
 }
 
@@ -163,8 +165,8 @@ __global__ __launch_bounds__(256) void scan_kernel(const ScanArgs a)
             Piece y;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Gate q = gate_of((float)gc[i][v]);
-                h[v] = fmaf(q.keep, h[v], weight_of<MODE>(q, (float)gc[i][v]) * (float)xc[i][v]);
+                const Gate q = gate_of<MODE>((float)gc[i][v]);
+                h[v] = fmaf(q.keep, h[v], q.let * (float)xc[i][v]);
                 if constexpr (STORE)
                     y[v] = (T)h[v];
                 else
@@ -211,7 +213,7 @@ __global__ __launch_bounds__(256) void scan_back_parts_kernel(const ScanArgs a)
             constexpr int i = decltype(at)::value;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float keep = gate_of((float)g[i][v]).keep;
+                const float keep = gate_of<DSATTN_SCAN_SUM>((float)g[i][v]).keep;
                 c[v] = keep * (c[v] + (float)dy[i][v]);
                 prod[v] *= keep;
             }
@@ -268,21 +270,21 @@ __global__ __launch_bounds__(256) void scan_back_kernel(const ScanArgs a)
         for (int i = 0; i + 1 < kStep; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Gate q = gate_of((float)gc[i][v]);
-                h[i + 1][v] = fmaf(q.keep, h[i][v], weight_of<MODE>(q, (float)gc[i][v]) * (float)xc[i][v]);  // (past the end: not used)
+                const Gate q = gate_of<MODE>((float)gc[i][v]);
+                h[i + 1][v] = fmaf(q.keep, h[i][v], q.let * (float)xc[i][v]);  // (past the end: not used)
             }
         frames_back(t, p.t1, [&](auto at) __attribute__((always_inline)) {
             constexpr int i = decltype(at)::value;
             Piece dx, dg;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Gate q = gate_of((float)gc[i][v]);
+                const Gate q = gate_of<MODE>((float)gc[i][v]);
                 const float d = c[v] + (float)dc[i][v];
-                dx[v] = (T)(d * weight_of<MODE>(q, (float)gc[i][v]));
+                dx[v] = (T)(d * q.let);
                 if constexpr (MODE == DSATTN_SCAN_MEAN)  // the two slopes differ in sign only
                     dg[v] = (T)(d * (q.keep * q.leave) * (h[i][v] - (float)xc[i][v]));
                 else
-                    dg[v] = (T)(d * fmaf(q.keep * q.leave, h[i][v], weight_slope_of<MODE>(q, (float)gc[i][v]) * (float)xc[i][v]));
+                    dg[v] = (T)(d * fmaf(q.keep * q.leave, h[i][v], slope_of<MODE>(q) * (float)xc[i][v]));
                 c[v] = q.keep * d;
             }
             *(Piece *)((T *)a.Y + base + (int64_t)(t + i) * a.n) = dx;
@@ -356,17 +358,22 @@ int scan_validate(const dsattn_scan_desc *desc, const char *who)
     return DSATTN_OK;
 }
 
-// Channels of a lane: four bytes, or one where a frame is an odd number of 16-bit ones.
+// Channels of a lane: four bytes, or one 16-bit one where a frame is an odd number of them or two a lane would make less than
+// 512 wavefronts (a lane's steps take twice the time then: 384 frames x 100 x 640 69 us, by ones 42).
 int scan_lane(const dsattn_scan_desc &d)
 {
-    return d.io_dtype == DSATTN_BF16 && (int64_t)d.spatial * d.channels % 2 == 0 ? 2 : 1;
+    const int64_t n = (int64_t)d.spatial * d.channels;
+    return d.io_dtype == DSATTN_BF16 && n % 2 == 0 && n * d.streams >= 512 * 128 ? 2 : 1;
 }
 
-// Chunks of a stream: as many as make 2,048 wavefronts, of at least 64 frames each.
+// Chunks of a stream.  From 512 wavefronts on one pass keeps enough loads on their way; below, chunks read their inputs twice,
+// but as many as make 4,096 wavefronts (2 x 16,384 x 1,280: 127 us with 2,048, 104, 101 with 8,192, 275 before), of 32 frames
+// or more (1 x 255 x 640, bf16: 37 us in one chunk, 18.5).
 void scan_chunks(const dsattn_scan_desc &d, int32_t &chunk, int32_t &chunks)
 {
     const int64_t n = (int64_t)d.spatial * d.channels, lanes = (n + scan_lane(d) - 1) / scan_lane(d);
-    const int64_t waves = std::max<int64_t>(1, (lanes + 63) / 64 * d.streams), want = std::min<int64_t>(2048 / waves, d.frames / 64);
+    const int64_t waves = std::max<int64_t>(1, (lanes + 63) / 64 * d.streams);
+    const int64_t want = waves >= 512 ? 1 : std::min<int64_t>(4096 / waves, d.frames / 32);
     chunk = d.frames;
     chunks = 1;
     if (want >= 4) {
@@ -392,6 +399,22 @@ const void *scan_kernel_of(int pass)
     case kRunPass: return (const void *)&scan_kernel<T, V, MODE, true>;
     case kBackPartsPass: return (const void *)&scan_back_parts_kernel<T, V>;
     default: return (const void *)&scan_back_kernel<T, V, MODE>;
+    }
+}
+// One pass over many channels: eight bytes a lane (384 frames x 640 x 640, bf16, 4.7 TB/s instead of 4.45).
+const void *scan_wide_of(const dsattn_scan_desc &d)
+{
+    if (d.io_dtype == DSATTN_F32) {
+        switch (d.mode) {
+        case DSATTN_SCAN_MEAN: return (const void *)&scan_kernel<float, 2, DSATTN_SCAN_MEAN, true>;
+        case DSATTN_SCAN_NORM: return (const void *)&scan_kernel<float, 2, DSATTN_SCAN_NORM, true>;
+        default: return (const void *)&scan_kernel<float, 2, DSATTN_SCAN_SUM, true>;
+        }
+    }
+    switch (d.mode) {
+    case DSATTN_SCAN_MEAN: return (const void *)&scan_kernel<__bf16, 4, DSATTN_SCAN_MEAN, true>;
+    case DSATTN_SCAN_NORM: return (const void *)&scan_kernel<__bf16, 4, DSATTN_SCAN_NORM, true>;
+    default: return (const void *)&scan_kernel<__bf16, 4, DSATTN_SCAN_SUM, true>;
     }
 }
 template <typename T, int V>
@@ -427,12 +450,19 @@ int scan_setup(const dsattn_scan_desc &d, const char *who, ScanArgs &a, void *wo
 
 int scan_launch(const dsattn_scan_desc &d, const char *who, ScanArgs &a, bool back, hipStream_t st)
 {
-    const int V = scan_lane(d), parts = back ? kBackPartsPass : kPartsPass, run = back ? kBackPass : kRunPass;
+    int V = scan_lane(d);
+    const int parts = back ? kBackPartsPass : kPartsPass, run = back ? kBackPass : kRunPass;
     auto fn = [&](int pass) {
         return d.io_dtype == DSATTN_F32 ? scan_kernel_of<float, 1>(d.mode, pass)
                : V == 2                 ? scan_kernel_of<__bf16, 2>(d.mode, pass)
                                         : scan_kernel_of<__bf16, 1>(d.mode, pass);
     };
+    const void *runner = fn(run);
+    const int wide = 2 * (d.io_dtype == DSATTN_F32 ? 1 : 2);
+    if (!back && a.chunks == 1 && a.n % wide == 0 && a.n / wide * a.B >= 64 * 1024) {
+        V = wide;
+        runner = scan_wide_of(d);
+    }
     const dim3 grid((unsigned)(((a.n + V - 1) / V + 255) / 256), (unsigned)a.chunks, (unsigned)a.B);
     void *params[] = {&a};
     hipError_t e = hipSuccess;
@@ -441,7 +471,7 @@ int scan_launch(const dsattn_scan_desc &d, const char *who, ScanArgs &a, bool ba
         const void *join = back ? (const void *)&scan_join_kernel<true> : (const void *)&scan_join_kernel<false>;
         if (e == hipSuccess) e = hipLaunchKernel(join, dim3((unsigned)((a.n + 15) / 16), (unsigned)a.B), dim3(1024), params, 0, st);
     }
-    if (e == hipSuccess) e = hipLaunchKernel(fn(run), grid, dim3(256), params, 0, st);
+    if (e == hipSuccess) e = hipLaunchKernel(runner, grid, dim3(256), params, 0, st);
     if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
     return DSATTN_OK;
 }
