@@ -10,6 +10,13 @@
 namespace dsattn {
 namespace {
 
+// Column sums of parts of the rows, to be added up: by workgroups of their own behind those of another kernel.
+struct JoinArgs {
+    const float *sums;  // [parts][No]
+    float *db[2];       // [Cout] each, or null
+    int32_t parts, Cout, No, groups;  // groups: workgroups, of 16 columns each
+};
+
 struct GradWArgs {
     const void *dz, *X;  // [M][No], [M][Cin]
     void *dW[2];         // [Cout][Cin] each, or null
@@ -18,6 +25,8 @@ struct GradWArgs {
     int32_t Cin, Cout, No;               // No: n_w Cout
     int32_t tiles_n, tiles, items, per_xcd;  // column tiles (of X); all; tiles * splits; ceil(items / 8)
     int32_t stages;                      // of a split
+    int32_t groups;                      // workgroups of the product; those behind join the column sums
+    JoinArgs join;
     int32_t whole, whole_xcd, rest_xcd;  // 256 x 256 tiles: column tiles that are not half empty; items of an XCD of those and of the others
 };
 
@@ -35,13 +44,13 @@ template <typename T, int W>
 struct Cols {
     static constexpr int ES = (int)sizeof(T), KS = kRow / ES, RB = W * ES, CPR = RB / 16, PER = 16 / ES;
     static constexpr int RPI = 64 / CPR;  // rows of a load instruction
-    static_assert(CPR * RPI == 64 && (ES == 2 ? CPR >= 8 : CPR >= 16), "whole rows");
+    static_assert(CPR * RPI == 64 && (ES == 2 ? CPR >= 4 : CPR >= 8), "whole rows");
     using Frag = typename Mul<T>::Frag;
     // where chunk c of row k lies: position c ^ swizzle(k)
     static __device__ __forceinline__ int swizzle(int k)
     {
-        if constexpr (ES == 4) return 4 * ((k >> 2) & 3);
-        return 2 * (CPR >= 16 ? (k & 3) | ((k >> 1) & 4) : k & 3);
+        if constexpr (ES == 4) return 4 * ((k >> 2) & (CPR >= 16 ? 3 : 1));
+        return 2 * (CPR >= 16 ? (k & 3) | ((k >> 1) & 4) : CPR == 8 ? k & 3 : (k >> 1) & 1);
     }
     // a lane's place within row 0 of a fragment of columns 16 blk .., and the row (of the first read)
     static __device__ __forceinline__ int row(int lane) { return ES == 4 ? 4 * (lane >> 4) : 8 * (lane >> 4) + ((lane & 15) >> 2); }
@@ -92,6 +101,31 @@ __device__ __forceinline__ void grad_w_store(const GradWArgs &a, int split, bool
     *(Quad *)(to + (int64_t)(o < a.Cout ? o : o - a.Cout) * a.Cin + c) = q;
 }
 
+// 16 columns a workgroup; `part`: 16 floats for every 16 threads and one more.
+template <int THREADS>
+__device__ __forceinline__ void join_columns(const JoinArgs &a, int block, float *part)
+{
+    constexpr int W = THREADS / 16;
+    const int l = threadIdx.x & 15, w = threadIdx.x >> 4, c = block * 16 + l;
+    float v = 0.f;
+    if (c < a.No)
+#pragma unroll 8
+        for (int p = w; p < a.parts; p += W) v += a.sums[(int64_t)p * a.No + c];
+    part[w * 17 + l] = v;
+    __syncthreads();
+    for (int h = W / 2; h > 0; h >>= 1) {
+        if (w < h) part[w * 17 + l] += part[(w + h) * 17 + l];
+        __syncthreads();
+    }
+    float *to = c < a.Cout ? a.db[0] : a.db[1];
+    if (w == 0 && c < a.No && to) to[c < a.Cout ? c : c - a.Cout] = part[l];
+}
+__global__ __launch_bounds__(1024) void grad_join_kernel(const JoinArgs a)
+{
+    __shared__ float part[64 * 17];
+    join_columns<1024>(a, (int)blockIdx.x, part);
+}
+
 // One tile of one split a workgroup, two LDS slots, two workgroups on a compute unit.
 template <typename T, int MB, int NB, int WVM, int WVN>
 __global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const GradWArgs a)
@@ -105,6 +139,7 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const Gr
     constexpr int ABYTES = BM * kRow, BUF = (BM + BN) * kRow;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     // workgroup -> split and tile: XCD x (= blockIdx % 8) owns a contiguous run of items, the tiles of a split one after the other
+    if ((int)blockIdx.x >= a.groups) return join_columns<64 * NW>(a.join, (int)blockIdx.x - a.groups, (float *)smem);
     const int item = (int)(blockIdx.x % kXcds) * a.per_xcd + (int)(blockIdx.x / kXcds);
     if (item >= a.items) return;  // whole workgroup: no barrier has been reached yet
     const int split = item / a.tiles, tile = item - split * a.tiles;
@@ -179,6 +214,100 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const Gr
             grad_w_store<T>(a, split, parts, o0 + 16 * (wm * MB + i) + (lane & 15), c0 + 16 * (wn * NB + j) + 4 * (lane >> 4), acc[i][j]);
 }
 
+// dz of many rows: tiles of 256 rows of X by 128 of W, four wavefronts with 64 x 128 each, two workgroups on a compute unit.  The
+// epilogue, 30 vector instructions for each number of a gated dz, takes as long as the multiplies; with two wavefronts of
+// different workgroups on a SIMD the one's runs under the other's.  (The product's persistent kernel, whose wavefronts are all
+// at the same place, takes 400 us for 40,960 x 640 x 2 x 2,560, GELU.)  Stages of 64 bytes of a row, three LDS slots: a stage's loads
+// have two stages to arrive.  Chunk c of row r lies at position c ^ r / 2 % 4.
+template <bool GATED, int ACT>
+__global__ __launch_bounds__(256, 2) void grad_dz_large_kernel(const ActArgs a)
+{
+    using T = __bf16;
+    using M = Mul<T>;
+    constexpr int BS = 16, MB = 4, NB = 8, BM = 256, BN = 128, RB = 64, G = 4, H = 2;  // load instructions of a wavefront
+    constexpr int ABYTES = BM * RB, SLOT = (BM + BN) * RB, BO = GATED ? BN / 2 : BN;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    __shared__ __attribute__((aligned(16))) float cols[BN];
+    // workgroup -> tile: XCD x (= blockIdx % 8) owns a contiguous run of tiles, numbered in panels of a.panel column tiles
+    const int tile = (int)(blockIdx.x % kXcds) * a.per_xcd + (int)(blockIdx.x / kXcds);
+    if (tile >= a.tiles || (int)(blockIdx.x / kXcds) >= a.per_xcd) return;  // whole workgroup: no barrier has been reached yet
+    const int tiles_m = a.tiles / a.tiles_n, row = tile / a.panel, pn = row / tiles_m, mt = row - pn * tiles_m;
+    const int64_t m0 = (int64_t)mt * BM;
+    const int n0 = (pn * a.panel + tile - row * a.panel) * BO;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rowbytes = a.Cin * 2, stages = (rowbytes + RB - 1) / RB;
+    const int lr = lane >> 2, lc = (lane & 3) ^ ((lr >> 1) & 3);
+    const __amdgpu_buffer_rsrc_t xres = rows_from(a.X, m0, a.M, rowbytes);
+    const __amdgpu_buffer_rsrc_t wres0 = rows_from(a.W[0], n0, a.Cout, rowbytes);
+    const __amdgpu_buffer_rsrc_t wres1 = GATED ? rows_from(a.W[1], n0, a.Cout, rowbytes) : wres0;
+    const uint32_t xoff = (uint32_t)((wv * (16 * G) + lr) * rowbytes + lc * 16);
+    uint32_t woff[H];
+#pragma unroll
+    for (int l = 0; l < H; ++l) woff[l] = (uint32_t)((channel_of<BS, GATED>(wv * (16 * H) + 16 * l) + lr) * rowbytes + lc * 16);
+    auto issue_stage = [&](int ks, int slot) __attribute__((always_inline)) {
+        const bool live = ks * RB + lc * 16 < rowbytes;
+        unsigned char *as = smem + slot * SLOT + wv * (G * 1024), *bs = smem + slot * SLOT + ABYTES + wv * (H * 1024);
+#pragma unroll
+        for (int l = 0; l < G; ++l)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xres, (__attribute__((address_space(3))) void *)(as + l * 1024), 16,
+                                                     live ? xoff + (uint32_t)(16 * l * rowbytes + ks * RB) : kOob, 0, 0, 0);
+#pragma unroll
+        for (int l = 0; l < H; ++l) {
+            const uint32_t off = live ? woff[l] + (uint32_t)(ks * RB) : kOob;
+            if (GATED && l == 1)  // (blocks of 16 rows of the gate and of the value by turns)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(wres1, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16, (uint32_t)off, 0, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(wres0, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16, (uint32_t)off, 0, 0, 0);
+        }
+    };
+    issue_stage(0, 0);
+    if (stages > 1) issue_stage(1, 1);
+    if (threadIdx.x < BN) {
+        float b, s;
+        column<BS, GATED, false>(a, n0, threadIdx.x, b, s);
+        cols[threadIdx.x] = b;
+    }
+    typename M::Acc acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = typename M::Acc{};
+    const int l16 = lane & 15, at = l16 * RB + (((lane >> 4) ^ ((l16 >> 1) & 3)) * 16);
+    int slot = 0, fill = 2;
+    for (int ks = 0; ks < stages; ++ks) {
+        // this wavefront's loads of stage ks have landed (the next stage's may be on their way), and its reads of stage ks - 1,
+        // whose slot stage ks + 2 goes into, are done; behind the barrier everybody's are
+        asm volatile("" ::: "memory");
+        if (ks + 1 < stages)
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(G + H));
+        else
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if (ks + 2 < stages) issue_stage(ks + 2, fill);
+        const unsigned char *ab = smem + slot * SLOT + wv * (16 * MB * RB) + at, *bb = smem + slot * SLOT + ABYTES + at;
+        typename M::Frag af[MB], bf[NB];
+#pragma unroll
+        for (int i = 0; i < MB; ++i) af[i] = *(const bf16x8 *)(ab + i * (16 * RB));
+#pragma unroll
+        for (int j = 0; j < NB; ++j) bf[j] = *(const bf16x8 *)(bb + j * (16 * RB));
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int i = 0; i < MB; ++i) acc[i][j] = M::mul(bf[j], af[i], acc[i][j]);
+        slot = slot == 2 ? 0 : slot + 1;
+        fill = fill == 2 ? 0 : fill + 1;
+    }
+    // everybody is through with the ring: it becomes the staging area
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    epilogue_grad<T, MB, NB, GATED, T, ACT>(a, acc, m0 + wv * (16 * MB), n0, cols, smem + wv * kGradBytes<T, GATED>, lane);
+}
+constexpr int kDzLargeLds = 3 * 384 * 64;
+
 // Large ones: 256 x 256 tiles, eight wavefronts (two per SIMD) whose parts are 64 columns of dz by 128 of X.  Two LDS slots; the
 // multiplies of a stage run in halves (columns of dz [0, 32), then [32, 64) of a part) over one set of fragments that is refilled in
 // place, and LDS reads and the loads of the next stage but one sit between the matrix instructions by hand, as in the
@@ -192,6 +321,7 @@ __global__ __launch_bounds__(512, 2) void grad_w_large_kernel(const GradWArgs a)
     constexpr int MB = 4, NB = 8, KS = K::KS, G = 4, NL = 2 * G;
     constexpr int ABYTES = 256 * kRow, SLOT = 2 * ABYTES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    if ((int)blockIdx.x >= a.groups) return join_columns<512>(a.join, (int)blockIdx.x - a.groups, (float *)smem);
     // workgroup -> item: every XCD has a run of the items of whole tiles, and then one of the others
     const int xcd = (int)(blockIdx.x % kXcds), idx = (int)(blockIdx.x / kXcds), tiles_m = a.tiles / a.tiles_n;
     const int splits = a.items / a.tiles;
@@ -376,6 +506,115 @@ __global__ __launch_bounds__(256) void grad_w_join_kernel(const GradWArgs a)
     *(Quad *)(to + (i < half ? i : i - half)) = q;
 }
 
+// dX of few rows: dX = sum dz_k W_k, 32 x 32 a workgroup, whose eight wavefronts share the contraction as in act_small_kernel
+// (a wavefront takes every eighth stage through two LDS slots of its own).  W's rows are what is contracted over, and are
+// read transposed; stages do not cross from one set to the other.  160 x 1,280 x 1,280: GRAD_X_SMALL_US; turned by a kernel of its own
+// first 3.4 + 5.1 us.
+struct GradXArgs {
+    const void *dz;  // [M][No]
+    const void *W[2];
+    void *dX;
+    int64_t M;
+    int32_t Cin, Cout, No, tiles_n;
+};
+template <typename T>
+__global__ __launch_bounds__(512, 2) void grad_x_small_kernel(const GradXArgs a)
+{
+    using M = Mul<T>;
+    using B = Cols<T, 32>;
+    constexpr int NW = 8, SR = 36, SLOT = 64 * kRow, KS = B::KS;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const int mt = (int)blockIdx.x / a.tiles_n;
+    const int64_t m0 = (int64_t)mt * 32;
+    const int n0 = ((int)blockIdx.x - mt * a.tiles_n) * 32;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int zbytes = a.No * B::ES, xbytes = a.Cin * B::ES, setbytes = a.Cout * B::ES;
+    const __amdgpu_buffer_rsrc_t zres = rows_from(a.dz, m0, a.M, zbytes);
+    unsigned char *mem = smem + wv * (2 * SLOT);
+    const int lr = lane >> 3, lc = (lane & 7) ^ lr;
+    const uint32_t zoff = (uint32_t)(lr * zbytes + lc * 16), next = (uint32_t)(8 * zbytes);
+    uint32_t woff[4];
+#pragma unroll
+    for (int l = 0; l < 4; ++l) {
+        const int r = l * B::RPI + lane / B::CPR, c = (lane % B::CPR) ^ B::swizzle(r);
+        woff[l] = n0 + c * B::PER < a.Cin ? (uint32_t)(r * xbytes + c * 16) : kOob;
+    }
+    const int per = (a.Cout + KS - 1) / KS, stages = a.No / a.Cout * per;  // of a set, of all
+    auto issue = [&](int ks, int slot) __attribute__((always_inline)) {
+        const int set = ks >= per ? 1 : 0, k = ks - set * per;
+        const bool live = k * kRow + lc * 16 < setbytes;
+        const uint32_t o = zoff + (uint32_t)(set * setbytes + k * kRow);
+        const __amdgpu_buffer_rsrc_t wres = cols_from(set ? a.W[1] : a.W[0], (int64_t)k * KS, a.Cout, xbytes, n0 * B::ES);
+#pragma unroll
+        for (int l = 0; l < 4; ++l) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(zres, (__attribute__((address_space(3))) void *)(mem + slot * SLOT + l * 1024), 16,
+                                                     live ? o + l * next : kOob, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wres, (__attribute__((address_space(3))) void *)(mem + slot * SLOT + 4096 + l * 1024), 16,
+                                                     (uint32_t)woff[l], 0, 0, 0);
+        }
+    };
+    f32x4 acc[2][2] = {};
+    int koff[2], wp[2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) koff[kk] = M::offset(lane, kk);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) wp[j] = 4096 + B::row(lane) * B::RB + B::place(lane, j);
+    if (wv < stages) issue(wv, 0);
+    int slot = 0;
+    for (int ks = wv; ks < stages; ks += NW) {
+        const bool more = ks + NW < stages;
+        if (more) issue(ks + NW, slot ^ 1);
+        asm volatile("" ::: "memory");
+        if (more)
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(8));  // all but the stage just asked for have landed
+        else
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        const unsigned char *buf = mem + slot * SLOT;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            typename M::Frag x[2], w[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                x[i] = M::read(buf + l16 * kRow + i * (16 * kRow), koff[kk]);
+                w[i] = B::read(buf + kk * (KS / 2 * B::RB) + wp[i]);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[i][j] = M::mul(w[j], x[i], acc[i][j]);
+        }
+        // the slot's reads are done before it is asked to be filled again
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // (LDS operations only)
+        asm volatile("" ::: "memory");
+        slot ^= 1;
+    }
+    // the sums, in the place of the wavefront's slots
+    float(*sums)[32][SR] = (float(*)[32][SR])smem;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *(f32x4 *)&sums[wv][16 * i + l16][16 * j + 4 * lg] = acc[i][j];
+    __syncthreads();
+    const int row = (int)threadIdx.x >> 4, c = 2 * ((int)threadIdx.x & 15);
+    const int64_t m = m0 + row;
+    if (m >= a.M || n0 + c >= a.Cin) return;
+    typedef T Pair __attribute__((ext_vector_type(2)));  // (Cin is even)
+    Pair y;
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+        float z = 0.f;
+#pragma unroll
+        for (int v = 0; v < NW; ++v) z += sums[v][row][c + o];
+        y[o] = (T)z;
+    }
+    *(Pair *)((T *)a.dX + m * a.Cin + n0 + c) = y;
+}
+
 // W_0 and W_1 below each other, transposed: [Cin][n_w Cout].  64 x 64 tiles through LDS.
 template <typename T>
 __global__ __launch_bounds__(256) void grad_turn_kernel(const void *W0, const void *W1, void *Wt, int Cin, int Cout, int No)
@@ -437,25 +676,6 @@ __global__ __launch_bounds__(256) void grad_sums_kernel(const void *dz, int64_t 
 #pragma unroll
     for (int q = 0; q < 16; ++q) t += part[q][threadIdx.x];
     sums[(int64_t)blockIdx.y * No + cc] = t;
-}
-
-// The parts' column sums added up: 16 columns a workgroup, 64 threads to each.
-__global__ __launch_bounds__(1024) void grad_join_kernel(const float *sums, int parts, int Cout, int No, float *db0, float *db1)
-{
-    __shared__ float part[64][17];
-    const int l = threadIdx.x & 15, w = threadIdx.x >> 4, c = (int)blockIdx.x * 16 + l;
-    float v = 0.f;
-    if (c < No)
-#pragma unroll 4
-        for (int p = w; p < parts; p += 64) v += sums[(int64_t)p * No + c];
-    part[w][l] = v;
-    __syncthreads();
-    for (int h = 32; h > 0; h >>= 1) {
-        if (w < h) part[w][l] += part[w + h][l];
-        __syncthreads();
-    }
-    float *to = c < Cout ? db0 : db1;
-    if (w == 0 && c < No && to) to[c < Cout ? c : c - Cout] = part[0][l];
 }
 
 }  // namespace

@@ -163,8 +163,9 @@ struct GradLaunch {
     bool tiles = false;                         // on the matrix cores
     const void *dz_fn = nullptr;                // kernel of dz; null: dz is dY
     int dz_rows, dz_cols, dz_waves, dz_lds;     // its tile, wavefronts and bytes of LDS
-    bool dz_stream, dz_small;
+    bool dz_large, dz_small;
     int part_rows;                              // rows of a part of the column sums
+    bool x_small;                               // dX by the kernel for few rows; else W is turned for a product
     const void *w_fn;                           // kernel of dW
     int w_rows, w_cols, w_waves, w_lds, splits, stages;
     size_t dz, turned, sums, partial, bytes;    // places in the workspace, and its size
@@ -185,12 +186,12 @@ const GradVariant kDzTiles[2][2] = {{DSATTN_GRAD_TILE(float, 2, 4, 4, 2), DSATTN
 const void *const kDzSmall[2][2] = {
     {(const void *)&act_small_kernel<float, false, float, true>, (const void *)&act_small_kernel<float, true, float, true>},
     {(const void *)&act_small_kernel<__bf16, false, __bf16, true>, (const void *)&act_small_kernel<__bf16, true, __bf16, true>}};
-#define DSATTN_GRAD_STREAM(G, ACT) (const void *)&act_stream_kernel<__bf16, 4, 8, G, __bf16, ACT, true>
-const void *const kDzStream[2][DSATTN_ACT_SILU + 1] = {
-    {nullptr, DSATTN_GRAD_STREAM(false, DSATTN_ACT_RELU), DSATTN_GRAD_STREAM(false, DSATTN_ACT_GELU),
-     DSATTN_GRAD_STREAM(false, DSATTN_ACT_GELU_TANH), DSATTN_GRAD_STREAM(false, DSATTN_ACT_SILU)},
-    {DSATTN_GRAD_STREAM(true, DSATTN_ACT_NONE), DSATTN_GRAD_STREAM(true, DSATTN_ACT_RELU), DSATTN_GRAD_STREAM(true, DSATTN_ACT_GELU),
-     DSATTN_GRAD_STREAM(true, DSATTN_ACT_GELU_TANH), DSATTN_GRAD_STREAM(true, DSATTN_ACT_SILU)}};
+#define DSATTN_GRAD_LARGE(G, ACT) (const void *)&grad_dz_large_kernel<G, ACT>
+const void *const kDzLarge[2][DSATTN_ACT_SILU + 1] = {
+    {nullptr, DSATTN_GRAD_LARGE(false, DSATTN_ACT_RELU), DSATTN_GRAD_LARGE(false, DSATTN_ACT_GELU),
+     DSATTN_GRAD_LARGE(false, DSATTN_ACT_GELU_TANH), DSATTN_GRAD_LARGE(false, DSATTN_ACT_SILU)},
+    {DSATTN_GRAD_LARGE(true, DSATTN_ACT_NONE), DSATTN_GRAD_LARGE(true, DSATTN_ACT_RELU), DSATTN_GRAD_LARGE(true, DSATTN_ACT_GELU),
+     DSATTN_GRAD_LARGE(true, DSATTN_ACT_GELU_TANH), DSATTN_GRAD_LARGE(true, DSATTN_ACT_SILU)}};
 
 const void *const kWTiles[2][2] = {  // 64 x 64, 128 x 128
     {(const void *)&grad_w_tile_kernel<float, 2, 2, 2, 2>, (const void *)&grad_w_tile_kernel<float, 2, 4, 4, 2>},
@@ -230,7 +231,7 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
     g.tiles = true;
     // dz
     const int64_t stages = (rowbytes + kRow - 1) / kRow;
-    g.dz_stream = g.dz_small = false;
+    g.dz_large = g.dz_small = false;
     g.part_rows = 256;
     if (!grad_is_dy(d)) {
         g.part_rows = 32;
@@ -244,11 +245,12 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
         } else if (!f32 && tile_estimate(256, tiles(d.rows, No, 256, 256), stages) <
                                std::min(tile_estimate(128, tiles(d.rows, No, 128, 128), stages),
                                         tile_estimate(64, tiles(d.rows, No, 64, 64), stages))) {
-            g.dz_stream = true;
-            g.dz_fn = kDzStream[gated][d.act];
-            g.dz_rows = g.dz_cols = 256;
-            g.dz_waves = 8;
-            g.dz_lds = kStreamLds;
+            g.dz_large = true;
+            g.dz_fn = kDzLarge[gated][d.act];
+            g.dz_rows = 256;
+            g.dz_cols = 128;
+            g.dz_waves = 4;
+            g.dz_lds = kDzLargeLds;
             g.part_rows = 64;
         } else {
             if (f32 ? tiles(d.rows, No, 128, 128) < 384
@@ -264,8 +266,9 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
         g.dz = g.bytes;
         g.bytes += aligned((size_t)d.rows * No * es);
     }
+    g.x_small = small_is_faster(d.io_dtype, tiles(d.rows, d.c_in, 32, 32), (No * es + kRow - 1) / kRow);
     g.turned = g.bytes;
-    g.bytes += aligned((size_t)No * d.c_in * es);
+    if (!g.x_small) g.bytes += aligned((size_t)No * d.c_in * es);
     g.sums = g.bytes;
     g.bytes += aligned((size_t)((d.rows + g.part_rows - 1) / g.part_rows) * No * sizeof(float));
     // dW
@@ -295,7 +298,7 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
     return g;
 }
 
-// The kernels one after the other: dz with its parts of the column sums, those joined, W turned, dX, dW.
+// The kernels one after the other: dz with its parts of the column sums, W turned, dX, dW with the sums joined behind it.
 int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const GradArgs &a, const char *who, char *space, hipStream_t st)
 {
     const int No = d.n_w * d.c_out;
@@ -327,14 +330,9 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         z.tiles_n = (d.c_out + cols - 1) / cols;
         z.tiles = (int32_t)((d.rows + g.dz_rows - 1) / g.dz_rows) * z.tiles_n;
         z.per_xcd = (z.tiles + kXcds - 1) / kXcds;
-        z.panel = act_panel(z.tiles_n);
-        int dev = 0, per_xcd = z.per_xcd;
-        if (g.dz_stream) {
-            e = hipGetDevice(&dev);
-            per_xcd = std::min(per_xcd, (compute_units(dev) + kXcds - 1) / kXcds);
-        }
+        z.panel = g.dz_large ? act_panel(z.tiles_n) : 1;
         void *params[] = {&z};
-        launch(g.dz_fn, dim3(g.dz_small ? (unsigned)z.tiles : (unsigned)per_xcd * kXcds), 64 * g.dz_waves, params, g.dz_lds);
+        launch(g.dz_fn, dim3(g.dz_small ? (unsigned)z.tiles : (unsigned)z.per_xcd * kXcds), 64 * g.dz_waves, params, g.dz_lds);
     } else if (sums) {
         const void *dz = a.dz;
         int64_t M = d.rows;
@@ -343,13 +341,17 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         launch(f32 ? (const void *)&grad_sums_kernel<float> : (const void *)&grad_sums_kernel<__bf16>,
                dim3((unsigned)(No + 127) / 128, (unsigned)n_parts), 256, params, 0);
     }
-    if (sums) {
-        int n = n_parts, Cout = d.c_out, no = No;
-        float *db0 = a.db[0], *db1 = a.db[1];
-        void *params[] = {&parts, &n, &Cout, &no, &db0, &db1};
-        launch((const void *)&grad_join_kernel, dim3((unsigned)(No + 15) / 16), 1024, params, 0);
+    const JoinArgs join{parts, {a.db[0], a.db[1]}, n_parts, d.c_out, No, sums ? (No + 15) / 16 : 0};
+    if (sums && !a.dW[0] && !a.dW[1]) {
+        void *params[] = {(void *)&join};
+        launch((const void *)&grad_join_kernel, dim3((unsigned)join.groups), 1024, params, 0);
     }
-    if (a.dX) {
+    if (a.dX && g.x_small) {
+        GradXArgs x{a.dz, {a.W[0], a.W[1]}, a.dX, d.rows, d.c_in, d.c_out, No, (d.c_in + 31) / 32};
+        void *params[] = {&x};
+        launch(f32 ? (const void *)&grad_x_small_kernel<float> : (const void *)&grad_x_small_kernel<__bf16>,
+               dim3((unsigned)((d.rows + 31) / 32 * x.tiles_n)), 512, params, kSmallLds);
+    } else if (a.dX) {
         const void *W0 = a.W[0], *W1 = a.W[1];
         void *Wt = space + g.turned;
         int Cin = d.c_in, Cout = d.c_out, no = No;
@@ -377,16 +379,17 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         w.items = w.tiles * g.splits;
         w.per_xcd = (w.items + kXcds - 1) / kXcds;
         w.stages = g.stages;
-        unsigned groups = (unsigned)w.per_xcd * kXcds;
+        w.groups = w.per_xcd * kXcds;
+        w.join = join;
         if (g.w_rows == 256) {
             const int half = d.c_in % 256 != 0 && d.c_in % 256 <= 128 ? 1 : 0, tm = w.tiles / w.tiles_n;
             w.whole = w.tiles_n - half;
             w.whole_xcd = (tm * w.whole * g.splits + kXcds - 1) / kXcds;
             w.rest_xcd = (tm * half * g.splits + kXcds - 1) / kXcds;
-            groups = (unsigned)(w.whole_xcd + w.rest_xcd) * kXcds;
+            w.groups = (w.whole_xcd + w.rest_xcd) * kXcds;
         }
         void *params[] = {&w};
-        launch(g.w_fn, dim3(groups), 64 * g.w_waves, params, g.w_lds);
+        launch(g.w_fn, dim3((unsigned)(w.groups + join.groups)), 64 * g.w_waves, params, g.w_lds);
         if (g.splits > 1)
             launch(f32 ? (const void *)&grad_w_join_kernel<float> : (const void *)&grad_w_join_kernel<__bf16>,
                    dim3((unsigned)(((int64_t)No * d.c_in / 4 + 255) / 256)), 256, params, 0);
