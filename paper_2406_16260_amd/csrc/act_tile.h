@@ -327,8 +327,14 @@ __device__ __forceinline__ void act_slope_fast(float x, float &y, float &d)
     }
 }
 
-template <typename TO, bool GATED>
-constexpr int kGradBytes = (GATED ? 2 : 1) * 16 * (32 * (int)sizeof(TO) + (sizeof(TO) == 2 ? 8 : 16));
+// 64 channels of a pass (a whole line of 16-bit numbers) or as many as the part has, and a staged row of them: 16 bytes longer, so
+// that the quads of 16 rows lie in different banks
+template <int NB, bool GATED>
+constexpr int kGradWidth = (GATED ? 8 : 16) * NB < 64 ? (GATED ? 8 : 16) * NB : 64;
+template <typename TO, int NB, bool GATED>
+constexpr int kGradRow = kGradWidth<NB, GATED> * (int)sizeof(TO) + 16;
+template <typename TO, int NB, bool GATED>
+constexpr int kGradBytes = (GATED ? 2 : 1) * 16 * kGradRow<TO, NB, GATED>;
 
 // the sum over 16 neighbouring lanes, in all of them
 template <int ROR>
@@ -338,74 +344,69 @@ __device__ __forceinline__ float plus_turned(float v)
 }
 __device__ __forceinline__ float sum_of_16(float v) { return plus_turned<1>(plus_turned<2>(plus_turned<4>(plus_turned<8>(v)))); }
 
-// WHOLE: all of the part's rows and channels are there.  (Rows of Cout numbers are whole 16-byte pieces.)
-template <typename T, int MB, int NB, bool GATED, typename TO, int ACT, bool WHOLE>
-__device__ __forceinline__ void epilogue_grad_part(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], int64_t m0, int c0,
-                                                   const float *bias, unsigned char *stage, int lane)
-{
-    constexpr int BS = 16, NO = GATED ? 2 : 1, ES = (int)sizeof(TO), NP = 2 * NO, CP = NB / NP;  // passes of a row block
-    static_assert(Mul<T>::BS == BS && NB % NP == 0, "blocks of 16, whole passes");
-    constexpr int SB = 32 * ES + (ES == 2 ? 8 : 16), PER = 16 / ES, CPR = 32 / PER, IT = 16 * CPR / 64;
-    constexpr int PASSES = MB * CP, AHEAD = PASSES < 4 ? PASSES : 4;
+// What comes in of dy: lane's pieces of each pass, the passes of a row block one channel group after the other.
+template <typename TO, int MB, int NB, bool GATED>
+struct GradIn {
+    static constexpr int W = kGradWidth<NB, GATED>, PER = 16 / (int)sizeof(TO), CPR = W / PER, IT = 16 * CPR / 64;
+    static constexpr int NP = W / 16 * (GATED ? 2 : 1), CP = NB / NP, PASSES = MB * CP, AHEAD = PASSES < 4 ? PASSES : 4;
+    static_assert(NB % NP == 0 && IT * 64 == 16 * CPR, "whole passes");
     typedef TO Piece __attribute__((ext_vector_type(PER)));
-    typedef TO Quad __attribute__((ext_vector_type(4)));
-    typedef uint32_t Half __attribute__((ext_vector_type(2)));
-    const int rl = lane % BS, cq = 4 * (lane / BS), ch = lane % CPR * PER, row0 = lane / CPR;
-    const int left_rows = (int)min(a.M - m0, (int64_t)(BS * MB)), left = a.Cout - c0;
-    auto there = [&](int pass, int it) __attribute__((always_inline)) {
-        return WHOLE || (pass % MB * BS + row0 + 64 / CPR * it < left_rows && pass / MB * 32 + ch < left);
-    };
-    const TO *dy = (const TO *)a.R + m0 * a.Cout + c0;
-    TO *dz = (TO *)a.Y + m0 * NO * a.Cout + c0;
-    const uint32_t from = (uint32_t)(row0 * a.Cout + ch), to = (uint32_t)(row0 * NO * a.Cout + ch);
     Piece r[AHEAD][IT];
-    auto fetch = [&](int pass) __attribute__((always_inline)) {
+    // (rows of Cout numbers are whole pieces)
+    __device__ __forceinline__ void fetch(const ActArgs &a, int pass, int64_t m0, int c0, int lane, bool whole)
+    {
+        const int row0 = lane / CPR, ch = lane % CPR * PER;
+        const TO *dy = (const TO *)a.R + m0 * a.Cout + c0;
+        const uint32_t from = (uint32_t)(row0 * a.Cout + ch);
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
+            const int row = pass % MB * 16 + 64 / CPR * it, c = pass / MB * W;
             Piece x{};
-            if (there(pass, it)) x = *(const Piece *)(dy + (int64_t)(pass % MB * BS + 64 / CPR * it) * a.Cout + pass / MB * 32 + from);
+            if (whole || (row + row0 < a.M - m0 && c + ch < a.Cout - c0)) x = *(const Piece *)(dy + (int64_t)row * a.Cout + c + from);
             r[pass % AHEAD][it] = x;
         }
-    };
-    // (8-byte accesses: a staged row of bf16 is 72 bytes)
-    auto put_piece = [&](unsigned char *at, const Piece &x) __attribute__((always_inline)) {
-        const i32x4 w = __builtin_bit_cast(i32x4, x);
-        *(Half *)at = Half{(uint32_t)w[0], (uint32_t)w[1]};
-        *(Half *)(at + 8) = Half{(uint32_t)w[2], (uint32_t)w[3]};
-    };
-    auto get_piece = [&](const unsigned char *at) __attribute__((always_inline)) {
-        const Half lo = *(const Half *)at, hi = *(const Half *)(at + 8);
-        return __builtin_bit_cast(Piece, (i32x4){(int)lo[0], (int)lo[1], (int)hi[0], (int)hi[1]});
-    };
-#pragma unroll
-    for (int p = 0; p < AHEAD; ++p) fetch(p);
+    }
+};
+
+// acc: the products on top of the biases that they began with.  WHOLE: all of the part's rows and channels are there.
+template <typename T, int MB, int NB, bool GATED, typename TO, int ACT, bool WHOLE>
+__device__ __forceinline__ void epilogue_grad_part(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], GradIn<TO, MB, NB, GATED> &in,
+                                                   int64_t m0, int c0, unsigned char *stage, int lane)
+{
+    using In = GradIn<TO, MB, NB, GATED>;
+    using Piece = typename In::Piece;
+    constexpr int BS = 16, NO = GATED ? 2 : 1, ES = (int)sizeof(TO), NP = In::NP, W = In::W, CPR = In::CPR, IT = In::IT;
+    constexpr int SB = kGradRow<TO, NB, GATED>, PASSES = In::PASSES, AHEAD = In::AHEAD;
+    static_assert(Mul<T>::BS == BS, "blocks of 16");
+    typedef TO Quad __attribute__((ext_vector_type(4)));
+    const int rl = lane % BS, cq = 4 * (lane / BS), ch = lane % CPR * In::PER, row0 = lane / CPR;
+    const int left_rows = (int)min(a.M - m0, (int64_t)(BS * MB)), left = a.Cout - c0;
+    TO *dz = (TO *)a.Y + m0 * NO * a.Cout + c0;
+    const uint32_t to = (uint32_t)(row0 * NO * a.Cout + ch);
     f32x4 sum[NP];
 #pragma unroll
     for (int pass = 0; pass < PASSES; ++pass) {
-        const int i = pass % MB, jp = pass / MB * NP;  // (the rows of 32 channels one after the other: fewer sums at a time)
+        const int i = pass % MB, jp = pass / MB * NP;  // (the rows of a group of channels one after the other: fewer sums at a time)
         if (i == 0)
 #pragma unroll
             for (int j = 0; j < NP; ++j) sum[j] = f32x4{};
 #pragma unroll
-        for (int it = 0; it < IT; ++it) put_piece(stage + (row0 + 64 / CPR * it) * SB + ch * ES, r[pass % AHEAD][it]);
+        for (int it = 0; it < IT; ++it) *(Piece *)(stage + (row0 + 64 / CPR * it) * SB + ch * ES) = in.r[pass % AHEAD][it];
         wave_sync();
-        if (pass + AHEAD < PASSES) fetch(pass + AHEAD);
+        if (pass + AHEAD < PASSES) in.fetch(a, pass + AHEAD, m0, c0, lane, WHOLE);
         const bool live = WHOLE || BS * i + rl < left_rows;  // (rows past the end: a bias that is infinite would be NaN in the sums)
 #pragma unroll
         for (int j = 0; j < NP; j += NO) {
             unsigned char *at = stage + rl * SB + (BS * j / NO + cq) * ES;
             const Quad g = *(const Quad *)at;
-            const f32x4 b0 = *(const f32x4 *)(bias + BS * (jp + j) + cq);
-            f32x4 b1{};
-            if constexpr (GATED) b1 = *(const f32x4 *)(bias + BS * (jp + j + 1) + cq);
             Quad t0, t1{};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float z0 = acc[i][jp + j][e] + b0[e], gy = (float)g[e];
+                const float z0 = acc[i][jp + j][e], gy = (float)g[e];
                 float y, d, dz0;
                 act_slope_fast<ACT>(z0, y, d);
                 if constexpr (GATED) {
-                    const float z1 = acc[i][jp + j + 1][e] + b1[e], dz1 = gy * y;
+                    const float z1 = acc[i][jp + j + 1][e], dz1 = gy * y;
                     dz0 = gy * (z1 * d);
                     t1[e] = (TO)dz1;
                     sum[j + 1][e] += live ? dz1 : 0.f;
@@ -425,9 +426,10 @@ __device__ __forceinline__ void epilogue_grad_part(const ActArgs &a, const typen
         for (int k = 0; k < NO; ++k)
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
-                const Piece x = get_piece(stage + k * (16 * SB) + (row0 + 64 / CPR * it) * SB + ch * ES);
-                if (there(pass, it))
-                    *(Piece *)(dz + ((int64_t)(BS * i + 64 / CPR * it) * NO + k) * a.Cout + pass / MB * 32 + to) = x;
+                const int row = BS * i + 64 / CPR * it, c = pass / MB * W;
+                const Piece x = *(const Piece *)(stage + k * (16 * SB) + (row0 + 64 / CPR * it) * SB + ch * ES);
+                if (WHOLE || (row + row0 < left_rows && c + ch < left))
+                    *(Piece *)(dz + ((int64_t)row * NO + k) * a.Cout + c + to) = x;
             }
         wave_sync();
         if (i == MB - 1 && a.sums) {
@@ -437,7 +439,7 @@ __device__ __forceinline__ void epilogue_grad_part(const ActArgs &a, const typen
                 f32x4 v;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = sum_of_16(sum[j][e]);
-                const int c = pass / MB * 32 + BS * (j / NO) + cq;
+                const int c = pass / MB * W + BS * (j / NO) + cq;
                 if (rl == 0 && c < left) *(f32x4 *)(sums + (j % NO) * a.Cout + c) = v;
             }
         }
@@ -445,13 +447,27 @@ __device__ __forceinline__ void epilogue_grad_part(const ActArgs &a, const typen
     }
 }
 template <typename T, int MB, int NB, bool GATED, typename TO, int ACT>
-__device__ __forceinline__ void epilogue_grad(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], int64_t m0, int c0,
-                                              const float *bias, unsigned char *stage, int lane)
+__device__ __forceinline__ void epilogue_grad(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], GradIn<TO, MB, NB, GATED> &in,
+                                              int64_t m0, int c0, unsigned char *stage, int lane)
 {
     if (a.M - m0 >= 16 * MB && a.Cout - c0 >= 16 * NB / (GATED ? 2 : 1))
-        epilogue_grad_part<T, MB, NB, GATED, TO, ACT, true>(a, acc, m0, c0, bias, stage, lane);
+        epilogue_grad_part<T, MB, NB, GATED, TO, ACT, true>(a, acc, in, m0, c0, stage, lane);
     else if (a.M > m0)
-        epilogue_grad_part<T, MB, NB, GATED, TO, ACT, false>(a, acc, m0, c0, bias, stage, lane);
+        epilogue_grad_part<T, MB, NB, GATED, TO, ACT, false>(a, acc, in, m0, c0, stage, lane);
+}
+// (the first of them: before the multiplies are through)
+template <typename TO, int MB, int NB, bool GATED>
+__device__ __forceinline__ void epilogue_grad_fetch(const ActArgs &a, GradIn<TO, MB, NB, GATED> &in, int64_t m0, int c0, int lane)
+{
+    if (a.M <= m0) return;
+    const bool whole = a.M - m0 >= 16 * MB && a.Cout - c0 >= 16 * NB / (GATED ? 2 : 1);
+    if (whole) {
+#pragma unroll
+        for (int q = 0; q < in.AHEAD; ++q) in.fetch(a, q, m0, c0, lane, true);
+    } else {
+#pragma unroll
+        for (int q = 0; q < in.AHEAD; ++q) in.fetch(a, q, m0, c0, lane, false);
+    }
 }
 
 // Small products: 32 rows of X by 32 rows of W a workgroup, whose eight wavefronts share the contraction: a wavefront takes
@@ -673,10 +689,14 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const ActAr
     }
 
     typename M::Acc acc[MB][NB];
+    if constexpr (GRAD) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+    for (int j = 0; j < NB; ++j) {
+        typename M::Acc first{};
+        if constexpr (GRAD) first = *(const f32x4 *)(&cols[0][wn * BS * NB] + BS * j + 4 * (lane / BS));
 #pragma unroll
-        for (int j = 0; j < NB; ++j) acc[i][j] = typename M::Acc{};
+        for (int i = 0; i < MB; ++i) acc[i][j] = first;
+    }
     int koff[2];
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) koff[kk] = M::offset(lane, kk);
@@ -712,10 +732,12 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const ActAr
     asm volatile("" ::: "memory");
     constexpr int CHP = BS * NB / (GATED ? 2 : 1);  // output channels of the part
     if constexpr (GRAD) {
-        static_assert(NW * kGradBytes<TO, GATED> <= 2 * BUF, "the staging area fits in the ring");
+        static_assert(NW * kGradBytes<TO, NB, GATED> <= 2 * BUF, "the staging area fits in the ring");
+        GradIn<TO, MB, NB, GATED> in;
+        epilogue_grad_fetch(a, in, m0 + wm * BS * MB, n0 + wn * CHP, lane);
         with_act(a.act, [&](auto act) __attribute__((always_inline)) {
-            epilogue_grad<T, MB, NB, GATED, TO, decltype(act)::value>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, &cols[0][wn * BS * NB],
-                                                                      smem + wv * kGradBytes<TO, GATED>, lane);
+            epilogue_grad<T, MB, NB, GATED, TO, decltype(act)::value>(a, acc, in, m0 + wm * BS * MB, n0 + wn * CHP,
+                                                                      smem + wv * kGradBytes<TO, NB, GATED>, lane);
         });
         return;
     }
@@ -875,7 +897,7 @@ __device__ __forceinline__ void epilogue_beside(const ActArgs &a, const typename
 // next tile's first one is on its way into the other slot.  A wavefront's part is MB x NB blocks; its multiplies run in
 // halves (X blocks [0, HB), then [HB, MB)) so that one set of fragments, refilled in place under the multiplies, is
 // enough beside the accumulators: LDS reads and the next stage's loads sit between the matrix instructions by hand.
-template <typename T, int MB, int NB, bool GATED, typename TO, int ACT, bool GRAD = false>
+template <typename T, int MB, int NB, bool GATED, typename TO, int ACT>
 __global__ __launch_bounds__(512, 2) void act_stream_kernel(const ActArgs a)
 {
     using M = Mul<T>;
@@ -1110,9 +1132,7 @@ __global__ __launch_bounds__(512, 2) void act_stream_kernel(const ActArgs a)
             if constexpr (SCALED) cols[COLS + le + 64 * u] = csc[u];
         }
         wave_sync();
-        if constexpr (GRAD)
-            epilogue_grad<T, MB, NB, GATED, TO, ACT>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, cols, own, le);
-        else if (a.R)
+        if (a.R)
             epilogue_beside<T, MB, NB, GATED, TO, SCALED, ACT, true>(a, acc, m0 + wm * BS * MB, n0 + wn * CHP, cols, cols + COLS,
                                                                      xs, own, le);
         else

@@ -267,12 +267,16 @@ __global__ __launch_bounds__(256, 2) void grad_dz_large_kernel(const ActArgs a)
         column<BS, GATED, false>(a, n0, threadIdx.x, b, s);
         cols[threadIdx.x] = b;
     }
+    __syncthreads();
     typename M::Acc acc[MB][NB];
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+    for (int j = 0; j < NB; ++j) {
+        const f32x4 first = *(const f32x4 *)(cols + BS * j + 4 * (lane >> 4));
 #pragma unroll
-        for (int j = 0; j < NB; ++j) acc[i][j] = typename M::Acc{};
+        for (int i = 0; i < MB; ++i) acc[i][j] = first;
+    }
     const int l16 = lane & 15, at = l16 * RB + (((lane >> 4) ^ ((l16 >> 1) & 3)) * 16);
+    GradIn<T, MB, NB, GATED> in;
     int slot = 0, fill = 2;
     for (int ks = 0; ks < stages; ++ks) {
         // this wavefront's loads of stage ks have landed (the next stage's may be on their way), and its reads of stage ks - 1,
@@ -286,6 +290,7 @@ __global__ __launch_bounds__(256, 2) void grad_dz_large_kernel(const ActArgs a)
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
         if (ks + 2 < stages) issue_stage(ks + 2, fill);
+        if (ks + 1 == stages) epilogue_grad_fetch(a, in, m0 + wv * (16 * MB), n0, lane);
         const unsigned char *ab = smem + slot * SLOT + wv * (16 * MB * RB) + at, *bb = smem + slot * SLOT + ABYTES + at;
         typename M::Frag af[MB], bf[NB];
 #pragma unroll
@@ -301,10 +306,10 @@ __global__ __launch_bounds__(256, 2) void grad_dz_large_kernel(const ActArgs a)
     }
     // everybody is through with the ring: it becomes the staging area
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // (LDS operations only)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    epilogue_grad<T, MB, NB, GATED, T, ACT>(a, acc, m0 + wv * (16 * MB), n0, cols, smem + wv * kGradBytes<T, GATED>, lane);
+    epilogue_grad<T, MB, NB, GATED, T, ACT>(a, acc, in, m0 + wv * (16 * MB), n0, smem + wv * kGradBytes<T, NB, GATED>, lane);
 }
 constexpr int kDzLargeLds = 3 * 384 * 64;
 
