@@ -871,13 +871,16 @@ def dsattn_sink_forward(streams, frames, spatial, heads, kv_heads, head_dim, sin
 
 def _addresses(who, dev, items):
     """The addresses of (tensor or None, name, numel, dtype code): the path of an ordinary call, and the general checks."""
-    out = []
+    tensor, types, out = _torch.Tensor, _DTYPES, []
     for t, _, numel, code in items:
-        p = None if t is None else _addr(t, numel, code, dev)
-        if p is None and t is not None:
+        if t is None:
+            out.append(None)
+        elif (isinstance(t, tensor) and t.dtype is types.get(code) and t.numel() == numel and t.get_device() == dev
+                and t.is_contiguous()):
+            out.append(t.data_ptr())
+        else:
             _check_tensors(who, items, "current")
             return [_ptr(s[0]) for s in items]
-        out.append(p)
     return out
 
 

@@ -75,5 +75,32 @@ int compute_units(int dev)
     return n;
 }
 
+// The default cap on dynamic LDS is 64 KB; it is raised once for a kernel and device (0.4 us a call otherwise).
+hipError_t allow_lds(const void *fn, int lds)
+{
+    if (lds <= 64 << 10) return hipSuccess;
+    struct Slot {
+        std::atomic<const void *> fn;
+        std::atomic<uint64_t> devices;
+    };
+    static Slot slots[64];  // (a kernel that finds no place is asked for each time)
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    Slot *mine = nullptr;
+    const size_t at = ((uintptr_t)fn >> 3) * 0x9e3779b97f4a7c15ull >> 58;
+    for (size_t i = 0; dev < 64 && i < 64 && !mine; ++i) {
+        Slot &s = slots[(at + i) % 64];
+        const void *there = s.fn.load(std::memory_order_acquire);
+        if (!there && s.fn.compare_exchange_strong(there, fn, std::memory_order_acq_rel)) there = fn;
+        if (there == fn) mine = &s;
+    }
+    const uint64_t bit = (uint64_t)1 << (dev & 63);
+    if (mine && (mine->devices.load(std::memory_order_acquire) & bit)) return hipSuccess;
+    e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e == hipSuccess && mine) mine->devices.fetch_or(bit, std::memory_order_acq_rel);
+    return e;
+}
+
 }  // namespace
 }  // namespace dsattn

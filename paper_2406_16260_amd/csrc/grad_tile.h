@@ -12,7 +12,8 @@ namespace {
 
 // Column sums of parts of the rows, to be added up: by workgroups of their own behind those of another kernel.
 struct JoinArgs {
-    const float *sums;  // [parts][No]
+    const void *sums;   // [parts][No]
+    bool half;          // of bf16: few rows of dY itself
     float *db[2];       // [Cout] each, or null
     int32_t parts, Cout, No, groups;  // groups: workgroups, of 16 columns each
 };
@@ -108,9 +109,15 @@ __device__ __forceinline__ void join_columns(const JoinArgs &a, int block, float
     constexpr int W = THREADS / 16;
     const int l = threadIdx.x & 15, w = threadIdx.x >> 4, c = block * 16 + l;
     float v = 0.f;
-    if (c < a.No)
+    if (c < a.No) {
+        if (a.half) {
 #pragma unroll 8
-        for (int p = w; p < a.parts; p += W) v += a.sums[(int64_t)p * a.No + c];
+            for (int p = w; p < a.parts; p += W) v += (float)((const __bf16 *)a.sums)[(int64_t)p * a.No + c];
+        } else {
+#pragma unroll 8
+            for (int p = w; p < a.parts; p += W) v += ((const float *)a.sums)[(int64_t)p * a.No + c];
+        }
+    }
     part[w * 17 + l] = v;
     __syncthreads();
     for (int h = W / 2; h > 0; h >>= 1) {

@@ -197,21 +197,33 @@ const void *const kWTiles[2][2] = {  // 64 x 64, 128 x 128
     {(const void *)&grad_w_tile_kernel<float, 2, 2, 2, 2>, (const void *)&grad_w_tile_kernel<float, 2, 4, 4, 2>},
     {(const void *)&grad_w_tile_kernel<__bf16, 2, 2, 2, 2>, (const void *)&grad_w_tile_kernel<__bf16, 2, 4, 4, 2>}};
 
-// Estimated us of the weights' gradient by tiles of a size, tm x tn of them (the last of 256 may be half empty) and splits of
-// `stages` stages: rounds on the compute units (two workgroups of the 128 x 128 kernel and four of the 64 x 64 one share a
-// unit), each of the stages' time and a start and an end.
-double w_estimate(int size, int64_t tm, int64_t tn, int64_t cin, int64_t splits, int64_t stages, bool f32)
+// Estimated us of the weights' gradient by tiles of a size, tm x tn of them (the last column of 256 may be half empty) and splits of
+// `stages` stages.  256: rounds of one workgroup a compute unit.  Smaller ones: a stage takes its latency, or the unit's
+// throughput for the workgroups that share it (two of 128 x 128, five of 64 x 64; more come after them).  The splits' sums are
+// joined by a kernel of its own.  Measured us (dW alone, in a captured graph; tile / splits), rows x c_in x c_out:
+//                                 64 / 1   64 / 4   128 / 1   128 / 4   256 / 1    best
+//    bf16   640 x   640 x   640      6.3        -      10.0         -      22.5    64 / 1 6.3
+//         2,560 x 1,280 x 1,280     25.1     27.3      32.3      25.0      56.7    128 / 2 23.8
+//        10,240 x 1,280 x 1,280     83.5     61.3     113.5      50.0     192.5    256 / 8 49.6
+//        10,240 x   320 x   320     78.6     24.8     107.6      33.7     189.3    64 / 8 13.5
+//        40,960 x   320 x 1,280    306.2     84.0     411.9     103.6     728.3    128 / 16 50.3
+//         1,000 x 4,096 x 4,096        -        -      46.2         -      37.7    256 / 1 37.7
+//    fp32   640 x   640 x   640     17.2     15.6      45.0      20.8              64 / 2 13.7
+//        10,240 x 1,280 x 1,280    354.0    293.7     653.7     316.4              128 / 12 282.7
+//        10,240 x   320 x   320    209.8     59.7     646.5     169.8              64 / 16 32.7
+double w_estimate(int size, int64_t tm, int64_t tn, int64_t cin, int64_t splits, int64_t stages, bool f32, double numbers)
 {
-    const double st = (double)stages;
+    const double st = (double)stages, join = splits > 1 ? 4.0 + 8.0 * (double)splits * numbers / 7e6 : 0.0;
     if (size == 256) {
         const int64_t half = cin % 256 != 0 && cin % 256 <= 128 ? 1 : 0, f = (tm * (tn - half) * splits + 7) / 8, h = (tm * half * splits + 7) / 8;
         const int64_t rounds = (f + 31) / 32, spare = rounds * 32 - f;
         const double t = (double)rounds + 0.6 * (double)((std::max<int64_t>(0, h - spare) + 31) / 32);
-        return t * (1.3 * st + 7.0);
+        return t * (1.2 * st + 7.0) + join;
     }
-    const int64_t n = tm * tn * splits, fit = size == 128 ? 512 : 1024;
-    const double rounds = (double)(n / fit) + (n % fit ? std::max(0.55, (double)(n % fit) / (double)fit) : 0.0);
-    return rounds * (st * (size == 128 ? (f32 ? 4.0 : 1.25) : (f32 ? 2.1 : 0.75)) + 4.0);
+    const double latency = size == 128 ? (f32 ? 2.0 : 0.67) : (f32 ? 0.65 : 0.45), each = size == 128 ? (f32 ? 2.0 : 0.5) : (f32 ? 0.55 : 0.2);
+    const int64_t n = tm * tn * splits, fit = size == 128 ? 2 : 5;
+    const double c = n <= 256 * fit ? (double)((n + 255) / 256) : (double)n / 256.0 + 0.5;
+    return st * std::max(latency + 0.05 * (std::min(c, (double)fit) - 1.0), each * c) + 4.0 + join;
 }
 
 GradLaunch grad_pick(const dsattn_linear_act_desc &d)
@@ -278,11 +290,10 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
     for (int size : {64, 128, 256}) {
         if (size == 256 && f32) break;
         const int64_t tm = (No + size - 1) / size, tn = (d.c_in + size - 1) / size;
-        for (int64_t splits = 1; splits <= std::min<int64_t>(64, std::max<int64_t>(1, all / 4)); ++splits) {
+        for (int64_t splits = 1; splits <= std::min<int64_t>(64, std::max<int64_t>(1, all / 2)); ++splits) {
             const int64_t stages = (all + splits - 1) / splits, used = (all + stages - 1) / stages;
             if (used != splits) continue;
-            const double t = w_estimate(size, tm, tn, d.c_in, splits, stages, f32) +
-                             (splits > 1 ? 3.0 + 8e-6 * (double)(splits * No) * (double)d.c_in / 5.0 : 0.0);
+            const double t = w_estimate(size, tm, tn, d.c_in, splits, stages, f32, (double)No * (double)d.c_in);
             if (t >= us) continue;
             us = t;
             g.w_rows = g.w_cols = size;
@@ -305,12 +316,12 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
     const bool f32 = d.io_dtype == DSATTN_F32, sums = a.db[0] || a.db[1];
     hipError_t e = hipSuccess;
     auto launch = [&](const void *fn, dim3 grid, int threads, void **params, int lds) {
-        // the default cap on dynamic LDS is 64 KB
-        if (e == hipSuccess && lds > 64 << 10) e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e == hipSuccess) e = allow_lds(fn, lds);
         if (e == hipSuccess) e = hipLaunchKernel(fn, grid, dim3((unsigned)threads), params, (size_t)lds, st);
     };
     float *parts = (float *)(space + g.sums);
     const int n_parts = (int)((d.rows + g.part_rows - 1) / g.part_rows);
+    const bool direct = !g.dz_fn && d.rows <= 1024;  // few rows of dY: summed up at once
     if (g.dz_fn) {
         ActArgs z{};
         z.X = a.X;
@@ -333,7 +344,7 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         z.panel = g.dz_large ? act_panel(z.tiles_n) : 1;
         void *params[] = {&z};
         launch(g.dz_fn, dim3(g.dz_small ? (unsigned)z.tiles : (unsigned)z.per_xcd * kXcds), 64 * g.dz_waves, params, g.dz_lds);
-    } else if (sums) {
+    } else if (sums && !direct) {
         const void *dz = a.dz;
         int64_t M = d.rows;
         int no = No;
@@ -341,7 +352,12 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         launch(f32 ? (const void *)&grad_sums_kernel<float> : (const void *)&grad_sums_kernel<__bf16>,
                dim3((unsigned)(No + 127) / 128, (unsigned)n_parts), 256, params, 0);
     }
-    const JoinArgs join{parts, {a.db[0], a.db[1]}, n_parts, d.c_out, No, sums ? (No + 15) / 16 : 0};
+    JoinArgs join{parts, false, {a.db[0], a.db[1]}, n_parts, d.c_out, No, sums ? (No + 15) / 16 : 0};
+    if (direct) {
+        join.sums = a.dz;
+        join.half = !f32;
+        join.parts = (int)d.rows;
+    }
     if (sums && !a.dW[0] && !a.dW[1]) {
         void *params[] = {(void *)&join};
         launch((const void *)&grad_join_kernel, dim3((unsigned)join.groups), 1024, params, 0);
