@@ -24,7 +24,20 @@ struct ActArgs {
     int32_t Cin, Cout, n_w, act;
     int32_t tiles_n, tiles, per_xcd;  // column tiles; all of them; ceil(tiles / 8)
     int32_t panel;                    // persistent kernels: column tiles that are numbered together
-    float *sums;                      // gradients: [parts of rows][n_w Cout], column sums; R is dy and Y is dz then
+};
+
+// W_0 and W_1 below each other, transposed, for the product that gives dX: 64 x 64 numbers a workgroup, of workgroups behind
+// those of another kernel.
+struct TurnArgs {
+    const void *W[2];  // [Cout][Cin] each
+    void *Wt;          // [Cin][No]
+    int32_t Cin, Cout, No, tiles_c;
+};
+// Gradients: R is dy, Y is dz.
+struct ActGradArgs : ActArgs {
+    float *sums;     // [parts of rows][n_w Cout], column sums, or null
+    int32_t groups;  // workgroups of the product; those behind turn W
+    TurnArgs turn;
 };
 
 struct e4m3 { uint8_t bits; };
@@ -327,6 +340,33 @@ __device__ __forceinline__ void act_slope_fast(float x, float &y, float &d)
     }
 }
 
+template <typename T, int THREADS>
+__device__ __forceinline__ void turn_tile(const TurnArgs &a, int block, unsigned char *smem)
+{
+    constexpr int PER = 16 / (int)sizeof(T), CPR = 64 / PER, ROWS = THREADS / CPR, SR = 64 + 4 / (int)sizeof(T);
+    typedef T Piece __attribute__((ext_vector_type(PER)));
+    T *tile = (T *)smem;  // [64][SR]
+    const int ot = block / a.tiles_c, o0 = ot * 64, c0 = (block - ot * a.tiles_c) * 64, r = threadIdx.x / CPR, p = threadIdx.x % CPR * PER;
+#pragma unroll
+    for (int i = 0; i < 64; i += ROWS) {
+        const int o = o0 + r + i, c = c0 + p;
+        Piece x{};
+        if (o < a.No && c < a.Cin) x = *(const Piece *)((const T *)(o < a.Cout ? a.W[0] : a.W[1]) + (int64_t)(o < a.Cout ? o : o - a.Cout) * a.Cin + c);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) tile[(p + e) * SR + r + i] = x[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 64; i += ROWS) {
+        const int c = c0 + r + i, o = o0 + p;
+        if (c >= a.Cin || o >= a.No) continue;
+        Piece x;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) x[e] = tile[(r + i) * SR + p + e];
+        *(Piece *)((T *)a.Wt + (int64_t)c * a.No + o) = x;
+    }
+}
+
 // 64 channels of a pass (a whole line of 16-bit numbers) or as many as the part has, and a staged row of them: 16 bytes longer, so
 // that the quads of 16 rows lie in different banks
 template <int NB, bool GATED>
@@ -353,7 +393,7 @@ struct GradIn {
     typedef TO Piece __attribute__((ext_vector_type(PER)));
     Piece r[AHEAD][IT];
     // (rows of Cout numbers are whole pieces)
-    __device__ __forceinline__ void fetch(const ActArgs &a, int pass, int64_t m0, int c0, int lane, bool whole)
+    __device__ __forceinline__ void fetch(const ActGradArgs &a, int pass, int64_t m0, int c0, int lane, bool whole)
     {
         const int row0 = lane / CPR, ch = lane % CPR * PER;
         const TO *dy = (const TO *)a.R + m0 * a.Cout + c0;
@@ -370,7 +410,7 @@ struct GradIn {
 
 // acc: the products on top of the biases that they began with.  WHOLE: all of the part's rows and channels are there.
 template <typename T, int MB, int NB, bool GATED, typename TO, int ACT, bool WHOLE>
-__device__ __forceinline__ void epilogue_grad_part(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], GradIn<TO, MB, NB, GATED> &in,
+__device__ __forceinline__ void epilogue_grad_part(const ActGradArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], GradIn<TO, MB, NB, GATED> &in,
                                                    int64_t m0, int c0, unsigned char *stage, int lane)
 {
     using In = GradIn<TO, MB, NB, GATED>;
@@ -447,7 +487,7 @@ __device__ __forceinline__ void epilogue_grad_part(const ActArgs &a, const typen
     }
 }
 template <typename T, int MB, int NB, bool GATED, typename TO, int ACT>
-__device__ __forceinline__ void epilogue_grad(const ActArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], GradIn<TO, MB, NB, GATED> &in,
+__device__ __forceinline__ void epilogue_grad(const ActGradArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], GradIn<TO, MB, NB, GATED> &in,
                                               int64_t m0, int c0, unsigned char *stage, int lane)
 {
     if (a.M - m0 >= 16 * MB && a.Cout - c0 >= 16 * NB / (GATED ? 2 : 1))
@@ -457,7 +497,7 @@ __device__ __forceinline__ void epilogue_grad(const ActArgs &a, const typename M
 }
 // (the first of them: before the multiplies are through)
 template <typename TO, int MB, int NB, bool GATED>
-__device__ __forceinline__ void epilogue_grad_fetch(const ActArgs &a, GradIn<TO, MB, NB, GATED> &in, int64_t m0, int c0, int lane)
+__device__ __forceinline__ void epilogue_grad_fetch(const ActGradArgs &a, GradIn<TO, MB, NB, GATED> &in, int64_t m0, int c0, int lane)
 {
     if (a.M <= m0) return;
     const bool whole = a.M - m0 >= 16 * MB && a.Cout - c0 >= 16 * NB / (GATED ? 2 : 1);
@@ -477,7 +517,7 @@ __device__ __forceinline__ void epilogue_grad_fetch(const ActArgs &a, GradIn<TO,
 // them one by one: 160 x 1,280 x 1,280 7.6 us, 1 x 5,120 x 1,280 13 us.)
 constexpr int kSmallLds = 8 * 2 * 64 * kRow;
 template <typename T, bool GATED, typename TO, bool GRAD = false>
-__global__ __launch_bounds__(512, 2) void act_small_kernel(const ActArgs a)
+__global__ __launch_bounds__(512, 2) void act_small_kernel(const std::conditional_t<GRAD, ActGradArgs, ActArgs> a)
 {
     using M = Mul<T>;
     constexpr int BS = M::BS, NW = 8, SR = 36, SLOT = 64 * kRow;
@@ -625,7 +665,7 @@ __global__ __launch_bounds__(512, 2) void act_small_kernel(const ActArgs a)
 // One tile a workgroup: two LDS slots, two to four workgroups on a compute unit, whose loads and barriers hide behind each
 // other's multiplies.  A workgroup of WVM x WVN wavefronts computes a (BS MB WVM) x (BS NB WVN) tile.
 template <typename T, int MB, int NB, int WVM, int WVN, bool GATED, typename TO, bool GRAD = false>
-__global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const ActArgs a)
+__global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const std::conditional_t<GRAD, ActGradArgs, ActArgs> a)
 {
     using M = Mul<T>;
     constexpr int BS = M::BS, NW = WVM * WVN;
@@ -637,6 +677,8 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const ActAr
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     __shared__ __attribute__((aligned(16))) float cols[2][BN];
 
+    if constexpr (GRAD)
+        if ((int)blockIdx.x >= a.groups) return turn_tile<T, 64 * NW>(a.turn, (int)blockIdx.x - a.groups, smem);
     // workgroup -> tile: XCD x (= blockIdx % 8) owns a contiguous run of tiles
     const int tile = (int)(blockIdx.x % kXcds) * a.per_xcd + (int)(blockIdx.x / kXcds);
     if (tile >= a.tiles) return;  // whole workgroup: no barrier has been reached yet

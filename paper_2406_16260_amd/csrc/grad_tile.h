@@ -227,7 +227,7 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const Gr
 // at the same place, takes 400 us for 40,960 x 640 x 2 x 2,560, GELU.)  Stages of 64 bytes of a row, three LDS slots: a stage's loads
 // have two stages to arrive.  Chunk c of row r lies at position c ^ r / 2 % 4.
 template <bool GATED, int ACT>
-__global__ __launch_bounds__(256, 2) void grad_dz_large_kernel(const ActArgs a)
+__global__ __launch_bounds__(256, 2) void grad_dz_large_kernel(const ActGradArgs a)
 {
     using T = __bf16;
     using M = Mul<T>;
@@ -235,9 +235,10 @@ __global__ __launch_bounds__(256, 2) void grad_dz_large_kernel(const ActArgs a)
     constexpr int ABYTES = BM * RB, SLOT = (BM + BN) * RB, BO = GATED ? BN / 2 : BN;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     __shared__ __attribute__((aligned(16))) float cols[BN];
+    if ((int)blockIdx.x >= a.groups) return turn_tile<T, 256>(a.turn, (int)blockIdx.x - a.groups, smem);
     // workgroup -> tile: XCD x (= blockIdx % 8) owns a contiguous run of tiles, numbered in panels of a.panel column tiles
     const int tile = (int)(blockIdx.x % kXcds) * a.per_xcd + (int)(blockIdx.x / kXcds);
-    if (tile >= a.tiles || (int)(blockIdx.x / kXcds) >= a.per_xcd) return;  // whole workgroup: no barrier has been reached yet
+    if (tile >= a.tiles) return;  // whole workgroup: no barrier has been reached yet
     const int tiles_m = a.tiles / a.tiles_n, row = tile / a.panel, pn = row / tiles_m, mt = row - pn * tiles_m;
     const int64_t m0 = (int64_t)mt * BM;
     const int n0 = (pn * a.panel + tile - row * a.panel) * BO;
@@ -498,16 +499,27 @@ __global__ __launch_bounds__(512, 2) void grad_w_large_kernel(const GradWArgs a)
 }
 constexpr int kLargeLds = 2 * 512 * kRow;
 
-// The splits' sums added up, in their order.
-template <typename T>
+// The splits' sums added up: G threads for four numbers, every G-th split each, these in their order (with many splits a thread
+// would wait for one read after the other).
+template <typename T, int G>
 __global__ __launch_bounds__(256) void grad_w_join_kernel(const GradWArgs a)
 {
-    const int64_t n = (int64_t)a.No * a.Cin, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= n) return;
-    const int splits = a.items / a.tiles;
-    f32x4 v = *(const f32x4 *)(a.partial + i);
+    constexpr int Q = 256 / G;  // fours of a workgroup
+    const int64_t n = (int64_t)a.No * a.Cin, i = ((int64_t)blockIdx.x * Q + (threadIdx.x % Q)) * 4;
+    const int splits = a.items / a.tiles, g = threadIdx.x / Q;
+    f32x4 v{};
+    if (i < n)
 #pragma unroll 4
-    for (int s = 1; s < splits; ++s) v += *(const f32x4 *)(a.partial + s * n + i);
+        for (int s = g; s < splits; s += G) v += *(const f32x4 *)(a.partial + s * n + i);
+    if constexpr (G > 1) {
+        __shared__ f32x4 part[G][Q];
+        part[g][threadIdx.x % Q] = v;
+        __syncthreads();
+        if (g) return;
+#pragma unroll
+        for (int q = 1; q < G; ++q) v += part[q][threadIdx.x];
+    }
+    if (i >= n) return;
     const int64_t half = (int64_t)a.Cout * a.Cin;
     T *to = (T *)(i < half ? a.dW[0] : a.dW[1]);
     if (!to) return;
@@ -627,32 +639,11 @@ __global__ __launch_bounds__(512, 2) void grad_x_small_kernel(const GradXArgs a)
     *(Pair *)((T *)a.dX + m * a.Cin + n0 + c) = y;
 }
 
-// W_0 and W_1 below each other, transposed: [Cin][n_w Cout].  64 x 64 tiles through LDS.
 template <typename T>
-__global__ __launch_bounds__(256) void grad_turn_kernel(const void *W0, const void *W1, void *Wt, int Cin, int Cout, int No)
+__global__ __launch_bounds__(256) void grad_turn_kernel(const TurnArgs a)
 {
-    constexpr int PER = 16 / (int)sizeof(T), CPR = 64 / PER, ROWS = 256 / CPR;
-    typedef T Piece __attribute__((ext_vector_type(PER)));
-    __shared__ T tile[64][64 + 4 / (int)sizeof(T)];
-    const int o0 = (int)blockIdx.x * 64, c0 = (int)blockIdx.y * 64, r = threadIdx.x / CPR, p = threadIdx.x % CPR * PER;
-#pragma unroll
-    for (int i = 0; i < 64; i += ROWS) {
-        const int o = o0 + r + i, c = c0 + p;
-        Piece x{};
-        if (o < No && c < Cin) x = *(const Piece *)((const T *)(o < Cout ? W0 : W1) + (int64_t)(o < Cout ? o : o - Cout) * Cin + c);
-#pragma unroll
-        for (int e = 0; e < PER; ++e) tile[p + e][r + i] = x[e];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 64; i += ROWS) {
-        const int c = c0 + r + i, o = o0 + p;
-        if (c >= Cin || o >= No) continue;
-        Piece x;
-#pragma unroll
-        for (int e = 0; e < PER; ++e) x[e] = tile[r + i][p + e];
-        *(Piece *)((T *)Wt + (int64_t)c * No + o) = x;
-    }
+    __shared__ __attribute__((aligned(16))) unsigned char smem[64 * (64 * sizeof(T) + 4)];
+    turn_tile<T, 256>(a, (int)blockIdx.x, smem);
 }
 
 // Column sums of 256 rows of a matrix, 128 columns a workgroup: part blockIdx.y.

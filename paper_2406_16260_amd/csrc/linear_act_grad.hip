@@ -193,6 +193,9 @@ const void *const kDzLarge[2][DSATTN_ACT_SILU + 1] = {
     {DSATTN_GRAD_LARGE(true, DSATTN_ACT_NONE), DSATTN_GRAD_LARGE(true, DSATTN_ACT_RELU), DSATTN_GRAD_LARGE(true, DSATTN_ACT_GELU),
      DSATTN_GRAD_LARGE(true, DSATTN_ACT_GELU_TANH), DSATTN_GRAD_LARGE(true, DSATTN_ACT_SILU)}};
 
+const void *const kWJoin[2][2] = {  // few splits, 16 and more
+    {(const void *)&grad_w_join_kernel<float, 1>, (const void *)&grad_w_join_kernel<float, 8>},
+    {(const void *)&grad_w_join_kernel<__bf16, 1>, (const void *)&grad_w_join_kernel<__bf16, 8>}};
 const void *const kWTiles[2][2] = {  // 64 x 64, 128 x 128
     {(const void *)&grad_w_tile_kernel<float, 2, 2, 2, 2>, (const void *)&grad_w_tile_kernel<float, 2, 4, 4, 2>},
     {(const void *)&grad_w_tile_kernel<__bf16, 2, 2, 2, 2>, (const void *)&grad_w_tile_kernel<__bf16, 2, 4, 4, 2>}};
@@ -309,7 +312,8 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
     return g;
 }
 
-// The kernels one after the other: dz with its parts of the column sums, W turned, dX, dW with the sums joined behind it.
+// The kernels one after the other: dz with its parts of the column sums and W turned behind it, dX, dW with the sums joined
+// behind it, its splits joined.
 int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const GradArgs &a, const char *who, char *space, hipStream_t st)
 {
     const int No = d.n_w * d.c_out;
@@ -319,11 +323,14 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         if (e == hipSuccess) e = allow_lds(fn, lds);
         if (e == hipSuccess) e = hipLaunchKernel(fn, grid, dim3((unsigned)threads), params, (size_t)lds, st);
     };
+    const TurnArgs turn{{a.W[0], a.W[1]}, space + g.turned, d.c_in, d.c_out, No, (d.c_in + 63) / 64};
+    const int turns = a.dX && !g.x_small ? (No + 63) / 64 * turn.tiles_c : 0;  // workgroups that turn W
+    bool turned = false;
     float *parts = (float *)(space + g.sums);
     const int n_parts = (int)((d.rows + g.part_rows - 1) / g.part_rows);
     const bool direct = !g.dz_fn && d.rows <= 1024;  // few rows of dY: summed up at once
     if (g.dz_fn) {
-        ActArgs z{};
+        ActGradArgs z{};
         z.X = a.X;
         z.R = a.dY;
         z.Y = a.dz;
@@ -342,8 +349,11 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         z.tiles = (int32_t)((d.rows + g.dz_rows - 1) / g.dz_rows) * z.tiles_n;
         z.per_xcd = (z.tiles + kXcds - 1) / kXcds;
         z.panel = g.dz_large ? act_panel(z.tiles_n) : 1;
+        z.groups = g.dz_small ? z.tiles : z.per_xcd * kXcds;
+        z.turn = turn;
         void *params[] = {&z};
-        launch(g.dz_fn, dim3(g.dz_small ? (unsigned)z.tiles : (unsigned)z.per_xcd * kXcds), 64 * g.dz_waves, params, g.dz_lds);
+        turned = turns && !g.dz_small;
+        launch(g.dz_fn, dim3((unsigned)(z.groups + (turned ? turns : 0))), 64 * g.dz_waves, params, g.dz_lds);
     } else if (sums && !direct) {
         const void *dz = a.dz;
         int64_t M = d.rows;
@@ -368,15 +378,13 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         launch(f32 ? (const void *)&grad_x_small_kernel<float> : (const void *)&grad_x_small_kernel<__bf16>,
                dim3((unsigned)((d.rows + 31) / 32 * x.tiles_n)), 512, params, kSmallLds);
     } else if (a.dX) {
-        const void *W0 = a.W[0], *W1 = a.W[1];
-        void *Wt = space + g.turned;
-        int Cin = d.c_in, Cout = d.c_out, no = No;
-        void *params[] = {&W0, &W1, &Wt, &Cin, &Cout, &no};
-        launch(f32 ? (const void *)&grad_turn_kernel<float> : (const void *)&grad_turn_kernel<__bf16>,
-               dim3((unsigned)(No + 63) / 64, (unsigned)(Cin + 63) / 64), 256, params, 0);
+        if (!turned) {
+            void *params[] = {(void *)&turn};
+            launch(f32 ? (const void *)&grad_turn_kernel<float> : (const void *)&grad_turn_kernel<__bf16>, dim3((unsigned)turns), 256, params, 0);
+        }
         if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
         const dsattn_linear_act_desc x{d.rows, No, d.c_in, 1, DSATTN_ACT_NONE, d.io_dtype, d.io_dtype, 0};
-        const int rc = dsattn_linear_act(&x, a.dz, nullptr, &Wt, nullptr, nullptr, nullptr, a.dX, st);
+        const int rc = dsattn_linear_act(&x, a.dz, nullptr, &turn.Wt, nullptr, nullptr, nullptr, a.dX, st);
         if (rc != DSATTN_OK) return rc;
     }
     if (a.dW[0] || a.dW[1]) {
@@ -406,9 +414,10 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         }
         void *params[] = {&w};
         launch(g.w_fn, dim3((unsigned)(w.groups + join.groups)), 64 * g.w_waves, params, g.w_lds);
-        if (g.splits > 1)
-            launch(f32 ? (const void *)&grad_w_join_kernel<float> : (const void *)&grad_w_join_kernel<__bf16>,
-                   dim3((unsigned)(((int64_t)No * d.c_in / 4 + 255) / 256)), 256, params, 0);
+        if (g.splits > 1) {
+            const int fours = g.splits >= 16 ? 32 : 256;  // of a workgroup
+            launch(kWJoin[!f32][g.splits >= 16], dim3((unsigned)(((int64_t)No * d.c_in / 4 + fours - 1) / fours)), 256, params, 0);
+        }
     }
     if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
     return DSATTN_OK;
