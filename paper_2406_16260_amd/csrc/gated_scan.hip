@@ -39,35 +39,36 @@ struct ScanArgs {
     int32_t chunk, chunks;    // frames of a chunk (a multiple of kStep), chunks of a stream
 };
 
-// e^-|g|, within an ulp or so: the product with log2(e) in two parts
-__device__ __forceinline__ float exp_minus_abs(float g)
+// e^x, within two ulps: 2^(x log2(e)), and what the product's rounding has left of x
+__device__ __forceinline__ float exp_of(float x)
 {
-    const float x = -fabsf(g), hi = x * 1.44269504f;
-    const float lo = fmaf(x, 1.44269504f, -hi) + x * 1.92596299e-8f;
-    const float e = __builtin_amdgcn_exp2f(hi);
-    return fmaf(e, lo * 0.693147181f, e);
+    const float p = x * 1.44269504f;
+    const float left = fmaf(p, 1.90465430e-9f, fmaf(p, -0.693147182f, x));  // x - p ln 2, ln 2 in two parts
+    const float e = __builtin_amdgcn_exp2f(p);
+    return fmaf(e, left, e);
 }
 
 // What a gate keeps, a = sigmoid(g), what it leaves, 1 - a, and what it lets in, w(a): each with a small relative error.  (The
 // instructions for quotients and roots, an ulp off at most, not the sequences that round them, which took twice the time.)
-// 1 - a^2 is (1 - a) (1 + a), and its root is taken with e^(-|g| / 2) outside, so that it does not underflow before w does.
+// With e = e^-g, a = 1 / (1 + e), 1 - a = e a, and 1 - a^2 = e a (1 + a), whose root is taken with e^(-g / 2) outside, so that it
+// does not underflow before w does.  Below -87 a gate counts as one of -87, 2^-125.5: e stays finite.
 struct Gate {
     float keep, leave, let;
 };
 template <int MODE>
 __device__ __forceinline__ Gate gate_of(float g)
 {
-    const bool open = g >= 0.f;  // (a NaN: no, and all are NaN)
+    const float x = g < -87.f ? 87.f : -g;  // (a NaN stays)
     Gate q;
     if constexpr (MODE == DSATTN_SCAN_NORM) {
-        const float h = exp_minus_abs(0.5f * g), e = h * h, big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
-        q.keep = open ? big : small;
-        q.leave = open ? small : big;
-        q.let = __builtin_amdgcn_sqrtf(fmaf(big, q.keep, big)) * (open ? h : 1.f);
+        const float h = exp_of(0.5f * x), e = h * h;
+        q.keep = __builtin_amdgcn_rcpf(1.f + e);
+        q.leave = e * q.keep;
+        q.let = h * __builtin_amdgcn_sqrtf(fmaf(q.keep, q.keep, q.keep));
     } else {
-        const float e = exp_minus_abs(g), big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
-        q.keep = open ? big : small;
-        q.leave = open ? small : big;
+        const float e = exp_of(x);
+        q.keep = __builtin_amdgcn_rcpf(1.f + e);
+        q.leave = e * q.keep;
         q.let = MODE == DSATTN_SCAN_MEAN ? q.leave : 1.f;
     }
     return q;
@@ -97,8 +98,8 @@ struct Place {
         j = (int)blockIdx.y;
         b = (int)blockIdx.z;
         const int count = a.counts ? min(max(a.counts[b], 0), a.T) : a.T;
-        t0 = min(j * a.chunk, count);
-        t1 = min(j * a.chunk + a.chunk, count);
+        t0 = (int)min((int64_t)j * a.chunk, (int64_t)count);
+        t1 = (int)min((int64_t)(j + 1) * a.chunk, (int64_t)count);
     }
 };
 

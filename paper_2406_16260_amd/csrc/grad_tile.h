@@ -532,8 +532,8 @@ __global__ __launch_bounds__(256) void grad_w_join_kernel(const GradWArgs a)
 
 // dX of few rows: dX = sum dz_k W_k, 32 x 32 a workgroup, whose eight wavefronts share the contraction as in act_small_kernel
 // (a wavefront takes every eighth stage through two LDS slots of its own).  W's rows are what is contracted over, and are
-// read transposed; stages do not cross from one set to the other.  160 x 1,280 x 1,280: GRAD_X_SMALL_US; turned by a kernel of its own
-// first 3.4 + 5.1 us.
+// read transposed; stages do not cross from one set to the other.  160 x 1,280 x 1,280: 4.9 us, and 3.4 + 5.1 where a
+// kernel of its own turns W first.
 struct GradXArgs {
     const void *dz;  // [M][No]
     const void *W[2];
@@ -646,15 +646,15 @@ __global__ __launch_bounds__(256) void grad_turn_kernel(const TurnArgs a)
     turn_tile<T, 256>(a, (int)blockIdx.x, smem);
 }
 
-// Column sums of 256 rows of a matrix, 128 columns a workgroup: part blockIdx.y.
+// Column sums of 256 rows of a matrix, 128 columns a workgroup: part blockIdx.x.
 template <typename T>
 __global__ __launch_bounds__(256) void grad_sums_kernel(const void *dz, int64_t M, int No, float *sums)
 {
     constexpr int PER = 8, ES = (int)sizeof(T);
     typedef T Piece __attribute__((ext_vector_type(16 / ES)));
     __shared__ float part[16][128 + 4];
-    const int l = threadIdx.x & 15, w = threadIdx.x >> 4, c = (int)blockIdx.x * 128 + l * PER;
-    const int64_t first = (int64_t)blockIdx.y * 256;
+    const int l = threadIdx.x & 15, w = threadIdx.x >> 4, c = (int)blockIdx.y * 128 + l * PER;
+    const int64_t first = (int64_t)blockIdx.x * 256;
     float v[PER] = {};
     if (c < No)
 #pragma unroll 4
@@ -673,12 +673,12 @@ __global__ __launch_bounds__(256) void grad_sums_kernel(const void *dz, int64_t 
 #pragma unroll
     for (int e = 0; e < PER; ++e) part[w][l * PER + e] = v[e];
     __syncthreads();
-    const int cc = (int)blockIdx.x * 128 + (int)threadIdx.x;
+    const int cc = (int)blockIdx.y * 128 + (int)threadIdx.x;
     if (threadIdx.x >= 128 || cc >= No) return;
     float t = 0.f;
 #pragma unroll
     for (int q = 0; q < 16; ++q) t += part[q][threadIdx.x];
-    sums[(int64_t)blockIdx.y * No + cc] = t;
+    sums[(int64_t)blockIdx.x * No + cc] = t;
 }
 
 }  // namespace

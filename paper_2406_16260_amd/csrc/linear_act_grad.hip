@@ -162,14 +162,20 @@ bool grad_is_dy(const dsattn_linear_act_desc &d) { return d.act == DSATTN_ACT_NO
 struct GradLaunch {
     bool tiles = false;                         // on the matrix cores
     const void *dz_fn = nullptr;                // kernel of dz; null: dz is dY
-    int dz_rows, dz_cols, dz_waves, dz_lds;     // its tile, wavefronts and bytes of LDS
-    bool dz_large, dz_small;
-    int part_rows;                              // rows of a part of the column sums
-    bool x_small;                               // dX by the kernel for few rows; else W is turned for a product
-    const void *w_fn;                           // kernel of dW
-    int w_rows, w_cols, w_waves, w_lds, splits, stages;
-    size_t dz, turned, sums, partial, bytes;    // places in the workspace, and its size
+    int dz_rows = 0, dz_cols = 0, dz_waves = 0, dz_lds = 0;    // its tile, wavefronts and bytes of LDS
+    bool dz_large = false, dz_small = false;
+    int part_rows = 256;                             // rows of a part of the column sums
+    bool x_small = false;                              // dX by the kernel for few rows; else W is turned for a product
+    const void *w_fn = nullptr;                          // kernel of dW
+    int w_rows = 0, w_cols = 0, w_waves = 0, w_lds = 0, splits = 1, stages = 0;
+    size_t dz = 0, turned = 0, sums = 0, partial = 0, bytes = 0;    // places in the workspace, and its size
 };
+
+// dX as a product of dz and the turned W
+dsattn_linear_act_desc product_of_dx(const dsattn_linear_act_desc &d)
+{
+    return {d.rows, d.n_w * d.c_out, d.c_in, 1, DSATTN_ACT_NONE, d.io_dtype, d.io_dtype, 0};
+}
 
 size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -234,20 +240,16 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
     GradLaunch g;
     const bool f32 = d.io_dtype == DSATTN_F32, gated = d.n_w == 2;
     const int64_t es = f32 ? 4 : 2, No = (int64_t)d.n_w * d.c_out, rowbytes = d.c_in * es;
-    g.dz = g.turned = g.sums = g.partial = g.bytes = 0;
     // rows are whole 16-byte chunks, and a tile's are addressed with 32-bit offsets
     const bool fits = rowbytes % 16 == 0 && d.c_out * es % 16 == 0 && rowbytes * 256 < ((int64_t)1 << 31) &&
                       No * es * 256 < ((int64_t)1 << 31) && No < 1 << 22 && !(d.flags & DSATTN_FLAG_FORCE_GENERIC);
     auto tiles = [&](int64_t m, int64_t n, int rows, int cols) { return (m + rows - 1) / rows * ((n + cols - 1) / cols); };
-    if (!fits || tiles(d.rows, No, 32, 32) >= (1 << 23) || tiles(No, d.c_in, 64, 64) >= (1 << 20)) {
-        if (!grad_is_dy(d)) g.bytes = (size_t)d.rows * No * sizeof(float);
-        return g;
-    }
+    GradLaunch vector;
+    vector.bytes = grad_is_dy(d) ? 0 : (size_t)d.rows * No * sizeof(float);
+    if (!fits || tiles(No, d.c_in, 64, 64) >= (1 << 20)) return vector;
     g.tiles = true;
     // dz
     const int64_t stages = (rowbytes + kRow - 1) / kRow;
-    g.dz_large = g.dz_small = false;
-    g.part_rows = 256;
     if (!grad_is_dy(d)) {
         g.part_rows = 32;
         const GradVariant *v = kDzTiles[!f32];
@@ -278,6 +280,8 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
             g.dz_lds = v->lds;
             g.part_rows = v->part;
         }
+        // (a launch has less than 2^32 threads, and tiles are numbered with 32 bits)
+        if (tiles(d.rows, No, g.dz_rows, g.dz_cols) >= ((int64_t)1 << 31) / (64 * g.dz_waves)) return vector;
         g.dz = g.bytes;
         g.bytes += aligned((size_t)d.rows * No * es);
     }
@@ -360,7 +364,7 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         int no = No;
         void *params[] = {&dz, &M, &no, &parts};
         launch(f32 ? (const void *)&grad_sums_kernel<float> : (const void *)&grad_sums_kernel<__bf16>,
-               dim3((unsigned)(No + 127) / 128, (unsigned)n_parts), 256, params, 0);
+               dim3((unsigned)n_parts, (unsigned)(No + 127) / 128), 256, params, 0);
     }
     JoinArgs join{parts, false, {a.db[0], a.db[1]}, n_parts, d.c_out, No, sums ? (No + 15) / 16 : 0};
     if (direct) {
@@ -383,7 +387,7 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
             launch(f32 ? (const void *)&grad_turn_kernel<float> : (const void *)&grad_turn_kernel<__bf16>, dim3((unsigned)turns), 256, params, 0);
         }
         if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
-        const dsattn_linear_act_desc x{d.rows, No, d.c_in, 1, DSATTN_ACT_NONE, d.io_dtype, d.io_dtype, 0};
+        const dsattn_linear_act_desc x = product_of_dx(d);
         const int rc = dsattn_linear_act(&x, a.dz, nullptr, &turn.Wt, nullptr, nullptr, nullptr, a.dX, st);
         if (rc != DSATTN_OK) return rc;
     }
@@ -487,7 +491,13 @@ int dsattn_linear_act_backward(const dsattn_linear_act_desc *desc, const void *X
     const hipStream_t st = (hipStream_t)stream;
     void *params[] = {&a};
     hipError_t e = hipSuccess;
-    if (g.tiles) return grad_launch(d, g, a, who, (char *)workspace, st);
+    if (g.tiles) {
+        const dsattn_linear_act_desc x = product_of_dx(d);
+        dsattn_conv_info info;
+        if (dX && !g.x_small && (dsattn_linear_act_info(&x, &info) != DSATTN_OK || (!info.kernel && d.rows * d.c_in / 256 >= 0xffffff)))
+            return fail(DSATTN_EUNSUPPORTED, "%s: too large for one launch", who);
+        return grad_launch(d, g, a, who, (char *)workspace, st);
+    }
     // (a launch has less than 2^32 threads)
     auto blocks = [](int64_t n) { return (n + 255) / 256; };
     if (blocks(d.rows * std::max(d.c_out, d.c_in)) > 0xffffff || blocks((int64_t)d.c_out * d.c_in) > 0x7fffff)
