@@ -268,14 +268,20 @@ __global__ __launch_bounds__(256, 2) void grad_dz_large_kernel(const ActGradArgs
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(wres0, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16, (uint32_t)off, 0, 0, 0);
         }
     };
-    issue_stage(0, 0);
-    if (stages > 1) issue_stage(1, 1);
     if (threadIdx.x < BN) {
         float b, s;
         column<BS, GATED, false>(a, n0, threadIdx.x, b, s);
         cols[threadIdx.x] = b;
     }
-    __syncthreads();
+    issue_stage(0, 0);
+    issue_stage(1, 1);  // (past the last stage: zeros)
+    issue_stage(2, 2);
+    const int l16 = lane & 15, at = l16 * RB + (((lane >> 4) ^ ((l16 >> 1) & 3)) * 16), aat = at + wv * (16 * MB * RB);
+    typename M::Frag af[2][MB], bf[NB];
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * (G + H)));  // stage 0 has landed
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     typename M::Acc acc[MB][NB];
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
@@ -283,41 +289,53 @@ __global__ __launch_bounds__(256, 2) void grad_dz_large_kernel(const ActGradArgs
 #pragma unroll
         for (int i = 0; i < MB; ++i) acc[i][j] = first;
     }
-    const int l16 = lane & 15, at = l16 * RB + (((lane >> 4) ^ ((l16 >> 1) & 3)) * 16);
-    GradIn<T, MB, NB, GATED> in;
-    int slot = 0, fill = 2;
-    for (int ks = 0; ks < stages; ++ks) {
-        // this wavefront's loads of stage ks have landed (the next stage's may be on their way), and its reads of stage ks - 1,
-        // whose slot stage ks + 2 goes into, are done; behind the barrier everybody's are
+#pragma unroll
+    for (int i = 0; i < MB; ++i) af[0][i] = *(const bf16x8 *)(smem + aat + i * (16 * RB));
+#pragma unroll
+    for (int j = 0; j < NB; ++j) bf[j] = *(const bf16x8 *)(smem + ABYTES + at + j * (16 * RB));
+    int slot = 0;
+    // stage ks, whose fragments are there; the next stage's are read as these are used up, into their places
+    auto step = [&](int ks, auto turn) __attribute__((always_inline)) {
+        constexpr int now = decltype(turn)::value;
+        // this wavefront's loads of the next stage have landed (those of the one after may be on their way), and its reads of this
+        // one, whose slot is filled again, are done; behind the barrier everybody's are
         asm volatile("" ::: "memory");
-        if (ks + 1 < stages)
+        if (ks + 2 < stages)
             __builtin_amdgcn_s_waitcnt(waitcnt_vm(G + H));
         else
             __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        if (ks + 2 < stages) issue_stage(ks + 2, fill);
-        if (ks + 1 == stages) epilogue_grad_fetch(a, in, m0 + wv * (16 * MB), n0, lane);
-        const unsigned char *ab = smem + slot * SLOT + wv * (16 * MB * RB) + at, *bb = smem + slot * SLOT + ABYTES + at;
-        typename M::Frag af[MB], bf[NB];
-#pragma unroll
-        for (int i = 0; i < MB; ++i) af[i] = *(const bf16x8 *)(ab + i * (16 * RB));
-#pragma unroll
-        for (int j = 0; j < NB; ++j) bf[j] = *(const bf16x8 *)(bb + j * (16 * RB));
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int i = 0; i < MB; ++i) acc[i][j] = M::mul(bf[j], af[i], acc[i][j]);
+        if (ks + 3 < stages) issue_stage(ks + 3, slot);
         slot = slot == 2 ? 0 : slot + 1;
-        fill = fill == 2 ? 0 : fill + 1;
+        const unsigned char *next = smem + slot * SLOT;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i) acc[i][j] = M::mul(bf[j], af[now][i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+            bf[j] = *(const bf16x8 *)(next + ABYTES + at + j * (16 * RB));
+            if (j < MB) af[1 - now][j] = *(const bf16x8 *)(next + aat + j * (16 * RB));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    for (int ks = 0;;) {
+        step(ks, std::integral_constant<int, 0>{});
+        if (++ks == stages) break;
+        step(ks, std::integral_constant<int, 1>{});
+        if (++ks == stages) break;
     }
+    int le = lane;
+    asm volatile("" : "+v"(le));  // (or the epilogue's addresses are kept alive through the main loop)
+    GradIn<T, MB, NB, GATED> in;
+    epilogue_grad_fetch(a, in, m0 + wv * (16 * MB), n0, le);
     // everybody is through with the ring: it becomes the staging area
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0xc07f);  // (LDS operations only)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    epilogue_grad<T, MB, NB, GATED, T, ACT>(a, acc, in, m0 + wv * (16 * MB), n0, smem + wv * kGradBytes<T, NB, GATED>, lane);
+    epilogue_grad<T, MB, NB, GATED, T, ACT>(a, acc, in, m0 + wv * (16 * MB), n0, smem + wv * kGradBytes<T, NB, GATED>, le);
 }
 constexpr int kDzLargeLds = 3 * 384 * 64;
 
