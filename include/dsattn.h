@@ -590,9 +590,8 @@ int dsattn_layernorm_backward_workspace(const dsattn_ln_desc *desc, size_t *byte
  *               sum's rounding)
  *   dY        : device, [rows, channels] of io_dtype, 16-byte aligned
  *   dsum      : device, like dY: the gradient that arrives at `sum` by other ways, or NULL for 0
- *   dX        : device, like dY; may be dY, dsum, X or residual itself (with more than 2,048 pieces of 8, 4, 2 or 1
- *               channels, as many as divide `channels`, 4 at most in fp32: only dsum, unless dgamma
- *               and dbeta are NULL)
+ *   dX        : device, like dY; may be dY, dsum, X or residual itself (with more than 16,384 channels, 8,192 in
+ *               fp32: only dsum, unless dgamma and dbeta are NULL)
  *   dgamma,
  *   dbeta     : device, [channels] fp32, or NULL: not wanted
  *   workspace : device, at least dsattn_layernorm_backward_workspace() bytes, 16-byte aligned; may be

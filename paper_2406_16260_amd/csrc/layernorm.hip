@@ -10,6 +10,7 @@
 //   368,640 x 1,280, bf16, residual and sum         692     5.45
 //   40,960 x 640, bf16, residual, all gradients     59.8    4.4, of which the joining kernel is 4.4 us
 //   368,640 x 1,280, the same                       1,021   4.6
+//   24,591 x 1,863, bf16, residual, then all gradients   75.5 and 105, the floors 72 and 90 (pieces of one number: 225 and 307)
 //   40 x 1,280                                      6.9, of which 4.3 are the host's marshalling and 2.6 its launch
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -50,7 +51,11 @@ struct LnBackArgs {
 // differences have squares below 2^-100 (and eps far less): both exact, so that rows of every size are normalised alike.
 struct RowStats {
     float unit, gain, mean, rest, rstd;
-    __device__ __forceinline__ float norm(float s) const { return ((s * unit - mean) * gain - rest) * rstd; }
+    __device__ __forceinline__ float norm(float s) const
+    {
+#pragma clang fp contract(off)
+        return ((s * unit - mean) * gain - rest) * rstd;
+    }
     // (one after the other: their product may be infinite where d is 0)
     __device__ __forceinline__ float slope(float d) const { return d * rstd * gain * unit; }
 };
@@ -83,6 +88,9 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*part)[N])
 template <typename Each, typename Sums>
 __device__ __forceinline__ RowStats row_stats(int C, float eps, Each each, Sums sums)
 {
+    // (mean and rest are rounded before they are used: one product and difference without that in some lanes only, and rows of
+    // equal numbers would not come to 0)
+#pragma clang fp contract(off)
     RowStats t{1.f, 1.f, 0.f, 0.f, 0.f};
     const float inv = 1.f / (float)C;
     float var = 0.f;
@@ -114,65 +122,99 @@ __device__ __forceinline__ RowStats row_stats(int C, float eps, Each each, Sums 
     return t;
 }
 
-template <typename T, int V>
+// A row is pieces of V numbers; a lane has every L-th of them, NV at most, of which all but the last are there in every lane.
+// ODD: V does not divide the row, whose last piece then begins where it ends with the row, V - 1 numbers at most of the one before
+// in it (`skip`, which sums leave out, and which both lanes write alike), and no piece is aligned but to a number: memory takes
+// 16 bytes from there all the same.  (Pieces of the 4, 2 or 1 numbers that divide the row instead: 30,000 x 1,284 in bf16 65 us
+// against 56, 50,000 x 250 20 against 17, 20,001 x 2,049 202 against 84, its gradients 408 against 116.)
+template <typename T, int V, int L, int NV, bool ODD>
 struct Row {
-    typedef T Piece __attribute__((ext_vector_type(V)));
+    typedef T Piece __attribute__((ext_vector_type(V), aligned(ODD ? sizeof(T) : sizeof(T) * V)));
     typedef float Floats __attribute__((ext_vector_type(V)));
-};
-
-// x + r of a row's pieces, in fp32; 0 behind its end.
-template <typename T, int V, int L, int NV>
-__device__ __forceinline__ void row_load(const void *X, const void *R, int64_t base, int at, int C, typename Row<T, V>::Floats (&s)[NV])
-{
-    using Piece = typename Row<T, V>::Piece;
-    Piece x[NV], r[NV];
+    typedef float FloatsThere __attribute__((ext_vector_type(V), aligned(ODD ? sizeof(float) : sizeof(float) * V)));
+    int c[NV], skip;
+    bool in;  // the last piece
+    __device__ __forceinline__ Row(int lane, int C)
+    {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = at + i * (L * V);
-        x[i] = Piece{};
-        r[i] = -Piece{};  // (-0, which leaves every x as it is)
-        if (c < C) {
-            x[i] = *(const Piece *)((const T *)X + base + c);
-            if (R) r[i] = *(const Piece *)((const T *)R + base + c);
+        for (int i = 0; i < NV; ++i) c[i] = (lane + i * L) * V;
+        in = c[NV - 1] < C;
+        skip = 0;
+        if constexpr (ODD) {
+            const int from = min(c[NV - 1], C - V);
+            skip = c[NV - 1] - from;
+            c[NV - 1] = from;
         }
     }
+    __device__ __forceinline__ bool has(int i) const { return i < NV - 1 || in; }
+    // f(piece, element) for each number that is the lane's own
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const
+    {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i)
+            if (has(i))
 #pragma unroll
-        for (int e = 0; e < V; ++e) s[i][e] = (float)x[i][e] + (float)r[i][e];
-}
+                for (int e = 0; e < V; ++e)
+                    if (!ODD || i < NV - 1 || e >= skip) f(i, e);
+    }
+    __device__ __forceinline__ void load(const T *row, Piece (&x)[NV]) const
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (has(i)) x[i] = *(const Piece *)(row + c[i]);
+    }
+    __device__ __forceinline__ void load_floats(const float *row, Floats (&x)[NV]) const
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (has(i)) x[i] = *(const FloatsThere *)(row + c[i]);
+    }
+    // x + r in fp32; 0 behind the row's end
+    __device__ __forceinline__ void load_sum(const void *X, const void *R, int64_t base, Floats (&s)[NV]) const
+    {
+        Piece x[NV], r[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            x[i] = Piece{};
+            r[i] = -Piece{};  // (-0, which leaves every x as it is)
+            if (!has(i)) continue;
+            x[i] = *(const Piece *)((const T *)X + base + c[i]);
+            if (R) r[i] = *(const Piece *)((const T *)R + base + c[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[i][e] = (float)x[i][e] + (float)r[i][e];
+    }
+};
 
-template <typename T, int V, int L, int NV, bool E8>
+template <typename T, int V, int L, int NV, bool E8, bool ODD>
 __global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_vec_kernel(const LnArgs a)
 {
-    using Piece = typename Row<T, V>::Piece;
-    using Floats = typename Row<T, V>::Floats;
+    using Pieces = Row<T, V, L, NV, ODD>;
+    using Piece = typename Pieces::Piece;
+    using Floats = typename Pieces::Floats;
     constexpr int THREADS = L <= 256 ? 256 : L, NW = L > 64 ? L / 64 : 1;
     __shared__ float part[NW][2];
     const int64_t row = (int64_t)blockIdx.x * (THREADS / L) + threadIdx.x / L;
-    const int C = a.C, at = (int)(threadIdx.x % L) * V;
+    const int C = a.C, lane = threadIdx.x % L;
+    const Pieces mine(lane, C);
     const bool there = row < a.rows;
     const int64_t base = (there ? row : a.rows - 1) * C;
     Floats s[NV];
-    row_load<T, V, L, NV>(a.X, a.R, base, at, C, s);
+    mine.load_sum(a.X, a.R, base, s);
     Floats g[NV], b[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = at + i * (L * V);
         g[i] = Floats{} + 1.f;
         b[i] = Floats{};
-        if (a.gamma && c < C) g[i] = *(const Floats *)(a.gamma + c);
-        if (a.beta && c < C) b[i] = *(const Floats *)(a.beta + c);
     }
+    if (a.gamma) mine.load_floats(a.gamma, g);
+    if (a.beta) mine.load_floats(a.beta, b);
     const RowStats t = row_stats(
         C, a.eps,
-        [&](auto f) __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (at + i * (L * V) < C)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) f(s[i][e]);
-        },
+        [&](auto f) __attribute__((always_inline)) { mine.each([&](int i, int e) __attribute__((always_inline)) { f(s[i][e]); }); },
         [&](float (&v)[2]) __attribute__((always_inline)) { row_sums<L, 2>(v, part); });
     Floats y[NV];
 #pragma unroll
@@ -182,11 +224,7 @@ __global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_vec_kernel(const LnArgs
     float inv = 1.f;
     if constexpr (E8) {
         float top = 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (at + i * (L * V) < C)
-#pragma unroll
-                for (int e = 0; e < V; ++e) top = max_or_nan(top, fabsf(y[i][e]));
+        mine.each([&](int i, int e) __attribute__((always_inline)) { top = max_or_nan(top, fabsf(y[i][e])); });
 #pragma unroll
         for (int w = 1; w < (L < 64 ? L : 64); w *= 2) top = max_or_nan(top, __shfl_xor(top, w));
         if constexpr (L > 64) {
@@ -198,24 +236,24 @@ __global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_vec_kernel(const LnArgs
         }
         float scale = top / 448.f;
         scale = scale < 0x1p-126f ? 0x1p-126f : scale;  // (a NaN stays)
-        if (there && at == 0) a.scales[row] = scale;
+        if (there && lane == 0) a.scales[row] = scale;
         inv = 1.f / scale;
     }
     if (!there) return;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = at + i * (L * V);
-        if (c >= C) continue;
+        if (!mine.has(i)) continue;
+        const int64_t at = base + mine.c[i];
         if (a.S) {
             Piece p;
 #pragma unroll
             for (int e = 0; e < V; ++e) p[e] = (T)s[i][e];
-            *(Piece *)((T *)a.S + base + c) = p;
+            *(Piece *)((T *)a.S + at) = p;
         }
         if constexpr (E8) {
-            uint8_t *to = (uint8_t *)a.Y + base + c;
+            typedef int Words __attribute__((ext_vector_type(V / 4 ? V / 4 : 1), aligned(ODD ? 1 : V)));
+            uint8_t *to = (uint8_t *)a.Y + at;
             if constexpr (V % 4 == 0) {
-                typedef int Words __attribute__((ext_vector_type(V / 4)));
                 Words w;
 #pragma unroll
                 for (int q = 0; q < V / 4; ++q) {
@@ -231,7 +269,7 @@ __global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_vec_kernel(const LnArgs
             Piece p;
 #pragma unroll
             for (int e = 0; e < V; ++e) p[e] = (T)y[i][e];
-            *(Piece *)((T *)a.Y + base + c) = p;
+            *(Piece *)((T *)a.Y + at) = p;
         }
     }
 }
@@ -290,67 +328,54 @@ __global__ __launch_bounds__(256) void ln_row_kernel(const LnArgs a)
 
 // A workgroup takes rows blockIdx.x, + gridDim.x, .. (times the rows that it has at once); a lane has the same channels of all of
 // them, adds up their dgamma and dbeta in registers, and the workgroup's sums go to `partial`: no atomics, one order.
-template <typename T, int V, int L, int NV>
+template <typename T, int V, int L, int NV, bool ODD>
 __global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_back_vec_kernel(const LnBackArgs a)
 {
-    using Piece = typename Row<T, V>::Piece;
-    using Floats = typename Row<T, V>::Floats;
+    using Pieces = Row<T, V, L, NV, ODD>;
+    using Piece = typename Pieces::Piece;
+    using Floats = typename Pieces::Floats;
     constexpr int THREADS = L <= 256 ? 256 : L, NW = L > 64 ? L / 64 : 1, PER = THREADS / L;
     __shared__ float part[NW][2];
-    const int C = a.C, at = (int)(threadIdx.x % L) * V, mine = threadIdx.x / L;
+    const int C = a.C, turn = threadIdx.x / L;
+    const Pieces mine(threadIdx.x % L, C);
     const float inv = 1.f / (float)C;
     Floats g[NV], dg[NV], db[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = at + i * (L * V);
         g[i] = Floats{} + 1.f;
         dg[i] = db[i] = Floats{};
-        if (a.gamma && c < C) g[i] = *(const Floats *)(a.gamma + c);
     }
+    if (a.gamma) mine.load_floats(a.gamma, g);
     for (int64_t first = (int64_t)blockIdx.x * PER; first < a.rows; first += (int64_t)gridDim.x * PER) {
-        const bool there = first + mine < a.rows;
-        const int64_t base = (there ? first + mine : a.rows - 1) * C;
+        const bool there = first + turn < a.rows;
+        const int64_t base = (there ? first + turn : a.rows - 1) * C;
         Piece dyp[NV], dsp[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = at + i * (L * V);
-            dyp[i] = dsp[i] = Piece{};
-            if (c < C) {
-                dyp[i] = *(const Piece *)((const T *)a.dY + base + c);
-                if (a.dS) dsp[i] = *(const Piece *)((const T *)a.dS + base + c);
-            }
-        }
+        for (int i = 0; i < NV; ++i) dyp[i] = dsp[i] = Piece{};
+        mine.load((const T *)a.dY + base, dyp);
+        if (a.dS) mine.load((const T *)a.dS + base, dsp);
         Floats s[NV];
-        row_load<T, V, L, NV>(a.X, a.R, base, at, C, s);
+        mine.load_sum(a.X, a.R, base, s);
         const RowStats t = row_stats(
             C, a.eps,
-            [&](auto f) __attribute__((always_inline)) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (at + i * (L * V) < C)
-#pragma unroll
-                        for (int e = 0; e < V; ++e) f(s[i][e]);
-            },
+            [&](auto f) __attribute__((always_inline)) { mine.each([&](int i, int e) __attribute__((always_inline)) { f(s[i][e]); }); },
             [&](float (&v)[2]) __attribute__((always_inline)) { row_sums<L, 2>(v, part); });
         float v[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                s[i][e] = t.norm(s[i][e]);
-                if (at + i * (L * V) < C) {  // (behind the row's end dy is 0, but n may be infinite)
-                    const float de = (float)dyp[i][e] * g[i][e];
-                    v[0] += de;
-                    v[1] = fmaf(de, s[i][e], v[1]);
-                }
-            }
+            for (int e = 0; e < V; ++e) s[i][e] = t.norm(s[i][e]);
+        mine.each([&](int i, int e) __attribute__((always_inline)) {  // (behind the row's end dy is 0, but n may be infinite)
+            const float de = (float)dyp[i][e] * g[i][e];
+            v[0] += de;
+            v[1] = fmaf(de, s[i][e], v[1]);
+        });
         row_sums<L, 2>(v, part);
         if (!there) continue;  // (rows of several wavefronts: PER is 1, and all of the workgroup are there)
         const float m0 = v[0] * inv, m1 = v[1] * inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = at + i * (L * V);
-            if (c >= C) continue;
+            if (!mine.has(i)) continue;
             Piece p;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -360,10 +385,11 @@ __global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_back_vec_kernel(const L
                 const float dx = t.slope(fmaf(dy, g[i][e], -m0) - n * m1);
                 p[e] = (T)(a.dS ? dx + (float)dsp[i][e] : dx);
             }
-            *(Piece *)((T *)a.dX + base + c) = p;
+            *(Piece *)((T *)a.dX + base + mine.c[i]) = p;
         }
     }
     if (!a.partial) return;
+    using FloatsThere = typename Pieces::FloatsThere;
     float *to = a.partial + (int64_t)blockIdx.x * 2 * C;
     if constexpr (PER > 1) {
         __shared__ Floats sums[256];
@@ -374,21 +400,19 @@ __global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_back_vec_kernel(const L
                 __syncthreads();
                 sums[threadIdx.x] = k ? db[i] : dg[i];
                 __syncthreads();
-                const int c = at + i * (L * V);
-                if (mine == 0 && c < C) {
+                if (turn == 0 && mine.has(i)) {
                     Floats v = sums[threadIdx.x];
 #pragma unroll
                     for (int w = 1; w < PER; ++w) v += sums[threadIdx.x + w * L];
-                    *(Floats *)(to + (int64_t)k * C + c) = v;
+                    *(FloatsThere *)(to + (int64_t)k * C + mine.c[i]) = v;
                 }
             }
     } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = at + i * (L * V);
-            if (c >= C) continue;
-            *(Floats *)(to + c) = dg[i];
-            *(Floats *)(to + (int64_t)C + c) = db[i];
+            if (!mine.has(i)) continue;
+            *(FloatsThere *)(to + mine.c[i]) = dg[i];
+            *(FloatsThere *)(to + (int64_t)C + mine.c[i]) = db[i];
         }
     }
 }
@@ -460,9 +484,9 @@ __global__ __launch_bounds__(1024) void ln_join_kernel(const float *partial, int
     if (g0 == 0 && c < C) to[c] = sums[0][threadIdx.x & 15];
 }
 
-// The kernel of a shape: pieces of as many numbers as divide the row, up to 16 bytes, and the fewest lanes that hold the row in
-// four pieces each (1,024 lanes: in two); null: longer.  The backward pass holds a row four times, which leaves 1,024 lanes
-// too few registers.
+// The kernel of a shape: pieces of 16 bytes (of one number for rows shorter than that), and the fewest lanes that hold the row in
+// four pieces each (1,024 lanes: in two), so that only the last piece of a lane may be missing; null: longer.  The backward pass
+// holds a row four times, which leaves 1,024 lanes too few registers.
 struct LnKernel {
     const void *fn;
     int lanes;
@@ -491,33 +515,31 @@ LnKernel ln_pick_of(int C)
     if (pieces <= 2048) return {ln_of<K, K::WIDE>((pieces + K::WIDE - 1) / K::WIDE), K::WIDE};
     return {nullptr, 0};
 }
-template <typename T, int VV, bool E8>
+template <typename T, int VV, bool E8, bool ODD>
 struct LnForward {
     static constexpr int V = VV, WIDE = 1024;
     template <int L, int NV>
-    static const void *of() { return (const void *)&ln_vec_kernel<T, V, L, NV, E8>; }
+    static const void *of() { return (const void *)&ln_vec_kernel<T, V, L, NV, E8, ODD>; }
 };
-template <typename T, int VV>
+template <typename T, int VV, bool ODD>
 struct LnBackward {
     static constexpr int V = VV, WIDE = 512;
     template <int L, int NV>
-    static const void *of() { return (const void *)&ln_back_vec_kernel<T, V, L, NV>; }
+    static const void *of() { return (const void *)&ln_back_vec_kernel<T, V, L, NV, ODD>; }
 };
 template <typename T, bool E8>
 LnKernel ln_pick(int C)
 {
-    if (sizeof(T) == 2 && C % 8 == 0) return ln_pick_of<LnForward<T, 16 / (int)sizeof(T), E8>>(C);
-    return C % 4 == 0   ? ln_pick_of<LnForward<T, 4, E8>>(C)
-           : C % 2 == 0 ? ln_pick_of<LnForward<T, 2, E8>>(C)
-                        : ln_pick_of<LnForward<T, 1, E8>>(C);
+    constexpr int V = 16 / (int)sizeof(T);
+    if (C < V) return {LnForward<T, 1, E8, false>::template of<8, 1>(), 8};
+    return C % V == 0 ? ln_pick_of<LnForward<T, V, E8, false>>(C) : ln_pick_of<LnForward<T, V, E8, true>>(C);
 }
 template <typename T>
 LnKernel ln_back_pick(int C)
 {
-    if (sizeof(T) == 2 && C % 8 == 0) return ln_pick_of<LnBackward<T, 16 / (int)sizeof(T)>>(C);
-    return C % 4 == 0   ? ln_pick_of<LnBackward<T, 4>>(C)
-           : C % 2 == 0 ? ln_pick_of<LnBackward<T, 2>>(C)
-                        : ln_pick_of<LnBackward<T, 1>>(C);
+    constexpr int V = 16 / (int)sizeof(T);
+    if (C < V) return {LnBackward<T, 1, false>::template of<8, 1>(), 8};
+    return C % V == 0 ? ln_pick_of<LnBackward<T, V, false>>(C) : ln_pick_of<LnBackward<T, V, true>>(C);
 }
 
 int ln_validate(const dsattn_ln_desc *desc, const char *who)
