@@ -21,11 +21,12 @@ namespace {
 //     640 x   640 x   640            5.5   5.1      10.0  14.9       5.4   4.5
 //     100 x 4,096 x 4,096           17.0  32.0      46.5  79.5      12.3  17.6
 //     640 x 1,280 x 1,280           12.3   8.8      30.0  28.0      11.6   6.3
-bool small_is_faster(int32_t type, int64_t small_tiles, int64_t stages)
+// `more`: us that the tiles cost besides.
+bool small_is_faster(int32_t type, int64_t small_tiles, int64_t stages, double more = 0.0)
 {
     static const double small_stage[] = {0.17, 0.07, 0.1}, tile_stage[] = {0.6, 0.27, 0.35};  // by dsattn_dtype
     const double rounds = (double)((small_tiles + 255) / 256);
-    return 1.5 + rounds * (1.2 + small_stage[type] * (double)stages) < 2.0 + tile_stage[type] * (double)stages;
+    return 1.5 + rounds * (1.2 + small_stage[type] * (double)stages) < 2.0 + tile_stage[type] * (double)stages + more;
 }
 
 // Estimated us of `tiles` tiles of 256 x 256 (persistent), 128 x 128 or 64 x 64 and `stages` stages, bf16 or 8 bits: a start,
@@ -75,7 +76,7 @@ int compute_units(int dev)
     return n;
 }
 
-// The default cap on dynamic LDS is 64 KB; it is raised once for a kernel and device (0.4 us a call otherwise).
+// The default cap on dynamic LDS is 64 KB; it is raised once for a kernel and device, not at every call.
 hipError_t allow_lds(const void *fn, int lds)
 {
     if (lds <= 64 << 10) return hipSuccess;

@@ -279,7 +279,13 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
             g.dz_lds = kDzLargeLds;
             g.part_rows = 64;
         } else {
-            if (f32 ? tiles(d.rows, No, 128, 128) < 384
+            // fp32: 64 x 64 where the last round of 128 x 128 (512, two a compute unit) would be so empty that they keep less
+            // than 0.8 of the card busy.  us, 128 x 128 and 64 x 64, GELU, rows x c_in x c_out:
+            //    5,000 x 1,280 x 1,280   164  152 (0.78)      4,096 x 4,096 x 4,096   977  1,029 (1.0)
+            //   20,000 x   640 x   640   173  147 (0.77)      8,192 x 2,560 x 2,560   777    809 (0.83)
+            //   10,240 x 1,280 x 1,280   320  287 (0.78)      6,000 x   640 x 1,280  91.3   94.5 (0.92)
+            const int64_t f32_tiles = tiles(d.rows, No, 128, 128);
+            if (f32 ? f32_tiles * 10 < (f32_tiles + 511) / 512 * 512 * 8
                     : tile_estimate(64, tiles(d.rows, No, 64, 64), stages) < tile_estimate(128, tiles(d.rows, No, 128, 128), stages))
                 ++v;
             g.dz_fn = v->fn[gated];
@@ -294,7 +300,11 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
         g.dz = g.bytes;
         g.bytes += aligned((size_t)d.rows * No * es);
     }
-    g.x_small = small_is_faster(d.io_dtype, tiles(d.rows, d.c_in, 32, 32), (No * es + kRow - 1) / kRow);
+    // Where no workgroups of dz's turn W behind theirs, a kernel of its own does: its launch, and a read and a write of W.  us,
+    // dX by the kernel for few rows and of a turned W, bf16: 160 x 2,560 x 320 5.5 and 8.8, 640 x 640 x 640 6.5 and 10.7,
+    // 1,000 x 640 x 640 8.7 and 10.7, 300 x 2,560 x 2,560 25 and 32, 2,560 x 640 x 640 19 and 11.
+    const double turn_us = grad_is_dy(d) || g.dz_small ? 2.5 + 5e-7 * (double)(No * rowbytes) : 0.0;
+    g.x_small = small_is_faster(d.io_dtype, tiles(d.rows, d.c_in, 32, 32), (No * es + kRow - 1) / kRow, turn_us);
     g.turned = g.bytes;
     if (!g.x_small) g.bytes += aligned((size_t)No * d.c_in * es);
     g.sums = g.bytes;
