@@ -595,7 +595,7 @@ int dsattn_layernorm_backward_workspace(const dsattn_ln_desc *desc, size_t *byte
  *   dgamma,
  *   dbeta     : device, [channels] fp32, or NULL: not wanted
  *   workspace : device, at least dsattn_layernorm_backward_workspace() bytes, 16-byte aligned; may be
- *               NULL if dgamma and dbeta are.  Contents are overwritten; calls that share a
+ *               NULL if dgamma and dbeta are.  Contents may be overwritten; calls that share a
  *               workspace must not overlap in time
  * Outputs overlap the inputs in no other way, and not each other.  Runs on the current device;
  * enqueues one to three kernels on `stream`; allocates nothing.  Errors: EINVAL, EUNSUPPORTED, EHIP.

@@ -39,7 +39,8 @@ struct LnBackArgs {
     const void *X, *R, *dY, *dS;
     const float *gamma;
     void *dX;
-    float *partial;  // [groups][2][C]: sums of dy n and of dy; null where neither is wanted
+    float *dgamma, *dbeta;  // a workgroup's sums of dy n and of dy go to these and `part` on from those of the one before, or null
+    int64_t part;
     struct RowStats *stats;  // long rows only
     int64_t rows;
     int32_t C;
@@ -327,7 +328,8 @@ __global__ __launch_bounds__(256) void ln_row_kernel(const LnArgs a)
 }
 
 // A workgroup takes rows blockIdx.x, + gridDim.x, .. (times the rows that it has at once); a lane has the same channels of all of
-// them, adds up their dgamma and dbeta in registers, and the workgroup's sums go to `partial`: no atomics, one order.
+// them, adds up their dgamma and dbeta in registers, and the workgroup's sums go to memory for
+// ln_join_kernel, or to the result where there is one workgroup only: no atomics, one order.
 template <typename T, int V, int L, int NV, bool ODD>
 __global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_back_vec_kernel(const LnBackArgs a)
 {
@@ -388,9 +390,9 @@ __global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_back_vec_kernel(const L
             *(Piece *)((T *)a.dX + base + mine.c[i]) = p;
         }
     }
-    if (!a.partial) return;
-    using FloatsThere = typename Pieces::FloatsThere;
-    float *to = a.partial + (int64_t)blockIdx.x * 2 * C;
+    if (!a.dgamma && !a.dbeta) return;
+    typedef float Loose __attribute__((ext_vector_type(V), aligned(sizeof(float))));  // (as much as the caller's are aligned)
+    const int64_t part_at = (int64_t)blockIdx.x * a.part;
     if constexpr (PER > 1) {
         __shared__ Floats sums[256];
 #pragma unroll
@@ -400,19 +402,20 @@ __global__ __launch_bounds__(L <= 256 ? 256 : L) void ln_back_vec_kernel(const L
                 __syncthreads();
                 sums[threadIdx.x] = k ? db[i] : dg[i];
                 __syncthreads();
-                if (turn == 0 && mine.has(i)) {
+                float *to = k ? a.dbeta : a.dgamma;
+                if (to && turn == 0 && mine.has(i)) {
                     Floats v = sums[threadIdx.x];
 #pragma unroll
                     for (int w = 1; w < PER; ++w) v += sums[threadIdx.x + w * L];
-                    *(FloatsThere *)(to + (int64_t)k * C + mine.c[i]) = v;
+                    *(Loose *)(to + part_at + mine.c[i]) = v;
                 }
             }
     } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (!mine.has(i)) continue;
-            *(FloatsThere *)(to + mine.c[i]) = dg[i];
-            *(FloatsThere *)(to + (int64_t)C + mine.c[i]) = db[i];
+            if (a.dgamma) *(Loose *)(a.dgamma + part_at + mine.c[i]) = dg[i];
+            if (a.dbeta) *(Loose *)(a.dbeta + part_at + mine.c[i]) = db[i];
         }
     }
 }
@@ -458,8 +461,8 @@ __global__ __launch_bounds__(256) void ln_back_col_kernel(const LnBackArgs a)
         dg = fmaf(dy, a.stats[row].norm(s), dg);
         db += dy;
     }
-    a.partial[((int64_t)blockIdx.y * 2) * C + c] = dg;
-    a.partial[((int64_t)blockIdx.y * 2 + 1) * C + c] = db;
+    a.dgamma[blockIdx.y * a.part + c] = dg;
+    a.dbeta[blockIdx.y * a.part + c] = db;
 }
 
 // The partial sums of `groups` workgroups added up: 16 columns a workgroup, 64 threads to each.
@@ -569,7 +572,11 @@ LnBackLaunch ln_back_launch(const dsattn_ln_desc &d)
     if (k.fn) {
         const int per = k.lanes <= 256 ? 256 / k.lanes : 1;
         l.threads = k.lanes <= 256 ? 256 : k.lanes;
-        l.groups = (int)std::min<int64_t>((d.rows + per - 1) / per, k.lanes <= 256 ? 1024 : 512);
+        // Few rows take turns in one workgroup, which needs no join after it.  us of a call with and without, bf16:
+        // 8 x 320 (two turns) 10.2 7.3, 16 x 320 (four) 10.2 7.7, 8 x 1,280 (two) 10.1 7.8, 16 x 1,280 (four) 10.1 12.1,
+        // 4 x 2,560 (four) 9.9 10.9.  (Turns are short where rows are.)
+        const int turns = d.channels * (d.io_dtype == DSATTN_F32 ? 4 : 2) <= 1024 ? 4 : 2;
+        l.groups = d.rows <= turns * per ? 1 : (int)std::min<int64_t>((d.rows + per - 1) / per, k.lanes <= 256 ? 1024 : 512);
     } else {
         l.groups = (int)((d.rows + kLongRows - 1) / kLongRows);
     }
@@ -674,7 +681,10 @@ int dsattn_layernorm_backward(const dsattn_ln_desc *desc, const void *X, const v
             if (overlap(outputs[o].p, outputs[o].n, outputs[q].p, outputs[q].n))
                 return fail(DSATTN_EINVAL, "%s: two outputs overlap", who);
     }
-    LnBackArgs a{X, residual, dY, dsum, gamma, dX, sums ? (float *)workspace : nullptr, nullptr, d.rows, d.channels, d.eps};
+    const bool join = sums && (!l.fn || l.groups > 1);
+    float *partial = (float *)workspace;
+    LnBackArgs a{X, residual, dY, dsum, gamma, dX, join ? partial : dgamma, join ? partial + d.channels : dbeta,
+                 2 * (int64_t)d.channels, nullptr, d.rows, d.channels, d.eps};
     const bool f32 = d.io_dtype == DSATTN_F32;
     const hipStream_t st = (hipStream_t)stream;
     void *params[] = {&a};
@@ -691,8 +701,7 @@ int dsattn_layernorm_backward(const dsattn_ln_desc *desc, const void *X, const v
         if (e == hipSuccess && sums)
             e = hipLaunchKernel(fn, dim3((unsigned)(d.channels + 255) / 256, (unsigned)l.groups), dim3(256), params, 0, st);
     }
-    if (e == hipSuccess && sums) {
-        const float *partial = a.partial;
+    if (e == hipSuccess && join) {
         int groups = l.groups, C = d.channels;
         void *args[] = {&partial, &groups, &C, &dgamma, &dbeta};
         e = hipLaunchKernel((const void *)&ln_join_kernel, dim3((unsigned)(C + 15) / 16, 2), dim3(1024), args, 0, st);

@@ -195,6 +195,30 @@ def test_in_place(C, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 8, 9, 16, 17, 64, 129])
+@pytest.mark.parametrize("C", [5, 60, 320, 1279, 2560, 8192, 9000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sums_of_few_rows(rows, C, dtype):
+    """In one workgroup, or joined; to places aligned to four bytes; one of the two alone."""
+    x, r, gamma, beta, dy, ds = inputs(rows, C, dtype, 400 + rows + C, True)
+    want = gradients(x, r, gamma, 1e-6, dy, ds)
+    t = [v.to(DEV) for v in (x, r, gamma, dy, ds)]
+    wanted = [torch.full((C + 8,), 7.0, device=DEV) for _ in range(3)]
+    dg, db, alone = (v[1 + i:1 + i + C] for i, v in enumerate(wanted))
+    for dgamma, dbeta in ((dg, db), (None, alone)):
+        dX = torch.empty_like(t[0])
+        B.dsattn_layernorm_backward(rows, C, t[0], t[3], dX, residual=t[1], gamma=t[2], dsum=t[4], dgamma=dgamma, dbeta=dbeta,
+                                    workspace=space(rows, C, dtype), io_dtype=CODE[dtype])
+        torch.cuda.synchronize()
+        near(dX.float(), want[0], half_step(dtype))
+    near(dg, want[1])
+    near(db, want[2])
+    assert (alone == db).all()
+    for i, v in enumerate(wanted):
+        assert (v[:1 + i] == 7.0).all() and (v[1 + i + C:] == 7.0).all(), "written past the ends"
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("C", [1, 7, 9, 65, 257, 515, 1279, 2049, 4099, 9999])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_in_place_at_odd_lengths(C, dtype):
