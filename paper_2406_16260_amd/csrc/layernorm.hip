@@ -576,7 +576,10 @@ LnBackLaunch ln_back_launch(const dsattn_ln_desc &d)
         // 8 x 320 (two turns) 10.2 7.3, 16 x 320 (four) 10.2 7.7, 8 x 1,280 (two) 10.1 7.8, 16 x 1,280 (four) 10.1 12.1,
         // 4 x 2,560 (four) 9.9 10.9.  (Turns are short where rows are.)
         const int turns = d.channels * (d.io_dtype == DSATTN_F32 ? 4 : 2) <= 1024 ? 4 : 2;
-        l.groups = d.rows <= turns * per ? 1 : (int)std::min<int64_t>((d.rows + per - 1) / per, k.lanes <= 256 ? 1024 : 512);
+        // Else 1,024 workgroups (40,960 x 640 41 us, of 512 50), but 512 where those have four turns or less: what they leave for
+        // the join is more than what they read (4,484 x 824 16.0 us with 1,024, 14.6, 2,000 x 4,096 29.8 and 25.6).
+        const int64_t all = (d.rows + per - 1) / per;
+        l.groups = d.rows <= turns * per ? 1 : (int)std::min<int64_t>(all, k.lanes <= 256 && all > 4 * 512 ? 1024 : 512);
     } else {
         l.groups = (int)((d.rows + kLongRows - 1) / kLongRows);
     }
