@@ -320,6 +320,17 @@ def test_bad_pointers_are_refused():
         assert f(*args, None) == B.DSATTN_EINVAL, args
 
 
+def test_launches_that_are_too_large_are_refused():
+    """At addresses that no tensor has, so that nothing else is wrong with the calls; nothing runs."""
+    lib, p = B.load(), [k << 50 for k in range(1, 9)]
+    for kw in (dict(streams=65536, frames=1, spatial=1, channels=1), dict(streams=1, frames=1, spatial=1 << 20, channels=1 << 13),
+               dict(streams=1 << 10, frames=3, spatial=1 << 13, channels=1 << 10)):
+        d = ctypes.byref(_desc(**kw))
+        assert lib.dsattn_gated_scan(d, None, p[0], p[1], None, p[2], None, None, None, 0, None) == B.DSATTN_EUNSUPPORTED, kw
+        assert lib.dsattn_gated_scan_backward(d, None, p[0], p[1], p[2], p[3], None, p[4], p[5], None, None, 0,
+                                              None) == B.DSATTN_EUNSUPPORTED, kw
+
+
 @pytest.mark.gpu
 def test_tensors_that_do_not_fit_are_refused():
     x = torch.zeros(2, 40, 3, 8, device=DEV, dtype=torch.bfloat16)

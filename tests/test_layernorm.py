@@ -399,6 +399,19 @@ def test_bad_pointers_are_refused():
         assert lib.dsattn_layernorm_backward(*args, None) == B.DSATTN_EINVAL, args
 
 
+def test_launches_that_are_too_large_are_refused():
+    """At addresses that no tensor has, so that nothing else is wrong with the calls; nothing runs."""
+    lib, p = B.load(), [k << 50 for k in range(1, 8)]
+    d = _desc(rows=1 << 24, channels=4096)  # 256 threads a row
+    assert lib.dsattn_layernorm(ctypes.byref(d), p[0], None, None, None, None, p[1], None, None) == B.DSATTN_EUNSUPPORTED
+    d = _desc(rows=1 << 24, channels=65536)
+    assert lib.dsattn_layernorm(ctypes.byref(d), p[0], None, None, None, None, p[1], None, None) == B.DSATTN_EUNSUPPORTED
+    for rows, sums in ((1 << 24, False), (64 * 65535 + 1, True)):
+        need = B.dsattn_layernorm_backward_workspace(rows, 20000)
+        assert lib.dsattn_layernorm_backward(ctypes.byref(_desc(rows=rows, channels=20000)), p[0], None, None, p[1], None, p[2],
+                                             p[3] if sums else None, None, p[4] if sums else None, need, None) == B.DSATTN_EUNSUPPORTED
+
+
 @pytest.mark.gpu
 def test_tensors_that_do_not_fit_are_refused():
     x = torch.zeros(4, 64, device=DEV, dtype=torch.bfloat16)

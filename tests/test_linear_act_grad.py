@@ -306,6 +306,17 @@ def test_bad_pointers_are_refused():
         assert f(*args, None) == B.DSATTN_EINVAL, args
 
 
+def test_launches_that_are_too_large_are_refused():
+    """At addresses that no tensor has, so that nothing else is wrong with the calls; nothing runs."""
+    lib, p = B.load(), [k << 50 for k in range(1, 8)]
+    for kw in (dict(rows=1 << 30, c_in=9, c_out=9, n_w=1, act=1), dict(rows=3, c_in=65537, c_out=65537, n_w=1, act=1),
+               dict(rows=1 << 30, c_in=64, c_out=64, n_w=1, act=0, flags=B.DSATTN_FLAG_FORCE_GENERIC)):
+        need = B.dsattn_linear_act_backward_workspace(kw["rows"], kw["c_in"], kw["c_out"], act=kw["act"], flags=kw.get("flags", 0))
+        w = (ctypes.c_void_p * 2)(p[1], None)
+        assert lib.dsattn_linear_act_backward(ctypes.byref(_desc(**kw)), p[0], w, None, p[2], p[3], None, None, p[4], need,
+                                              None) == B.DSATTN_EUNSUPPORTED, kw
+
+
 @pytest.mark.gpu
 def test_tensors_that_do_not_fit_are_refused():
     bf = dict(dtype=torch.bfloat16, device=DEV)
