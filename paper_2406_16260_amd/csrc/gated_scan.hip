@@ -55,14 +55,15 @@ __device__ __forceinline__ float exp_of(float x)
 // What a gate keeps, a = sigmoid(g), what it leaves, 1 - a, and what it lets in, w(a): each with a small relative error.  (The
 // instructions for quotients and roots, an ulp off at most, not the sequences that round them, which took twice the time.)
 // With e = e^-g, a = 1 / (1 + e), 1 - a = e a, and 1 - a^2 = e a (1 + a), whose root is taken with e^(-g / 2) outside, so that it
-// does not underflow before w does.  Below -87 a gate counts as one of -87, 2^-125.5: e stays finite.
+// does not underflow before w does.  Below -87 a gate counts as one of -87, 2^-125.5: e stays finite; beyond 210, where even
+// e^(-g / 2) is 0 in fp32, as one of 210: infinite logits are gates of 0 and of 1.
 struct Gate {
     float keep, leave, let;
 };
 template <int MODE>
 __device__ __forceinline__ Gate gate_of(float g)
 {
-    const float x = g < -87.f ? 87.f : -g;  // (a NaN stays)
+    const float x = __builtin_elementwise_minimum(__builtin_elementwise_maximum(-g, -210.f), 87.f);  // (a NaN stays)
     Gate q;
     if constexpr (MODE == DSATTN_SCAN_NORM) {
         const float h = exp_of(0.5f * x), e = h * h;

@@ -174,6 +174,36 @@ def test_far_gates(T, mode):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 40, 600])
+def test_gates_that_are_masks(T, dtype, mode):
+    """Logits of infinity, of the type's largest number and of some hundreds among ordinary ones, of either sign: frames that
+    leave the state as it is, and frames that begin anew."""
+    x, g, h0, dy, dend = inputs(2, T, 3, 64, dtype, 13)
+    far = torch.tensor([float("inf"), torch.finfo(TORCH[dtype]).max, 1e30, 1000.0, 209.0, 150.0, 95.0])
+    far = torch.cat([far, -far])
+    gen = torch.Generator().manual_seed(14)
+    which = torch.randint(0, len(far), g.shape, generator=gen)
+    g = torch.where(torch.rand(g.shape, generator=gen) < 0.3, far[which], g.float()).to(TORCH[dtype])
+    dev = [t.to(DEV) for t in (x, g, h0, dy, dend)]
+    Y, dX, dG = (torch.empty_like(dev[0]) for _ in range(3))
+    S, hT, dh = torch.empty(2, -(-T // STEP), 3, 64, device=DEV), torch.empty_like(dev[2]), torch.empty_like(dev[2])
+    kw = dict(mode=MODES[mode], workspace=space(2, T, 3, 64, dtype), io_dtype=CODE[dtype])
+    B.dsattn_gated_scan(2, T, 3, 64, dev[0], dev[1], Y, start_state=dev[2], end_state=hT, states=S, **kw)
+    B.dsattn_gated_scan_backward(2, T, 3, 64, dev[0], dev[1], S, dev[3], dX, dG, dend_state=dev[4], dstart_state=dh, **kw)
+    torch.cuda.synchronize()
+    for b in range(2):
+        h, e, _ = forward(x[b], g[b], h0[b], mode, T)
+        near(Y[b].float(), h[1:], e[1:], dtype, "Y")
+        near(hT[b], h[-1], e[-1], "f32", "state")
+        rx, rg, rh = backward(x[b], g[b], h0[b], mode, T, dy[b], dend[b])
+        near(dX[b].float(), *rx, dtype, "dX")
+        near(dG[b].float(), *rg, dtype, "dG")
+        near(dh[b], *rh, "f32", "dh0")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("Bs,T,P,C", [(1, 1, 160, 320), (2, 50, 9, 40), (1, 900, 1, 64)])
 def test_in_place_and_frame_by_frame(Bs, T, P, C, dtype):
