@@ -21,12 +21,12 @@ namespace {
 //     640 x   640 x   640            5.5   5.1      10.0  14.9       5.4   4.5
 //     100 x 4,096 x 4,096           17.0  32.0      46.5  79.5      12.3  17.6
 //     640 x 1,280 x 1,280           12.3   8.8      30.0  28.0      11.6   6.3
-// `more`: us that the tiles cost besides.
-bool small_is_faster(int32_t type, int64_t small_tiles, int64_t stages, double more = 0.0)
+// `more`: us that the tiles cost besides; `deep`: with two stages ahead.
+bool small_is_faster(int32_t type, int64_t small_tiles, int64_t stages, double more = 0.0, bool deep = false)
 {
     static const double small_stage[] = {0.17, 0.07, 0.1}, tile_stage[] = {0.6, 0.27, 0.35};  // by dsattn_dtype
     const double rounds = (double)((small_tiles + 255) / 256);
-    return 1.5 + rounds * (1.2 + small_stage[type] * (double)stages) < 2.0 + tile_stage[type] * (double)stages + more;
+    return 1.5 + rounds * (1.2 + small_stage[type] * (double)stages) < 2.0 + (deep ? 0.24 : tile_stage[type]) * (double)stages + more;
 }
 
 // Estimated us of `tiles` tiles of 256 x 256 (persistent), 128 x 128 or 64 x 64 and `stages` stages, bf16 or 8 bits: a start,
@@ -40,13 +40,14 @@ bool small_is_faster(int32_t type, int64_t small_tiles, int64_t stages, double m
 //     20,000 x 1,280 x   320     29.0  18.9     23.3  15.8    28.9  19.4
 //     40,960 x   320 x   320     19.2  17.4     17.6  14.4    22.4  19.7
 //      8,000 x   640 x   640     13.5  10.8     13.1  10.1    17.9  12.8
-double tile_estimate(int size, int64_t tiles, int64_t stages)
+// `deep`: with two stages ahead.
+double tile_estimate(int size, int64_t tiles, int64_t stages, bool deep = false)
 {
     const double st = (double)stages, n = (double)tiles;
     const int64_t full = tiles / 512, rest = tiles - 512 * full, rounds = (tiles + 255) / 256;
     if (size == 256) return 3.0 + (double)rounds * (1.22 * st + 5.0);
     if (size == 128)
-        return 3.0 + (double)full * (0.95 * st + 2.0) + (rest > 256 ? 0.82 * st + 2.6 : rest > 0 ? 0.61 * st + 2.9 : 0.0);
+        return 3.0 + (double)full * (0.95 * st + 2.0) + (rest > 256 ? 0.82 * st + 2.6 : rest > 0 ? (deep ? 0.54 : 0.61) * st + 2.9 : 0.0);
     static const double stage[] = {0.25, 0.3, 0.41, 0.61};
     return 4.0 + 1.3e-3 * n + st * (rounds > 4 ? std::max(1.0, 8.2e-4 * n) : stage[rounds - 1]);
 }

@@ -663,8 +663,8 @@ __global__ __launch_bounds__(512, 2) void act_small_kernel(const std::conditiona
 }
 
 // One tile a workgroup: two LDS slots, two to four workgroups on a compute unit, whose loads and barriers hide behind each
-// other's multiplies.  A workgroup of WVM x WVN wavefronts computes a (BS MB WVM) x (BS NB WVN) tile.
-template <typename T, int MB, int NB, int WVM, int WVN, bool GATED, typename TO, bool GRAD = false>
+// other's multiplies; more slots, and as many stages but one ahead, for workgroups that are alone.  A workgroup of WVM x WVN wavefronts computes a (BS MB WVM) x (BS NB WVN) tile.
+template <typename T, int MB, int NB, int WVM, int WVN, bool GATED, typename TO, bool GRAD = false, int SLOTS = 2>
 __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const std::conditional_t<GRAD, ActGradArgs, ActArgs> a)
 {
     using M = Mul<T>;
@@ -699,11 +699,11 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const std::
     const __amdgpu_buffer_rsrc_t wres0 = rows_from(a.W[0], n0, a.Cout, rowbytes);
     const __amdgpu_buffer_rsrc_t wres1 = GATED ? rows_from(a.W[1], n0, a.Cout, rowbytes) : wres0;
     const uint32_t xoff = (uint32_t)((wv * (8 * GA) + lr) * rowbytes + lc * 16);
-    int stage_no = 0;
+    int stage_no = 0, to = 0;  // the next stage that is asked for, and its slot
     auto issue_stage = [&]() __attribute__((always_inline)) {
         const bool live = stage_no * kRow + lc * 16 < rowbytes;
-        unsigned char *as = smem + (stage_no & 1) * BUF + wv * (GA * 1024);
-        unsigned char *bs = smem + (stage_no & 1) * BUF + ABYTES + wv * (GB * 1024);
+        unsigned char *as = smem + to * BUF + wv * (GA * 1024);
+        unsigned char *bs = smem + to * BUF + ABYTES + wv * (GB * 1024);
 #pragma unroll
         for (int l = 0; l < GA; ++l)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
@@ -721,8 +721,13 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const std::
                                                          live ? off : kOob, 0, 0, 0);
         }
         ++stage_no;
+        to = SLOTS == 2 ? to ^ 1 : to + 1 == SLOTS ? 0 : to + 1;
     };
+    const int stages = (rowbytes + kRow - 1) / kRow;
     issue_stage();
+#pragma unroll
+    for (int s = 1; s < SLOTS - 1; ++s)
+        if (s < stages) issue_stage();
     for (int r = threadIdx.x; r < BN; r += 64 * NW) {
         float b, s = 1.f;
         column<BS, GATED, SCALED>(a, n0, r, b, s);
@@ -743,17 +748,24 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const std::
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) koff[kk] = M::offset(lane, kk);
     const int abase = (wm * BS * MB + lane % BS) * kRow, bbase = ABYTES + (wn * BS * NB + lane % BS) * kRow;
-    const int stages = (rowbytes + kRow - 1) / kRow;
+    int slot = 0;
     for (int ks = 0; ks < stages; ++ks) {
-        // This wavefront's loads of stage ks have landed and its reads of stage ks - 1 are done; behind the
-        // barrier everybody's are, and the slot of stage ks - 1 is free.
+        // This wavefront's loads of stage ks have landed (those of the stages behind it may be on their way) and its reads of
+        // stage ks - 1 are done; behind the barrier everybody's are, and the slot of stage ks - 1 is free.
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        const int behind = stage_no - 1 - ks;
+        if (SLOTS > 3 && behind >= 2)
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * (GA + GB)));
+        else if (SLOTS > 2 && behind >= 1)
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(GA + GB));
+        else
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        if (ks + 1 < stages) issue_stage();
-        const unsigned char *buf = smem + (ks & 1) * BUF;
+        if (ks + SLOTS - 1 < stages) issue_stage();
+        const unsigned char *buf = smem + slot * BUF;
+        slot = SLOTS == 2 ? slot ^ 1 : slot + 1 == SLOTS ? 0 : slot + 1;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             typename M::Frag af[MB], bf[NB];

@@ -175,6 +175,7 @@ struct GradLaunch {
     bool dz_large = false, dz_small = false;
     int part_rows = 256;                             // rows of a part of the column sums
     bool x_small = false;                              // dX by the kernel for few rows; else W is turned for a product
+    int x_deep = 0;                                    // by tiles of 64 or 128 with two stages ahead, or 0: dsattn_linear_act
     const void *w_fn = nullptr;                          // kernel of dW
     int w_rows = 0, w_cols = 0, w_waves = 0, w_lds = 0, splits = 1, stages = 0;
     size_t dz = 0, turned = 0, sums = 0, partial = 0, bytes = 0;    // places in the workspace, and its size
@@ -198,6 +199,27 @@ struct GradVariant {
       (const void *)&act_tile_kernel<T, MB, NB, WVM, WVN, true, T, true>}}
 const GradVariant kDzTiles[2][2] = {{DSATTN_GRAD_TILE(float, 2, 4, 4, 2), DSATTN_GRAD_TILE(float, 1, 4, 4, 1)},
                                     {DSATTN_GRAD_TILE(__bf16, 2, 4, 4, 2), DSATTN_GRAD_TILE(__bf16, 1, 4, 4, 1)}};
+// bf16, two stages ahead.  Where tiles are so few that all are on the card at once, a long row's stages wait for their loads less
+// than with one ahead, which leaves the LDS to more workgroups.  us of 64 x 64 tiles, and of 128 x 128, one ahead and two (dz with
+// its sums joined, in a captured graph), rows x c_in x c_out:
+//     150 x 4,312 x 3,272 (156 tiles, 52)      44.7  28.5    65.7  48.0
+//     300 x 2,560 x 2,560 (200, 60)            26.3  18.4    36.7  30.7
+//   1,000 x 1,280 x 1,280 (320, 80)            17.1  14.9    21.5  20.7
+//   2,560 x 1,280 x 1,280 (800, 200)           23.4  25.8    24.5  22.1
+//   1,000 x 4,096 x 4,096 (1,024, 256)         61.4  82.4    51.8  48.7
+//   2,560 x   640 x   640 (400, 100; 10 stages)  10.8  11.1    14.0  14.4
+#define DSATTN_GRAD_DEEP(MB, NB, WVM, WVN)                                                                  \
+    {16 * MB * WVM, 16 * NB * WVN, WVM * WVN, 3 * (16 * MB * WVM + 16 * NB * WVN) * kRow, 16 * MB,          \
+     {(const void *)&act_tile_kernel<__bf16, MB, NB, WVM, WVN, false, __bf16, true, 3>,                     \
+      (const void *)&act_tile_kernel<__bf16, MB, NB, WVM, WVN, true, __bf16, true, 3>}}
+const GradVariant kDzDeep[2] = {DSATTN_GRAD_DEEP(2, 4, 4, 2), DSATTN_GRAD_DEEP(1, 4, 4, 1)};
+const void *const kXDeep[2] = {(const void *)&act_tile_kernel<__bf16, 2, 4, 4, 2, false, __bf16, false, 3>,
+                               (const void *)&act_tile_kernel<__bf16, 2, 2, 2, 2, false, __bf16, false, 3>};
+bool deep_is_faster(bool f32, int size, int64_t tiles, int64_t stages)
+{
+    return !f32 && stages >= 16 && tiles <= (size == 64 ? 512 : 256);
+}
+
 const void *const kDzSmall[2][2] = {
     {(const void *)&act_small_kernel<float, false, float, true>, (const void *)&act_small_kernel<float, true, float, true>},
     {(const void *)&act_small_kernel<__bf16, false, __bf16, true>, (const void *)&act_small_kernel<__bf16, true, __bf16, true>}};
@@ -262,15 +284,16 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
     if (!grad_is_dy(d)) {
         g.part_rows = 32;
         const GradVariant *v = kDzTiles[!f32];
-        if (small_is_faster(d.io_dtype, tiles(d.rows, No, 32, 32), stages)) {
+        const int64_t n64 = tiles(d.rows, No, 64, 64), n128 = tiles(d.rows, No, 128, 128);
+        const bool deep64 = deep_is_faster(f32, 64, n64, stages), deep128 = deep_is_faster(f32, 128, n128, stages);
+        const double us64 = tile_estimate(64, n64, stages), us128 = tile_estimate(128, n128, stages, deep128);
+        if (small_is_faster(d.io_dtype, tiles(d.rows, No, 32, 32), stages, 0.0, deep64)) {
             g.dz_small = true;
             g.dz_fn = kDzSmall[!f32][gated];
             g.dz_rows = g.dz_cols = 32;
             g.dz_waves = 8;
             g.dz_lds = kSmallLds;
-        } else if (!f32 && tile_estimate(256, tiles(d.rows, No, 256, 256), stages) <
-                               std::min(tile_estimate(128, tiles(d.rows, No, 128, 128), stages),
-                                        tile_estimate(64, tiles(d.rows, No, 64, 64), stages))) {
+        } else if (!f32 && tile_estimate(256, tiles(d.rows, No, 256, 256), stages) < std::min(us128, us64)) {
             g.dz_large = true;
             g.dz_fn = kDzLarge[gated][d.act];
             g.dz_rows = 256;
@@ -284,10 +307,9 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
             //    5,000 x 1,280 x 1,280   164  152 (0.78)      4,096 x 4,096 x 4,096   977  1,029 (1.0)
             //   20,000 x   640 x   640   173  147 (0.77)      8,192 x 2,560 x 2,560   777    809 (0.83)
             //   10,240 x 1,280 x 1,280   320  287 (0.78)      6,000 x   640 x 1,280  91.3   94.5 (0.92)
-            const int64_t f32_tiles = tiles(d.rows, No, 128, 128);
-            if (f32 ? f32_tiles * 10 < (f32_tiles + 511) / 512 * 512 * 8
-                    : tile_estimate(64, tiles(d.rows, No, 64, 64), stages) < tile_estimate(128, tiles(d.rows, No, 128, 128), stages))
-                ++v;
+            const bool by64 = f32 ? n128 * 10 < (n128 + 511) / 512 * 512 * 8 : us64 < us128;
+            if (by64 ? deep64 : deep128) v = kDzDeep;
+            v += by64;
             g.dz_fn = v->fn[gated];
             g.dz_rows = v->rows;
             g.dz_cols = v->cols;
@@ -304,7 +326,14 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
     // dX by the kernel for few rows and of a turned W, bf16: 160 x 2,560 x 320 5.5 and 8.8, 640 x 640 x 640 6.5 and 10.7,
     // 1,000 x 640 x 640 8.7 and 10.7, 300 x 2,560 x 2,560 25 and 32, 2,560 x 640 x 640 19 and 11.
     const double turn_us = grad_is_dy(d) || g.dz_small ? 2.5 + 5e-7 * (double)(No * rowbytes) : 0.0;
-    g.x_small = small_is_faster(d.io_dtype, tiles(d.rows, d.c_in, 32, 32), (No * es + kRow - 1) / kRow, turn_us);
+    const int64_t x_stages = (No * es + kRow - 1) / kRow, x64 = tiles(d.rows, d.c_in, 64, 64), x128 = tiles(d.rows, d.c_in, 128, 128);
+    const bool x_deep64 = deep_is_faster(f32, 64, x64, x_stages), x_deep128 = deep_is_faster(f32, 128, x128, x_stages);
+    g.x_small = small_is_faster(d.io_dtype, tiles(d.rows, d.c_in, 32, 32), x_stages, turn_us, x_deep64);
+    if (!g.x_small && !f32) {
+        const double us64 = tile_estimate(64, x64, x_stages), us128 = tile_estimate(128, x128, x_stages, x_deep128);
+        if (std::min(us64, us128) <= tile_estimate(256, tiles(d.rows, d.c_in, 256, 256), x_stages))
+            g.x_deep = us64 < us128 ? (x_deep64 ? 64 : 0) : x_deep128 ? 128 : 0;
+    }
     g.turned = g.bytes;
     if (!g.x_small) g.bytes += aligned((size_t)No * d.c_in * es);
     g.sums = g.bytes;
@@ -405,10 +434,28 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
             void *params[] = {(void *)&turn};
             launch(f32 ? (const void *)&grad_turn_kernel<float> : (const void *)&grad_turn_kernel<__bf16>, dim3((unsigned)turns), 256, params, 0);
         }
-        if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
-        const dsattn_linear_act_desc x = product_of_dx(d);
-        const int rc = dsattn_linear_act(&x, a.dz, nullptr, &turn.Wt, nullptr, nullptr, nullptr, a.dX, st);
-        if (rc != DSATTN_OK) return rc;
+        if (g.x_deep) {
+            ActArgs x{};
+            x.X = a.dz;
+            x.W[0] = turn.Wt;
+            x.Y = a.dX;
+            x.M = d.rows;
+            x.Cin = No;
+            x.Cout = d.c_in;
+            x.n_w = 1;
+            x.act = DSATTN_ACT_NONE;
+            x.tiles_n = (d.c_in + g.x_deep - 1) / g.x_deep;
+            x.tiles = (int32_t)((d.rows + g.x_deep - 1) / g.x_deep) * x.tiles_n;
+            x.per_xcd = (x.tiles + kXcds - 1) / kXcds;
+            x.panel = 1;
+            void *params[] = {&x};
+            launch(kXDeep[g.x_deep == 64], dim3((unsigned)(x.per_xcd * kXcds)), g.x_deep == 64 ? 256 : 512, params, 3 * 2 * g.x_deep * kRow);
+        } else {
+            if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
+            const dsattn_linear_act_desc x = product_of_dx(d);
+            const int rc = dsattn_linear_act(&x, a.dz, nullptr, &turn.Wt, nullptr, nullptr, nullptr, a.dX, st);
+            if (rc != DSATTN_OK) return rc;
+        }
     }
     if (a.dW[0] || a.dW[1]) {
         GradWArgs w{};
