@@ -24,6 +24,7 @@ struct ActArgs {
     int32_t Cin, Cout, n_w, act;
     int32_t tiles_n, tiles, per_xcd;  // column tiles; all of them; ceil(tiles / 8)
     int32_t panel;                    // persistent kernels: column tiles that are numbered together
+    int32_t tiles_m;                  // gradients' tiles: row tiles where they are numbered column by column, or 0
 };
 
 // W_0 and W_1 below each other, transposed, for the product that gives dX: 64 x 64 numbers a workgroup, of workgroups behind
@@ -682,10 +683,11 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const std::
     // workgroup -> tile: XCD x (= blockIdx % 8) owns a contiguous run of tiles
     const int tile = (int)(blockIdx.x % kXcds) * a.per_xcd + (int)(blockIdx.x / kXcds);
     if (tile >= a.tiles) return;  // whole workgroup: no barrier has been reached yet
-    const int mt = tile / a.tiles_n;
+    const bool by_column = (GRAD || SLOTS > 2) && a.tiles_m;
+    const int mt = by_column ? tile % a.tiles_m : tile / a.tiles_n, nt = by_column ? tile / a.tiles_m : tile - mt * a.tiles_n;
     const int64_t m0 = (int64_t)mt * BM;
     constexpr int BO = GATED ? BN / 2 : BN;  // output channels of the tile
-    const int n0 = (tile - mt * a.tiles_n) * BO;
+    const int n0 = nt * BO;
 
     const int lane = threadIdx.x & 63;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

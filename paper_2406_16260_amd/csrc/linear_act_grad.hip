@@ -398,7 +398,9 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         }
         const int cols = g.dz_cols / d.n_w;
         z.tiles_n = (d.c_out + cols - 1) / cols;
-        z.tiles = (int32_t)((d.rows + g.dz_rows - 1) / g.dz_rows) * z.tiles_n;
+        const int32_t tiles_m = (int32_t)((d.rows + g.dz_rows - 1) / g.dz_rows);
+        z.tiles = tiles_m * z.tiles_n;
+        z.tiles_m = down_reads_less(tiles_m, z.tiles_n) ? tiles_m : 0;
         z.per_xcd = (z.tiles + kXcds - 1) / kXcds;
         z.panel = g.dz_large ? act_panel(z.tiles_n) : 1;
         z.groups = g.dz_small ? z.tiles : z.per_xcd * kXcds;
@@ -445,7 +447,9 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
             x.n_w = 1;
             x.act = DSATTN_ACT_NONE;
             x.tiles_n = (d.c_in + g.x_deep - 1) / g.x_deep;
-            x.tiles = (int32_t)((d.rows + g.x_deep - 1) / g.x_deep) * x.tiles_n;
+            const int32_t tiles_m = (int32_t)((d.rows + g.x_deep - 1) / g.x_deep);
+            x.tiles = tiles_m * x.tiles_n;
+            x.tiles_m = down_reads_less(tiles_m, x.tiles_n) ? tiles_m : 0;
             x.per_xcd = (x.tiles + kXcds - 1) / kXcds;
             x.panel = 1;
             void *params[] = {&x};
