@@ -168,6 +168,14 @@ def test_large_sizes(M, K, N, act, gated):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("act,gated", [("none", False), ("gelu", True), ("silu", False)])
+@pytest.mark.parametrize("M,K,N", [(500, 1288, 1304), (350, 2056, 1096), (1100, 1032, 1048), (2500, 1288, 1272), (130, 4104, 2056)])
+def test_some_hundred_long_rows(M, K, N, act, gated):
+    """Stages that are asked for two ahead, tiles down the columns, ends within a stage and a tile."""
+    run(M, K, N, "bf16", act, gated)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M,K,N", [(4100, 320, 648), (700, 1288, 640)])
 def test_large_sizes_in_fp32(M, K, N):
     run(M, K, N, "f32", "gelu", True)
