@@ -511,6 +511,21 @@ __device__ __forceinline__ void epilogue_grad_fetch(const ActGradArgs &a, GradIn
     }
 }
 
+// A workgroup's tile of the gradients' small kernels: along the rows, or, with tiles_m, down the columns, a run of tiles on an XCD.
+template <typename A>
+__device__ __forceinline__ bool small_tile(const A &a, int &mt, int &nt)
+{
+    if (!a.tiles_m) {
+        mt = (int)blockIdx.x / a.tiles_n;
+        nt = (int)blockIdx.x - mt * a.tiles_n;
+        return true;
+    }
+    const int tile = (int)(blockIdx.x % kXcds) * a.per_xcd + (int)(blockIdx.x / kXcds);
+    nt = tile / a.tiles_m;
+    mt = tile - nt * a.tiles_m;
+    return tile < a.tiles;
+}
+
 // Small products: 32 rows of X by 32 rows of W a workgroup, whose eight wavefronts share the contraction: a wavefront takes
 // every eighth stage through two LDS slots of its own, waits for nobody, and the eight sums are added up in LDS at the
 // end, in an order that does not change.  What such a call takes is latency, an eighth of a row's length of it.  (Fetched in
@@ -526,9 +541,15 @@ __global__ __launch_bounds__(512, 2) void act_small_kernel(const std::conditiona
     static_assert(BS == 16, "two blocks of 16 rows of either");
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     constexpr int BO = GATED ? 16 : 32;
-    const int mt = (int)blockIdx.x / a.tiles_n;
+    int mt, nt;
+    if constexpr (GRAD) {
+        if (!small_tile(a, mt, nt)) return;
+    } else {
+        mt = (int)blockIdx.x / a.tiles_n;
+        nt = (int)blockIdx.x - mt * a.tiles_n;
+    }
     const int64_t m0 = (int64_t)mt * 32;
-    const int n0 = ((int)blockIdx.x - mt * a.tiles_n) * BO;
+    const int n0 = nt * BO;
     const int lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rowbytes = a.Cin * (int)sizeof(T);

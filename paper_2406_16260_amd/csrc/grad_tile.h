@@ -560,6 +560,7 @@ struct GradXArgs {
     void *dX;
     int64_t M;
     int32_t Cin, Cout, No, tiles_n;
+    int32_t tiles_m, tiles, per_xcd;  // tiles_m: row tiles where tiles are numbered down the columns, or 0
 };
 template <typename T>
 __global__ __launch_bounds__(512, 2) void grad_x_small_kernel(const GradXArgs a)
@@ -568,9 +569,10 @@ __global__ __launch_bounds__(512, 2) void grad_x_small_kernel(const GradXArgs a)
     using B = Cols<T, 32>;
     constexpr int NW = 8, SR = 36, SLOT = 64 * kRow, KS = B::KS;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    const int mt = (int)blockIdx.x / a.tiles_n;
+    int mt, nt;
+    if (!small_tile(a, mt, nt)) return;
     const int64_t m0 = (int64_t)mt * 32;
-    const int n0 = ((int)blockIdx.x - mt * a.tiles_n) * 32;
+    const int n0 = nt * 32;
     const int lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int zbytes = a.No * B::ES, xbytes = a.Cin * B::ES, setbytes = a.Cout * B::ES;

@@ -377,6 +377,10 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
     };
     const TurnArgs turn{{a.W[0], a.W[1]}, space + g.turned, d.c_in, d.c_out, No, (d.c_in + 63) / 64};
     const int turns = a.dX && !g.x_small ? (No + 63) / 64 * turn.tiles_c : 0;  // workgroups that turn W
+    // W beyond what the L2s hold: the small kernels go down its columns and read it once.  us, along and down:
+    // 64 x 4,096 x 4,096 41.1 37.2, 130 x 4,104 x 2,056 (dX, dW) 42.4 32.0, 128 x 4,096 x 2 x 4,096 111 95.3; 160 x 1,280 x 1,280
+    // 17.6 18.4
+    const bool large_w = (int64_t)No * d.c_in * (f32 ? 4 : 2) >= 8 << 20;
     bool turned = false;
     float *parts = (float *)(space + g.sums);
     const int n_parts = (int)((d.rows + g.part_rows - 1) / g.part_rows);
@@ -400,10 +404,10 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         z.tiles_n = (d.c_out + cols - 1) / cols;
         const int32_t tiles_m = (int32_t)((d.rows + g.dz_rows - 1) / g.dz_rows);
         z.tiles = tiles_m * z.tiles_n;
-        z.tiles_m = down_reads_less(tiles_m, z.tiles_n) ? tiles_m : 0;
+        z.tiles_m = (g.dz_small ? tiles_m > 1 && large_w : down_reads_less(tiles_m, z.tiles_n)) ? tiles_m : 0;
         z.per_xcd = (z.tiles + kXcds - 1) / kXcds;
         z.panel = g.dz_large ? act_panel(z.tiles_n) : 1;
-        z.groups = g.dz_small ? z.tiles : z.per_xcd * kXcds;
+        z.groups = g.dz_small && !z.tiles_m ? z.tiles : z.per_xcd * kXcds;
         z.turn = turn;
         void *params[] = {&z};
         turned = turns && !g.dz_small;
@@ -427,10 +431,14 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         launch((const void *)&grad_join_kernel, dim3((unsigned)join.groups), 1024, params, 0);
     }
     if (a.dX && g.x_small) {
+        const int tiles_m = (int)((d.rows + 31) / 32);
         GradXArgs x{a.dz, {a.W[0], a.W[1]}, a.dX, d.rows, d.c_in, d.c_out, No, (d.c_in + 31) / 32};
+        x.tiles_m = tiles_m > 1 && large_w ? tiles_m : 0;
+        x.tiles = tiles_m * x.tiles_n;
+        x.per_xcd = (x.tiles + kXcds - 1) / kXcds;
         void *params[] = {&x};
         launch(f32 ? (const void *)&grad_x_small_kernel<float> : (const void *)&grad_x_small_kernel<__bf16>,
-               dim3((unsigned)((d.rows + 31) / 32 * x.tiles_n)), 512, params, kSmallLds);
+               dim3((unsigned)(x.tiles_m ? x.per_xcd * kXcds : x.tiles)), 512, params, kSmallLds);
     } else if (a.dX) {
         if (!turned) {
             void *params[] = {(void *)&turn};
