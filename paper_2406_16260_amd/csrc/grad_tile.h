@@ -552,7 +552,7 @@ __global__ __launch_bounds__(256) void grad_w_join_kernel(const GradWArgs a)
 
 // dX of few rows: dX = sum dz_k W_k, 32 x 32 a workgroup, whose eight wavefronts share the contraction as in act_small_kernel
 // (a wavefront takes every eighth stage through two LDS slots of its own).  W's rows are what is contracted over, and are
-// read transposed; stages do not cross from one set to the other.  160 x 1,280 x 1,280: 4.9 us, and 3.4 + 5.1 where a
+// read transposed; stages do not cross from one set to the other.  A long contraction for few tiles is split over workgroups.  160 x 1,280 x 1,280: 4.9 us, and 3.4 + 5.1 where a
 // kernel of its own turns W first.
 struct GradXArgs {
     const void *dz;  // [M][No]
@@ -561,6 +561,8 @@ struct GradXArgs {
     int64_t M;
     int32_t Cin, Cout, No, tiles_n;
     int32_t tiles_m, tiles, per_xcd;  // tiles_m: row tiles where tiles are numbered down the columns, or 0
+    int32_t span;                     // stages of a split (blockIdx.y)
+    float *partial;                   // [splits][M][Cin], or null: one split
 };
 template <typename T>
 __global__ __launch_bounds__(512, 2) void grad_x_small_kernel(const GradXArgs a)
@@ -586,7 +588,8 @@ __global__ __launch_bounds__(512, 2) void grad_x_small_kernel(const GradXArgs a)
         const int r = l * B::RPI + lane / B::CPR, c = (lane % B::CPR) ^ B::swizzle(r);
         woff[l] = n0 + c * B::PER < a.Cin ? (uint32_t)(r * xbytes + c * 16) : kOob;
     }
-    const int per = (a.Cout + KS - 1) / KS, stages = a.No / a.Cout * per;  // of a set, of all
+    const int per = (a.Cout + KS - 1) / KS;  // stages of a set
+    const int first = (int)blockIdx.y * a.span, stages = min(a.No / a.Cout * per, first + a.span);
     auto issue = [&](int ks, int slot) __attribute__((always_inline)) {
         const int set = ks >= per ? 1 : 0, k = ks - set * per;
         const bool live = k * kRow + lc * 16 < setbytes;
@@ -606,9 +609,9 @@ __global__ __launch_bounds__(512, 2) void grad_x_small_kernel(const GradXArgs a)
     for (int kk = 0; kk < 2; ++kk) koff[kk] = M::offset(lane, kk);
 #pragma unroll
     for (int j = 0; j < 2; ++j) wp[j] = 4096 + B::row(lane) * B::RB + B::place(lane, j);
-    if (wv < stages) issue(wv, 0);
+    if (first + wv < stages) issue(first + wv, 0);
     int slot = 0;
-    for (int ks = wv; ks < stages; ks += NW) {
+    for (int ks = first + wv; ks < stages; ks += NW) {
         const bool more = ks + NW < stages;
         if (more) issue(ks + NW, slot ^ 1);
         asm volatile("" ::: "memory");
@@ -650,14 +653,17 @@ __global__ __launch_bounds__(512, 2) void grad_x_small_kernel(const GradXArgs a)
     const int64_t m = m0 + row;
     if (m >= a.M || n0 + c >= a.Cin) return;
     typedef T Pair __attribute__((ext_vector_type(2)));  // (Cin is even)
+    typedef float Floats __attribute__((ext_vector_type(2)));
+    Floats z{};
+#pragma unroll
+    for (int v = 0; v < NW; ++v) z += *(const Floats *)&sums[v][row][c];
+    if (a.partial) {
+        *(Floats *)(a.partial + ((int64_t)blockIdx.y * a.M + m) * a.Cin + n0 + c) = z;
+        return;
+    }
     Pair y;
 #pragma unroll
-    for (int o = 0; o < 2; ++o) {
-        float z = 0.f;
-#pragma unroll
-        for (int v = 0; v < NW; ++v) z += sums[v][row][c + o];
-        y[o] = (T)z;
-    }
+    for (int o = 0; o < 2; ++o) y[o] = (T)z[o];
     *(Pair *)((T *)a.dX + m * a.Cin + n0 + c) = y;
 }
 

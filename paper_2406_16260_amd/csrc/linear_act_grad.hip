@@ -175,10 +175,11 @@ struct GradLaunch {
     bool dz_large = false, dz_small = false;
     int part_rows = 256;                             // rows of a part of the column sums
     bool x_small = false;                              // dX by the kernel for few rows; else W is turned for a product
+    int x_splits = 1, x_span = 0;                      // the former's splits of the contraction, and their stages
     int x_deep = 0;                                    // by tiles of 64 or 128 with two stages ahead, or 0: dsattn_linear_act
     const void *w_fn = nullptr;                          // kernel of dW
     int w_rows = 0, w_cols = 0, w_waves = 0, w_lds = 0, splits = 1, stages = 0;
-    size_t dz = 0, turned = 0, sums = 0, partial = 0, bytes = 0;    // places in the workspace, and its size
+    size_t dz = 0, turned = 0, sums = 0, partial = 0, x_partial = 0, bytes = 0;    // places in the workspace, and its size
 };
 
 // dX as a product of dz and the turned W
@@ -334,6 +335,20 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
         if (std::min(us64, us128) <= tile_estimate(256, tiles(d.rows, d.c_in, 256, 256), x_stages))
             g.x_deep = us64 < us128 ? (x_deep64 ? 64 : 0) : x_deep128 ? 128 : 0;
     }
+    if (g.x_small) {
+        // One round of workgroups leaves the card to a longer contraction's splits, of three stages a wavefront or more, joined by
+        // a kernel of its own.  us of a call, bf16 and fp32: 1 x 392 x 2 x 5,040 33 71, with splits 22 32; 44 x 72 x 2 x 4,040 29 52,
+        // 21 22; 32 x 2,048 x 4,096 30 50, 28 40.
+        const int64_t all = d.n_w * ((d.c_out * es + kRow - 1) / kRow), n = tiles(d.rows, d.c_in, 32, 32);
+        const int64_t splits = std::min(256 / n, all / 24);
+        g.x_span = (int)all;
+        if (splits >= 2) {
+            g.x_span = (int)((all + splits - 1) / splits);
+            g.x_splits = (int)((all + g.x_span - 1) / g.x_span);
+            g.x_partial = g.bytes;
+            g.bytes += aligned((size_t)g.x_splits * d.rows * d.c_in * sizeof(float));
+        }
+    }
     g.turned = g.bytes;
     if (!g.x_small) g.bytes += aligned((size_t)No * d.c_in * es);
     g.sums = g.bytes;
@@ -374,6 +389,12 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
     auto launch = [&](const void *fn, dim3 grid, int threads, void **params, int lds) {
         if (e == hipSuccess) e = allow_lds(fn, lds);
         if (e == hipSuccess) e = hipLaunchKernel(fn, grid, dim3((unsigned)threads), params, (size_t)lds, st);
+    };
+    auto join_splits = [&](GradWArgs &w) {
+        const bool many = w.items / w.tiles >= 16;
+        const int fours = many ? 32 : 256;  // of a workgroup
+        void *params[] = {&w};
+        launch(kWJoin[!f32][many], dim3((unsigned)(((int64_t)w.No * w.Cin / 4 + fours - 1) / fours)), 256, params, 0);
     };
     const TurnArgs turn{{a.W[0], a.W[1]}, space + g.turned, d.c_in, d.c_out, No, (d.c_in + 63) / 64};
     const int turns = a.dX && !g.x_small ? (No + 63) / 64 * turn.tiles_c : 0;  // workgroups that turn W
@@ -436,9 +457,21 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         x.tiles_m = tiles_m > 1 && large_w ? tiles_m : 0;
         x.tiles = tiles_m * x.tiles_n;
         x.per_xcd = (x.tiles + kXcds - 1) / kXcds;
+        x.span = g.x_span;
+        x.partial = g.x_splits > 1 ? (float *)(space + g.x_partial) : nullptr;
         void *params[] = {&x};
         launch(f32 ? (const void *)&grad_x_small_kernel<float> : (const void *)&grad_x_small_kernel<__bf16>,
-               dim3((unsigned)(x.tiles_m ? x.per_xcd * kXcds : x.tiles)), 512, params, kSmallLds);
+               dim3((unsigned)(x.tiles_m ? x.per_xcd * kXcds : x.tiles), (unsigned)g.x_splits), 512, params, kSmallLds);
+        if (g.x_splits > 1) {
+            GradWArgs s{};  // (one matrix of rows x c_in)
+            s.dW[0] = a.dX;
+            s.partial = x.partial;
+            s.No = s.Cout = (int)d.rows;
+            s.Cin = d.c_in;
+            s.tiles = 1;
+            s.items = g.x_splits;
+            join_splits(s);
+        }
     } else if (a.dX) {
         if (!turned) {
             void *params[] = {(void *)&turn};
@@ -496,10 +529,7 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
         }
         void *params[] = {&w};
         launch(g.w_fn, dim3((unsigned)(w.groups + join.groups)), 64 * g.w_waves, params, g.w_lds);
-        if (g.splits > 1) {
-            const int fours = g.splits >= 16 ? 32 : 256;  // of a workgroup
-            launch(kWJoin[!f32][g.splits >= 16], dim3((unsigned)(((int64_t)No * d.c_in / 4 + fours - 1) / fours)), 256, params, 0);
-        }
+        if (g.splits > 1) join_splits(w);
     }
     if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
     return DSATTN_OK;

@@ -176,6 +176,15 @@ def test_some_hundred_long_rows(M, K, N, act, gated):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("act,gated", [("none", False), ("gelu", True), ("silu", False)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(1, 8, 5120), (1, 392, 5040), (33, 72, 4040), (100, 136, 3208), (160, 264, 2568)])
+def test_few_rows_of_many_channels(M, K, N, dtype, act, gated):
+    """dX's contraction split over workgroups, the last split a part of one."""
+    run(M, K, N, dtype, act, gated)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M,K,N", [(4100, 320, 648), (700, 1288, 640)])
 def test_large_sizes_in_fp32(M, K, N):
     run(M, K, N, "f32", "gelu", True)
