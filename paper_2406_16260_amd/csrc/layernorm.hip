@@ -7,9 +7,9 @@
 // The mean is taken off twice, the second time that of the differences: what the first left of it by rounding (a row whose
 // mean is 1,000 times its spread would lose ten bits of the spread to that) is gone, and the variance comes with it.
 // us and TB/s (a large copy 5.1):
-//   368,640 x 1,280, bf16, residual and sum         692     5.45
-//   40,960 x 640, bf16, residual, all gradients     59.8    4.4, of which the joining kernel is 4.4 us
-//   368,640 x 1,280, the same                       1,021   4.6
+//   368,640 x 1,280, bf16, residual and sum         656     5.75
+//   40,960 x 640, bf16, residual, all gradients     59.6    4.4, of which the joining kernel is 4.3 us
+//   368,640 x 1,280, the same                       968     4.9
 //   24,591 x 1,863, bf16, residual, then all gradients   75.5 and 105, the floors 72 and 90 (pieces of one number: 225 and 307)
 //   40 x 1,280                                      6.9, of which 4.3 are the host's marshalling and 2.6 its launch
 #include <hip/hip_runtime.h>
