@@ -134,7 +134,7 @@ __global__ __launch_bounds__(1024) void grad_join_kernel(const JoinArgs a)
 }
 
 // One tile of one split a workgroup, two LDS slots, two workgroups on a compute unit.
-template <typename T, int MB, int NB, int WVM, int WVN>
+template <typename T, int MB, int NB, int WVM, int WVN, int SLOTS = 2>
 __global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const GradWArgs a)
 {
     using M = Mul<T>;
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const Gr
     const int64_t first = (int64_t)split * a.stages * KS;
     const int stages = (int)min((int64_t)a.stages, (a.M - first + KS - 1) / KS);
     // (without the casts of the offsets the compiler's host pass has no stub of this kernel)
-    auto issue_stage = [&](int ks) __attribute__((always_inline)) {
-        unsigned char *as = smem + (ks & 1) * BUF + wv * (GA * 1024), *bs = smem + (ks & 1) * BUF + ABYTES + wv * (GB * 1024);
+    auto issue_stage = [&](int ks, int to) __attribute__((always_inline)) {
+        unsigned char *as = smem + to * BUF + wv * (GA * 1024), *bs = smem + to * BUF + ABYTES + wv * (GB * 1024);
         const int64_t k0 = first + (int64_t)ks * KS;
         const __amdgpu_buffer_rsrc_t zres = cols_from(a.dz, k0, a.M, zbytes, o0 * A::ES);
         const __amdgpu_buffer_rsrc_t xres = cols_from(a.X, k0, a.M, xbytes, c0 * B::ES);
@@ -189,17 +189,27 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const Gr
     for (int i = 0; i < MB; ++i) ap[i] = A::row(lane) * A::RB + A::place(lane, wm * MB + i);
 #pragma unroll
     for (int j = 0; j < NB; ++j) bp[j] = ABYTES + B::row(lane) * B::RB + B::place(lane, wn * NB + j);
-    issue_stage(0);
+    constexpr int AHEAD = SLOTS - 1;
+    static_assert(SLOTS <= 3, "one stage or two ahead");
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s)
+        if (s < stages) issue_stage(s, s);
+    int slot = 0, next = AHEAD;
     for (int ks = 0; ks < stages; ++ks) {
-        // This wavefront's loads of stage ks have landed and its reads of stage ks - 1 are done; behind the
-        // barrier everybody's are, and the slot of stage ks - 1 is free.
+        // This wavefront's loads of stage ks have landed (those of the one behind it may be on their way) and its reads of
+        // stage ks - 1 are done; behind the barrier everybody's are, and the slot of stage ks - 1 is free.
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+        if (SLOTS > 2 && ks + 1 < stages)
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(GA + GB));
+        else
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        if (ks + 1 < stages) issue_stage(ks + 1);
-        const unsigned char *buf = smem + (ks & 1) * BUF;
+        if (ks + AHEAD < stages) issue_stage(ks + AHEAD, next);
+        const unsigned char *buf = smem + slot * BUF;
+        slot = slot + 1 == SLOTS ? 0 : slot + 1;
+        next = next + 1 == SLOTS ? 0 : next + 1;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             typename M::Frag af[MB], bf[NB];

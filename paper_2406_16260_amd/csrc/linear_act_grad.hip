@@ -209,6 +209,7 @@ const GradVariant kDzTiles[2][2] = {{DSATTN_GRAD_TILE(float, 2, 4, 4, 2), DSATTN
 //   2,560 x 1,280 x 1,280 (800, 200)           23.4  25.8    24.5  22.1
 //   1,000 x 4,096 x 4,096 (1,024, 256)         61.4  82.4    51.8  48.7
 //   2,560 x   640 x   640 (400, 100; 10 stages)  10.8  11.1    14.0  14.4
+// dW by one split: 2,560 x 1,280 x 1,280 (400) 25.2 20.8, 5,000 x 1,280 x 2,560 (200 of 128 x 128) 56.3 48.9, (800) 71.5 75.3.
 #define DSATTN_GRAD_DEEP(MB, NB, WVM, WVN)                                                                  \
     {16 * MB * WVM, 16 * NB * WVN, WVM * WVN, 3 * (16 * MB * WVM + 16 * NB * WVN) * kRow, 16 * MB,          \
      {(const void *)&act_tile_kernel<__bf16, MB, NB, WVM, WVN, false, __bf16, true, 3>,                     \
@@ -237,6 +238,8 @@ const void *const kWJoin[2][2] = {  // few splits, 16 and more
 const void *const kWTiles[2][2] = {  // 64 x 64, 128 x 128
     {(const void *)&grad_w_tile_kernel<float, 2, 2, 2, 2>, (const void *)&grad_w_tile_kernel<float, 2, 4, 4, 2>},
     {(const void *)&grad_w_tile_kernel<__bf16, 2, 2, 2, 2>, (const void *)&grad_w_tile_kernel<__bf16, 2, 4, 4, 2>}};
+const void *const kWDeep[2] = {(const void *)&grad_w_tile_kernel<__bf16, 2, 2, 2, 2, 3>,  // two stages ahead
+                               (const void *)&grad_w_tile_kernel<__bf16, 2, 4, 4, 2, 3>};
 
 // Estimated us of the weights' gradient by tiles of a size, tm x tn of them (the last column of 256 may be half empty) and splits of
 // `stages` stages.  256: rounds of one workgroup a compute unit.  Smaller ones: a stage takes its latency, or the unit's
@@ -252,7 +255,8 @@ const void *const kWTiles[2][2] = {  // 64 x 64, 128 x 128
 //    fp32   640 x   640 x   640     17.2     15.6      45.0      20.8              64 / 2 13.7
 //        10,240 x 1,280 x 1,280    354.0    293.7     653.7     316.4              128 / 12 282.7
 //        10,240 x   320 x   320    209.8     59.7     646.5     169.8              64 / 16 32.7
-double w_estimate(int size, int64_t tm, int64_t tn, int64_t cin, int64_t splits, int64_t stages, bool f32, double numbers)
+double w_estimate(int size, int64_t tm, int64_t tn, int64_t cin, int64_t splits, int64_t stages, bool f32, double numbers,
+                  bool deep)
 {
     const double st = (double)stages, join = splits > 1 ? 4.0 + 8.0 * (double)splits * numbers / 7e6 : 0.0;
     if (size == 256) {
@@ -261,7 +265,7 @@ double w_estimate(int size, int64_t tm, int64_t tn, int64_t cin, int64_t splits,
         const double t = (double)rounds + 0.6 * (double)((std::max<int64_t>(0, h - spare) + 31) / 32);
         return t * (1.2 * st + 7.0) + join;
     }
-    const double latency = size == 128 ? (f32 ? 2.0 : 0.67) : (f32 ? 0.65 : 0.45), each = size == 128 ? (f32 ? 2.0 : 0.5) : (f32 ? 0.55 : 0.2);
+    const double latency = size == 128 ? (f32 ? 2.0 : deep ? 0.55 : 0.67) : (f32 ? 0.65 : deep ? 0.3 : 0.45), each = size == 128 ? (f32 ? 2.0 : 0.5) : (f32 ? 0.55 : 0.2);
     const int64_t n = tm * tn * splits, fit = size == 128 ? 2 : 5;
     const double c = n <= 256 * fit ? (double)((n + 255) / 256) : (double)n / 256.0 + 0.5;
     return st * std::max(latency + 0.05 * (std::min(c, (double)fit) - 1.0), each * c) + 4.0 + join;
@@ -357,14 +361,17 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
     const int KS = kRow / (int)es;
     const int64_t all = (d.rows + KS - 1) / KS;
     double us = 1e30;
+    bool w_deep = false;
     for (int size : {64, 128, 256}) {
         if (size == 256 && f32) break;
         const int64_t tm = (No + size - 1) / size, tn = (d.c_in + size - 1) / size;
         for (int64_t splits = 1; splits <= std::min<int64_t>(64, std::max<int64_t>(1, all / 2)); ++splits) {
             const int64_t stages = (all + splits - 1) / splits, used = (all + stages - 1) / stages;
             if (used != splits) continue;
-            const double t = w_estimate(size, tm, tn, d.c_in, splits, stages, f32, (double)No * (double)d.c_in);
+            const bool deep = size < 256 && deep_is_faster(f32, size, tm * tn * splits, stages);
+            const double t = w_estimate(size, tm, tn, d.c_in, splits, stages, f32, (double)No * (double)d.c_in, deep);
             if (t >= us) continue;
+            w_deep = deep;
             us = t;
             g.w_rows = g.w_cols = size;
             g.splits = (int)splits;
@@ -372,8 +379,8 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
         }
     }
     g.w_waves = g.w_rows == 64 ? 4 : 8;
-    g.w_lds = 2 * (g.w_rows + g.w_cols) * kRow;
-    g.w_fn = g.w_rows == 256 ? (const void *)&grad_w_large_kernel : kWTiles[!f32][g.w_rows == 128];
+    g.w_lds = (w_deep ? 3 : 2) * (g.w_rows + g.w_cols) * kRow;
+    g.w_fn = g.w_rows == 256 ? (const void *)&grad_w_large_kernel : w_deep ? kWDeep[g.w_rows == 128] : kWTiles[!f32][g.w_rows == 128];
     g.partial = g.bytes;
     if (g.splits > 1) g.bytes += aligned((size_t)g.splits * No * d.c_in * sizeof(float));
     return g;
