@@ -84,8 +84,15 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*part)[N])
     }
 }
 
+constexpr float kLargest = 0x1.fffffep127f;
+
 // each(f) calls f(s) for the lane's numbers of the row, sums(v) adds v over the row's lanes: whether another turn is needed
 // depends on sums only, which all lanes of a row have.
+// The mean is that of numbers times 2^-21, whose sum is within fp32's range (what that takes of numbers below 2^-105 is part of the
+// rest).  Where what it is off by, the rest, is more than a quarter of the spread, it is put right by that and the turn taken again:
+// the mean of a row of equal numbers is then that number itself, its variance 0, and that of numbers which differ in their last
+// bits loses no more to the rest's square than it has.  Only then are the squares asked whether they are within range: eps is lost
+// beside a variance in `unit`s (1e-6 * 2^-150), which has to be that of numbers that do differ.
 template <typename Each, typename Sums>
 __device__ __forceinline__ RowStats row_stats(int C, float eps, Each each, Sums sums)
 {
@@ -94,12 +101,11 @@ __device__ __forceinline__ RowStats row_stats(int C, float eps, Each each, Sums 
 #pragma clang fp contract(off)
     RowStats t{1.f, 1.f, 0.f, 0.f, 0.f};
     const float inv = 1.f / (float)C;
-    float var = 0.f;
-    for (int turn = 0;; ++turn) {
-        float v[2] = {0.f, 0.f};
-        each([&](float s) __attribute__((always_inline)) { v[0] = fmaf(s, t.unit, v[0]); });
-        sums(v);
-        t.mean = v[0] * inv;
+    float v[2] = {0.f, 0.f}, var;
+    each([&](float s) __attribute__((always_inline)) { v[0] = fmaf(s, 0x1p-21f, v[0]); });
+    sums(v);
+    t.mean = fminf(fmaxf(v[0] * inv * 0x1p21f, -kLargest), kLargest);
+    for (int better = 0;;) {
         v[0] = v[1] = 0.f;
         each([&](float s) __attribute__((always_inline)) {
             const float d = (s * t.unit - t.mean) * t.gain;
@@ -108,14 +114,28 @@ __device__ __forceinline__ RowStats row_stats(int C, float eps, Each each, Sums 
         });
         sums(v);
         t.rest = v[0] * inv;
-        var = fmaf(-t.rest, t.rest, v[1] * inv);
-        if (turn == 1) break;
-        if (!(v[1] < INFINITY))
+        const float square = v[1] * inv;
+        var = fmaf(-t.rest, t.rest, square);
+        const bool beyond = !(v[1] < INFINITY), off = var < 0.9375f * square;
+        if (__builtin_expect(v[1] >= 0x1p-100f && !beyond && !off, 1)) break;
+        if (better < 3 && (beyond || off)) {
+            const float mean = t.mean + t.rest * (t.gain == 1.f ? 1.f : 0x1p-100f);
+            if (mean != t.mean && fabsf(mean) < INFINITY) {
+                t.mean = mean;
+                ++better;
+                continue;
+            }
+        }
+        if (t.unit != 1.f || t.gain != 1.f) break;
+        if (beyond) {
             t.unit = 0x1p-75f;
-        else if (v[1] < 0x1p-100f && eps < 0x1p-80f)
+            t.mean *= t.unit;
+        } else if (eps < 0x1p-80f && v[1] < 0x1p-100f) {
             t.gain = 0x1p100f;
-        else
+        } else {
             break;
+        }
+        better = 0;
     }
     // (var is not below 0 but by rounding; a NaN stays)
     const float g = t.unit * t.gain;
