@@ -384,7 +384,7 @@ void scan_chunks(const dsattn_scan_desc &d, int32_t &chunk, int32_t &chunks)
     chunks = 1;
     if (want >= 4) {
         chunk = (int32_t)(((d.frames + want - 1) / want + kStep - 1) / kStep * kStep);
-        chunks = (d.frames + chunk - 1) / chunk;
+        chunks = (int32_t)(((int64_t)d.frames + chunk - 1) / chunk);
     }
 }
 
