@@ -611,8 +611,9 @@ int dsattn_layernorm_backward(const dsattn_ln_desc *desc, const void *X, const v
  * with w by `mode`.  States are fp32 throughout.  Frames are [streams, frames, P, channels] as in
  * dsattn_sink_forward; a stream goes on in a later call with the state that it left, one frame a
  * call or many.  Many frames of few channels are cut into chunks and joined, so that a
- * stream's last bits depend on how it is cut into calls.  Infinite logits are gates of 0 and 1; an infinite
- * state stays infinite or is NaN.
+ * stream's last bits depend on how it is cut into calls.  Logits of -87 and less, minus infinity among
+ * them, are gates of 0: such a frame begins anew, free of the (finite) state before it.  Infinite ones are
+ * gates of 1; numbers exp(-g) below 2^-126 count as 0.  An infinite state stays infinite or is NaN.
  */
 #define DSATTN_SCAN_FRAMES 16 /* frames between two of the states kept for the backward pass */
 

@@ -55,8 +55,9 @@ __device__ __forceinline__ float exp_of(float x)
 // What a gate keeps, a = sigmoid(g), what it leaves, 1 - a, and what it lets in, w(a): each with a small relative error.  (The
 // instructions for quotients and roots, an ulp off at most, not the sequences that round them, which took twice the time.)
 // With e = e^-g, a = 1 / (1 + e), 1 - a = e a, and 1 - a^2 = e a (1 + a), whose root is taken with e^(-g / 2) outside, so that it
-// does not underflow before w does.  Below -87 a gate counts as one of -87, 2^-125.5: e stays finite; beyond 210, where even
-// e^(-g / 2) is 0 in fp32, as one of 210: infinite logits are gates of 0 and of 1.
+// does not underflow before w does.  From -87 down, where e would soon be infinite, e is that of -87 and nothing is kept (2^-125.5 at
+// most is left out): a frame that begins anew is free of the state before it, of whatever size that is.  Beyond 210, where even
+// e^(-g / 2) is 0 in fp32, a gate is one of 210: infinite logits are gates of 0 and of 1.
 struct Gate {
     float keep, leave, let;
 };
@@ -76,6 +77,7 @@ __device__ __forceinline__ Gate gate_of(float g)
         q.leave = e * q.keep;
         q.let = MODE == DSATTN_SCAN_MEAN ? q.leave : 1.f;
     }
+    if (x >= 87.f) q.keep = 0.f;  // (not of a NaN)
     return q;
 }
 // dw / dg
