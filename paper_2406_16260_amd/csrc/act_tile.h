@@ -685,7 +685,8 @@ __global__ __launch_bounds__(512, 2) void act_small_kernel(const std::conditiona
 }
 
 // One tile a workgroup: two LDS slots, two to four workgroups on a compute unit, whose loads and barriers hide behind each
-// other's multiplies; more slots, and as many stages but one ahead, for workgroups that are alone.  A workgroup of WVM x WVN wavefronts computes a (BS MB WVM) x (BS NB WVN) tile.
+// other's multiplies; three slots, two stages ahead, for workgroups that are alone.  A workgroup of WVM x WVN wavefronts computes
+// a (BS MB WVM) x (BS NB WVN) tile.
 template <typename T, int MB, int NB, int WVM, int WVN, bool GATED, typename TO, bool GRAD = false, int SLOTS = 2>
 __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const std::conditional_t<GRAD, ActGradArgs, ActArgs> a)
 {
@@ -695,6 +696,7 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const std::
     constexpr int BM = BS * MB * WVM, BN = BS * NB * WVN;
     constexpr int GA = BM / 8 / NW, GB = BN / 8 / NW;  // 8-row groups (one load instruction) per wavefront
     static_assert(GA * 8 * NW == BM && GB * 8 * NW == BN, "the wavefronts share the loads evenly");
+    static_assert(SLOTS == 2 || SLOTS == 3, "one stage or two ahead");
     constexpr int ABYTES = BM * kRow, BUF = (BM + BN) * kRow;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     __shared__ __attribute__((aligned(16))) float cols[2][BN];
@@ -773,13 +775,10 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void act_tile_kernel(const std::
     const int abase = (wm * BS * MB + lane % BS) * kRow, bbase = ABYTES + (wn * BS * NB + lane % BS) * kRow;
     int slot = 0;
     for (int ks = 0; ks < stages; ++ks) {
-        // This wavefront's loads of stage ks have landed (those of the stages behind it may be on their way) and its reads of
+        // This wavefront's loads of stage ks have landed (those of the one behind it may be on their way) and its reads of
         // stage ks - 1 are done; behind the barrier everybody's are, and the slot of stage ks - 1 is free.
         asm volatile("" ::: "memory");
-        const int behind = stage_no - 1 - ks;
-        if (SLOTS > 3 && behind >= 2)
-            __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * (GA + GB)));
-        else if (SLOTS > 2 && behind >= 1)
+        if (SLOTS > 2 && ks + 1 < stages)
             __builtin_amdgcn_s_waitcnt(waitcnt_vm(GA + GB));
         else
             __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));

@@ -399,15 +399,17 @@ size_t scan_bytes(const dsattn_scan_desc &d)
 
 enum { kPartsPass, kRunPass, kBackPartsPass, kBackPass };
 
+// (two channels a lane are 512 wavefronts or more, which are in one chunk)
 template <typename T, int V, int MODE>
 const void *scan_kernel_of(int pass)
 {
-    switch (pass) {
-    case kPartsPass: return (const void *)&scan_kernel<T, V, MODE, false>;
-    case kRunPass: return (const void *)&scan_kernel<T, V, MODE, true>;
-    case kBackPartsPass: return (const void *)&scan_back_parts_kernel<T, V>;
-    default: return (const void *)&scan_back_kernel<T, V, MODE>;
+    if (pass == kRunPass) return (const void *)&scan_kernel<T, V, MODE, true>;
+    if (pass == kBackPass) return (const void *)&scan_back_kernel<T, V, MODE>;
+    if constexpr (V == 1) {
+        if (pass == kPartsPass) return (const void *)&scan_kernel<T, V, MODE, false>;
+        if (pass == kBackPartsPass) return (const void *)&scan_back_parts_kernel<T, V>;
     }
+    return nullptr;
 }
 // One pass over many channels: eight bytes a lane (384 frames x 640 x 640, bf16, 4.7 TB/s instead of 4.45).
 const void *scan_wide_of(const dsattn_scan_desc &d)

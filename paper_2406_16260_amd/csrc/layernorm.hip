@@ -519,7 +519,8 @@ const void *ln_of(int nv)
 {
     if constexpr (L == 64)
         if (nv == 1) return K::template of<L, 1>();
-    if (nv <= 2) return K::template of<L, 2>();
+    if constexpr (L != 512)  // (what 512 lanes have begins where 256 end, at three pieces each)
+        if (nv <= 2) return K::template of<L, 2>();
     if constexpr (L < 1024) {
         if (nv == 3) return K::template of<L, 3>();
         if (nv == 4) return K::template of<L, 4>();

@@ -379,7 +379,7 @@ GradLaunch grad_pick(const dsattn_linear_act_desc &d)
         }
     }
     g.w_waves = g.w_rows == 64 ? 4 : 8;
-    g.w_lds = (w_deep ? 3 : 2) * (g.w_rows + g.w_cols) * kRow;
+    g.w_lds = g.w_rows == 256 ? kLargeLds : (w_deep ? 3 : 2) * (g.w_rows + g.w_cols) * kRow;
     g.w_fn = g.w_rows == 256 ? (const void *)&grad_w_large_kernel : w_deep ? kWDeep[g.w_rows == 128] : kWTiles[!f32][g.w_rows == 128];
     g.partial = g.bytes;
     if (g.splits > 1) g.bytes += aligned((size_t)g.splits * No * d.c_in * sizeof(float));
