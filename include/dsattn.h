@@ -613,7 +613,8 @@ int dsattn_layernorm_backward(const dsattn_ln_desc *desc, const void *X, const v
  * call or many.  Many frames of few channels are cut into chunks and joined, so that a
  * stream's last bits depend on how it is cut into calls.  Logits of -87 and less, minus infinity among
  * them, are gates of 0: such a frame begins anew, free of the (finite) state before it.  Infinite ones are
- * gates of 1; numbers exp(-g) below 2^-126 count as 0.  An infinite state stays infinite or is NaN.
+ * gates of 1; beside that numbers exp(-g) below 2^-126 count as 0, and what a gate keeps or leaves is off
+ * by 2^-125 at most.  An infinite state stays infinite or is NaN.
  */
 #define DSATTN_SCAN_FRAMES 16 /* frames between two of the states kept for the backward pass */
 

@@ -11,7 +11,7 @@
 // us and TB/s (a large copy 5.1):
 //   384 frames x 640 x 640, bf16, forward           197     4.8
 //   384 frames x 160 x 1,280, bf16, backward        172     4.7
-//   2 x 16,384 frames x 1, x 1,280, bf16, forward   97      2.6, 4.3 of what is read twice; 88 in a loop over one set of tensors
+//   2 x 16,384 frames x 1, x 1,280, bf16, forward   98      2.6, 4.3 of what is read twice
 //   1 frame x 160 x 1,280, bf16                     7.4     of which 4.8 are the host's marshalling and 2.6 its launch
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -55,16 +55,18 @@ __device__ __forceinline__ float exp_of(float x)
 // What a gate keeps, a = sigmoid(g), what it leaves, 1 - a, and what it lets in, w(a): each with a small relative error.  (The
 // instructions for quotients and roots, an ulp off at most, not the sequences that round them, which took twice the time.)
 // With e = e^-g, a = 1 / (1 + e), 1 - a = e a, and 1 - a^2 = e a (1 + a), whose root is taken with e^(-g / 2) outside, so that it
-// does not underflow before w does.  From -87 down, where e would soon be infinite, e is that of -87 and nothing is kept (2^-125.5 at
-// most is left out): a frame that begins anew is free of the state before it, of whatever size that is.  Beyond 210, where even
-// e^(-g / 2) is 0 in fp32, a gate is one of 210: infinite logits are gates of 0 and of 1.
+// does not underflow before w does.  Below -87, where e would soon be infinite, e is that of -87, and what a gate of -87 keeps,
+// 2^-125.5, is taken off what every gate does: it is 0 there, so that a frame that begins anew is free of the state before it, of
+// whatever size that is, and unchanged from 2^-100 up.  (One instruction; with a comparison and a choice 384 frames x 640 x 640 197 us
+// and 2,304 x 160 x 320 226, instead of 194.6 and 215.)  Beyond 210, where even e^(-g / 2) is 0 in fp32, a gate is one of 210: infinite
+// logits are gates of 0 and of 1.
 struct Gate {
     float keep, leave, let;
 };
+constexpr float kFar = 87.f;
 template <int MODE>
-__device__ __forceinline__ Gate gate_of(float g)
+__device__ __forceinline__ Gate gate_at(float x)  // x: -g
 {
-    const float x = __builtin_elementwise_minimum(__builtin_elementwise_maximum(-g, -210.f), 87.f);  // (a NaN stays)
     Gate q;
     if constexpr (MODE == DSATTN_SCAN_NORM) {
         const float h = exp_of(0.5f * x), e = h * h;
@@ -77,7 +79,21 @@ __device__ __forceinline__ Gate gate_of(float g)
         q.leave = e * q.keep;
         q.let = MODE == DSATTN_SCAN_MEAN ? q.leave : 1.f;
     }
-    if (x >= 87.f) q.keep = 0.f;  // (not of a NaN)
+    return q;
+}
+// What a gate of -87 keeps, by the instructions that gates come from.
+template <int MODE>
+__device__ __forceinline__ float least_kept()
+{
+    float x = kFar;
+    asm volatile("" : "+v"(x));  // (or the compiler works it out by arithmetic of its own)
+    return gate_at<MODE>(x).keep;
+}
+template <int MODE>
+__device__ __forceinline__ Gate gate_of(float g, float least)
+{
+    Gate q = gate_at<MODE>(__builtin_elementwise_minimum(__builtin_elementwise_maximum(-g, -210.f), kFar));  // (a NaN stays)
+    q.keep -= least;
     return q;
 }
 // dw / dg
@@ -123,6 +139,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const ScanArgs a)
     if (p.c >= a.n) return;
     const int64_t base = (int64_t)p.b * a.T * a.n + p.c0, part = ((int64_t)p.b * a.chunks + p.j) * a.n + p.c;
     const T *X = (const T *)a.X + base, *G = (const T *)a.G + base;
+    const float least = least_kept<MODE>();
     float h[V], prod[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -163,7 +180,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const ScanArgs a)
             Piece y;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Gate q = gate_of<MODE>((float)gc[i][v]);
+                const Gate q = gate_of<MODE>((float)gc[i][v], least);
                 h[v] = fmaf(q.keep, h[v], q.let * (float)xc[i][v]);
                 if constexpr (STORE)
                     y[v] = (T)h[v];
@@ -196,6 +213,7 @@ __global__ __launch_bounds__(256) void scan_back_parts_kernel(const ScanArgs a)
     if (p.c >= a.n) return;
     const int64_t base = (int64_t)p.b * a.T * a.n + p.c0, part = ((int64_t)p.b * a.chunks + p.j) * a.n + p.c;
     const T *G = (const T *)a.G + base, *dY = (const T *)a.dY + base;
+    const float least = least_kept<DSATTN_SCAN_SUM>();
     float c[V], prod[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -215,7 +233,7 @@ __global__ __launch_bounds__(256) void scan_back_parts_kernel(const ScanArgs a)
             if (!decltype(whole)::value && t + i >= p.t1) continue;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float keep = gate_of<DSATTN_SCAN_SUM>((float)g[i][v]).keep;
+                const float keep = gate_of<DSATTN_SCAN_SUM>((float)g[i][v], least).keep;
                 c[v] = keep * (c[v] + (float)dy[i][v]);
                 prod[v] *= keep;
             }
@@ -240,6 +258,7 @@ __global__ __launch_bounds__(256) void scan_back_kernel(const ScanArgs a)
     const int64_t base = (int64_t)p.b * a.T * a.n + p.c0, part = ((int64_t)p.b * a.chunks + p.j) * a.n + p.c;
     const T *X = (const T *)a.X + base, *G = (const T *)a.G + base, *dY = (const T *)a.dY + base;
     const float *S = a.states_in + (int64_t)p.b * a.steps * a.n + p.c;
+    const float least = least_kept<MODE>();
     float c[V];
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -273,7 +292,7 @@ __global__ __launch_bounds__(256) void scan_back_kernel(const ScanArgs a)
         for (int i = 0; i + 1 < kStep; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Gate q = gate_of<MODE>((float)gc[i][v]);
+                const Gate q = gate_of<MODE>((float)gc[i][v], least);
                 h[i + 1][v] = fmaf(q.keep, h[i][v], q.let * (float)xc[i][v]);  // (past the end: not used)
             }
 #pragma unroll
@@ -282,7 +301,7 @@ __global__ __launch_bounds__(256) void scan_back_kernel(const ScanArgs a)
             Piece dx, dg;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Gate q = gate_of<MODE>((float)gc[i][v]);
+                const Gate q = gate_of<MODE>((float)gc[i][v], least);
                 const float d = c[v] + (float)dc[i][v];
                 dx[v] = (T)(d * q.let);
                 if constexpr (MODE == DSATTN_SCAN_MEAN)  // the two slopes differ in sign only
