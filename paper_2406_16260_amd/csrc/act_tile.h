@@ -312,8 +312,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *p, int64
 }
 
 // Gradients of the activation's argument and of its gate: dz_0 = dy [* z_1] act'(z_0), dz_1 = dy act(z_0).  A wavefront's part as
-// in epilogue(); 16 rows x 32 channels at a time through the wavefront's own kGradBytes, into which dy comes (two passes
-// ahead) and from which dz leaves, as rows of n_w Cout numbers.  The columns' sums over the part's rows, in fp32 of unrounded dz, go
+// in epilogue(); 16 rows x 64 channels at a time through the wavefront's own kGradBytes, into which dy comes (up to four passes
+// ahead) and from which dz leaves, as rows of n_w Cout numbers in the operands' type.  The columns' sums over the part's rows, in fp32 of unrounded dz, go
 // to row `part` of a.sums.
 // Both derivatives take x within +-100: beyond, its factor is 0, and 0 * infinity would be NaN.
 template <int ACT>
@@ -352,7 +352,8 @@ __device__ __forceinline__ void turn_tile(const TurnArgs &a, int block, unsigned
     for (int i = 0; i < 64; i += ROWS) {
         const int o = o0 + r + i, c = c0 + p;
         Piece x{};
-        if (o < a.No && c < a.Cin) x = *(const Piece *)((const T *)(o < a.Cout ? a.W[0] : a.W[1]) + (int64_t)(o < a.Cout ? o : o - a.Cout) * a.Cin + c);
+        const T *w = (const T *)(o < a.Cout ? a.W[0] : a.W[1]);
+        if (o < a.No && c < a.Cin) x = *(const Piece *)(w + (int64_t)(o < a.Cout ? o : o - a.Cout) * a.Cin + c);
 #pragma unroll
         for (int e = 0; e < PER; ++e) tile[(p + e) * SR + r + i] = x[e];
     }
@@ -411,8 +412,8 @@ struct GradIn {
 
 // acc: the products on top of the biases that they began with.  WHOLE: all of the part's rows and channels are there.
 template <typename T, int MB, int NB, bool GATED, typename TO, int ACT, bool WHOLE>
-__device__ __forceinline__ void epilogue_grad_part(const ActGradArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], GradIn<TO, MB, NB, GATED> &in,
-                                                   int64_t m0, int c0, unsigned char *stage, int lane)
+__device__ __forceinline__ void epilogue_grad_part(const ActGradArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB],
+                                                   GradIn<TO, MB, NB, GATED> &in, int64_t m0, int c0, unsigned char *stage, int lane)
 {
     using In = GradIn<TO, MB, NB, GATED>;
     using Piece = typename In::Piece;
@@ -488,8 +489,8 @@ __device__ __forceinline__ void epilogue_grad_part(const ActGradArgs &a, const t
     }
 }
 template <typename T, int MB, int NB, bool GATED, typename TO, int ACT>
-__device__ __forceinline__ void epilogue_grad(const ActGradArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB], GradIn<TO, MB, NB, GATED> &in,
-                                              int64_t m0, int c0, unsigned char *stage, int lane)
+__device__ __forceinline__ void epilogue_grad(const ActGradArgs &a, const typename Mul<T>::Acc (&acc)[MB][NB],
+                                              GradIn<TO, MB, NB, GATED> &in, int64_t m0, int c0, unsigned char *stage, int lane)
 {
     if (a.M - m0 >= 16 * MB && a.Cout - c0 >= 16 * NB / (GATED ? 2 : 1))
         epilogue_grad_part<T, MB, NB, GATED, TO, ACT, true>(a, acc, in, m0, c0, stage, lane);

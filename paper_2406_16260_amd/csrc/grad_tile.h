@@ -28,7 +28,8 @@ struct GradWArgs {
     int32_t stages;                      // of a split
     int32_t groups;                      // workgroups of the product; those behind join the column sums
     JoinArgs join;
-    int32_t whole, whole_xcd, rest_xcd;  // 256 x 256 tiles: column tiles that are not half empty; items of an XCD of those and of the others
+    // 256 x 256 tiles: column tiles that are not half empty; items of an XCD of those and of the others
+    int32_t whole, whole_xcd, rest_xcd;
 };
 
 // Four numbers of a column, transposed by the LDS.  (The pointer is restrict for what the compiler makes of it: a read that it
@@ -174,10 +175,12 @@ __global__ __launch_bounds__(64 * WVM * WVN, 2) void grad_w_tile_kernel(const Gr
         const __amdgpu_buffer_rsrc_t xres = cols_from(a.X, k0, a.M, xbytes, c0 * B::ES);
 #pragma unroll
         for (int l = 0; l < GA; ++l)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(zres, (__attribute__((address_space(3))) void *)(as + l * 1024), 16, (uint32_t)aoff[l], 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(zres, (__attribute__((address_space(3))) void *)(as + l * 1024), 16,
+                                                     (uint32_t)aoff[l], 0, 0, 0);
 #pragma unroll
         for (int l = 0; l < GB; ++l)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(xres, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16, (uint32_t)boff[l], 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xres, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16,
+                                                     (uint32_t)boff[l], 0, 0, 0);
     };
     typename M::Acc acc[MB][NB];
 #pragma unroll
@@ -274,9 +277,11 @@ __global__ __launch_bounds__(256, 2) void grad_dz_large_kernel(const ActGradArgs
         for (int l = 0; l < H; ++l) {
             const uint32_t off = live ? woff[l] + (uint32_t)(ks * RB) : kOob;
             if (GATED && l == 1)  // (blocks of 16 rows of the gate and of the value by turns)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(wres1, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16, (uint32_t)off, 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(wres1, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16,
+                                                         (uint32_t)off, 0, 0, 0);
             else
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(wres0, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16, (uint32_t)off, 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(wres0, (__attribute__((address_space(3))) void *)(bs + l * 1024), 16,
+                                                         (uint32_t)off, 0, 0, 0);
         }
     };
     if (threadIdx.x < BN) {
@@ -355,7 +360,7 @@ constexpr int kDzLargeLds = 3 * 384 * 64;
 // place, and LDS reads and the loads of the next stage but one sit between the matrix instructions by hand, as in the
 // product's persistent kernel.  Where X has no more than 128 columns left, the four wavefronts of its other half, one
 // of each SIMD, only load, and the tile takes little more than half the time.  No bank conflicts (counted).  5,120 x 640 over 40,960
-// rows: 241 us, 1,117 TFLOP/s, 5 splits and 10 us to join them (tiles of 128 x 128 412 us).
+// rows: 241 us, 1,117 TFLOP/s, 4 splits and 10 us to join them (tiles of 128 x 128 412 us).
 __global__ __launch_bounds__(512, 2) void grad_w_large_kernel(const GradWArgs a)
 {
     using T = __bf16;
@@ -562,8 +567,8 @@ __global__ __launch_bounds__(256) void grad_w_join_kernel(const GradWArgs a)
 
 // dX of few rows: dX = sum dz_k W_k, 32 x 32 a workgroup, whose eight wavefronts share the contraction as in act_small_kernel
 // (a wavefront takes every eighth stage through two LDS slots of its own).  W's rows are what is contracted over, and are
-// read transposed; stages do not cross from one set to the other.  A long contraction for few tiles is split over workgroups.  160 x 1,280 x 1,280: 4.9 us, and 3.4 + 5.1 where a
-// kernel of its own turns W first.
+// read transposed; stages do not cross from one set to the other.  A long contraction for few tiles is split over workgroups.
+// 160 x 1,280 x 1,280: 4.9 us, and 3.4 + 5.1 where a kernel of its own turns W first.
 struct GradXArgs {
     const void *dz;  // [M][No]
     const void *W[2];
@@ -609,8 +614,8 @@ __global__ __launch_bounds__(512, 2) void grad_x_small_kernel(const GradXArgs a)
         for (int l = 0; l < 4; ++l) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(zres, (__attribute__((address_space(3))) void *)(mem + slot * SLOT + l * 1024), 16,
                                                      live ? o + l * next : kOob, 0, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(wres, (__attribute__((address_space(3))) void *)(mem + slot * SLOT + 4096 + l * 1024), 16,
-                                                     (uint32_t)woff[l], 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wres, (__attribute__((address_space(3))) void *)(mem + slot * SLOT + 4096 + l * 1024),
+                                                     16, (uint32_t)woff[l], 0, 0, 0);
         }
     };
     f32x4 acc[2][2] = {};

@@ -7,7 +7,7 @@
 // The mean is taken off twice, the second time that of the differences: what the first left of it by rounding (a row whose
 // mean is 1,000 times its spread would lose ten bits of the spread to that) is gone, and the variance comes with it.
 // us and TB/s (a large copy 5.1):
-//   368,640 x 1,280, bf16, residual and sum         656     5.75
+//   368,640 x 1,280, bf16, residual and sum         656-670 5.75
 //   40,960 x 640, bf16, residual, all gradients     59.6    4.4, of which the joining kernel is 4.3 us
 //   368,640 x 1,280, the same                       968     4.9
 //   24,591 x 1,863, bf16, residual, then all gradients   75.5 and 105, the floors 72 and 90 (pieces of one number: 225 and 307)
@@ -685,15 +685,17 @@ int dsattn_layernorm_backward(const dsattn_ln_desc *desc, const void *X, const v
     const dsattn_ln_desc &d = *desc;
     if (d.out_dtype != d.io_dtype) return fail(DSATTN_EINVAL, "%s: gradients are of the input's dtype", who);
     if (!X || !dY || !dX) return fail(DSATTN_EINVAL, "%s: null pointer", who);
-    if (((uintptr_t)X | (uintptr_t)residual | (uintptr_t)gamma | (uintptr_t)dY | (uintptr_t)dsum | (uintptr_t)dX | (uintptr_t)workspace) & 15u)
+    if (((uintptr_t)X | (uintptr_t)residual | (uintptr_t)gamma | (uintptr_t)dY | (uintptr_t)dsum | (uintptr_t)dX |
+         (uintptr_t)workspace) & 15u)
         return fail(DSATTN_EINVAL, "%s: pointers must be 16-byte aligned", who);
     if (((uintptr_t)dgamma | (uintptr_t)dbeta) & 3u) return fail(DSATTN_EINVAL, "%s: gradients of weights must be 4-byte aligned", who);
     const LnBackLaunch l = ln_back_launch(d);
     const bool sums = dgamma || dbeta;
     if (sums && (!workspace || workspace_bytes < l.bytes)) return fail(DSATTN_EINVAL, "%s: workspace of %zu bytes needed", who, l.bytes);
     const int64_t n = d.rows * d.channels * (d.io_dtype == DSATTN_BF16 ? 2 : 4), cn = 4 * (int64_t)d.channels;
-    const struct { const void *p; int64_t n; } inputs[] = {{X, n}, {residual, n}, {dY, n}, {dsum, n}, {gamma, cn}},
-                                               outputs[] = {{dX, n}, {dgamma, cn}, {dbeta, cn}, {sums ? workspace : nullptr, (int64_t)l.bytes}};
+    const struct { const void *p; int64_t n; }
+        inputs[] = {{X, n}, {residual, n}, {dY, n}, {dsum, n}, {gamma, cn}},
+        outputs[] = {{dX, n}, {dgamma, cn}, {dbeta, cn}, {sums ? workspace : nullptr, (int64_t)l.bytes}};
     for (int o = 0; o < 4; ++o) {
         for (int i = 0; i < 5; ++i) {
             // (dX in the place of an input: not where rows are long and their columns are read again for the sums)

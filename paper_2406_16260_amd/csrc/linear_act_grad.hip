@@ -3,9 +3,13 @@
 //   z_k = X W_k^T + b_k again,  dz_0 = dy [* z_1] act'(z_0),  dz_1 = dy * act(z_0)
 //   dX = sum dz_k W_k,  dW_k = dz_k^T X,  db_k = column sums of dz_k
 //
-// Three products of the forward pass's size.  z is computed again: nothing is kept between the passes but X (z of 40,960 x 2 x 2,560 would be 420 MB, written and read in 165 us, a product 206 us at 1,300 TFLOP/s).
-// dz goes through memory in the operands' type, to the other two.  dX is the product of dz with W turned (X W^T kernels then do
-// it); dW contracts over rows, which grad_tile.h reads transposed, its rows split over the card where W has few tiles.
+// Three products of the forward pass's size.  z is computed again: nothing is kept between the passes but X (z of 40,960 x 2 x
+// 2,560 would be 420 MB, written and read in 165 us, a product 206 us at 1,300 TFLOP/s).
+// dz goes through memory in the operands' type, to the other two: in bf16 that is its only rounding to fewer bits than fp32, and all
+// that dX and dW are less exact by than an fp32 dz's would be (of the 2-norm, 2.35 * 10^-3 against 1.66 for the outputs' own
+// rounding).  Two bf16 parts of dz would take twice the multiplies of both products and twice the traffic of dz.
+// dX is the product of dz with W turned (X W^T kernels then do it); dW contracts over rows, which grad_tile.h reads transposed, its
+// rows split over the card where W has few tiles.
 // No atomics: splits and parts are joined in an order that the shape alone decides.  us, of which dz, dX, dW with its join:
 //   40,960 x 640 x 2 x 2,560, GELU gate, bf16   876    363  241  262    (920 TFLOP/s; a large library product 1,300)
 //   25,920 x 5,120 x 1,280, bias, bf16          614     20  263  331    (1,110 TFLOP/s)
@@ -260,12 +264,14 @@ double w_estimate(int size, int64_t tm, int64_t tn, int64_t cin, int64_t splits,
 {
     const double st = (double)stages, join = splits > 1 ? 4.0 + 8.0 * (double)splits * numbers / 7e6 : 0.0;
     if (size == 256) {
-        const int64_t half = cin % 256 != 0 && cin % 256 <= 128 ? 1 : 0, f = (tm * (tn - half) * splits + 7) / 8, h = (tm * half * splits + 7) / 8;
+        const int64_t half = cin % 256 != 0 && cin % 256 <= 128 ? 1 : 0;
+        const int64_t f = (tm * (tn - half) * splits + 7) / 8, h = (tm * half * splits + 7) / 8;
         const int64_t rounds = (f + 31) / 32, spare = rounds * 32 - f;
         const double t = (double)rounds + 0.6 * (double)((std::max<int64_t>(0, h - spare) + 31) / 32);
         return t * (1.2 * st + 7.0) + join;
     }
-    const double latency = size == 128 ? (f32 ? 2.0 : deep ? 0.55 : 0.67) : (f32 ? 0.65 : deep ? 0.3 : 0.45), each = size == 128 ? (f32 ? 2.0 : 0.5) : (f32 ? 0.55 : 0.2);
+    const double latency = size == 128 ? (f32 ? 2.0 : deep ? 0.55 : 0.67) : (f32 ? 0.65 : deep ? 0.3 : 0.45);
+    const double each = size == 128 ? (f32 ? 2.0 : 0.5) : (f32 ? 0.55 : 0.2);
     const int64_t n = tm * tn * splits, fit = size == 128 ? 2 : 5;
     const double c = n <= 256 * fit ? (double)((n + 255) / 256) : (double)n / 256.0 + 0.5;
     return st * std::max(latency + 0.05 * (std::min(c, (double)fit) - 1.0), each * c) + 4.0 + join;
@@ -482,7 +488,8 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
     } else if (a.dX) {
         if (!turned) {
             void *params[] = {(void *)&turn};
-            launch(f32 ? (const void *)&grad_turn_kernel<float> : (const void *)&grad_turn_kernel<__bf16>, dim3((unsigned)turns), 256, params, 0);
+            launch(f32 ? (const void *)&grad_turn_kernel<float> : (const void *)&grad_turn_kernel<__bf16>, dim3((unsigned)turns), 256,
+                   params, 0);
         }
         if (g.x_deep) {
             ActArgs x{};
@@ -501,7 +508,8 @@ int grad_launch(const dsattn_linear_act_desc &d, const GradLaunch &g, const Grad
             x.per_xcd = (x.tiles + kXcds - 1) / kXcds;
             x.panel = 1;
             void *params[] = {&x};
-            launch(kXDeep[g.x_deep == 64], dim3((unsigned)(x.per_xcd * kXcds)), g.x_deep == 64 ? 256 : 512, params, 3 * 2 * g.x_deep * kRow);
+            launch(kXDeep[g.x_deep == 64], dim3((unsigned)(x.per_xcd * kXcds)), g.x_deep == 64 ? 256 : 512, params,
+                   3 * 2 * g.x_deep * kRow);
         } else {
             if (e != hipSuccess) return fail(DSATTN_EHIP, "%s: %s", who, hipGetErrorString(e));
             const dsattn_linear_act_desc x = product_of_dx(d);

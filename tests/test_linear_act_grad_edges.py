@@ -7,7 +7,8 @@ import test_linear_act_grad as G
 from paper_2406_16260_amd import binding as B
 
 DEV = "cuda:0"
-SIZES = [(33, 72, 4040), (160, 264, 520), (350, 2056, 1096), (640, 640, 640), (1100, 1032, 1048), (4100, 640, 1288), (8200, 1032, 1288), (10000, 512, 2048)]
+SIZES = [(33, 72, 4040), (160, 264, 520), (350, 2056, 1096), (640, 640, 640), (1100, 1032, 1048), (4100, 640, 1288), (8200, 1032, 1288),
+         (10000, 512, 2048)]
 
 
 @pytest.mark.gpu
