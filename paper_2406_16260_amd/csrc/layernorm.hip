@@ -88,11 +88,12 @@ constexpr float kLargest = 0x1.fffffep127f;
 
 // each(f) calls f(s) for the lane's numbers of the row, sums(v) adds v over the row's lanes: whether another turn is needed
 // depends on sums only, which all lanes of a row have.
-// The mean is that of numbers times 2^-21, whose sum is within fp32's range (what that takes of numbers below 2^-105 is part of the
-// rest).  Where what it is off by, the rest, is more than a quarter of the spread, it is put right by that and the turn taken again:
-// the mean of a row of equal numbers is then that number itself, its variance 0, and that of numbers which differ in their last
-// bits loses no more to the rest's square than it has.  Only then are the squares asked whether they are within range: eps is lost
-// beside a variance in `unit`s (1e-6 * 2^-150), which has to be that of numbers that do differ.
+// Means are those of numbers times 2^-21, whose sums are within fp32's range (what that takes of the mean of numbers below 2^-105 is
+// part of the rest; differences as small as that have a gain, or an eps that is far more).  Where what the mean is off by, the rest,
+// is more than a quarter of the spread, it is put right by that and the turn taken again: the mean of a row of equal numbers is then
+// that number itself, its variance 0, and that of numbers which differ in their last bits loses no more to the rest's square
+// than it has.  Only then are the squares asked whether they are within range: eps is lost beside a variance in `unit`s
+// (1e-6 * 2^-150), which has to be that of numbers that do differ.
 template <typename Each, typename Sums>
 __device__ __forceinline__ RowStats row_stats(int C, float eps, Each each, Sums sums)
 {
@@ -109,11 +110,11 @@ __device__ __forceinline__ RowStats row_stats(int C, float eps, Each each, Sums 
         v[0] = v[1] = 0.f;
         each([&](float s) __attribute__((always_inline)) {
             const float d = (s * t.unit - t.mean) * t.gain;
-            v[0] += d;
+            v[0] = fmaf(d, 0x1p-21f, v[0]);
             v[1] = fmaf(d, d, v[1]);
         });
         sums(v);
-        t.rest = v[0] * inv;
+        t.rest = v[0] * inv * 0x1p21f;
         const float square = v[1] * inv;
         var = fmaf(-t.rest, t.rest, square);
         const bool beyond = !(v[1] < INFINITY), off = var < 0.9375f * square;

@@ -107,3 +107,13 @@ def test_rows_that_differ_in_a_last_bit(C, size, share):
     tol = 2 * tol * gamma.double().abs() + 3 * N.U * ((n * gamma).abs() + beta.double().abs())
     off = (Y.cpu().double() - y).abs()
     assert (off <= tol).all(), f"{(off / tol).max().item()} of the tolerance"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [65537, 999999, 1 << 20])
+def test_the_longest_rows(C, dtype, residual):
+    """Sums of 4,096 numbers a lane, whose first mean is off by some hundred units of the last bit."""
+    test_rows_of_equal_numbers_are_beta(C, dtype, dtype, residual, 1e-6)
+    test_gradients_of_rows_of_equal_numbers(C, dtype, residual)
