@@ -117,3 +117,26 @@ def test_the_longest_rows(C, dtype, residual):
     """Sums of 4,096 numbers a lane, whose first mean is off by some hundred units of the last bit."""
     test_rows_of_equal_numbers_are_beta(C, dtype, dtype, residual, 1e-6)
     test_gradients_of_rows_of_equal_numbers(C, dtype, residual)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("most", [1, 3, 1000, 1 << 20])
+@pytest.mark.parametrize("C", [7, 63, 320, 1280, 4099, 20001])
+def test_rows_of_the_smallest_numbers(C, most):
+    """Whole multiples of 2^-149 have the norm of those whole numbers, eps 0 (twice the tolerance, as for rows that differ in a last bit:
+    a mean of few units of the last bit is that far off before its rest is taken off)."""
+    g = torch.Generator().manual_seed(C + most)
+    x = torch.randint(0, most + 1, (5, C), generator=g).float()
+    x[:, 0], x[:, 1] = 0.0, float(most)
+    x[3:] = x[3:] - most // 2
+    _, _, gamma, beta, _, _ = N.inputs(1, C, "f32", 9, False)
+    Y = torch.full((5, C), float("nan"), device=DEV)
+    tiny = torch.ldexp(x, torch.tensor(-149))
+    assert torch.equal(tiny.double() * 2.0 ** 149, x.double())
+    B.dsattn_layernorm(5, C, tiny.to(DEV), Y, gamma=gamma.to(DEV), beta=beta.to(DEV), io_dtype=B.DSATTN_F32, eps=0.0)
+    torch.cuda.synchronize()
+    _, _, n, _, tol, _ = N.normed(x, None, 0.0)
+    y = n * gamma.double() + beta.double()
+    tol = 2 * tol * gamma.double().abs() + 3 * N.U * ((n * gamma).abs() + beta.double().abs())
+    off = (Y.cpu().double() - y).abs()
+    assert (off <= tol).all(), f"{(off / tol).max().item()} of the tolerance"
